@@ -453,6 +453,67 @@ int palu_attn_decode_staged(const palu_layer_desc* desc, int32_t batch, int32_t 
                             float* out, void* workspace, size_t workspace_bytes, void* stream,
                             void* const* stage_events);
 
+/*
+ * Decode attention over a PAGED latent cache, with a sliding window and a few first rows that stay visible.
+ * Every sequence keeps its latents in pages of page_rows rows that lie anywhere in a pool, and its page table says
+ * where: row t of sequence b (its position is t) is row t % page_rows of page
+ * page_table[b*table_stride + t / page_rows].  Attention as in palu_attn_decode (Sec. 2.1 Eq. 2, K rebuilt and
+ * rotated on the fly, values contracted in latent space) over the rows
+ *     t < n_sink  or  t >= seq_lens[b] - window          (window > 0; the newest row counts)
+ * or over all seq_lens[b] rows (window = 0; n_sink then has no effect).  Rows are appended with palu_encode /
+ * palu_encode_kv, whose dst_row is page_table[b][t / page_rows]*page_rows + t % page_rows.  Several new tokens of one
+ * sequence (a speculative-decoding check) are entries of the batch with the same page-table row and a
+ * length of their own.
+ *
+ *   max_len      upper bound of seq_lens (values are clamped to [0, max_len]); max_len <= table_stride * page_rows
+ *   q            DEVICE [batch, n_heads*q_per_kv, d_head] act_dtype, before RoPE
+ *   q_pos        DEVICE int32 [batch] position of each query, clamped to [0, rope_table_len), or NULL: seq_lens[b] - 1
+ *   hk, hv       DEVICE [n_pages, page_rows, R] act_dtype (quantized caches: PALU_ERR_UNSUPPORTED); page_rows is a power
+ *                of two, n_pages * page_rows < 2^31
+ *   page_table   DEVICE int32 [batch, table_stride].  Entries are clamped to [0, n_pages); those of pages
+ *                without an attended row are not read
+ *   seq_lens     DEVICE int32 [batch], or NULL (all max_len).  0: an idle slot, whose output is zeros
+ *   rope_table   as for palu_attn_decode; rope_table_len >= max_len
+ *   out          DEVICE [batch, n_heads*q_per_kv, d_head] act_dtype (what the output projection takes)
+ *   workspace    DEVICE, palu_attn_paged_workspace_bytes(...) bytes for the same desc, batch, max_len, window, n_sink.
+ *                Calls sharing a workspace must be ordered on one stream
+ * Ranks up to PALU_PAGED_MAX_RANK.  q, hk, hv, B_k, B_v, table, out and workspace are 16-byte aligned.
+ * Only attended rows are read: what lies in other rows, numbers or not, has no effect.
+ *
+ * Arithmetic.  Keys are rebuilt and rotated in float32.  A float16 layer's keys, queries and probabilities enter the
+ * matrix instructions as pairs of float16 numbers (2^-21 relative), so that the error is that of the output's
+ * rounding; a bfloat16 layer's keys and queries as one float16 number each (2^-11; the output is rounded to 2^-9),
+ * its probabilities as a pair of bfloat16 numbers.  Entries of rotated keys are right up to 5e5 in magnitude, of
+ * queries up to 6e4.  Sums, maxima and merged results are float32.
+ */
+enum { PALU_PAGED_MAX_RANK = 512 };
+int palu_attn_paged_workspace_bytes(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window,
+                                    int32_t n_sink, size_t* out_bytes);
+int palu_attn_paged(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window, int32_t n_sink,
+                    const void* q, const int32_t* q_pos, const void* hk, const void* hv, int32_t n_pages, int32_t page_rows,
+                    const int32_t* page_table, int32_t table_stride, const int32_t* seq_lens,
+                    const void* Bk, const void* Bv, const void* rope_table, int32_t rope_table_len,
+                    void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same for a batch whose sequences share their first prefix_len rows (a system prompt, a document with several
+ * questions, samples of one prompt): those rows are read through the page table of sequence 0 alone, once for the
+ * whole batch, and their keys are rebuilt once for all queries.  Rows from prefix_len on are each sequence's own,
+ * through its own page table (of which entries for whole shared pages are not read; a page that the prefix ends
+ * in is read from sequence 0's for rows before prefix_len, from the sequence's own for rows behind).  No window.
+ * A sequence shorter than the prefix attends its first seq_lens[b] rows; the latents of shared rows have to be finite
+ * numbers then (of rows that a sequence does not attend, zero times the latent enters its sum).
+ *   prefix_len   0 <= prefix_len <= max_len
+ * Everything else as for palu_attn_paged; workspace of palu_attn_prefix_workspace_bytes(...) bytes.
+ */
+int palu_attn_prefix_workspace_bytes(const palu_layer_desc* desc, int32_t batch, int32_t prefix_len, int32_t max_len,
+                                     size_t* out_bytes);
+int palu_attn_prefix(const palu_layer_desc* desc, int32_t batch, int32_t prefix_len, int32_t max_len,
+                     const void* q, const int32_t* q_pos, const void* hk, const void* hv, int32_t n_pages, int32_t page_rows,
+                     const int32_t* page_table, int32_t table_stride, const int32_t* seq_lens,
+                     const void* Bk, const void* Bv, const void* rope_table, int32_t rope_table_len,
+                     void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -103,6 +103,13 @@ def load_library():
     lib.palu_decode_step_t.argtypes = [dp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32,
                                        vp, vp, sz, vp]
     lib.palu_decode_step_t.restype = ctypes.c_int
+    paged = [vp, vp, vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, i32, vp, vp, sz, vp]
+    lib.palu_attn_paged_workspace_bytes.argtypes = [dp, i32, i32, i32, i32, szp]
+    lib.palu_attn_paged.argtypes = [dp, i32, i32, i32, i32] + paged
+    lib.palu_attn_prefix_workspace_bytes.argtypes = [dp, i32, i32, i32, szp]
+    lib.palu_attn_prefix.argtypes = [dp, i32, i32, i32] + paged
+    for name in ("palu_attn_paged_workspace_bytes", "palu_attn_paged", "palu_attn_prefix_workspace_bytes", "palu_attn_prefix"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("palu_rope_table_bytes", "palu_rope_table_init", "palu_encode_workspace_bytes", "palu_encode",
                  "palu_quant_latent", "palu_attn_decode_workspace_bytes", "palu_attn_decode"):
         getattr(lib, name).restype = ctypes.c_int
@@ -408,3 +415,67 @@ def palu_decode_step(desc: LayerDesc, batch: int, seq_len: int, max_seq: int, x,
         _ptr(k_pos), _ptr(seq_lens), _ptr(Bk), _ptr(Bv), _ptr(rope_table), int(rope_table_len), _ptr(out),
         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "palu_decode_step")
     return out
+
+
+def palu_attn_paged_workspace_bytes(desc: LayerDesc, batch: int, max_len: int, window: int = 0, n_sink: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().palu_attn_paged_workspace_bytes(desc.ref(), batch, max_len, window, n_sink, ctypes.byref(out)),
+           "palu_attn_paged_workspace_bytes")
+    return int(out.value)
+
+
+def palu_attn_prefix_workspace_bytes(desc: LayerDesc, batch: int, prefix_len: int, max_len: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().palu_attn_prefix_workspace_bytes(desc.ref(), batch, prefix_len, max_len, ctypes.byref(out)),
+           "palu_attn_prefix_workspace_bytes")
+    return int(out.value)
+
+
+def _paged_call(fn, where, desc, sizes, q, q_pos, hk, hv, page_table, seq_lens, Bk, Bv, rope_table, rope_table_len, out,
+                workspace, stream):
+    """hk, hv: [n_pages, page_rows, R]; page_table: [batch, pages per sequence]."""
+    import torch
+    _need_cuda(q, q_pos, hk, hv, page_table, seq_lens, Bk, Bv, rope_table, out, workspace)
+    n_pages, page_rows = int(hk.shape[0]), int(hk.shape[1])
+    if tuple(hv.shape[:2]) != (n_pages, page_rows):
+        raise ValueError("hk and hv need the same pages")
+    act = torch.float16 if desc.act_dtype == PALU_F16 else torch.bfloat16
+    if any(t.dtype != act for t in (q, hk, hv, Bk, Bv, out)):
+        raise ValueError(f"q, hk, hv, Bk, Bv and out need dtype {act}")
+    if any(t is not None and t.dtype != torch.int32 for t in (q_pos, page_table, seq_lens)):
+        raise ValueError("q_pos, page_table and seq_lens need dtype torch.int32")
+    if (hk.dim() != 3 or hv.dim() != 3 or hk.shape[2] != desc.R_k or hv.shape[2] != desc.R_v or page_table.dim() != 2
+            or page_table.shape[0] != sizes[0] or any(t.numel() != sizes[0] * desc.n_q_heads * desc.d_head for t in (q, out))
+            or any(t is not None and t.numel() != sizes[0] for t in (q_pos, seq_lens))):
+        raise ValueError("shapes do not fit the layer and the batch")
+    _check(fn(desc.ref(), *sizes, _ptr(q), _ptr(q_pos), _ptr(hk), _ptr(hv), n_pages, page_rows, _ptr(page_table),
+              int(page_table.shape[1]), _ptr(seq_lens), _ptr(Bk), _ptr(Bv), _ptr(rope_table), int(rope_table_len), _ptr(out),
+              _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), where)
+    return out
+
+
+def palu_attn_paged(desc: LayerDesc, batch: int, max_len: int, q, q_pos, hk, hv, page_table, seq_lens, Bk, Bv, rope_table,
+                    rope_table_len: int, window: int = 0, n_sink: int = 0, out=None, workspace=None, stream=None):
+    """Decode attention over pages hk, hv [n_pages, page_rows, R], every sequence over its newest `window` and first
+    `n_sink` rows (window 0: all rows)."""
+    import torch
+    if out is None:
+        out = torch.empty((batch, desc.n_q_heads, desc.d_head), dtype=q.dtype, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(palu_attn_paged_workspace_bytes(desc, batch, max_len, window, n_sink), dtype=torch.uint8,
+                                device=q.device)
+    return _paged_call(load_library().palu_attn_paged, "palu_attn_paged", desc, (batch, max_len, window, n_sink), q, q_pos, hk, hv,
+                       page_table, seq_lens, Bk, Bv, rope_table, rope_table_len, out, workspace, stream)
+
+
+def palu_attn_prefix(desc: LayerDesc, batch: int, prefix_len: int, max_len: int, q, q_pos, hk, hv, page_table, seq_lens, Bk, Bv,
+                     rope_table, rope_table_len: int, out=None, workspace=None, stream=None):
+    """Decode attention of a batch whose first `prefix_len` rows are those of sequence 0, read and rebuilt once for all."""
+    import torch
+    if out is None:
+        out = torch.empty((batch, desc.n_q_heads, desc.d_head), dtype=q.dtype, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(palu_attn_prefix_workspace_bytes(desc, batch, prefix_len, max_len), dtype=torch.uint8,
+                                device=q.device)
+    return _paged_call(load_library().palu_attn_prefix, "palu_attn_prefix", desc, (batch, prefix_len, max_len), q, q_pos, hk, hv,
+                       page_table, seq_lens, Bk, Bv, rope_table, rope_table_len, out, workspace, stream)

@@ -32,7 +32,7 @@ FLAT = ["-DPALU_SCORE_FLAT=1"]
 
 def sources():
     """(source file, extra flags, object name) of every translation unit."""
-    vgpr = ["score16_shared_forms.hip", "score_forms.hip", "score_forms_lowbit.hip", "score16_forms.hip", "pv.hip", "api.hip"]
+    vgpr = ["score16_shared_forms.hip", "score_forms.hip", "score_forms_lowbit.hip", "score16_forms.hip", "pv.hip", "api.hip", "paged.hip"]
     units = [(f, VGPR_FORM, "") for f in vgpr]
     units += [(f, VGPR_FORM + FLAT, "_flat") for f in ("score16_shared_forms.hip", "score16_forms.hip")]
     units += [("attend16_forms.hip", VGPR_FORM, ""), ("attend16_forms.hip", VGPR_FORM + FLAT, "_flat"), ("attend16_forms.hip", VGPR_FORM + ["-DPALU_ATTEND_SHARED=1"], "_shared"),

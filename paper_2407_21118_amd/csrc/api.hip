@@ -2033,3 +2033,5 @@ int palu_decode_step_t(const palu_layer_desc* desc, int32_t batch, int32_t seq_l
 }
 
 }  // extern "C"
+
+#include "paged_api.hip"

@@ -1,0 +1,105 @@
+// What the host side and the kernels of attention over a paged latent cache share (paged.hip).
+#pragma once
+
+#include "palu_dev.h"
+
+namespace palu {
+
+constexpr int kPagedTile = 64;                 // tokens per tile: positions 64 i .. 64 i + 63
+constexpr int kPagedThreads = 512;             // eight wavefronts, two per SIMD
+
+// Layer metadata; heads are KEY/VALUE heads here.  Everything indexed by the group is 32 bits wide: beside an array of 16-bit
+// numbers with the same index the compiler addresses these from a base that lies on no whole word, and scalar loads drop its low bits.
+struct PagedMeta {
+  int n_heads;
+  int n_groups;
+  int qpk;                                     // query heads per key/value head
+  int k_off[PALU_MAX_GROUPS + 1];
+  int v_off[PALU_MAX_GROUPS + 1];
+  int bk_off[PALU_MAX_GROUPS + 1];             // element offset of group j inside the concatenated B_k
+  int bv_off[PALU_MAX_GROUPS + 1];
+  int o_off[PALU_MAX_GROUPS];                  // value ranks of all heads before group j, summed: where its partial results begin
+  int head_off[PALU_MAX_GROUPS + 1];
+  uint8_t group_of_head[PALU_MAX_HEADS];
+};
+
+// Rows that a sequence of L rows attends: t < sink and lo <= t < L, in tiles 0 .. sink_tiles - 1 and from tile0 on.
+struct PagedSpan {
+  int sink, lo, sink_tiles, tile0, n_tiles;
+};
+// first: rows before it belong to the shared prefix and are attended elsewhere (no window, no sinks then)
+__host__ __device__ __forceinline__ PagedSpan paged_span(int L, int first, int window, int n_sink) {
+  PagedSpan s;
+  s.lo = first;
+  s.sink = 0;
+  if (window > 0 && L - window > n_sink) {     // else the window reaches the first rows: everything is attended
+    s.lo = L - window;
+    s.sink = n_sink;
+  }
+  s.sink_tiles = (s.sink + kPagedTile - 1) / kPagedTile;
+  s.tile0 = s.lo / kPagedTile;
+  if (s.tile0 < s.sink_tiles) s.tile0 = s.sink_tiles;
+  const int end = (L + kPagedTile - 1) / kPagedTile;
+  s.n_tiles = L <= s.lo ? 0 : s.sink_tiles + (end > s.tile0 ? end - s.tile0 : 0);
+  return s;
+}
+
+// A unit: up to four adjacent key/value heads of one group whose keys one workgroup rebuilds.
+struct PagedUnit {
+  uint32_t bits;                               // first head | heads << 8 | group << 16
+  __host__ __device__ int h0() const { return bits & 255; }
+  __host__ __device__ int nh() const { return (bits >> 8) & 255; }
+  __host__ __device__ int group() const { return bits >> 16; }
+};
+
+struct PagedArgs {
+  const uint16_t* hk;                          // [n_pages * page_rows, R_k]
+  const uint16_t* hv;
+  const uint16_t* q;                           // [batch, n_heads * qpk, 128], before RoPE
+  const uint16_t* Bk;
+  const float* rope;                           // angle table, layout in palu_dev.h
+  const int32_t* q_pos;                        // [batch] or NULL: the newest row's
+  const int32_t* page_table;                   // [batch, table_stride]
+  const int32_t* seq_lens;                     // [batch] or NULL: max_len
+  float* o_part;                               // [slot][rows * sum of value ranks over the heads]: sums of exp2(score - max) * latent
+  float* ml_part;                              // [slot][head][row][2]: the maximum and the sum
+  long long R_k, R_v;
+  int n_pages, page_shift, table_stride, rope_len;
+  int max_len, first, window, n_sink;
+  int pos_len;                                 // rows of a sequence where seq_lens is NULL (max_len: those of the tokens in question)
+  int batch;
+  int n_units;
+  int rows;                                    // query rows per key/value head: qpk, or batch * qpk where the tokens are shared
+  int n_row_blocks, block_rows;
+  int chunk_tiles;                             // tiles per workgroup, at most
+  int n_slots;                                 // partial results per sequence, or of the shared tokens
+  long long o_stride;                          // floats of o_part per slot
+  float scale;                                 // log2(e) / sqrt(128)
+  PagedMeta meta;
+  PagedUnit units[PALU_MAX_HEADS];
+};
+static_assert(sizeof(PagedArgs) <= 4096, "kernel arguments");
+
+struct PagedMergeArgs {
+  const float* o_part;                         // the sequences' own partial results ...
+  const float* ml_part;
+  const float* o_shared;                       // ... and those of the shared tokens (n_shared slots)
+  const float* ml_shared;
+  const uint16_t* Bv;
+  const int32_t* seq_lens;
+  uint16_t* out;                               // [batch, n_heads * qpk, 128]
+  int max_len, first, window, n_sink;
+  int batch;
+  int chunk_tiles, n_slots, n_shared;
+  long long o_stride, o_shared_stride;
+  PagedMeta meta;
+};
+
+using PagedFn = void (*)(PagedArgs);
+// The instantiation for units of at most nh heads (4, 2, 1); big_k, big_v: ranks above 256; pt: tiles of 16 packed query rows
+// (nh * block_rows of them at most); shared: the tokens are those of a prefix, the rows all sequences'
+PagedFn paged_fn(int act, int nh, bool big_k, bool big_v, int pt, bool shared);
+using PagedMergeFn = void (*)(PagedMergeArgs);
+PagedMergeFn paged_merge_fn(int act);
+
+}  // namespace palu

@@ -1,0 +1,286 @@
+// Host side of attention over a paged latent cache (part of the translation unit api.hip).
+
+#include "paged.h"
+
+namespace {
+
+// Key/value heads of one rank class, cut into units: one launch of paged_kernel.
+struct PagedClass {
+  bool big_k, big_v;
+  int nh, pt;                              // heads per unit, tiles of 16 packed query rows
+  int n_row_blocks, block_rows;
+  int n_units;
+  PagedUnit units[PALU_MAX_HEADS];
+};
+struct PagedPlan {
+  PagedMeta meta;
+  int rows;                                // query rows per key/value head
+  int n_cls;
+  PagedClass cls[4];
+  int chunk_tiles, n_slots;                // 0 slots: nothing to attend
+  long long o_stride, ml_stride;           // floats per slot
+};
+
+int check_paged_desc(const palu_layer_desc* desc, PagedMeta* pm) {
+  Meta m;
+  const int st = check_desc(desc, &m);
+  if (st != PALU_OK) return st;
+  if (latent_bits(desc->k_latent_dtype) || latent_bits(desc->v_latent_dtype)) return PALU_ERR_UNSUPPORTED;
+  std::memset(pm, 0, sizeof(*pm));
+  pm->n_heads = desc->n_heads;
+  pm->n_groups = desc->n_groups;
+  pm->qpk = m.qpk;
+  int o = 0;
+  for (int j = 0; j <= desc->n_groups; ++j) {
+    pm->head_off[j] = desc->group_head_off[j];
+    pm->k_off[j] = m.k_off[j];
+    pm->v_off[j] = m.v_off[j];
+    pm->bk_off[j] = m.bk_off[j] / m.qpk;       // Meta counts query heads
+    pm->bv_off[j] = m.bv_off[j] / m.qpk;
+    if (j == desc->n_groups) break;
+    if (m.k_off[j + 1] - m.k_off[j] > PALU_PAGED_MAX_RANK || m.v_off[j + 1] - m.v_off[j] > PALU_PAGED_MAX_RANK) return PALU_ERR_UNSUPPORTED;
+    pm->o_off[j] = o;
+    o += (desc->group_head_off[j + 1] - desc->group_head_off[j]) * (m.v_off[j + 1] - m.v_off[j]);
+    for (int h = desc->group_head_off[j]; h < desc->group_head_off[j + 1]; ++h) pm->group_of_head[h] = (uint8_t)j;
+  }
+  return PALU_OK;
+}
+
+// batch: sequences whose tokens are attended one by one (1 where they are shared); max_tiles: tiles of 64 tokens of the longest
+void plan_paged(const PagedMeta& m, int rows, int batch, int max_tiles, PagedPlan* p) {
+  p->meta = m;
+  p->rows = rows;
+  p->n_cls = 0;
+  long long wgs = 0;
+  int sum_rv = 0;
+  for (int j = 0; j < m.n_groups; ++j) sum_rv += (m.head_off[j + 1] - m.head_off[j]) * (m.v_off[j + 1] - m.v_off[j]);
+  for (int cls = 0; cls < 4; ++cls) {
+    const bool big_k = (cls & 1) != 0, big_v = (cls & 2) != 0;
+    int most = 0;                              // heads in a group of the class
+    auto in_class = [&](int j) { return (m.k_off[j + 1] - m.k_off[j] > 256) == big_k && (m.v_off[j + 1] - m.v_off[j] > 256) == big_v; };
+    for (int j = 0; j < m.n_groups; ++j)
+      if (in_class(j)) most = std::max(most, m.head_off[j + 1] - m.head_off[j]);
+    if (!most) continue;
+    PagedClass& c = p->cls[p->n_cls++];
+    c.big_k = big_k;
+    c.big_v = big_v;
+    // A unit of more heads reads its latents once for all of them; a unit of more rows rebuilds its keys once for all of those.
+    const int row_limit = big_k ? 32 : 64;     // packed rows
+    c.nh = big_k ? (most >= 2 ? 2 : 1) : (most >= 3 ? 4 : most);
+    while (c.nh > 1 && c.nh * rows > row_limit) c.nh /= 2;
+    c.n_row_blocks = ceil_div(rows, row_limit / c.nh);
+    c.block_rows = ceil_div(rows, c.n_row_blocks);
+    c.pt = c.nh * c.block_rows <= 16 ? 1 : row_limit / 16;
+    c.n_units = 0;
+    for (int first = 0;; first += c.nh) {      // round robin over the groups: neighbouring workgroups, which go to different L2 caches,
+      bool any = false;                        // take different groups, and the units of one group meet in one
+      for (int j = 0; j < m.n_groups; ++j) {
+        const int s = m.head_off[j + 1] - m.head_off[j];
+        if (!in_class(j) || first >= s) continue;
+        any = true;
+        c.units[c.n_units++].bits = (uint32_t)(m.head_off[j] + first) | (uint32_t)std::min(c.nh, s - first) << 8 | (uint32_t)j << 16;
+      }
+      if (!any) break;
+    }
+    wgs += (long long)c.n_units * c.n_row_blocks;
+  }
+  wgs *= batch;
+  p->o_stride = (long long)rows * sum_rv;
+  p->ml_stride = (long long)rows * m.n_heads * 2;
+  p->chunk_tiles = 1;
+  p->n_slots = 0;
+  if (max_tiles <= 0) return;
+  // Tiles per workgroup: one workgroup is resident per compute unit, and loading its weights costs about as much as two tiles.
+  const int cus = device_cu_count();
+  double best = 1e300;
+  for (int n = 1; n <= max_tiles && n <= 1024; ++n) {
+    const int tiles = ceil_div(max_tiles, n);
+    const double rounds = (double)((wgs * ceil_div(max_tiles, tiles) + cus - 1) / cus);
+    const double cost = rounds * (2.0 + tiles) + 0.05 * n;
+    if (cost < best) {
+      best = cost;
+      p->chunk_tiles = tiles;
+    }
+  }
+  p->n_slots = ceil_div(max_tiles, p->chunk_tiles);
+}
+
+// the largest number of tiles that a sequence of up to max_len rows has
+int paged_max_tiles(int max_len, int first, int window, int n_sink) {
+  const long long all = ceil_div(max_len, kPagedTile) - first / kPagedTile;
+  if (window <= 0) return max_len > first ? (int)all : 0;
+  return (int)std::min<long long>(all, ((long long)n_sink + kPagedTile - 1) / kPagedTile + ((long long)window + kPagedTile - 2) / kPagedTile + 1);
+}
+
+size_t paged_part_bytes(const PagedPlan& p, int batch, size_t* ml_offset) {
+  *ml_offset = align_up((size_t)batch * p.n_slots * p.o_stride * sizeof(float));
+  return *ml_offset + align_up((size_t)batch * p.n_slots * p.ml_stride * sizeof(float));
+}
+
+struct PagedCall {
+  int batch, prefix, max_len, window, n_sink;
+  PagedPlan own, shared;
+  size_t own_ml, shared_at, shared_ml, total;
+};
+
+int plan_paged_call(const palu_layer_desc* desc, int batch, int prefix, int max_len, int window, int n_sink, PagedCall* c) {
+  PagedMeta m;
+  const int st = check_paged_desc(desc, &m);
+  if (st != PALU_OK) return st;
+  if (batch <= 0 || max_len <= 0 || prefix < 0 || prefix > max_len || window < 0 || n_sink < 0) return PALU_ERR_INVALID_ARG;
+  if (batch > 65535) return PALU_ERR_UNSUPPORTED;
+  if (max_len > (1 << 30)) return PALU_ERR_UNSUPPORTED;      // positions of the angle table
+  c->batch = batch;
+  c->prefix = prefix;
+  c->max_len = max_len;
+  c->window = window;
+  c->n_sink = window > 0 ? n_sink : 0;
+  plan_paged(m, m.qpk, batch, paged_max_tiles(max_len, prefix, window, c->n_sink), &c->own);
+  plan_paged(m, batch * m.qpk, 1, ceil_div(prefix, kPagedTile), &c->shared);
+  c->shared_at = paged_part_bytes(c->own, batch, &c->own_ml);
+  c->total = c->shared_at + paged_part_bytes(c->shared, 1, &c->shared_ml);
+  if (c->total < kAlign) c->total = kAlign;
+  for (const PagedPlan* p : {&c->own, &c->shared})
+    for (int i = 0; i < p->n_cls; ++i)
+      if ((long long)p->cls[i].n_units * p->cls[i].n_row_blocks * p->n_slots * (p == &c->own ? batch : 1) > 0x7fffffffLL) return PALU_ERR_UNSUPPORTED;
+  return PALU_OK;
+}
+
+int launch_paged(const PagedPlan& p, PagedArgs& a, int act, int n_seq, bool shared, hipStream_t s) {
+  if (p.n_slots == 0) return PALU_OK;
+  a.meta = p.meta;
+  a.rows = p.rows;
+  a.chunk_tiles = p.chunk_tiles;
+  a.n_slots = p.n_slots;
+  a.o_stride = p.o_stride;
+  for (int i = 0; i < p.n_cls; ++i) {
+    const PagedClass& c = p.cls[i];
+    a.n_units = c.n_units;
+    a.n_row_blocks = c.n_row_blocks;
+    a.block_rows = c.block_rows;
+    std::memcpy(a.units, c.units, sizeof(PagedUnit) * c.n_units);
+    hipLaunchKernelGGL(paged_fn(act, c.nh, c.big_k, c.big_v, c.pt, shared), dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)),
+                       dim3(kPagedThreads), 0, s, a);
+    const int st = launch_ok();
+    if (st != PALU_OK) return st;
+  }
+  return PALU_OK;
+}
+
+int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32_t max_len, int32_t window, int32_t n_sink,
+               const void* q, const int32_t* q_pos, const void* hk, const void* hv, int32_t n_pages, int32_t page_rows,
+               const int32_t* page_table, int32_t table_stride, const int32_t* seq_lens, const void* Bk, const void* Bv,
+               const void* rope_table, int32_t rope_table_len, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  PagedCall c;
+  int st = plan_paged_call(desc, batch, prefix, max_len, window, n_sink, &c);
+  if (st != PALU_OK) return st;
+  if (!q || !hk || !hv || !page_table || !Bk || !Bv || !rope_table || !out || !workspace) return PALU_ERR_INVALID_ARG;
+  if (n_pages <= 0 || page_rows <= 0 || table_stride <= 0) return PALU_ERR_INVALID_ARG;
+  if ((long long)table_stride * page_rows < max_len || rope_table_len < max_len) return PALU_ERR_INVALID_ARG;
+  for (const void* p : {q, hk, hv, Bk, Bv, rope_table, (const void*)out, (const void*)workspace})
+    if (reinterpret_cast<uintptr_t>(p) & 15) return PALU_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)q_pos, (const void*)page_table, (const void*)seq_lens})
+    if (reinterpret_cast<uintptr_t>(p) & 3) return PALU_ERR_INVALID_ARG;
+  if ((page_rows & (page_rows - 1)) != 0 || (long long)n_pages * page_rows > 0x7fffffffLL) return PALU_ERR_UNSUPPORTED;
+  if (workspace_bytes < c.total) return PALU_ERR_WORKSPACE_TOO_SMALL;
+
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const PagedMeta& m = c.own.meta;
+  PagedArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.hk = static_cast<const uint16_t*>(hk);
+  a.hv = static_cast<const uint16_t*>(hv);
+  a.q = static_cast<const uint16_t*>(q);
+  a.Bk = static_cast<const uint16_t*>(Bk);
+  a.rope = static_cast<const float*>(rope_table);
+  a.q_pos = q_pos;
+  a.page_table = page_table;
+  a.seq_lens = seq_lens;
+  a.R_k = m.k_off[m.n_groups];
+  a.R_v = m.v_off[m.n_groups];
+  a.n_pages = n_pages;
+  a.page_shift = __builtin_ctz((unsigned)page_rows);
+  a.table_stride = table_stride;
+  a.rope_len = rope_table_len;
+  a.pos_len = max_len;
+  a.batch = batch;
+  a.scale = (float)(1.4426950408889634 / std::sqrt((double)PALU_D_HEAD));
+
+  PagedMergeArgs e;
+  std::memset(&e, 0, sizeof(e));
+  e.o_part = reinterpret_cast<const float*>(ws);
+  e.ml_part = reinterpret_cast<const float*>(ws + c.own_ml);
+  e.o_shared = reinterpret_cast<const float*>(ws + c.shared_at);
+  e.ml_shared = reinterpret_cast<const float*>(ws + c.shared_at + c.shared_ml);
+
+  a.max_len = prefix;                          // shared tokens: nothing of them is before, and no window
+  a.o_part = const_cast<float*>(e.o_shared);
+  a.ml_part = const_cast<float*>(e.ml_shared);
+  if ((st = launch_paged(c.shared, a, desc->act_dtype, 1, true, s)) != PALU_OK) return st;
+  a.max_len = max_len;
+  a.first = prefix;
+  a.window = c.window;
+  a.n_sink = c.n_sink;
+  a.o_part = const_cast<float*>(e.o_part);
+  a.ml_part = const_cast<float*>(e.ml_part);
+  if ((st = launch_paged(c.own, a, desc->act_dtype, batch, false, s)) != PALU_OK) return st;
+
+  e.Bv = static_cast<const uint16_t*>(Bv);
+  e.seq_lens = seq_lens;
+  e.out = static_cast<uint16_t*>(out);
+  e.max_len = max_len;
+  e.first = prefix;
+  e.window = c.window;
+  e.n_sink = c.n_sink;
+  e.batch = batch;
+  e.chunk_tiles = c.own.chunk_tiles;
+  e.n_slots = c.own.n_slots;
+  e.o_stride = c.own.o_stride;
+  e.n_shared = c.shared.n_slots;
+  e.o_shared_stride = c.shared.o_stride;
+  e.meta = m;
+  hipLaunchKernelGGL(paged_merge_fn(desc->act_dtype), dim3((unsigned)ceil_div(batch * m.qpk, 16), (unsigned)m.n_heads), dim3(256), 0, s, e);
+  return launch_ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+int palu_attn_paged_workspace_bytes(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window, int32_t n_sink,
+                                    size_t* out_bytes) {
+  PagedCall c;
+  const int st = plan_paged_call(desc, batch, 0, max_len, window, n_sink, &c);
+  if (st != PALU_OK) return st;
+  if (!out_bytes) return PALU_ERR_INVALID_ARG;
+  *out_bytes = c.total;
+  return PALU_OK;
+}
+
+int palu_attn_paged(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window, int32_t n_sink,
+                    const void* q, const int32_t* q_pos, const void* hk, const void* hv, int32_t n_pages, int32_t page_rows,
+                    const int32_t* page_table, int32_t table_stride, const int32_t* seq_lens, const void* Bk, const void* Bv,
+                    const void* rope_table, int32_t rope_table_len, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return paged_impl(desc, batch, 0, max_len, window, n_sink, q, q_pos, hk, hv, n_pages, page_rows, page_table, table_stride, seq_lens,
+                    Bk, Bv, rope_table, rope_table_len, out, workspace, workspace_bytes, stream);
+}
+
+int palu_attn_prefix_workspace_bytes(const palu_layer_desc* desc, int32_t batch, int32_t prefix_len, int32_t max_len, size_t* out_bytes) {
+  PagedCall c;
+  const int st = plan_paged_call(desc, batch, prefix_len, max_len, 0, 0, &c);
+  if (st != PALU_OK) return st;
+  if (!out_bytes) return PALU_ERR_INVALID_ARG;
+  *out_bytes = c.total;
+  return PALU_OK;
+}
+
+int palu_attn_prefix(const palu_layer_desc* desc, int32_t batch, int32_t prefix_len, int32_t max_len,
+                     const void* q, const int32_t* q_pos, const void* hk, const void* hv, int32_t n_pages, int32_t page_rows,
+                     const int32_t* page_table, int32_t table_stride, const int32_t* seq_lens, const void* Bk, const void* Bv,
+                     const void* rope_table, int32_t rope_table_len, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return paged_impl(desc, batch, prefix_len, max_len, 0, 0, q, q_pos, hk, hv, n_pages, page_rows, page_table, table_stride, seq_lens,
+                    Bk, Bv, rope_table, rope_table_len, out, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"
