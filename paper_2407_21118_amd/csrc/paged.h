@@ -5,7 +5,7 @@
 
 namespace palu {
 
-constexpr int kPagedTile = 64;                 // tokens per tile: positions 64 i .. 64 i + 63
+constexpr int kPagedTile = 32;                 // tokens per tile: positions 32 i .. 32 i + 31
 constexpr int kPagedThreads = 512;             // eight wavefronts, two per SIMD
 
 // Layer metadata; heads are KEY/VALUE heads here.  Everything indexed by the group is 32 bits wide: beside an array of 16-bit
@@ -44,13 +44,48 @@ __host__ __device__ __forceinline__ PagedSpan paged_span(int L, int first, int w
   return s;
 }
 
-// A unit: up to four adjacent key/value heads of one group whose keys one workgroup rebuilds.
+// A unit: up to four adjacent key/value heads whose keys one workgroup rebuilds, of one group or of several adjacent ones
+// of equal ranks and size, whose latents lie side by side.
 struct PagedUnit {
-  uint32_t bits;                               // first head | heads << 8 | group << 16
+  uint32_t bits;                               // first head | heads << 8 | group of the first << 16 | groups << 24
   __host__ __device__ int h0() const { return bits & 255; }
   __host__ __device__ int nh() const { return (bits >> 8) & 255; }
-  __host__ __device__ int group() const { return bits >> 16; }
+  __host__ __device__ int group() const { return (bits >> 16) & 255; }
+  __host__ __device__ int n_groups() const { return bits >> 24; }
 };
+
+// LDS of a workgroup, in bytes from its start; rows: packed query rows.  Tiles are staged n_stages deep.
+struct PagedLds {
+  int k_pieces, v_pieces;                      // 16-byte pieces per staged row, padding included
+  int q_pitch;                                 // bytes per packed query row
+  int stage_k, stage_v;                        // bytes per staged tile
+  int k, v, base, ang, entries, q, s, p, alpha, total;
+};
+constexpr int kPagedScorePitch = 36;           // floats per row of scores: a tile and 16 bytes
+constexpr int kPagedProbPitch = 144;           // bytes per row of probabilities: hi, lo and 16 bytes
+constexpr int kPagedAngPitch = kDHead + 4;     // floats per token of the angles of the first 16 positions
+constexpr int kPagedMaxStages = 8;
+constexpr int kPagedEntrySlots = 16;           // tiles whose page-table entries are held
+__host__ __device__ __forceinline__ PagedLds paged_lds(int k_cols, int v_cols, int rows, int row_tiles, int planes, bool pairs, bool pipelined, bool ang, int n_stages) {
+  PagedLds l;
+  l.k_pieces = (k_cols / 8 + 7) & ~7;
+  l.v_pieces = (v_cols / 8 + 15) & ~15;
+  l.q_pitch = kDHead * 2 * (pairs ? 2 : 1) + 16;
+  l.stage_k = kPagedTile * l.k_pieces * 16;
+  l.stage_v = kPagedTile * l.v_pieces * 16;
+  l.k = 0;
+  l.v = l.k + n_stages * l.stage_k;
+  l.base = l.v + n_stages * l.stage_v;
+  l.ang = l.base + n_stages * (kPagedTile / 16) * kDHead * 4;
+  l.entries = l.ang + (ang ? 16 * kPagedAngPitch * 4 : 0);
+  l.q = l.entries + kPagedEntrySlots * kPagedTile * 4;
+  l.s = l.q + (rows * l.q_pitch + 15) / 16 * 16;
+  l.p = l.s + (pipelined ? 2 : 1) * planes * row_tiles * 16 * kPagedScorePitch * 4;
+  l.alpha = l.p + (pipelined ? 2 : 1) * row_tiles * 16 * kPagedProbPitch;
+  l.total = l.alpha + (pipelined ? 2 : 1) * row_tiles * 16 * 4;
+  return l;
+}
+constexpr int kPagedLdsBytes = 160 * 1024;     // of a compute unit
 
 struct PagedArgs {
   const uint16_t* hk;                          // [n_pages * page_rows, R_k]
@@ -72,6 +107,8 @@ struct PagedArgs {
   int rows;                                    // query rows per key/value head: qpk, or batch * qpk where the tokens are shared
   int n_row_blocks, block_rows;
   int chunk_tiles;                             // tiles per workgroup, at most
+  int n_stages;                                // tiles staged in LDS
+  int shared;                                  // the tokens are those of the shared prefix
   int n_slots;                                 // partial results per sequence, or of the shared tokens
   long long o_stride;                          // floats of o_part per slot
   float scale;                                 // log2(e) / sqrt(128)
@@ -96,9 +133,14 @@ struct PagedMergeArgs {
 };
 
 using PagedFn = void (*)(PagedArgs);
-// The instantiation for units of at most nh heads (4, 2, 1); big_k, big_v: ranks above 256; pt: tiles of 16 packed query rows
-// (nh * block_rows of them at most); shared: the tokens are those of a prefix, the rows all sequences'
-PagedFn paged_fn(int act, int nh, bool big_k, bool big_v, int pt, bool shared);
+// The instantiations: nh: heads per unit, at most (4 or 2); fq: wavefronts that share a head's features; pt: tiles of 16 packed query
+// rows; vb: blocks of 256 value columns
+struct PagedForm {
+  int nh, fq, pt, vb;
+  bool pipelined() const { return pt == 1 && fq == 2; }
+  bool ang() const { return !pipelined(); }
+};
+PagedFn paged_fn(int act, const PagedForm& f);
 using PagedMergeFn = void (*)(PagedMergeArgs);
 PagedMergeFn paged_merge_fn(int act);
 

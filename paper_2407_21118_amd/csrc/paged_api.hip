@@ -4,10 +4,10 @@
 
 namespace {
 
-// Key/value heads of one rank class, cut into units: one launch of paged_kernel.
+// Units that one launch of paged_kernel takes: key/value heads of one rank class.
 struct PagedClass {
-  bool big_k, big_v;
-  int nh, pt;                              // heads per unit, tiles of 16 packed query rows
+  PagedForm form;
+  int n_stages, lds_bytes;
   int n_row_blocks, block_rows;
   int n_units;
   PagedUnit units[PALU_MAX_HEADS];
@@ -46,42 +46,60 @@ int check_paged_desc(const palu_layer_desc* desc, PagedMeta* pm) {
   return PALU_OK;
 }
 
-// batch: sequences whose tokens are attended one by one (1 where they are shared); max_tiles: tiles of 64 tokens of the longest
-void plan_paged(const PagedMeta& m, int rows, int batch, int max_tiles, PagedPlan* p) {
+// batch: sequences whose tokens are attended one by one (1 where they are shared); max_tiles: tiles of the longest
+int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, PagedPlan* p) {
   p->meta = m;
   p->rows = rows;
   p->n_cls = 0;
   long long wgs = 0;
   int sum_rv = 0;
-  for (int j = 0; j < m.n_groups; ++j) sum_rv += (m.head_off[j + 1] - m.head_off[j]) * (m.v_off[j + 1] - m.v_off[j]);
+  auto rk = [&](int j) { return m.k_off[j + 1] - m.k_off[j]; };
+  auto rv = [&](int j) { return m.v_off[j + 1] - m.v_off[j]; };
+  auto heads = [&](int j) { return m.head_off[j + 1] - m.head_off[j]; };
+  for (int j = 0; j < m.n_groups; ++j) sum_rv += heads(j) * rv(j);
   for (int cls = 0; cls < 4; ++cls) {
     const bool big_k = (cls & 1) != 0, big_v = (cls & 2) != 0;
-    int most = 0;                              // heads in a group of the class
-    auto in_class = [&](int j) { return (m.k_off[j + 1] - m.k_off[j] > 256) == big_k && (m.v_off[j + 1] - m.v_off[j] > 256) == big_v; };
-    for (int j = 0; j < m.n_groups; ++j)
-      if (in_class(j)) most = std::max(most, m.head_off[j + 1] - m.head_off[j]);
-    if (!most) continue;
+    auto in_class = [&](int j) { return (rk(j) > 256) == big_k && (rv(j) > 256) == big_v; };
+    int any = 0;
+    for (int j = 0; j < m.n_groups; ++j) any += in_class(j);
+    if (!any) continue;
     PagedClass& c = p->cls[p->n_cls++];
-    c.big_k = big_k;
-    c.big_v = big_v;
     // A unit of more heads reads its latents once for all of them; a unit of more rows rebuilds its keys once for all of those.
-    const int row_limit = big_k ? 32 : 64;     // packed rows
-    c.nh = big_k ? (most >= 2 ? 2 : 1) : (most >= 3 ? 4 : most);
-    while (c.nh > 1 && c.nh * rows > row_limit) c.nh /= 2;
-    c.n_row_blocks = ceil_div(rows, row_limit / c.nh);
+    const int row_limit = big_k ? 16 : (big_v ? 32 : 64);    // packed rows: the accumulators of so many fit beside the weights
+    c.form.fq = big_k ? 4 : 2;
+    c.form.vb = big_v ? 2 : 1;
+    c.form.nh = !big_k && 4 * rows <= row_limit ? 4 : 2;
+    c.n_row_blocks = ceil_div(rows, row_limit / c.form.nh);
     c.block_rows = ceil_div(rows, c.n_row_blocks);
-    c.pt = c.nh * c.block_rows <= 16 ? 1 : row_limit / 16;
+    c.form.pt = c.form.nh * c.block_rows <= 16 ? 1 : row_limit / 16;
+    // Units: whole adjacent groups of equal ranks and size side by side, as far as 256 columns and the heads go (ranks in whole 64s:
+    // the staged rows' layout), else parts of one group.  [first unit of a run of groups, heads already taken]
     c.n_units = 0;
-    for (int first = 0;; first += c.nh) {      // round robin over the groups: neighbouring workgroups, which go to different L2 caches,
-      bool any = false;                        // take different groups, and the units of one group meet in one
+    int k_cols = 0, v_cols = 0;
+    for (int first = 0;; first += c.form.nh) {               // round robin over the groups: neighbouring workgroups, which go to different
+      bool more = false;                                     // L2 caches, take different groups, and the units of one group meet in one
       for (int j = 0; j < m.n_groups; ++j) {
-        const int s = m.head_off[j + 1] - m.head_off[j];
-        if (!in_class(j) || first >= s) continue;
-        any = true;
-        c.units[c.n_units++].bits = (uint32_t)(m.head_off[j] + first) | (uint32_t)std::min(c.nh, s - first) << 8 | (uint32_t)j << 16;
+        if (!in_class(j) || first >= heads(j)) continue;
+        int n = 1;
+        if (rk(j) % 64 == 0)
+          while (j + n < m.n_groups && rk(j + n) == rk(j) && rv(j + n) == rv(j) && heads(j + n) == heads(j) && (n + 1) * heads(j) <= c.form.nh &&
+                 (n + 1) * rk(j) <= 256 && (n + 1) * rv(j) <= 256)
+            ++n;
+        more = true;
+        const int nh = std::min(c.form.nh, n * heads(j) - first);
+        c.units[c.n_units++].bits = (uint32_t)(m.head_off[j] + first) | (uint32_t)nh << 8 | (uint32_t)j << 16 | (uint32_t)n << 24;
+        k_cols = std::max(k_cols, n * rk(j));
+        v_cols = std::max(v_cols, n * rv(j));
+        j += n - 1;
       }
-      if (!any) break;
+      if (!more) break;
     }
+    const int packed = c.form.nh * c.block_rows;
+    auto lds_bytes = [&](int stages) { return paged_lds(k_cols, v_cols, packed, c.form.pt, c.form.fq, act == PALU_F16, c.form.pipelined(), c.form.ang(), stages).total; };
+    c.n_stages = 2;
+    while (c.n_stages < kPagedMaxStages && lds_bytes(c.n_stages + 1) <= kPagedLdsBytes) ++c.n_stages;
+    c.lds_bytes = lds_bytes(c.n_stages);
+    if (c.lds_bytes > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;
     wgs += (long long)c.n_units * c.n_row_blocks;
   }
   wgs *= batch;
@@ -89,20 +107,21 @@ void plan_paged(const PagedMeta& m, int rows, int batch, int max_tiles, PagedPla
   p->ml_stride = (long long)rows * m.n_heads * 2;
   p->chunk_tiles = 1;
   p->n_slots = 0;
-  if (max_tiles <= 0) return;
-  // Tiles per workgroup: one workgroup is resident per compute unit, and loading its weights costs about as much as two tiles.
+  if (max_tiles <= 0) return PALU_OK;
+  // Tiles per workgroup: one workgroup is resident per compute unit, and loading its weights costs about as much as four tiles.
   const int cus = device_cu_count();
   double best = 1e300;
   for (int n = 1; n <= max_tiles && n <= 1024; ++n) {
     const int tiles = ceil_div(max_tiles, n);
     const double rounds = (double)((wgs * ceil_div(max_tiles, tiles) + cus - 1) / cus);
-    const double cost = rounds * (2.0 + tiles) + 0.05 * n;
+    const double cost = rounds * (4.0 + tiles) + 0.05 * n;
     if (cost < best) {
       best = cost;
       p->chunk_tiles = tiles;
     }
   }
   p->n_slots = ceil_div(max_tiles, p->chunk_tiles);
+  return PALU_OK;
 }
 
 // the largest number of tiles that a sequence of up to max_len rows has
@@ -135,8 +154,9 @@ int plan_paged_call(const palu_layer_desc* desc, int batch, int prefix, int max_
   c->max_len = max_len;
   c->window = window;
   c->n_sink = window > 0 ? n_sink : 0;
-  plan_paged(m, m.qpk, batch, paged_max_tiles(max_len, prefix, window, c->n_sink), &c->own);
-  plan_paged(m, batch * m.qpk, 1, ceil_div(prefix, kPagedTile), &c->shared);
+  int st2 = plan_paged(m, desc->act_dtype, m.qpk, batch, paged_max_tiles(max_len, prefix, window, c->n_sink), &c->own);
+  if (st2 == PALU_OK) st2 = plan_paged(m, desc->act_dtype, batch * m.qpk, 1, ceil_div(prefix, kPagedTile), &c->shared);
+  if (st2 != PALU_OK) return st2;
   c->shared_at = paged_part_bytes(c->own, batch, &c->own_ml);
   c->total = c->shared_at + paged_part_bytes(c->shared, 1, &c->shared_ml);
   if (c->total < kAlign) c->total = kAlign;
@@ -159,8 +179,11 @@ int launch_paged(const PagedPlan& p, PagedArgs& a, int act, int n_seq, bool shar
     a.n_row_blocks = c.n_row_blocks;
     a.block_rows = c.block_rows;
     std::memcpy(a.units, c.units, sizeof(PagedUnit) * c.n_units);
-    hipLaunchKernelGGL(paged_fn(act, c.nh, c.big_k, c.big_v, c.pt, shared), dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)),
-                       dim3(kPagedThreads), 0, s, a);
+    a.n_stages = c.n_stages;
+    a.shared = shared;
+    const PagedFn fn = paged_fn(act, c.form);
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, kPagedLdsBytes) != hipSuccess) return PALU_ERR_HIP;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)), dim3(kPagedThreads), (unsigned)c.lds_bytes, s, a);
     const int st = launch_ok();
     if (st != PALU_OK) return st;
   }
