@@ -6,7 +6,8 @@
 namespace palu {
 
 constexpr int kPagedTile = 32;                 // tokens per tile: positions 32 i .. 32 i + 31
-constexpr int kPagedThreads = 512;             // eight wavefronts, two per SIMD
+constexpr int kPagedThreads = 256;             // four wavefronts, one per SIMD
+constexpr int kPagedWideThreads = 512;
 
 // Layer metadata; heads are KEY/VALUE heads here.  Everything indexed by the group is 32 bits wide: beside an array of 16-bit
 // numbers with the same index the compiler addresses these from a base that lies on no whole word, and scalar loads drop its low bits.
@@ -54,20 +55,50 @@ struct PagedUnit {
   __host__ __device__ int n_groups() const { return bits >> 24; }
 };
 
-// LDS of a workgroup, in bytes from its start; rows: packed query rows.  Tiles are staged n_stages deep.
+constexpr int kPagedProbPitch = 144;           // bytes per row of probabilities: a tile's hi, its lo and 16 bytes
+constexpr int kPagedMaxStages = 8;
+constexpr int kPagedEntrySlots = 16;           // tiles whose page-table entries are held
+constexpr int kPagedRowSlots = 8;              // ... and whose tokens' rows of the cache
+constexpr int kPagedLdsBytes = 160 * 1024;     // of a compute unit
+
+// LDS of a workgroup of paged_kernel, in bytes from its start.  Tiles are staged n_stages deep, rows in 16-byte
+// pieces, as many of them as a power of two (at least 8, of values 16).
 struct PagedLds {
-  int k_pieces, v_pieces;                      // 16-byte pieces per staged row, padding included
+  int k_pieces, v_pieces;                      // per staged row, padding included
   int q_pitch;                                 // bytes per packed query row
   int stage_k, stage_v;                        // bytes per staged tile
+  int k, v, base, entries, rows, q, p, alpha, total;
+};
+// n_groups groups of the unit, ks steps of 32 key channels each; rows: packed query rows, in row_tiles tiles of 16
+__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, bool pairs, int n_stages) {
+  PagedLds l;
+  l.k_pieces = n_groups * ks * 4 <= 8 ? 8 : (n_groups * ks * 4 <= 16 ? 16 : 32);
+  l.v_pieces = v_cols <= 128 ? 16 : (v_cols <= 256 ? 32 : 64);
+  l.q_pitch = kDHead * 2 * (pairs ? 2 : 1) + 16;
+  l.stage_k = kPagedTile * l.k_pieces * 16;
+  l.stage_v = kPagedTile * l.v_pieces * 16;
+  l.k = 0;
+  l.v = l.k + n_stages * l.stage_k;
+  l.base = l.v + n_stages * l.stage_v;
+  l.entries = l.base + (n_stages + 1) * (kPagedTile / 16) * kDHead * 4;
+  l.rows = l.entries + kPagedEntrySlots * kPagedTile * 4;
+  l.q = l.rows + kPagedRowSlots * kPagedTile * 4;
+  l.p = l.q + rows * l.q_pitch;
+  l.alpha = l.p + 2 * (row_tiles * 16 + 1) * kPagedProbPitch;
+  l.total = l.alpha + 2 * (row_tiles * 16 + 4) * 4;
+  return l;
+}
+
+// ... of paged_wide_kernel (key ranks above 256).
+struct PagedWideLds {
+  int k_pieces, v_pieces, q_pitch, stage_k, stage_v;
   int k, v, base, ang, entries, q, s, p, alpha, total;
 };
 constexpr int kPagedScorePitch = 36;           // floats per row of scores: a tile and 16 bytes
-constexpr int kPagedProbPitch = 144;           // bytes per row of probabilities: hi, lo and 16 bytes
 constexpr int kPagedAngPitch = kDHead + 4;     // floats per token of the angles of the first 16 positions
-constexpr int kPagedMaxStages = 8;
-constexpr int kPagedEntrySlots = 16;           // tiles whose page-table entries are held
-__host__ __device__ __forceinline__ PagedLds paged_lds(int k_cols, int v_cols, int rows, int row_tiles, int planes, bool pairs, bool pipelined, bool ang, int n_stages) {
-  PagedLds l;
+constexpr int kPagedWideParts = 4;             // wavefronts that share a head's features
+__host__ __device__ __forceinline__ PagedWideLds paged_wide_lds(int k_cols, int v_cols, int rows, bool pairs, int n_stages) {
+  PagedWideLds l;
   l.k_pieces = (k_cols / 8 + 7) & ~7;
   l.v_pieces = (v_cols / 8 + 15) & ~15;
   l.q_pitch = kDHead * 2 * (pairs ? 2 : 1) + 16;
@@ -77,15 +108,14 @@ __host__ __device__ __forceinline__ PagedLds paged_lds(int k_cols, int v_cols, i
   l.v = l.k + n_stages * l.stage_k;
   l.base = l.v + n_stages * l.stage_v;
   l.ang = l.base + n_stages * (kPagedTile / 16) * kDHead * 4;
-  l.entries = l.ang + (ang ? 16 * kPagedAngPitch * 4 : 0);
+  l.entries = l.ang + 16 * kPagedAngPitch * 4;
   l.q = l.entries + kPagedEntrySlots * kPagedTile * 4;
   l.s = l.q + (rows * l.q_pitch + 15) / 16 * 16;
-  l.p = l.s + (pipelined ? 2 : 1) * planes * row_tiles * 16 * kPagedScorePitch * 4;
-  l.alpha = l.p + (pipelined ? 2 : 1) * row_tiles * 16 * kPagedProbPitch;
-  l.total = l.alpha + (pipelined ? 2 : 1) * row_tiles * 16 * 4;
+  l.p = l.s + kPagedWideParts * 16 * kPagedScorePitch * 4;
+  l.alpha = l.p + 16 * kPagedProbPitch;
+  l.total = l.alpha + 16 * 4;
   return l;
 }
-constexpr int kPagedLdsBytes = 160 * 1024;     // of a compute unit
 
 struct PagedArgs {
   const uint16_t* hk;                          // [n_pages * page_rows, R_k]
@@ -133,15 +163,14 @@ struct PagedMergeArgs {
 };
 
 using PagedFn = void (*)(PagedArgs);
-// The instantiations: nh: heads per unit, at most (4 or 2); fq: wavefronts that share a head's features; pt: tiles of 16 packed query
-// rows; vb: blocks of 256 value columns
+// The instantiations of paged_kernel: ks: steps of 32 key channels (2, 4, 6 or 8); pt: tiles of 16 packed query rows; vb: blocks
+// of 256 value columns.  ks = 0: paged_wide_kernel, for key ranks above 256
 struct PagedForm {
-  int nh, fq, pt, vb;
-  bool pipelined() const { return pt == 1 && fq == 2; }
-  bool ang() const { return !pipelined(); }
+  int ks, pt, vb;
 };
-PagedFn paged_fn(int act, const PagedForm& f);
+template <typename T> PagedFn paged_form(const PagedForm& f);
+template <typename T> PagedFn paged_wide_form(int vb);
 using PagedMergeFn = void (*)(PagedMergeArgs);
-PagedMergeFn paged_merge_fn(int act);
+template <typename T> PagedMergeFn paged_merge_form();
 
 }  // namespace palu

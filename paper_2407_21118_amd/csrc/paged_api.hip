@@ -4,7 +4,7 @@
 
 namespace {
 
-// Units that one launch of paged_kernel takes: key/value heads of one rank class.
+// Units that one launch takes: key/value heads of one rank class.
 struct PagedClass {
   PagedForm form;
   int n_stages, lds_bytes;
@@ -12,11 +12,12 @@ struct PagedClass {
   int n_units;
   PagedUnit units[PALU_MAX_HEADS];
 };
+constexpr int kPagedMaxClasses = 10;       // steps of key channels 2, 4, 6, 8 or above, value columns up to 256 or above
 struct PagedPlan {
   PagedMeta meta;
   int rows;                                // query rows per key/value head
   int n_cls;
-  PagedClass cls[4];
+  PagedClass cls[kPagedMaxClasses];
   int chunk_tiles, n_slots;                // 0 slots: nothing to attend
   long long o_stride, ml_stride;           // floats per slot
 };
@@ -57,45 +58,51 @@ int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, 
   auto rv = [&](int j) { return m.v_off[j + 1] - m.v_off[j]; };
   auto heads = [&](int j) { return m.head_off[j + 1] - m.head_off[j]; };
   for (int j = 0; j < m.n_groups; ++j) sum_rv += heads(j) * rv(j);
-  for (int cls = 0; cls < 4; ++cls) {
-    const bool big_k = (cls & 1) != 0, big_v = (cls & 2) != 0;
-    auto in_class = [&](int j) { return (rk(j) > 256) == big_k && (rv(j) > 256) == big_v; };
-    int any = 0;
-    for (int j = 0; j < m.n_groups; ++j) any += in_class(j);
-    if (!any) continue;
+  auto steps = [&](int j) { return rk(j) > 256 ? 0 : (rk(j) / 32 + 1) / 2 * 2; };
+  for (int cls = 0; cls < kPagedMaxClasses; ++cls) {
+    const int ks = cls % 5 * 2, vb = cls / 5 + 1;
+    auto in_class = [&](int j) { return steps(j) == ks && (rv(j) > 256) == (vb == 2); };
+    int most = 0;                                            // heads in a unit
+    for (int j = 0; j < m.n_groups; ++j)
+      if (in_class(j)) most = std::max(most, heads(j));
+    if (!most) continue;
     PagedClass& c = p->cls[p->n_cls++];
-    // A unit of more heads reads its latents once for all of them; a unit of more rows rebuilds its keys once for all of those.
-    const int row_limit = big_k ? 16 : (big_v ? 32 : 64);    // packed rows: the accumulators of so many fit beside the weights
-    c.form.fq = big_k ? 4 : 2;
-    c.form.vb = big_v ? 2 : 1;
-    c.form.nh = !big_k && 4 * rows <= row_limit ? 4 : 2;
-    c.n_row_blocks = ceil_div(rows, row_limit / c.form.nh);
-    c.block_rows = ceil_div(rows, c.n_row_blocks);
-    c.form.pt = c.form.nh * c.block_rows <= 16 ? 1 : row_limit / 16;
     // Units: whole adjacent groups of equal ranks and size side by side, as far as 256 columns and the heads go (ranks in whole 64s:
-    // the staged rows' layout), else parts of one group.  [first unit of a run of groups, heads already taken]
+    // the staged rows' layout), else parts of one group.  A unit of more heads reads its latents once for all of them.
+    const int unit_heads = ks ? 4 : 2;
     c.n_units = 0;
-    int k_cols = 0, v_cols = 0;
-    for (int first = 0;; first += c.form.nh) {               // round robin over the groups: neighbouring workgroups, which go to different
+    int k_groups = 1, k_cols = 0, v_cols = 0;
+    most = std::min(most, unit_heads);
+    for (int first = 0;; first += unit_heads) {              // round robin over the groups: neighbouring workgroups, which go to different
       bool more = false;                                     // L2 caches, take different groups, and the units of one group meet in one
       for (int j = 0; j < m.n_groups; ++j) {
         if (!in_class(j) || first >= heads(j)) continue;
         int n = 1;
-        if (rk(j) % 64 == 0)
-          while (j + n < m.n_groups && rk(j + n) == rk(j) && rv(j + n) == rv(j) && heads(j + n) == heads(j) && (n + 1) * heads(j) <= c.form.nh &&
+        if (ks && rk(j) % 64 == 0)
+          while (j + n < m.n_groups && rk(j + n) == rk(j) && rv(j + n) == rv(j) && heads(j + n) == heads(j) && (n + 1) * heads(j) <= unit_heads &&
                  (n + 1) * rk(j) <= 256 && (n + 1) * rv(j) <= 256)
             ++n;
         more = true;
-        const int nh = std::min(c.form.nh, n * heads(j) - first);
+        const int nh = std::min(unit_heads, n * heads(j) - first);
         c.units[c.n_units++].bits = (uint32_t)(m.head_off[j] + first) | (uint32_t)nh << 8 | (uint32_t)j << 16 | (uint32_t)n << 24;
-        k_cols = std::max(k_cols, n * rk(j));
+        k_groups = std::max(k_groups, n);
+        k_cols = std::max(k_cols, rk(j));
         v_cols = std::max(v_cols, n * rv(j));
+        most = std::max(most, nh);
         j += n - 1;
       }
       if (!more) break;
     }
-    const int packed = c.form.nh * c.block_rows;
-    auto lds_bytes = [&](int stages) { return paged_lds(k_cols, v_cols, packed, c.form.pt, c.form.fq, act == PALU_F16, c.form.pipelined(), c.form.ang(), stages).total; };
+    // Query rows: 16 per head and, as far as accumulators go, 64 in all (32 beside two blocks of value columns)
+    const int row_limit = std::min(16, (ks ? (vb == 1 ? 64 : 32) : 16) / most);
+    c.n_row_blocks = ceil_div(rows, row_limit);
+    c.block_rows = ceil_div(rows, c.n_row_blocks);
+    const int packed = most * c.block_rows;
+    c.form = PagedForm{ks, packed <= 16 ? 1 : (vb == 1 ? 4 : 2), vb};
+    auto lds_bytes = [&](int stages) {
+      const bool pairs = act == PALU_F16;
+      return ks ? paged_lds(k_groups, ks, v_cols, packed, c.form.pt, pairs, stages).total : paged_wide_lds(k_cols, v_cols, packed, pairs, stages).total;
+    };
     c.n_stages = 2;
     while (c.n_stages < kPagedMaxStages && lds_bytes(c.n_stages + 1) <= kPagedLdsBytes) ++c.n_stages;
     c.lds_bytes = lds_bytes(c.n_stages);
@@ -181,11 +188,14 @@ int launch_paged(const PagedPlan& p, PagedArgs& a, int act, int n_seq, bool shar
     std::memcpy(a.units, c.units, sizeof(PagedUnit) * c.n_units);
     a.n_stages = c.n_stages;
     a.shared = shared;
-    const PagedFn fn = paged_fn(act, c.form);
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, kPagedLdsBytes) != hipSuccess) return PALU_ERR_HIP;
-    hipLaunchKernelGGL(fn, dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)), dim3(kPagedThreads), (unsigned)c.lds_bytes, s, a);
-    const int st = launch_ok();
+    const bool wide = c.form.ks == 0;
+    const PagedFn fn = wide ? (act == PALU_F16 ? paged_wide_form<F16>(c.form.vb) : paged_wide_form<BF16>(c.form.vb))
+                            : (act == PALU_F16 ? paged_form<F16>(c.form) : paged_form<BF16>(c.form));
+    int st = allow_lds(fn, (size_t)c.lds_bytes);
     if (st != PALU_OK) return st;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)), dim3(wide ? kPagedWideThreads : kPagedThreads),
+                       (unsigned)c.lds_bytes, s, a);
+    if ((st = launch_ok()) != PALU_OK) return st;
   }
   return PALU_OK;
 }
@@ -263,7 +273,7 @@ int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32
   e.n_shared = c.shared.n_slots;
   e.o_shared_stride = c.shared.o_stride;
   e.meta = m;
-  hipLaunchKernelGGL(paged_merge_fn(desc->act_dtype), dim3((unsigned)ceil_div(batch * m.qpk, 16), (unsigned)m.n_heads), dim3(256), 0, s, e);
+  hipLaunchKernelGGL(desc->act_dtype == PALU_F16 ? paged_merge_form<F16>() : paged_merge_form<BF16>(), dim3((unsigned)ceil_div(batch * m.qpk, 16), (unsigned)m.n_heads), dim3(256), 0, s, e);
   return launch_ok();
 }
 
