@@ -32,13 +32,14 @@ FLAT = ["-DPALU_SCORE_FLAT=1"]
 
 def sources():
     """(source file, extra flags, object name) of every translation unit."""
-    vgpr = ["score16_shared_forms.hip", "score_forms.hip", "score_forms_lowbit.hip", "score16_forms.hip", "pv.hip", "api.hip", "paged_wide.hip", "paged_merge.hip"]
+    vgpr = ["score16_shared_forms.hip", "score_forms.hip", "score_forms_lowbit.hip", "score16_forms.hip", "pv.hip", "api.hip", "paged_merge.hip"]
     units = [(f, VGPR_FORM, "") for f in vgpr]
     units += [(f, VGPR_FORM + FLAT, "_flat") for f in ("score16_shared_forms.hip", "score16_forms.hip")]
     units += [("attend16_forms.hip", VGPR_FORM, ""), ("attend16_forms.hip", VGPR_FORM + FLAT, "_flat"), ("attend16_forms.hip", VGPR_FORM + ["-DPALU_ATTEND_SHARED=1"], "_shared"),
               ("attend16_forms.hip", VGPR_FORM + ["-DPALU_ATTEND_SHARED=2"], "_shared_few")]
     units += [("attend16_mixed_forms.hip", VGPR_FORM, "")]
-    units += [("paged.hip", VGPR_FORM + ["-DPALU_PAGED_ACT=F16"], ""), ("paged.hip", VGPR_FORM + ["-DPALU_PAGED_ACT=BF16"], "_bf16")]
+    for act, suffix in (("F16", ""), ("BF16", "_bf16")):
+        units += [(f, VGPR_FORM + ["-DPALU_PAGED_ACT=" + act], suffix) for f in ("paged.hip", "paged_rows.hip")]
     units += [("encode_gemm.hip", [], "")]
     return [(os.path.join(CSRC, f), extra, os.path.splitext(f)[0] + suffix + ".o") for f, extra, suffix in units]
 

@@ -6,8 +6,8 @@
 namespace palu {
 
 constexpr int kPagedTile = 32;                 // tokens per tile: positions 32 i .. 32 i + 31
-constexpr int kPagedThreads = 256;             // four wavefronts, one per SIMD
-constexpr int kPagedWideThreads = 512;
+constexpr int kPagedThreads = 512;             // paged_kernel: eight wavefronts, two per SIMD
+constexpr int kPagedRowsThreads = 256;         // paged_rows_kernel: four
 
 // Layer metadata; heads are KEY/VALUE heads here.  Everything indexed by the group is 32 bits wide: beside an array of 16-bit
 // numbers with the same index the compiler addresses these from a base that lies on no whole word, and scalar loads drop its low bits.
@@ -61,18 +61,24 @@ constexpr int kPagedEntrySlots = 16;           // tiles whose page-table entries
 constexpr int kPagedRowSlots = 8;              // ... and whose tokens' rows of the cache
 constexpr int kPagedLdsBytes = 160 * 1024;     // of a compute unit
 
-// LDS of a workgroup of paged_kernel, in bytes from its start.  Tiles are staged n_stages deep, rows in 16-byte
-// pieces, as many of them as a power of two (at least 8, of values 16).
+// LDS of a workgroup, in bytes from its start.  Tiles are staged n_stages deep, rows in 16-byte pieces, as many of them as a power
+// of two (at least 8, of values 16).
 struct PagedLds {
-  int k_pieces, v_pieces;                      // per staged row, padding included
+  int k_pieces, v_pieces;
   int q_pitch;                                 // bytes per packed query row
   int stage_k, stage_v;                        // bytes per staged tile
-  int k, v, base, entries, rows, q, p, alpha, total;
+  int k, v, base, anchors, entries, rows, q, s, p, alpha, total;
 };
-// n_groups groups of the unit, ks steps of 32 key channels each; rows: packed query rows, in row_tiles tiles of 16
-__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, bool pairs, int n_stages) {
+constexpr int kPagedScorePitch = 36;           // floats per row of scores: a tile and 16 bytes
+constexpr int kPagedScoreSlots = 3;            // tiles whose scores are held
+constexpr int kPagedBaseSlots = 3;             // ... and whose first angles
+constexpr int kPagedAnchorTiles = 8;           // every so many tiles their angles come from the table
+// n_groups groups of the unit, ks steps of 32 key channels each; rows: packed query rows, in row_tiles tiles of 16; planes: partial
+// scores that are added up (0: none go through LDS)
+__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, int planes, bool pairs, int n_stages) {
   PagedLds l;
-  l.k_pieces = n_groups * ks * 4 <= 8 ? 8 : (n_groups * ks * 4 <= 16 ? 16 : 32);
+  const int k_pieces = n_groups * ks * 4;
+  l.k_pieces = k_pieces <= 8 ? 8 : (k_pieces <= 16 ? 16 : (k_pieces <= 32 ? 32 : 64));
   l.v_pieces = v_cols <= 128 ? 16 : (v_cols <= 256 ? 32 : 64);
   l.q_pitch = kDHead * 2 * (pairs ? 2 : 1) + 16;
   l.stage_k = kPagedTile * l.k_pieces * 16;
@@ -80,40 +86,14 @@ __host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int
   l.k = 0;
   l.v = l.k + n_stages * l.stage_k;
   l.base = l.v + n_stages * l.stage_v;
-  l.entries = l.base + (n_stages + 1) * (kPagedTile / 16) * kDHead * 4;
+  l.anchors = l.base + kPagedBaseSlots * (kPagedTile / 16) * kDHead * 4;
+  l.entries = l.anchors + kPagedMaxStages * kDHead * 4;
   l.rows = l.entries + kPagedEntrySlots * kPagedTile * 4;
   l.q = l.rows + kPagedRowSlots * kPagedTile * 4;
-  l.p = l.q + rows * l.q_pitch;
+  l.s = l.q + rows * l.q_pitch;
+  l.p = l.s + kPagedScoreSlots * planes * (rows + 1) * kPagedScorePitch * 4;
   l.alpha = l.p + 2 * (row_tiles * 16 + 1) * kPagedProbPitch;
   l.total = l.alpha + 2 * (row_tiles * 16 + 4) * 4;
-  return l;
-}
-
-// ... of paged_wide_kernel (key ranks above 256).
-struct PagedWideLds {
-  int k_pieces, v_pieces, q_pitch, stage_k, stage_v;
-  int k, v, base, ang, entries, q, s, p, alpha, total;
-};
-constexpr int kPagedScorePitch = 36;           // floats per row of scores: a tile and 16 bytes
-constexpr int kPagedAngPitch = kDHead + 4;     // floats per token of the angles of the first 16 positions
-constexpr int kPagedWideParts = 4;             // wavefronts that share a head's features
-__host__ __device__ __forceinline__ PagedWideLds paged_wide_lds(int k_cols, int v_cols, int rows, bool pairs, int n_stages) {
-  PagedWideLds l;
-  l.k_pieces = (k_cols / 8 + 7) & ~7;
-  l.v_pieces = (v_cols / 8 + 15) & ~15;
-  l.q_pitch = kDHead * 2 * (pairs ? 2 : 1) + 16;
-  l.stage_k = kPagedTile * l.k_pieces * 16;
-  l.stage_v = kPagedTile * l.v_pieces * 16;
-  l.k = 0;
-  l.v = l.k + n_stages * l.stage_k;
-  l.base = l.v + n_stages * l.stage_v;
-  l.ang = l.base + n_stages * (kPagedTile / 16) * kDHead * 4;
-  l.entries = l.ang + 16 * kPagedAngPitch * 4;
-  l.q = l.entries + kPagedEntrySlots * kPagedTile * 4;
-  l.s = l.q + (rows * l.q_pitch + 15) / 16 * 16;
-  l.p = l.s + kPagedWideParts * 16 * kPagedScorePitch * 4;
-  l.alpha = l.p + 16 * kPagedProbPitch;
-  l.total = l.alpha + 16 * 4;
   return l;
 }
 
@@ -163,13 +143,17 @@ struct PagedMergeArgs {
 };
 
 using PagedFn = void (*)(PagedArgs);
-// The instantiations of paged_kernel: ks: steps of 32 key channels (2, 4, 6 or 8); pt: tiles of 16 packed query rows; vb: blocks
-// of 256 value columns.  ks = 0: paged_wide_kernel, for key ranks above 256
+// The instantiations: paged_kernel (up to 16 packed query rows) by ks: steps of 32 key channels, 2, 4, 6, 8 (units of up to four heads), 12
+// or 16 (of two), and vb: blocks of 256 value columns; paged_rows_kernel (many: up to 16 rows per head, ks up to 8) likewise
 struct PagedForm {
-  int ks, pt, vb;
+  int ks, vb;
+  bool many;
+  int parts() const { return ks > 8 ? 4 : 2; }           // paged_kernel: wavefronts that share a head's features
+  int unit_heads() const { return 8 / parts(); }
+  int max_rows() const { return many ? (vb == 1 ? 64 : 32) : 16; }   // packed
 };
 template <typename T> PagedFn paged_form(const PagedForm& f);
-template <typename T> PagedFn paged_wide_form(int vb);
+template <typename T> PagedFn paged_rows_form(const PagedForm& f);
 using PagedMergeFn = void (*)(PagedMergeArgs);
 template <typename T> PagedMergeFn paged_merge_form();
 

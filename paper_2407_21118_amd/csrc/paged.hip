@@ -1,17 +1,18 @@
 // Decode attention over a paged latent cache: a sliding window with a few first rows (sinks), and a prefix that the
-// sequences of a batch share.
+// sequences of a batch share.  Up to 16 query rows (heads x rows) per workgroup; paged_rows.hip takes more.
 //
 //   out = softmax_t( RoPE(q, p) . RoPE(H_k[t] B_k, t) / sqrt(d_h) ) H_v[t] B_v
 //
-// One workgroup takes a unit (up to four key/value heads) and a run of tiles of 32 tokens, for up to 16 query rows per head.
-// It is four wavefronts, one per SIMD and one per head, whose 128 x r weights stay in the accumulation registers.
+// One workgroup takes a unit (up to four key/value heads, two where the key rank is above 256) and a run of tiles of 32 tokens.
+// Eight wavefronts, two per SIMD; FQ of them share a head: each has 64 / FQ of its rotation pairs, the weights for which stay
+// in 128 accumulation registers.
 //   keys    K^T = B_k^T H_k^T of 16 tokens at a time, from latents in LDS; rotated in float32 and multiplied by the
-//           rotated queries on the matrix cores, both between the matrix instructions of the next 16 tokens' keys.
-//   softmax in the wavefront: a lane holds one row's scores of 8 of the tile's tokens, four lanes the row.
-//   values  every wavefront contracts the probabilities of all heads' rows (through LDS) with its share of the value columns
-//           (read as two columns of eight tokens per lane: the transposition that the matrix operand wants is a byte
-//           permute).
-// One barrier per tile: in interval n are the keys of tile n, the softmax of n - 1 and the values of n - 2.  Latents,
+//           rotated queries on the matrix cores, both between the matrix instructions of the next 16 tokens' keys.  The
+//           scores over a wavefront's features go to LDS.
+//   softmax 16 lanes per row, four rows per wavefront: adds the partial scores, masks, keeps the running maximum and sum in float32.
+//   values  every wavefront contracts the probabilities of all rows with its 32 columns of the value latents (read as two
+//           columns of eight tokens per lane: the transposition that the matrix operand wants is a byte permute).
+// One barrier per tile: in interval n are the keys of tile n, the softmax of n - 2 and the values of n - 3.  Latents,
 // page-table entries and angles come by loads that write to LDS directly, n_stages - 1 tiles ahead, counted and
 // never drained while tiles follow: 5.3 TB/s at 2 us latency take 40 KB in flight per compute unit.
 // Partial results (unnormalised sums, maxima, row sums) are merged, normalised and multiplied by B_v in paged_merge_kernel.
@@ -28,306 +29,240 @@
 
 namespace palu {
 
-template <typename T, int KS, int PT, int VB>
-__global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
+template <typename T, int FQ, int KS, int VB>
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   constexpr bool PAIR = __is_same(T, F16);     // queries and keys as pairs hi + lo
-  constexpr int NB_V = 2 * VB;                 // blocks of 32 value columns per wavefront
+  constexpr int NH = 8 / FQ;
+  constexpr int FT = 8 / FQ;                   // tiles of 16 features per wavefront: low halves of the rotation pairs, then high halves
+  constexpr int NP = 16 / FQ;                  // rotation pairs per lane
+  constexpr int NT = NP / 4;                   // contraction steps of the query product: four pairs' low and high halves each
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, kg = lane >> 4;
 
-  // ---- what this workgroup does
-  const int bid = blockIdx.x;
-  const PagedUnit un = a.units[bid % a.n_units];
-  int rest = bid / a.n_units;
-  const int rb = rest % a.n_row_blocks;
-  rest /= a.n_row_blocks;
-  const bool shared = a.shared != 0;
-  const int seq = shared ? 0 : rest / a.n_slots;
-  const int chunk = rest - seq * a.n_slots;
-  int L = shared || !a.seq_lens ? a.max_len : a.seq_lens[seq];
-  L = __builtin_amdgcn_readfirstlane(max(0, min(L, a.max_len)));
-  const PagedSpan span = paged_span(L, a.first, a.window, a.n_sink);
-  const int n_chunks = (span.n_tiles + a.chunk_tiles - 1) / a.chunk_tiles;
-  if (chunk >= n_chunks) return;
-  const int i0 = (int)((long long)span.n_tiles * chunk / n_chunks), i1 = (int)((long long)span.n_tiles * (chunk + 1) / n_chunks);
-
-  const PagedMeta& m = a.meta;
-  const int g = un.group(), nh = un.nh(), h0 = un.h0();
-  const int rk = m.k_off[g + 1] - m.k_off[g], rv = m.v_off[g + 1] - m.v_off[g];
-  const int per_group = m.head_off[g + 1] - m.head_off[g];   // a unit of several groups takes whole ones
-  const int k_cols = un.n_groups() * rk, v_cols = un.n_groups() * rv;
-  const int row0 = rb * a.block_rows;
-  const int nr = min(a.block_rows, a.rows - row0);           // rows per head, at most 16
-  const int n_packed = nh * nr;
+  const PagedWork w(a);
+  if (w.idle()) return;
+  const int i0 = w.i0, i1 = w.i1, nr = w.nr, n_packed = w.n_packed;
   const int NB = a.n_stages;
-  const PagedLds ld = paged_lds(un.n_groups(), KS, v_cols, n_packed, PT, PAIR, NB);
+  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, n_packed, 1, FQ, PAIR, NB);
   const uint32_t lds0 = lds_addr(lds);
-  const bool works = wave < nh;                              // else: the same instructions, results nowhere
-  const int hh = works ? wave : 0;
-  const int hg = un.n_groups() > 1 ? hh / per_group : 0;     // the head's group inside the unit
-
-  // position of tile i, and the position whose row its token x reads (a masked token: the first attended one's)
-  auto tile_pos = [&](int i) { return kPagedTile * (i < span.sink_tiles ? i : span.tile0 + i - span.sink_tiles); };
-  auto token_of = [&](int t0, int x) __attribute__((always_inline)) {
-    const int t = t0 + x, head = t0 < span.sink ? t0 : max(t0, span.lo);
-    return t >= L || (t >= span.sink && t < span.lo) ? head : t;
-  };
-  const int32_t* pages = a.page_table + (size_t)seq * a.table_stride;
-  const int page_mask = (1 << a.page_shift) - 1;
+  const bool works = wave % NH < w.nh;                       // else: the same instructions, results nowhere
+  const int hh = works ? wave % NH : 0, fq = wave / NH;
+  const int fbase = (64 / FQ) * fq;                          // first rotation pair of this wavefront
+  const int hg = w.un.n_groups() > 1 ? hh / w.per_group : 0; // the head's group inside the unit
   const int E = 2 * NB - 1;                                  // entries are requested so many tiles ahead: early enough to be there when rows are made of them
   int* const entries = reinterpret_cast<int*>(lds + ld.entries);
   int* const rows = reinterpret_cast<int*>(lds + ld.rows);
-  // token x of tile i: its row, from its page-table entry
   auto make_row = [&](int i, int x) __attribute__((always_inline)) {
-    const int entry = max(0, min(entries[(i % kPagedEntrySlots) * kPagedTile + x], a.n_pages - 1));
-    rows[(i % kPagedRowSlots) * kPagedTile + x] = (entry << a.page_shift) + (token_of(tile_pos(i), x) & page_mask);
+    rows[(i % kPagedRowSlots) * kPagedTile + x] = w.row_of(i, x, entries[(i % kPagedEntrySlots) * kPagedTile + x]);
   };
 
-  // ---- requests of interval n: keys and angles of tile n + NB - 1, values of n + NB - 3, entries of n + E; the rows of tile
-  // n + NB.  An operation moves 64 16-byte pieces, lane i the i-th of them; a wavefront takes every fourth.  Piece p of a row is
-  // staged as piece p ^ key: of keys so that eight lanes that read eight tokens' same piece find it on all banks, of values so
-  // that the four tokens that the lane groups read do.  Pieces behind a row's last repeat its first.
-  const int ops_k = ld.k_pieces / 8, ops_v = ld.v_pieces / 8;   // per wavefront, each 256 / pieces tokens on
+  // ---- requests of interval n: keys of tile n + NB - 1, values of n + NB - 4, entries of n + E; the rows of tile
+  // n + NB.  An operation moves 64 16-byte pieces, lane i the i-th of them; a wavefront takes every eighth.
   const int id0 = wave * 64 + lane, x_k = id0 / ld.k_pieces, x_v = id0 / ld.v_pieces;
-  auto source = [&](const uint16_t* base, int col0, int cols, int p) __attribute__((always_inline)) {
-    return reinterpret_cast<const unsigned char*>(base + col0 + (p * 8 < cols ? p * 8 : 0));
-  };
-  const int p_k = (id0 % ld.k_pieces) ^ (4 * (x_k & 1) + (x_k >> 2 & 3));
-  const unsigned char* const src_k0 = source(a.hk, m.k_off[g], k_cols, p_k);
-  const unsigned char* const src_k1 = source(a.hk, m.k_off[g], k_cols, p_k ^ 2);    // (32 pieces: eight tokens on)
-  const unsigned char* const src_v = source(a.hv, m.v_off[g], v_cols, (id0 % ld.v_pieces) ^ (4 * (x_v & 3)));
+  const int p_k = (id0 % ld.k_pieces) ^ paged_key_swizzle(x_k);
+  const unsigned char* const src_k0 = paged_source(a.hk, a.meta.k_off[w.g], w.k_cols, p_k);
+  const unsigned char* const src_k1 = FQ == 4 ? paged_source(a.hk, a.meta.k_off[w.g], w.k_cols, p_k ^ 2) : src_k0;   // (64 pieces: eight tokens on)
+  const unsigned char* const src_v = paged_source(a.hv, a.meta.v_off[w.g], w.v_cols, (id0 % ld.v_pieces) ^ paged_value_swizzle(x_v));
   const uint32_t k_pitch = (uint32_t)a.R_k * 2, v_pitch = (uint32_t)a.R_v * 2;
-  auto request_keys = [&](int j, int stage, int stage_base) __attribute__((always_inline)) {
+  auto request_keys = [&](int j, int stage) __attribute__((always_inline)) {
     const int* r = rows + (j % kPagedRowSlots) * kPagedTile + x_k;
     const uint32_t dst = lds0 + stage + wave * 1024;
-    if (ops_k == 4) {
+    if (FQ == 4) {                                           // rows of 64 pieces
       const uint32_t r0 = r[0], r1 = r[8], r2 = r[16], r3 = r[24];
       load_to_lds(src_k0 + (uint64_t)r0 * k_pitch, dst);
-      load_to_lds(src_k1 + (uint64_t)r1 * k_pitch, dst + 4096);
-      load_to_lds(src_k0 + (uint64_t)r2 * k_pitch, dst + 8192);
-      load_to_lds(src_k1 + (uint64_t)r3 * k_pitch, dst + 12288);
-    } else if (ops_k == 2) {
+      load_to_lds(src_k1 + (uint64_t)r1 * k_pitch, dst + 8192);
+      load_to_lds(src_k0 + (uint64_t)r2 * k_pitch, dst + 16384);
+      load_to_lds(src_k1 + (uint64_t)r3 * k_pitch, dst + 24576);
+    } else if (ld.k_pieces == 32) {
       const uint32_t r0 = r[0], r1 = r[16];
       load_to_lds(src_k0 + (uint64_t)r0 * k_pitch, dst);
-      load_to_lds(src_k0 + (uint64_t)r1 * k_pitch, dst + 4096);
-    } else {
+      load_to_lds(src_k0 + (uint64_t)r1 * k_pitch, dst + 8192);
+    } else if (ld.k_pieces == 16 || wave < 4) {
       load_to_lds(src_k0 + (uint64_t)(uint32_t)r[0] * k_pitch, dst);
     }
-    const int p = min(tile_pos(j) + 16 * (wave >> 1), a.rope_len - 1);   // angles: (sub-tile, cos | sin) of this wavefront, lane: pair
-    load_to_lds4(a.rope + rope_f32_index(p, lane, wave & 1, kRopeTableStride), lds0 + stage_base + wave * 256);
   };
   auto request_values = [&](int j, int stage) __attribute__((always_inline)) {
     const int* r = rows + (j % kPagedRowSlots) * kPagedTile + x_v;
     const uint32_t dst = lds0 + stage + wave * 1024;
     if (VB == 2) {                                           // rows of 64 pieces
-      uint32_t y[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = r[4 * k];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) load_to_lds(src_v + (uint64_t)y[k] * v_pitch, dst + 4096 * k);
-    } else if (ops_v == 4) {
       const uint32_t r0 = r[0], r1 = r[8], r2 = r[16], r3 = r[24];
       load_to_lds(src_v + (uint64_t)r0 * v_pitch, dst);
-      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 4096);
-      load_to_lds(src_v + (uint64_t)r2 * v_pitch, dst + 8192);
-      load_to_lds(src_v + (uint64_t)r3 * v_pitch, dst + 12288);
-    } else {
+      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 8192);
+      load_to_lds(src_v + (uint64_t)r2 * v_pitch, dst + 16384);
+      load_to_lds(src_v + (uint64_t)r3 * v_pitch, dst + 24576);
+    } else if (ld.v_pieces == 32) {
       const uint32_t r0 = r[0], r1 = r[16];
       load_to_lds(src_v + (uint64_t)r0 * v_pitch, dst);
-      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 4096);
+      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 8192);
+    } else {
+      load_to_lds(src_v + (uint64_t)(uint32_t)r[0] * v_pitch, dst);
     }
   };
   auto request_entries = [&](int n) __attribute__((always_inline)) {
     const int je = n + E;
-    if (wave == 3 && je < i1 && lane < kPagedTile)
-      load_to_lds4(pages + (token_of(tile_pos(je), lane) >> a.page_shift), lds0 + ld.entries + (je % kPagedEntrySlots) * (kPagedTile * 4));
-    if (wave == 2 && n >= i0 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
+    if (wave == 6 && je < i1 && lane < kPagedTile) load_to_lds4(w.entry_of(je, lane), lds0 + ld.entries + (je % kPagedEntrySlots) * (kPagedTile * 4));
+    if (wave == 5 && n >= i0 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
   };
-  const int per_interval = ops_k + ops_v + 1;
-  // Stages in use, as LDS offsets: keys of tile n and values of tile n - 2 (the stage before is requested into), angles of n and n - 1
-  // (and the one before that).
-  const int base_bytes = (kPagedTile / 16) * kDHead * 4;
-  auto before = [](int at, int first, int size, int n) { return at == first ? first + (n - 1) * size : at - size; };
-  auto behind = [](int at, int first, int size, int n) { return at + size == first + n * size ? first : at + size; };
-  int k_at = ld.k + (i0 % NB) * ld.stage_k, v_at = ld.v + ((i0 + 2 * NB - 2) % NB) * ld.stage_v;
-  int b_at = ld.base + (i0 % (NB + 1)) * base_bytes, b_old = before(b_at, ld.base, base_bytes, NB + 1);
+  const int per_interval = (ld.k_pieces / 2 + 7 - wave) / 8 + (ld.v_pieces / 2 + 7 - wave) / 8;
+  // Stages in use, as LDS offsets: keys of tile n and values of tile n - 3 (the stage before is requested into), angles of n and n - 1.
+  const PagedRing ring_k{ld.k, ld.stage_k, NB}, ring_v{ld.v, ld.stage_v, NB}, ring_b{ld.base, (kPagedTile / 16) * kDHead * 4, kPagedBaseSlots};
+  int k_at = ring_k.stage(i0), v_at = ring_v.stage(i0 + 3 * NB - 3), b_at = ring_b.stage(i0), b_old = ring_b.before(b_at);
 
   // ---- prologue
   for (int x = tid; x < kPagedTile * E; x += kPagedThreads) {   // entries of the first tiles, and rows of those that are requested at once
     const int i = i0 + x / kPagedTile;
     if (i < i1) {
-      entries[(i % kPagedEntrySlots) * kPagedTile + x % kPagedTile] = pages[token_of(tile_pos(i), x % kPagedTile) >> a.page_shift];
+      entries[(i % kPagedEntrySlots) * kPagedTile + x % kPagedTile] = *w.entry_of(i, x % kPagedTile);
       if (i < i0 + NB) make_row(i, x % kPagedTile);
     }
   }
   lds_barrier();
-  for (int j = i0; j < min(i0 + NB - 1, i1); ++j) request_keys(j, ld.k + (j % NB) * ld.stage_k, ld.base + (j % (NB + 1)) * base_bytes);
-  for (int j = i0; j < min(i0 + NB - 3, i1); ++j) request_values(j, ld.v + (j % NB) * ld.stage_v);
+  for (int j = i0; j < min(i0 + NB - 1, i1); ++j) request_keys(j, ring_k.stage(j));
+  for (int j = i0; j < min(i0 + NB - 4, i1); ++j) request_values(j, ring_v.stage(j));
 
-  // A sub-tile's 16 tokens are columns of its keys in the order 0 4 8 12 1 5 .., so that a lane's four scores are of tokens 4 apart:
-  // operands of the value product whose lane groups read tokens side by side.
-  const int tok = 4 * (col & 3) + (col >> 2);
-  // angles of position tok, of this lane's 16 rotation pairs 16 kg ..; scaled
-  float ang_c[16], ang_s[16];
+  PagedAngles angles{w, lds, lds0, ld.base, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
+  if (wave == 3) angles.begin(NB);
+
+  const int tok = paged_token(col);
+  // angles of position tok, of this lane's rotation pairs fbase + NP kg ..; scaled
+  float ang_c[NP], ang_s[NP];
 #pragma unroll
-  for (int p = 0; p < 16; ++p) {
-    ang_c[p] = kKeyScale * a.rope[rope_f32_index(tok, 16 * kg + p, 0, kRopeTableStride)];
-    ang_s[p] = kKeyScale * a.rope[rope_f32_index(tok, 16 * kg + p, 1, kRopeTableStride)];
+  for (int p = 0; p < NP; ++p) {
+    ang_c[p] = kKeyScale * a.rope[rope_f32_index(tok, fbase + NP * kg + p, 0, kRopeTableStride)];
+    ang_s[p] = kKeyScale * a.rope[rope_f32_index(tok, fbase + NP * kg + p, 1, kRopeTableStride)];
   }
-  // rotated queries: [packed row][hi | lo][feature]
-  for (int x = tid; x < n_packed * kHalf; x += kPagedThreads) {
-    const int f = x & 63, pr = x >> 6;
-    const int h = pr / nr, r = pr - h * nr;
-    int b = seq, qh = row0 + r;
-    if (shared) { b = qh / m.qpk; qh -= b * m.qpk; }
-    const uint16_t* qp = a.q + ((size_t)b * m.n_heads * m.qpk + (h0 + h) * m.qpk + qh) * kDHead;
-    const float x0 = T::to_float(qp[f]), x1 = T::to_float(qp[f + kHalf]);
-    int pos = a.q_pos ? a.q_pos[b] : (a.seq_lens ? a.seq_lens[b] : a.pos_len) - 1;
-    pos = max(0, min(pos, a.rope_len - 1));
-    const float k = a.scale / kKeyScale;
-    const float c = a.rope[rope_f32_index(pos, f, 0, kRopeTableStride)] * k, s = a.rope[rope_f32_index(pos, f, 1, kRopeTableStride)] * k;
-    uint32_t hi, lo;
-    split2<F16>(x0 * c - x1 * s, x1 * c + x0 * s, &hi, &lo);
-    uint16_t* q = reinterpret_cast<uint16_t*>(lds + ld.q + pr * ld.q_pitch) + f;
-    q[0] = (uint16_t)hi;
-    q[kHalf] = (uint16_t)(hi >> 16);
-    if (PAIR) {
-      q[kDHead] = (uint16_t)lo;
-      q[kDHead + kHalf] = (uint16_t)(lo >> 16);
-    }
-  }
+  w.rotate_queries<T>(lds + ld.q, ld.q_pitch, kPagedThreads);
 
-  // weights: feature 4 m + j (j < 4) or 64 + 4 m + j - 4 is row m of tile j, so that a lane holds both features of a rotation
-  // pair.  A lane reads its four features of either half from eight rows of B_k and transposes them.  They stay in the
-  // accumulation registers, which the matrix instructions read as they are.
-  uint4v W[KS][8];
+  // weights.  FQ = 2: rotation pair fbase + 2 m + j is row m of tile j (low half) and 2 + j (high half); FQ = 4: pair fbase + m of tiles
+  // 0 and 1.  A lane reads its features from eight rows of B_k and transposes them.  They stay in the accumulation registers, which the
+  // matrix instructions read as they are.
+  uint4v W[KS][FT];
   {
-    const int width = per_group * kDHead;
-    const uint16_t* B = a.Bk + m.bk_off[g] + (size_t)hg * rk * width + (size_t)(hh + h0 - m.head_off[g] - hg * per_group) * kDHead + 4 * col;
+    const int width = w.per_group * kDHead;
+    const uint16_t* B = a.Bk + w.weights_of(hh, hg) + fbase;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      uint2v v[2][8];
-      if (32 * ks < rk) {
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+        uint32_t v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint16_t* w = B + (size_t)(32 * ks + 8 * kg + e) * width;
-          v[0][e] = *reinterpret_cast<const uint2v*>(w);
-          v[1][e] = *reinterpret_cast<const uint2v*>(w + kHalf);
+          v[e] = 0;
+          if (32 * ks < w.rk) {
+            const uint16_t* row = B + (size_t)(32 * ks + 8 * kg + e) * width + side * kHalf;
+            v[e] = FQ == 2 ? *reinterpret_cast<const uint32_t*>(row + 2 * col) : (uint32_t)row[col];
+          }
         }
-      } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[0][e] = v[1][e] = uint2v{0, 0};
+        for (int i = 0; i < 4; ++i) {
+          W[ks][side * (FT / 2)][i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x05040100u);
+          if (FQ == 2) W[ks][side * (FT / 2) + FT / 2 - 1][i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x07060302u);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          W[ks][j][i] = __builtin_amdgcn_perm(v[j >> 2][2 * i + 1][(j >> 1) & 1], v[j >> 2][2 * i][(j >> 1) & 1], (j & 1) ? 0x07060302u : 0x05040100u);
-        asm volatile("" : "+a"(W[ks][j]));
-      }
+      for (int j = 0; j < FT; ++j) asm volatile("" : "+a"(W[ks][j]));
     }
   }
 
-  const int n_blocks = v_cols / 32;                          // of 32 value columns: block wave + 4 v is this wavefront's
-  const int n_pt = (n_packed + 15) / 16;
-  float4v O[NB_V][PT][2];
+  const int n_blocks = w.v_cols / 32;                        // of 32 value columns: block wave + 8 v is this wavefront's
+  float4v O[VB][2];
 #pragma unroll
-  for (int v = 0; v < NB_V; ++v)
-#pragma unroll
-    for (int p = 0; p < PT; ++p) O[v][p][0] = O[v][p][1] = float4v{0, 0, 0, 0};
+  for (int v = 0; v < VB; ++v) O[v][0] = O[v][1] = float4v{0, 0, 0, 0};
 
-  // softmax state of row col (the sum: over this lane's tokens); rows of the cache it may see
+  // softmax state of the lanes of the last four wavefronts: row, two of its tokens; rows of the cache that the row may see
+  const int srow = 4 * (wave & 3) + (lane >> 4), stok = 16 * (col >> 3) + 8 * (col & 1) + (col >> 1 & 3);
   float run_max = -INFINITY, run_sum = 0.f;
-  const bool live = works && col < nr;
-  int limit = L;
-  if (shared && live) limit = min(L, a.seq_lens ? a.seq_lens[(row0 + col) / m.qpk] : L);
-  int all_see = limit;                                       // rows that every row of the wavefront sees
-#pragma unroll
-  for (int d = 1; d < 16; d *= 2) all_see = min(all_see, __shfl_xor(all_see, d));
-  all_see = __builtin_amdgcn_readfirstlane(all_see);
-  const int prow = live ? hh * nr + col : PT * 16;           // where its probabilities go; of no row: behind the last
+  const int limit = srow < n_packed ? w.limit_of(srow % nr) : w.L;
 
   wait_vm(0);
   lds_barrier();
+  const int steady = wait_class((NB - 2) * per_interval);
 
-  const unsigned char* const q_row = lds + ld.q + (hh * nr + min(col, nr - 1)) * ld.q_pitch + 32 * kg;
-  const int h_key = 4 * (tok & 1) + (tok >> 2 & 3);
+  const int my_row = works && col < nr ? hh * nr + col : n_packed;       // where this lane's scores go; of no row: behind the last
+  const unsigned char* const q_row = lds + ld.q + (hh * nr + min(col, nr - 1)) * ld.q_pitch + 2 * (fbase + NP * kg);
+  const int h_key = paged_key_swizzle(tok);
   const int h_lane = tok * ld.k_pieces * 16 + hg * KS * 64, off0 = h_lane + (kg ^ h_key) * 16, off1 = h_lane + ((4 + kg) ^ h_key) * 16;
-  const int v_lane = kg * ld.v_pieces * 16, v_pitch16 = 4 * ld.v_pieces * 16;
-
+  const int v_lane = kg * ld.v_pieces * 16 + (col & 3) * 4, v_pitch16 = 4 * ld.v_pieces * 16;
   float minus_one = -1.f;                                    // (not a constant to the compiler, which would make a conversion and a subtraction of `less`)
   asm("" : "+s"(minus_one));
-  float4v acc[2][8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) acc[0][j] = acc[1][j] = float4v{0, 0, 0, 0};
-  float4v score[2];
 
-  // Keys of sub-tile `sub` of the tile staged at k_stage into acc[sub]; between their matrix instructions the previous sub-tile's, whose
-  // tile has its angles at b_stage, are rotated, split and multiplied by the queries into score[1 - sub].  The vector work is 64 steps of
-  // about three instructions (a matrix instruction takes the issue slots of four), a step or more behind every matrix instruction.
-  auto keys = [&](auto sub_c, int k_stage, int b_stage) __attribute__((always_inline)) {
+  float4v acc[2][FT];
+#pragma unroll
+  for (int j = 0; j < FT; ++j) acc[0][j] = acc[1][j] = float4v{0, 0, 0, 0};
+
+  // Keys of sub-tile `sub` of the tile staged at k_stage into acc[sub]; between their matrix instructions the previous sub-tile's, of tile
+  // `np` with its angles at b_stage, are rotated, split and multiplied by the queries.  The vector work is 8 steps of about three
+  // instructions for every two pairs (a matrix instruction takes the issue slots of four).
+  auto keys = [&](auto sub_c, int k_stage, int np, int b_stage) __attribute__((always_inline)) {
     constexpr int sub = decltype(sub_c)::value, old = 1 - sub;
-    constexpr int kSlots = KS * 8;
+    constexpr int kSlots = KS * FT, kSteps = NP * 4;
     const unsigned char* h0p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off0;
     const unsigned char* h1p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off1;
-    const float* bas = reinterpret_cast<const float*>(lds + b_stage) + old * kDHead + 16 * kg;
+    const float* bas = reinterpret_cast<const float*>(lds + b_stage) + old * kDHead + fbase + NP * kg;
     uint4v af[3];
     af[0] = *reinterpret_cast<const uint4v*>(h0p);
     af[1] = *reinterpret_cast<const uint4v*>(h1p);
-    float4v bc[2], bs[2];                                    // angles of four pairs, and of the next four
-    bc[0] = *reinterpret_cast<const float4v*>(bas);
-    bs[0] = *reinterpret_cast<const float4v*>(bas + kHalf);
-    uint32_t khi[4][4], klo[4][4];                           // [2 side + half][pairs]: contraction steps, feature 64 side + 16 kg + 8 half + ..
-    float4v dot[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    float4v bc[NT], bs[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      bc[t] = *reinterpret_cast<const float4v*>(bas + 4 * t);
+      bs[t] = *reinterpret_cast<const float4v*>(bas + 4 * t + kHalf);
+    }
+    uint32_t khi[4], klo[4];                                 // of a contraction step: low halves of four pairs, high halves
+    float4v dot = {0, 0, 0, 0};
+    uint2v ql[2], qh[2];
     float t1, t2, c, s, lo[2], hi[2], l0, l1, l2;
     uint32_t x, y;
     auto step = [&](int e) __attribute__((always_inline)) {
-      const int pa = 2 * (e >> 3), pb = pa + 1, q4 = pa >> 2, at = (e >> 3) & 3, half = e >> 5;   // pairs pa and pb
-      const float4v c0 = bc[q4 & 1], s0 = bs[q4 & 1];
-      if ((e & 15) == 0 && q4 + 1 < 4) {
-        bc[(q4 + 1) & 1] = *reinterpret_cast<const float4v*>(bas + 4 * (q4 + 1));
-        bs[(q4 + 1) & 1] = *reinterpret_cast<const float4v*>(bas + 4 * (q4 + 1) + kHalf);
-      }
-      const float kl0 = acc[old][pa & 3][pa >> 2], kh0 = acc[old][4 + (pa & 3)][pa >> 2], kl1 = acc[old][pb & 3][pb >> 2], kh1 = acc[old][4 + (pb & 3)][pb >> 2];
+      const int pa = 2 * (e >> 3), pb = pa + 1, t = pa >> 2, at = (e >> 3) & 1;   // pairs pa and pb
+      auto low = [&](int p) { return FQ == 2 ? acc[old][p & 1][p >> 1] : acc[old][0][p]; };
+      auto high = [&](int p) { return FQ == 2 ? acc[old][FT / 2 + (p & 1)][p >> 1] : acc[old][1][p]; };
       switch (e & 7) {
         case 0:
-          t1 = ang_s[pa] * s0[pa & 3];
-          t2 = ang_c[pa] * s0[pa & 3];
-          c = __builtin_fmaf(ang_c[pa], c0[pa & 3], -t1);
+          if (at == 0) {                                     // the step's queries
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              qh[u] = *reinterpret_cast<const uint2v*>(q_row + u * 128 + 8 * t);
+              if (PAIR) ql[u] = *reinterpret_cast<const uint2v*>(q_row + 256 + u * 128 + 8 * t);
+            }
+          }
+          t1 = ang_s[pa] * bs[t][pa & 3];
+          t2 = ang_c[pa] * bs[t][pa & 3];
+          c = __builtin_fmaf(ang_c[pa], bc[t][pa & 3], -t1);
           break;
         case 1:
-          s = __builtin_fmaf(ang_s[pa], c0[pa & 3], t2);
-          t1 = kh0 * s;
-          t2 = kl0 * s;
+          s = __builtin_fmaf(ang_s[pa], bc[t][pa & 3], t2);
+          t1 = high(pa) * s;
+          t2 = low(pa) * s;
           break;
         case 2:
-          lo[0] = __builtin_fmaf(kl0, c, -t1);
-          hi[0] = __builtin_fmaf(kh0, c, t2);
-          t1 = ang_s[pb] * s0[pb & 3];
+          lo[0] = __builtin_fmaf(low(pa), c, -t1);
+          hi[0] = __builtin_fmaf(high(pa), c, t2);
+          t1 = ang_s[pb] * bs[t][pb & 3];
           break;
         case 3:
-          t2 = ang_c[pb] * s0[pb & 3];
-          c = __builtin_fmaf(ang_c[pb], c0[pb & 3], -t1);
-          s = __builtin_fmaf(ang_s[pb], c0[pb & 3], t2);
+          t2 = ang_c[pb] * bs[t][pb & 3];
+          c = __builtin_fmaf(ang_c[pb], bc[t][pb & 3], -t1);
+          s = __builtin_fmaf(ang_s[pb], bc[t][pb & 3], t2);
           break;
         case 4:
-          t1 = kh1 * s;
-          t2 = kl1 * s;
-          lo[1] = __builtin_fmaf(kl1, c, -t1);
+          t1 = high(pb) * s;
+          t2 = low(pb) * s;
+          lo[1] = __builtin_fmaf(low(pb), c, -t1);
           break;
         case 5:
-          hi[1] = __builtin_fmaf(kh1, c, t2);
+          hi[1] = __builtin_fmaf(high(pb), c, t2);
           // (the empty statements: a product and its rounding stay two instructions.  As one, they would round the exact product to hi
           // where lo is measured from the float32 one, and take one instruction per number instead of one per two.)
           asm("" : "+v"(lo[0]), "+v"(lo[1]), "+v"(hi[0]), "+v"(hi[1]));
           x = pack2<F16>(lo[0], lo[1]);
           y = pack2<F16>(hi[0], hi[1]);
           if (PAIR) asm("" : "+v"(x), "+v"(y));
-          khi[half][at] = x;
-          khi[2 + half][at] = y;
+          khi[at] = x;
+          khi[2 + at] = y;
           break;
         case 6:
           if (PAIR) {
@@ -338,91 +273,77 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
           break;
         case 7:
           if (PAIR) {
-            klo[half][at] = pack2<F16>(l0, l1);
-            klo[2 + half][at] = pack2<F16>(l2, less<F16>(hi[1], y >> 16, minus_one));
+            klo[at] = pack2<F16>(l0, l1);
+            klo[2 + at] = pack2<F16>(l2, less<F16>(hi[1], y >> 16, minus_one));
+          }
+          if (at == 1) {
+            const uint4v h = {khi[0], khi[1], khi[2], khi[3]}, q = {qh[0].x, qh[0].y, qh[1].x, qh[1].y};
+            dot = mma<F16>(h, q, dot);
+            if (PAIR) {
+              const uint4v l = {klo[0], klo[1], klo[2], klo[3]}, r = {ql[0].x, ql[0].y, ql[1].x, ql[1].y};
+              dot = mma<F16>(h, r, dot);
+              dot = mma<F16>(l, q, dot);
+            }
           }
           break;
-      }
-    };
-    auto products = [&](int half) __attribute__((always_inline)) {
-#pragma unroll
-      for (int side = 0; side < 2; ++side) {
-        const int k = 2 * side + half;
-        const uint4v kh = {khi[k][0], khi[k][1], khi[k][2], khi[k][3]};
-        const uint4v qh = *reinterpret_cast<const uint4v*>(q_row + side * 128 + half * 16);
-        dot[side] = mma<F16>(kh, qh, dot[side]);
-        if (PAIR) {
-          const uint4v kl = {klo[k][0], klo[k][1], klo[k][2], klo[k][3]};
-          const uint4v ql = *reinterpret_cast<const uint4v*>(q_row + 256 + side * 128 + half * 16);
-          dot[side] = mma<F16>(kh, ql, dot[side]);
-          dot[side] = mma<F16>(kl, qh, dot[side]);
-        }
       }
     };
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       if (ks + 2 < KS) af[(ks + 2) % 3] = *reinterpret_cast<const uint4v*>(((ks & 1) ? h1p : h0p) + ((ks + 2) >> 1) * 128);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int slot = ks * 8 + j;
+      for (int j = 0; j < FT; ++j) {
+        const int slot = ks * FT + j;
         acc[sub][j] = mma<T>(W[ks][j], af[ks % 3], ks == 0 ? float4v{0, 0, 0, 0} : acc[sub][j]);
 #pragma unroll
-        for (int e = slot * 64 / kSlots; e < (slot + 1) * 64 / kSlots; ++e) {
-          step(e);
-          if (e == 31) products(0);
-        }
+        for (int e = slot * kSteps / kSlots; e < (slot + 1) * kSteps / kSlots; ++e) step(e);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    products(1);
-    score[old] = dot[0] + dot[1];
+    // lane: query row col, tokens kg + 4 i of sub-tile old
+    float* score = reinterpret_cast<float*>(lds + ld.s) + ((np + kPagedScoreSlots) % kPagedScoreSlots * FQ + fq) * (n_packed + 1) * kPagedScorePitch;
+    *reinterpret_cast<float4v*>(score + my_row * kPagedScorePitch + 16 * old + 4 * kg) = dot;
   };
 
-  // ---- softmax of tile n: this lane has tokens kg + 4 i and 16 + kg + 4 i of row col
+  // ---- softmax of tile n: this lane has scores 2 col and 2 col + 1 of row srow, of tokens stok and stok + 4
   auto softmax = [&](int n) __attribute__((always_inline)) {
-    const int buf = n & 1, t0 = tile_pos(n);
-    float s[8];
+    const int buf = n & 1, t0 = w.tile_pos(n) + stok, r = min(srow, n_packed);
+    const float* row = reinterpret_cast<const float*>(lds + ld.s) + (n % kPagedScoreSlots * FQ * (n_packed + 1) + r) * kPagedScorePitch + 2 * col;
+    float s0 = row[0], s1 = row[1];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = score[e >> 2][e & 3];
-    const bool whole = t0 + kPagedTile <= all_see && (t0 + kPagedTile <= span.sink || t0 >= span.lo);
-    if (!whole) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int t = t0 + 4 * e + kg;
-        if (t >= limit || (t >= span.sink && t < span.lo)) s[e] = -INFINITY;
-      }
+    for (int f = 1; f < FQ; ++f) {
+      s0 += row[f * (n_packed + 1) * kPagedScorePitch];
+      s1 += row[f * (n_packed + 1) * kPagedScorePitch + 1];
     }
-    float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    top = max_of_4(top);
-    const float now = fmaxf(run_max, top);
+    if (t0 >= limit || (t0 >= w.span.sink && t0 < w.span.lo)) s0 = -INFINITY;
+    if (t0 + 4 >= limit || (t0 + 4 >= w.span.sink && t0 + 4 < w.span.lo)) s1 = -INFINITY;
+    const float now = fmaxf(run_max, max_of_row(fmaxf(s0, s1)));
     const float zero = now == -INFINITY ? 0.f : now;         // no row seen yet: exp2(-inf) = 0 below
     const float alpha = __builtin_amdgcn_exp2f(run_max - zero);
-    float sum = 0.f;
-    uint32_t ph[4], pl[4];
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(s[e] - zero), p1 = __builtin_amdgcn_exp2f(s[e + 1] - zero);
-      sum += p0 + p1;
-      split2<T>(p0, p1, &ph[e / 2], &pl[e / 2]);
-    }
+    const float p0 = __builtin_amdgcn_exp2f(s0 - zero), p1 = __builtin_amdgcn_exp2f(s1 - zero);
+    uint32_t hi, lo;
+    split2<T>(p0, p1, &hi, &lo);
     run_max = now;
-    run_sum = run_sum * alpha + sum;
-    // in the order of the value product's contraction: lane group kg, token kg + 4 i
-    unsigned char* P = lds + ld.p + (buf * (PT * 16 + 1) + prow) * kPagedProbPitch + 16 * kg;
-    *reinterpret_cast<uint4v*>(P) = uint4v{ph[0], ph[1], ph[2], ph[3]};
-    *reinterpret_cast<uint4v*>(P + 64) = uint4v{pl[0], pl[1], pl[2], pl[3]};
-    reinterpret_cast<float*>(lds + ld.alpha)[buf * (PT * 16 + 4) + prow] = alpha;
+    run_sum = run_sum * alpha + (p0 + p1);
+    // in the order of the value product's contraction: lane group kg', token kg' + 4 e
+    unsigned char* P = lds + ld.p + (buf * 17 + min(srow, 16)) * kPagedProbPitch + 16 * (col >> 1 & 3) + 8 * (col >> 3) + 4 * (col & 1);
+    *reinterpret_cast<uint32_t*>(P) = hi;
+    *reinterpret_cast<uint32_t*>(P + 64) = lo;
+    reinterpret_cast<float*>(lds + ld.alpha)[buf * 20 + srow] = alpha;
   };
 
   // ---- values of tile n, staged at v_stage
   auto values = [&](int n, int v_stage) __attribute__((always_inline)) {
     const int buf = n & 1;
+    const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (buf * 20 + 4 * kg) * 4);
+    const unsigned char* P = lds + ld.p + (buf * 17 + col) * kPagedProbPitch + 16 * kg;
+    const uint4v hi = *reinterpret_cast<const uint4v*>(P), lo = *reinterpret_cast<const uint4v*>(P + 64);
 #pragma unroll
-    for (int v = 0; v < NB_V; ++v) {
-      if (v > 0 && 4 * v >= n_blocks) break;                 // (a block behind the last, of a wavefront whose neighbours have one: nothing that is stored)
-      const int block = wave + 4 * v;
+    for (int v = 0; v < VB; ++v) {
+      const int block = wave + 8 * v;
+      if (block >= n_blocks) break;
       uint32_t x[8];                                         // tokens kg + 4 e
-      const unsigned char* row = lds + v_stage + v_lane + ((block * 4 + (col >> 2)) ^ (4 * kg)) * 16 + (col & 3) * 4;
+      const unsigned char* row = lds + v_stage + v_lane + ((block * 4 + (col >> 2)) ^ (4 * kg)) * 16;
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = *reinterpret_cast<const uint32_t*>(row + e * v_pitch16);
       uint4v f0, f1;
@@ -431,80 +352,64 @@ __global__ __launch_bounds__(kPagedThreads) void paged_kernel(PagedArgs a) {
         f0[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x05040100u);
         f1[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x07060302u);
       }
-#pragma unroll
-      for (int p = 0; p < PT; ++p) {
-        if (p > 0 && p >= n_pt) break;
-        const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (buf * (PT * 16 + 4) + 16 * p + 4 * kg) * 4);
-        const unsigned char* P = lds + ld.p + (buf * (PT * 16 + 1) + 16 * p + col) * kPagedProbPitch + 16 * kg;
-        const uint4v hi = *reinterpret_cast<const uint4v*>(P), lo = *reinterpret_cast<const uint4v*>(P + 64);
-        O[v][p][0] = mma<T>(hi, f0, O[v][p][0] * al);
-        O[v][p][1] = mma<T>(hi, f1, O[v][p][1] * al);
-        O[v][p][0] = mma<T>(lo, f0, O[v][p][0]);
-        O[v][p][1] = mma<T>(lo, f1, O[v][p][1]);
-      }
+      O[v][0] = mma<T>(hi, f0, O[v][0] * al);
+      O[v][1] = mma<T>(hi, f1, O[v][1] * al);
+      O[v][0] = mma<T>(lo, f0, O[v][0]);
+      O[v][1] = mma<T>(lo, f1, O[v][1]);
     }
   };
 
-  for (int n = i0; n < i1 + 2; ++n) {
-    if (n + NB - 1 < i1) request_keys(n + NB - 1, before(k_at, ld.k, ld.stage_k, NB), before(b_old, ld.base, base_bytes, NB + 1));
-    if (n + NB - 3 >= i0 && n + NB - 3 < i1) request_values(n + NB - 3, before(v_at, ld.v, ld.stage_v, NB));
+  for (int n = i0; n < i1 + 3; ++n) {
+    if (n + NB - 1 < i1) request_keys(n + NB - 1, ring_k.before(k_at));
+    if (n + NB - 4 >= i0 && n + NB - 4 < i1) request_values(n + NB - 4, ring_v.before(v_at));
     request_entries(n);
-    if (n <= i1) keys(IntC<0>(), k_at, b_old);               // (behind the last tile, and of the one before the first: nothing that is used)
-    if (n >= i0 + 2) values(n - 2, v_at);
-    if (n > i0 && n <= i1) softmax(n - 1);
-    if (n < i1) keys(IntC<1>(), k_at, b_at);
-    k_at = behind(k_at, ld.k, ld.stage_k, NB);
-    v_at = behind(v_at, ld.v, ld.stage_v, NB);
+    if (wave == 3) {
+      angles.request(n + NB);
+      if (n + 1 < i1) angles.make(n + 1);
+    }
+    if (wave >= 4 && 4 * (wave & 3) < n_packed && n >= i0 + 2 && n < i1 + 2) softmax(n - 2);
+    if (n <= i1) keys(IntC<0>(), k_at, n - 1, b_old);        // (behind the last tile, and of the one before the first: nothing that is used)
+    if (n >= i0 + 3) values(n - 3, v_at);
+    if (n < i1) keys(IntC<1>(), k_at, n, b_at);
+    k_at = ring_k.behind(k_at);
+    v_at = ring_v.behind(v_at);
     b_old = b_at;
-    b_at = behind(b_at, ld.base, base_bytes, NB + 1);
+    b_at = ring_b.behind(b_at);
     // what interval n + 1 reads was requested in n - NB + 2; the NB - 2 intervals since then may be outstanding where all of them
     // requested whole tiles
-    if (n + NB - 1 < i1) wait_vm((NB - 2) * (per_interval + (wave == 3 && n + E < i1 ? 1 : 0)));
+    if (n > i0 && n + NB - 1 < i1) wait_vm(steady);
     else wait_vm(0);
     lds_barrier();
   }
 
   // ---- partial results
-  run_sum += __shfl_xor(run_sum, 16);
-  run_sum += __shfl_xor(run_sum, 32);
-  const size_t slot = shared ? (size_t)chunk : (size_t)seq * a.n_slots + chunk;
-  if (live && kg == 0) {
-    float2* ml = reinterpret_cast<float2*>(a.ml_part) + slot * m.n_heads * a.rows + (size_t)(h0 + hh) * a.rows + row0 + col;
-    *ml = make_float2(run_max, run_sum);
-  }
 #pragma unroll
-  for (int v = 0; v < NB_V; ++v) {
-    const int block = wave + 4 * v;
+  for (int d = 1; d < 16; d *= 2) run_sum += __shfl_xor(run_sum, d);
+  if (wave >= 4 && srow < n_packed && col == 0) w.store_ml(srow / nr, srow % nr, run_max, run_sum);
+#pragma unroll
+  for (int v = 0; v < VB; ++v) {
+    const int block = wave + 8 * v;
     if (block >= n_blocks) continue;
-    const int bg = block * 32 / rv;                          // the group whose columns these are
-    const int c = block * 32 - bg * rv + 2 * col;
 #pragma unroll
-    for (int p = 0; p < PT; ++p) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int pr = 16 * p + 4 * kg + e;
-        if (pr < n_packed) {
-          const int h = pr / nr, r = pr - h * nr;
-          if (un.n_groups() > 1 && h / per_group != bg) continue;
-          const int ohead = m.o_off[g] + (h0 + h - m.head_off[g]) * rv;
-          float* o = a.o_part + slot * a.o_stride + (size_t)a.rows * ohead + (size_t)(row0 + r) * rv + c;
-          *reinterpret_cast<float2*>(o) = make_float2(O[v][p][0][e], O[v][p][1][e]);
-        }
-      }
-    }
+    for (int e = 0; e < 4; ++e)
+      if (4 * kg + e < n_packed) w.store_o(4 * kg + e, block * 32 + 2 * col, O[v][0][e], O[v][1][e]);
   }
 }
 
 namespace {
-template <typename T, int KS>
-PagedFn pick(const PagedForm& f) {
-  if (f.vb == 1) return f.pt == 1 ? paged_kernel<T, KS, 1, 1> : paged_kernel<T, KS, 4, 1>;
-  return f.pt == 1 ? paged_kernel<T, KS, 1, 2> : paged_kernel<T, KS, 2, 2>;
-}
+template <typename T, int FQ, int KS>
+PagedFn pick(int vb) { return vb == 1 ? paged_kernel<T, FQ, KS, 1> : paged_kernel<T, FQ, KS, 2>; }
 }  // namespace
 
 template <typename T> PagedFn paged_form(const PagedForm& f) {
-  return f.ks == 2 ? pick<T, 2>(f) : f.ks == 4 ? pick<T, 4>(f) : f.ks == 6 ? pick<T, 6>(f) : pick<T, 8>(f);
+  switch (f.ks) {
+    case 2: return pick<T, 2, 2>(f.vb);
+    case 4: return pick<T, 2, 4>(f.vb);
+    case 6: return pick<T, 2, 6>(f.vb);
+    case 8: return pick<T, 2, 8>(f.vb);
+    case 12: return pick<T, 4, 12>(f.vb);
+    default: return pick<T, 4, 16>(f.vb);
+  }
 }
 template PagedFn paged_form<PALU_PAGED_ACT>(const PagedForm&);
 

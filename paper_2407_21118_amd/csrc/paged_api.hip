@@ -12,7 +12,7 @@ struct PagedClass {
   int n_units;
   PagedUnit units[PALU_MAX_HEADS];
 };
-constexpr int kPagedMaxClasses = 10;       // steps of key channels 2, 4, 6, 8 or above, value columns up to 256 or above
+constexpr int kPagedMaxClasses = 12;       // steps of key channels 2, 4, 6, 8, 12, 16, value columns up to 256 or above
 struct PagedPlan {
   PagedMeta meta;
   int rows;                                // query rows per key/value head
@@ -58,27 +58,31 @@ int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, 
   auto rv = [&](int j) { return m.v_off[j + 1] - m.v_off[j]; };
   auto heads = [&](int j) { return m.head_off[j + 1] - m.head_off[j]; };
   for (int j = 0; j < m.n_groups; ++j) sum_rv += heads(j) * rv(j);
-  auto steps = [&](int j) { return rk(j) > 256 ? 0 : (rk(j) / 32 + 1) / 2 * 2; };
+  const int kSteps[6] = {2, 4, 6, 8, 12, 16};
+  auto steps = [&](int j) {
+    int i = 0;
+    while (kSteps[i] * 32 < rk(j)) ++i;
+    return kSteps[i];
+  };
   for (int cls = 0; cls < kPagedMaxClasses; ++cls) {
-    const int ks = cls % 5 * 2, vb = cls / 5 + 1;
+    const int ks = kSteps[cls % 6], vb = cls / 6 + 1;
     auto in_class = [&](int j) { return steps(j) == ks && (rv(j) > 256) == (vb == 2); };
-    int most = 0;                                            // heads in a unit
-    for (int j = 0; j < m.n_groups; ++j)
-      if (in_class(j)) most = std::max(most, heads(j));
-    if (!most) continue;
+    int any = 0;
+    for (int j = 0; j < m.n_groups; ++j) any += in_class(j);
+    if (!any) continue;
     PagedClass& c = p->cls[p->n_cls++];
+    c.form = PagedForm{ks, vb, false};
     // Units: whole adjacent groups of equal ranks and size side by side, as far as 256 columns and the heads go (ranks in whole 64s:
     // the staged rows' layout), else parts of one group.  A unit of more heads reads its latents once for all of them.
-    const int unit_heads = ks ? 4 : 2;
+    const int unit_heads = c.form.unit_heads();
     c.n_units = 0;
-    int k_groups = 1, k_cols = 0, v_cols = 0;
-    most = std::min(most, unit_heads);
+    int k_groups = 1, v_cols = 0, most = 1;                  // of a unit: groups, value columns, heads
     for (int first = 0;; first += unit_heads) {              // round robin over the groups: neighbouring workgroups, which go to different
       bool more = false;                                     // L2 caches, take different groups, and the units of one group meet in one
       for (int j = 0; j < m.n_groups; ++j) {
         if (!in_class(j) || first >= heads(j)) continue;
         int n = 1;
-        if (ks && rk(j) % 64 == 0)
+        if (rk(j) % 64 == 0)
           while (j + n < m.n_groups && rk(j + n) == rk(j) && rv(j + n) == rv(j) && heads(j + n) == heads(j) && (n + 1) * heads(j) <= unit_heads &&
                  (n + 1) * rk(j) <= 256 && (n + 1) * rv(j) <= 256)
             ++n;
@@ -86,27 +90,27 @@ int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, 
         const int nh = std::min(unit_heads, n * heads(j) - first);
         c.units[c.n_units++].bits = (uint32_t)(m.head_off[j] + first) | (uint32_t)nh << 8 | (uint32_t)j << 16 | (uint32_t)n << 24;
         k_groups = std::max(k_groups, n);
-        k_cols = std::max(k_cols, rk(j));
         v_cols = std::max(v_cols, n * rv(j));
         most = std::max(most, nh);
         j += n - 1;
       }
       if (!more) break;
     }
-    // Query rows: 16 per head and, as far as accumulators go, 64 in all (32 beside two blocks of value columns)
-    const int row_limit = std::min(16, (ks ? (vb == 1 ? 64 : 32) : 16) / most);
-    c.n_row_blocks = ceil_div(rows, row_limit);
-    c.block_rows = ceil_div(rows, c.n_row_blocks);
-    const int packed = most * c.block_rows;
-    c.form = PagedForm{ks, packed <= 16 ? 1 : (vb == 1 ? 4 : 2), vb};
+    // Query rows: 16 in all, or 16 per head and as many as accumulators go where there are more; as many blocks of them as it takes
+    c.form.many = ks <= 8 && most * rows > 16;
     auto lds_bytes = [&](int stages) {
-      const bool pairs = act == PALU_F16;
-      return ks ? paged_lds(k_groups, ks, v_cols, packed, c.form.pt, pairs, stages).total : paged_wide_lds(k_cols, v_cols, packed, pairs, stages).total;
+      const int packed = most * c.block_rows;
+      return paged_lds(k_groups, ks, v_cols, packed, c.form.many ? c.form.max_rows() / 16 : 1, c.form.many ? 0 : c.form.parts(), act == PALU_F16, stages).total;
     };
+    for (int limit = std::min(16, c.form.max_rows() / most); limit > 0; --limit) {   // (fewer where two stages leave no more LDS)
+      c.n_row_blocks = ceil_div(rows, limit);
+      c.block_rows = ceil_div(rows, c.n_row_blocks);
+      if (lds_bytes(2) <= kPagedLdsBytes) break;
+    }
+    if (lds_bytes(2) > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;
     c.n_stages = 2;
     while (c.n_stages < kPagedMaxStages && lds_bytes(c.n_stages + 1) <= kPagedLdsBytes) ++c.n_stages;
     c.lds_bytes = lds_bytes(c.n_stages);
-    if (c.lds_bytes > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;
     wgs += (long long)c.n_units * c.n_row_blocks;
   }
   wgs *= batch;
@@ -188,12 +192,11 @@ int launch_paged(const PagedPlan& p, PagedArgs& a, int act, int n_seq, bool shar
     std::memcpy(a.units, c.units, sizeof(PagedUnit) * c.n_units);
     a.n_stages = c.n_stages;
     a.shared = shared;
-    const bool wide = c.form.ks == 0;
-    const PagedFn fn = wide ? (act == PALU_F16 ? paged_wide_form<F16>(c.form.vb) : paged_wide_form<BF16>(c.form.vb))
-                            : (act == PALU_F16 ? paged_form<F16>(c.form) : paged_form<BF16>(c.form));
+    const PagedFn fn = act == PALU_F16 ? (c.form.many ? paged_rows_form<F16>(c.form) : paged_form<F16>(c.form))
+                                       : (c.form.many ? paged_rows_form<BF16>(c.form) : paged_form<BF16>(c.form));
     int st = allow_lds(fn, (size_t)c.lds_bytes);
     if (st != PALU_OK) return st;
-    hipLaunchKernelGGL(fn, dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)), dim3(wide ? kPagedWideThreads : kPagedThreads),
+    hipLaunchKernelGGL(fn, dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)), dim3(c.form.many ? kPagedRowsThreads : kPagedThreads),
                        (unsigned)c.lds_bytes, s, a);
     if ((st = launch_ok()) != PALU_OK) return st;
   }

@@ -48,26 +48,41 @@ __device__ __forceinline__ void load_to_lds(const void* g, uint32_t m0) {
 __device__ __forceinline__ void load_to_lds4(const void* g, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(m0), "v"(g) : "memory");
 }
-// waits until at most n (rounded down to what is listed) of this wavefront's vector-memory operations are outstanding
-__device__ __forceinline__ void wait_vm(int n) {
-  if (n >= 36) asm volatile("s_waitcnt vmcnt(36)" ::: "memory");
-  else if (n >= 30) asm volatile("s_waitcnt vmcnt(30)" ::: "memory");
-  else if (n >= 27) asm volatile("s_waitcnt vmcnt(27)" ::: "memory");
-  else if (n >= 24) asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
-  else if (n >= 20) asm volatile("s_waitcnt vmcnt(20)" ::: "memory");
-  else if (n >= 18) asm volatile("s_waitcnt vmcnt(18)" ::: "memory");
-  else if (n >= 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-  else if (n >= 14) asm volatile("s_waitcnt vmcnt(14)" ::: "memory");
-  else if (n >= 12) asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
-  else if (n >= 10) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
-  else if (n >= 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-  else if (n >= 6) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
-  else if (n == 5) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
-  else if (n == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-  else if (n == 3) asm volatile("s_waitcnt vmcnt(3)" ::: "memory");
-  else if (n == 2) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
-  else if (n == 1) asm volatile("s_waitcnt vmcnt(1)" ::: "memory");
-  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+// Waits until at most so many of this wavefront's vector-memory operations are outstanding: one of 16 numbers, by its index.
+__device__ __forceinline__ int wait_class(int n) { return n >= 48 ? 15 : (n >= 40 ? 14 : (n >= 32 ? 13 : (n >= 24 ? 12 : (n >= 16 ? 8 + (n - 16) / 2 : n / 2)))); }
+__device__ __forceinline__ void wait_vm(int cls) {
+#define PALU_WAIT(i, n) case i: asm volatile("s_waitcnt vmcnt(" #n ")" ::: "memory"); break
+  switch (cls) {
+    PALU_WAIT(1, 2);
+    PALU_WAIT(2, 4);
+    PALU_WAIT(3, 6);
+    PALU_WAIT(4, 8);
+    PALU_WAIT(5, 10);
+    PALU_WAIT(6, 12);
+    PALU_WAIT(7, 14);
+    PALU_WAIT(8, 16);
+    PALU_WAIT(9, 18);
+    PALU_WAIT(10, 20);
+    PALU_WAIT(11, 22);
+    PALU_WAIT(12, 24);
+    PALU_WAIT(13, 32);
+    PALU_WAIT(14, 40);
+    PALU_WAIT(15, 48);
+    default: asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+#undef PALU_WAIT
+}
+// the larger of x over 16 lanes
+__device__ __forceinline__ float max_of_row(float x) {
+  auto other = [&](auto ctrl) __attribute__((always_inline)) {
+    const int u = __builtin_bit_cast(int, x);
+    x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, decltype(ctrl)::value, 0xf, 0xf, false)));
+  };
+  other(IntC<0xB1>());                         // lane ^ 1, ^ 2 in a quad, mirrored in 8 lanes, mirrored in 16
+  other(IntC<0x4E>());
+  other(IntC<0x141>());
+  other(IntC<0x140>());
+  return x;
 }
 // the larger of x over the four lanes that differ in lane bits 4 and 5
 __device__ __forceinline__ float max_of_4(float x) {
@@ -81,6 +96,174 @@ __device__ __forceinline__ float max_of_4(float x) {
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
+
+// What a workgroup does.
+struct PagedWork {
+  const PagedArgs& a;
+  PagedUnit un;
+  bool shared;
+  int rb, seq, chunk, L;
+  PagedSpan span;
+  int i0, i1;                                  // its tiles
+  int g, nh, h0, rk, rv, per_group, k_cols, v_cols;
+  int row0, nr, n_packed;                      // query rows per head and in all
+
+  __device__ __forceinline__ PagedWork(const PagedArgs& args) : a(args) {
+    const int bid = blockIdx.x;
+    un = a.units[bid % a.n_units];
+    int rest = bid / a.n_units;
+    rb = rest % a.n_row_blocks;
+    rest /= a.n_row_blocks;
+    shared = a.shared != 0;
+    seq = shared ? 0 : rest / a.n_slots;
+    chunk = rest - seq * a.n_slots;
+    L = shared || !a.seq_lens ? a.max_len : a.seq_lens[seq];
+    L = __builtin_amdgcn_readfirstlane(max(0, min(L, a.max_len)));
+    span = paged_span(L, a.first, a.window, a.n_sink);
+    const int n_chunks = (span.n_tiles + a.chunk_tiles - 1) / a.chunk_tiles;
+    i0 = i1 = 0;
+    if (chunk >= n_chunks) return;
+    i0 = (int)((long long)span.n_tiles * chunk / n_chunks);
+    i1 = (int)((long long)span.n_tiles * (chunk + 1) / n_chunks);
+    const PagedMeta& m = a.meta;
+    g = un.group();
+    nh = un.nh();
+    h0 = un.h0();
+    rk = m.k_off[g + 1] - m.k_off[g];
+    rv = m.v_off[g + 1] - m.v_off[g];
+    per_group = m.head_off[g + 1] - m.head_off[g];           // a unit of several groups takes whole ones
+    k_cols = un.n_groups() * rk;
+    v_cols = un.n_groups() * rv;
+    row0 = rb * a.block_rows;
+    nr = min(a.block_rows, a.rows - row0);
+    n_packed = nh * nr;
+  }
+  __device__ __forceinline__ bool idle() const { return i0 >= i1; }
+  // position of tile i, and the position whose row its token x reads (a masked token: the first attended one's)
+  __device__ __forceinline__ int tile_pos(int i) const { return kPagedTile * (i < span.sink_tiles ? i : span.tile0 + i - span.sink_tiles); }
+  __device__ __forceinline__ int token_of(int t0, int x) const {
+    const int t = t0 + x, head = t0 < span.sink ? t0 : max(t0, span.lo);
+    return t >= L || (t >= span.sink && t < span.lo) ? head : t;
+  }
+  __device__ __forceinline__ const int32_t* entry_of(int i, int x) const {
+    return a.page_table + (size_t)seq * a.table_stride + (token_of(tile_pos(i), x) >> a.page_shift);
+  }
+  __device__ __forceinline__ int row_of(int i, int x, int entry) const {
+    return (max(0, min(entry, a.n_pages - 1)) << a.page_shift) + (token_of(tile_pos(i), x) & ((1 << a.page_shift) - 1));
+  }
+  // sequence of row r of a head's rows
+  __device__ __forceinline__ int sequence_of(int r) const { return shared ? (row0 + r) / a.meta.qpk : seq; }
+  // rows of the cache that it may see
+  __device__ __forceinline__ int limit_of(int r) const { return shared ? min(L, a.seq_lens ? a.seq_lens[sequence_of(r)] : L) : L; }
+  // element offset of the weights of head hh of the unit, whose group is its hg-th
+  __device__ __forceinline__ size_t weights_of(int hh, int hg) const {
+    const int width = per_group * kDHead;
+    return a.meta.bk_off[g] + (size_t)hg * rk * width + (size_t)(hh + h0 - a.meta.head_off[g] - hg * per_group) * kDHead;
+  }
+  __device__ __forceinline__ size_t slot() const { return shared ? (size_t)chunk : (size_t)seq * a.n_slots + chunk; }
+  __device__ __forceinline__ void store_ml(int hh, int r, float top, float sum) const {
+    reinterpret_cast<float2*>(a.ml_part)[slot() * a.meta.n_heads * a.rows + (size_t)(h0 + hh) * a.rows + row0 + r] = make_float2(top, sum);
+  }
+  // packed row pr, value columns c and c + 1 of the unit; rows of other groups than the columns' are dropped
+  __device__ __forceinline__ void store_o(int pr, int c, float x, float y) const {
+    const int h = pr / nr, r = pr - h * nr, cg = c / rv;
+    if (un.n_groups() > 1 && h / per_group != cg) return;
+    const int ohead = a.meta.o_off[g] + (h0 + h - a.meta.head_off[g]) * rv;
+    *reinterpret_cast<float2*>(a.o_part + slot() * a.o_stride + (size_t)a.rows * ohead + (size_t)(row0 + r) * rv + c - cg * rv) = make_float2(x, y);
+  }
+  // rotated and scaled queries as pairs (bfloat16 layers: single numbers) of float16: [packed row][hi | lo][feature]
+  template <typename T> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch, int threads) const {
+    for (int x = threadIdx.x; x < n_packed * kHalf; x += threads) {
+      const int f = x & 63, pr = x >> 6, h = pr / nr, r = pr - h * nr;
+      const int b = sequence_of(r), qh = shared ? row0 + r - b * a.meta.qpk : row0 + r;
+      const uint16_t* qp = a.q + ((size_t)b * a.meta.n_heads * a.meta.qpk + (h0 + h) * a.meta.qpk + qh) * kDHead;
+      const float x0 = T::to_float(qp[f]), x1 = T::to_float(qp[f + kHalf]);
+      int pos = a.q_pos ? a.q_pos[b] : (a.seq_lens ? a.seq_lens[b] : a.pos_len) - 1;
+      pos = max(0, min(pos, a.rope_len - 1));
+      const float k = a.scale / kKeyScale;
+      const float c = a.rope[rope_f32_index(pos, f, 0, kRopeTableStride)] * k, s = a.rope[rope_f32_index(pos, f, 1, kRopeTableStride)] * k;
+      uint32_t hi, lo;
+      split2<F16>(x0 * c - x1 * s, x1 * c + x0 * s, &hi, &lo);
+      uint16_t* y = reinterpret_cast<uint16_t*>(q + pr * pitch) + f;
+      y[0] = (uint16_t)hi;
+      y[kHalf] = (uint16_t)(hi >> 16);
+      if (__is_same(T, F16)) {
+        y[kDHead] = (uint16_t)lo;
+        y[kDHead + kHalf] = (uint16_t)(lo >> 16);
+      }
+    }
+  }
+};
+
+// A ring of n stages of `size` bytes from LDS byte `first` on: the stages before and behind `at`.
+struct PagedRing {
+  int first, size, n;
+  __device__ __forceinline__ int stage(int i) const { return first + i % n * size; }
+  __device__ __forceinline__ int before(int at) const { return at == first ? first + (n - 1) * size : at - size; }
+  __device__ __forceinline__ int behind(int at) const { return at + size == first + n * size ? first : at + size; }
+};
+
+// A sub-tile's 16 tokens are columns of its keys in the order 0 4 8 12 1 5 .., so that a lane's four scores are of tokens 4 apart:
+// operands of the value product whose lane groups read tokens side by side.
+__device__ __forceinline__ int paged_token(int col) { return 4 * (col & 3) + (col >> 2); }
+// Piece p of a staged row lies at piece p ^ key: of keys so that eight lanes that read eight tokens' same piece find it on all
+// banks, of values so that the four tokens that the lane groups read do.
+__device__ __forceinline__ int paged_key_swizzle(int x) { return 4 * (x & 1) + (x >> 2 & 3); }
+__device__ __forceinline__ int paged_value_swizzle(int x) { return 4 * (x & 3); }
+// where a lane that moves piece p (of `cols` columns from column col0 on; pieces behind the last repeat the first) finds it in a row
+__device__ __forceinline__ const unsigned char* paged_source(const uint16_t* base, int col0, int cols, int p) {
+  return reinterpret_cast<const unsigned char*>(base + col0 + (p * 8 < cols ? p * 8 : 0));
+}
+
+// Angles of every 16 tokens' first position, [sub-tile][cos 64 | sin 64] in LDS: one wavefront makes them, a lane per rotation pair, a tile
+// ahead, by turning those before by 16 positions, from anchors every kPagedAnchorTiles tiles (and where positions jump) that come
+// from the table, whose rows of one position lie in 128 cache lines: every tile's from there took a quarter of the time.  A turn rounds twice at
+// 2^-24: 1e-7 or so, as the table.
+struct PagedAngles {
+  const PagedWork& w;
+  unsigned char* lds;
+  uint32_t lds0;
+  int base, anchors, lane;
+  float c, s, turn_c, turn_s;                  // of the next tile; of 16 positions
+
+  __device__ __forceinline__ bool anchor(int j) const { return j > w.i0 + 1 && j < w.i1 && ((j - w.i0) % kPagedAnchorTiles == 0 || j == w.span.sink_tiles); }
+  __device__ __forceinline__ const float* table(int pos, int cs) const {
+    return w.a.rope + rope_f32_index(min(pos, w.a.rope_len - 1), lane, cs, kRopeTableStride);
+  }
+  __device__ __forceinline__ void request(int j) const {
+    if (!anchor(j)) return;
+    const uint32_t at = lds0 + anchors + j % kPagedMaxStages * (kDHead * 4);
+    load_to_lds4(table(w.tile_pos(j), 0), at);
+    load_to_lds4(table(w.tile_pos(j), 1), at + kHalf * 4);
+  }
+  __device__ __forceinline__ void make(int j) {
+    if (anchor(j)) {
+      const float* at = reinterpret_cast<const float*>(lds + anchors + j % kPagedMaxStages * (kDHead * 4));
+      c = at[lane];
+      s = at[kHalf + lane];
+    }
+    float* at = reinterpret_cast<float*>(lds + base + j % kPagedBaseSlots * (kPagedTile / 16) * kDHead * 4);
+#pragma unroll
+    for (int sub = 0; sub < kPagedTile / 16; ++sub) {
+      at[sub * kDHead + lane] = c;
+      at[sub * kDHead + kHalf + lane] = s;
+      const float next = __builtin_fmaf(c, turn_c, -(s * turn_s));
+      s = __builtin_fmaf(s, turn_c, c * turn_s);
+      c = next;
+    }
+  }
+  // angles of the first two tiles, and anchors up to tile i0 + stages - 1
+  __device__ __forceinline__ void begin(int stages) {
+    turn_c = *table(16, 0);
+    turn_s = *table(16, 1);
+    for (int j = w.i0; j <= w.i0 + 1 && j < w.i1; ++j) {
+      c = *table(w.tile_pos(j), 0);
+      s = *table(w.tile_pos(j), 1);
+      if (j == w.i0) make(j);
+    }
+    for (int j = w.i0 + 2; j < w.i0 + stages; ++j) request(j);
+  }
+};
 
 }  // namespace
 
