@@ -155,6 +155,7 @@ struct PagedForm {
 template <typename T> PagedFn paged_form(const PagedForm& f);
 template <typename T> PagedFn paged_rows_form(const PagedForm& f);
 using PagedMergeFn = void (*)(PagedMergeArgs);
-template <typename T> PagedMergeFn paged_merge_form();
+// rows: of one key/value head per workgroup, 1, 2, 4 or 8
+template <typename T> PagedMergeFn paged_merge_form(int rows);
 
 }  // namespace palu

@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 
   wait_vm(0);
   lds_barrier();
-  const int steady = wait_class((NB - 2) * per_interval);
+  const int steady = (NB - 2) * per_interval;
 
   const int my_row = works && col < nr ? hh * nr + col : n_packed;       // where this lane's scores go; of no row: behind the last
   const unsigned char* const q_row = lds + ld.q + (hh * nr + min(col, nr - 1)) * ld.q_pitch + 2 * (fbase + NP * kg);

@@ -276,7 +276,10 @@ int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32
   e.n_shared = c.shared.n_slots;
   e.o_shared_stride = c.shared.o_stride;
   e.meta = m;
-  hipLaunchKernelGGL(desc->act_dtype == PALU_F16 ? paged_merge_form<F16>() : paged_merge_form<BF16>(), dim3((unsigned)ceil_div(batch * m.qpk, 16), (unsigned)m.n_heads), dim3(256), 0, s, e);
+  int per_wg = 8;                              // rows of a head per workgroup: fewer until there are two workgroups per compute unit
+  while (per_wg > 1 && (long long)ceil_div(batch * m.qpk, per_wg) * m.n_heads < 2 * device_cu_count()) per_wg /= 2;
+  hipLaunchKernelGGL(desc->act_dtype == PALU_F16 ? paged_merge_form<F16>(per_wg) : paged_merge_form<BF16>(per_wg),
+                     dim3((unsigned)ceil_div(batch * m.qpk, per_wg), (unsigned)m.n_heads), dim3(256), 0, s, e);
   return launch_ok();
 }
 

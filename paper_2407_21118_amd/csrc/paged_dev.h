@@ -48,29 +48,16 @@ __device__ __forceinline__ void load_to_lds(const void* g, uint32_t m0) {
 __device__ __forceinline__ void load_to_lds4(const void* g, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(m0), "v"(g) : "memory");
 }
-// Waits until at most so many of this wavefront's vector-memory operations are outstanding: one of 16 numbers, by its index.
-__device__ __forceinline__ int wait_class(int n) { return n >= 48 ? 15 : (n >= 40 ? 14 : (n >= 32 ? 13 : (n >= 24 ? 12 : (n >= 16 ? 8 + (n - 16) / 2 : n / 2)))); }
-__device__ __forceinline__ void wait_vm(int cls) {
-#define PALU_WAIT(i, n) case i: asm volatile("s_waitcnt vmcnt(" #n ")" ::: "memory"); break
-  switch (cls) {
-    PALU_WAIT(1, 2);
-    PALU_WAIT(2, 4);
-    PALU_WAIT(3, 6);
-    PALU_WAIT(4, 8);
-    PALU_WAIT(5, 10);
-    PALU_WAIT(6, 12);
-    PALU_WAIT(7, 14);
-    PALU_WAIT(8, 16);
-    PALU_WAIT(9, 18);
-    PALU_WAIT(10, 20);
-    PALU_WAIT(11, 22);
-    PALU_WAIT(12, 24);
-    PALU_WAIT(13, 32);
-    PALU_WAIT(14, 40);
-    PALU_WAIT(15, 48);
-    default: asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+// Waits until at most n of this wavefront's vector-memory operations are outstanding, or fewer: 16, 8, 4 or none.  (A branch for every
+// number took 400 cycles a tile.)
+__device__ __forceinline__ void wait_vm(int n) {
+  if (n >= 8) {
+    if (n >= 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  } else {
+    if (n >= 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
-#undef PALU_WAIT
 }
 // the larger of x over 16 lanes
 __device__ __forceinline__ float max_of_row(float x) {

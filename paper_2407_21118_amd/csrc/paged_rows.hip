@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
 
   wait_vm(0);
   lds_barrier();
-  const int steady = wait_class((NB - 2) * per_interval);
+  const int steady = (NB - 2) * per_interval;
 
   const unsigned char* const q_row = lds + ld.q + (hh * nr + min(col, nr - 1)) * ld.q_pitch + 32 * kg;
   const int h_key = paged_key_swizzle(tok);
