@@ -56,7 +56,7 @@ struct PagedUnit {
 };
 
 constexpr int kPagedProbPitch = 144;           // bytes per row of probabilities: a tile's hi, its lo and 16 bytes
-constexpr int kPagedMaxStages = 8;
+constexpr int kPagedMaxStages = 6;
 constexpr int kPagedEntrySlots = 16;           // tiles whose page-table entries are held
 constexpr int kPagedRowSlots = 8;              // ... and whose tokens' rows of the cache
 constexpr int kPagedLdsBytes = 160 * 1024;     // of a compute unit
@@ -67,15 +67,18 @@ struct PagedLds {
   int k_pieces, v_pieces;
   int q_pitch;                                 // bytes per packed query row
   int stage_k, stage_v;                        // bytes per staged tile
-  int k, v, base, anchors, entries, rows, q, s, p, alpha, total;
+  int k, v, base, anchors, entries, rows, q, turned, ang, s, p, alpha, total;
 };
 constexpr int kPagedScorePitch = 36;           // floats per row of scores: a tile and 16 bytes
 constexpr int kPagedScoreSlots = 3;            // tiles whose scores are held
 constexpr int kPagedBaseSlots = 3;             // ... and whose first angles
+constexpr int kPagedAnchorSlots = 8;
+constexpr int kPagedTurnedSlots = 5;           // sub-tiles whose turned queries are held: the first of two tiles, the second of three
+constexpr int kPagedAngPitch = kDHead + 4;     // floats per token of the angles of the first 16 positions
 constexpr int kPagedAnchorTiles = 8;           // every so many tiles their angles come from the table
 // n_groups groups of the unit, ks steps of 32 key channels each; rows: packed query rows, in row_tiles tiles of 16; planes: partial
-// scores that are added up (0: none go through LDS)
-__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, int planes, bool pairs, int n_stages) {
+// scores that are added up (0: none go through LDS); turned: queries are turned to every sub-tile's first position, else keys by its angle
+__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, int planes, bool turned, bool pairs, int n_stages) {
   PagedLds l;
   const int k_pieces = n_groups * ks * 4;
   l.k_pieces = k_pieces <= 8 ? 8 : (k_pieces <= 16 ? 16 : (k_pieces <= 32 ? 32 : 64));
@@ -87,10 +90,12 @@ __host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int
   l.v = l.k + n_stages * l.stage_k;
   l.base = l.v + n_stages * l.stage_v;
   l.anchors = l.base + kPagedBaseSlots * (kPagedTile / 16) * kDHead * 4;
-  l.entries = l.anchors + kPagedMaxStages * kDHead * 4;
+  l.entries = l.anchors + kPagedAnchorSlots * kDHead * 4;
   l.rows = l.entries + kPagedEntrySlots * kPagedTile * 4;
   l.q = l.rows + kPagedRowSlots * kPagedTile * 4;
-  l.s = l.q + rows * l.q_pitch;
+  l.turned = l.q + rows * (turned ? kDHead * 4 : l.q_pitch);                   // (float32 numbers to be turned)
+  l.ang = l.turned + (turned ? kPagedTurnedSlots * rows * l.q_pitch : 0);
+  l.s = l.ang + (planes && !turned ? 16 * kPagedAngPitch * 4 : 0);
   l.p = l.s + kPagedScoreSlots * planes * (rows + 1) * kPagedScorePitch * 4;
   l.alpha = l.p + 2 * (row_tiles * 16 + 1) * kPagedProbPitch;
   l.total = l.alpha + 2 * (row_tiles * 16 + 4) * 4;
@@ -147,7 +152,8 @@ using PagedFn = void (*)(PagedArgs);
 // or 16 (of two), and vb: blocks of 256 value columns; paged_rows_kernel (many: up to 16 rows per head, ks up to 8) likewise
 struct PagedForm {
   int ks, vb;
-  bool many;
+  bool many;                               // paged_rows_kernel
+  bool turned;                             // paged_kernel: queries are turned to the tiles, for up to 8 packed rows
   int parts() const { return ks > 8 ? 4 : 2; }           // paged_kernel: wavefronts that share a head's features
   int unit_heads() const { return 8 / parts(); }
   int max_rows() const { return many ? (vb == 1 ? 64 : 32) : 16; }   // packed

@@ -29,13 +29,12 @@
 
 namespace palu {
 
-template <typename T, int FQ, int KS, int VB>
+template <typename T, int FQ, int KS, int VB, bool TURN>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   constexpr bool PAIR = __is_same(T, F16);     // queries and keys as pairs hi + lo
   constexpr int NH = 8 / FQ;
   constexpr int FT = 8 / FQ;                   // tiles of 16 features per wavefront: low halves of the rotation pairs, then high halves
   constexpr int NP = 16 / FQ;                  // rotation pairs per lane
-  constexpr int NT = NP / 4;                   // contraction steps of the query product: four pairs' low and high halves each
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -46,7 +45,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   if (w.idle()) return;
   const int i0 = w.i0, i1 = w.i1, nr = w.nr, n_packed = w.n_packed;
   const int NB = a.n_stages;
-  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, n_packed, 1, FQ, PAIR, NB);
+  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, n_packed, 1, FQ, TURN, PAIR, NB);
   const uint32_t lds0 = lds_addr(lds);
   const bool works = wave % NH < w.nh;                       // else: the same instructions, results nowhere
   const int hh = works ? wave % NH : 0, fq = wave / NH;
@@ -124,17 +123,26 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   for (int j = i0; j < min(i0 + NB - 4, i1); ++j) request_values(j, ring_v.stage(j));
 
   PagedAngles angles{w, lds, lds0, ld.base, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
-  if (wave == 3) angles.begin(NB);
+  if (wave == 3) {
+    angles.begin(NB + (TURN ? 1 : 0));
+    if (TURN && i0 + 1 < i1) angles.make(i0 + 1);
+  }
 
   const int tok = paged_token(col);
   // angles of position tok, of this lane's rotation pairs fbase + NP kg ..; scaled
   float ang_c[NP], ang_s[NP];
+  if (TURN) {
 #pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    ang_c[p] = kKeyScale * a.rope[rope_f32_index(tok, fbase + NP * kg + p, 0, kRopeTableStride)];
-    ang_s[p] = kKeyScale * a.rope[rope_f32_index(tok, fbase + NP * kg + p, 1, kRopeTableStride)];
+    for (int p = 0; p < NP; ++p) {
+      ang_c[p] = kKeyScale * a.rope[rope_f32_index(tok, fbase + NP * kg + p, 0, kRopeTableStride)];
+      ang_s[p] = kKeyScale * a.rope[rope_f32_index(tok, fbase + NP * kg + p, 1, kRopeTableStride)];
+    }
+  } else {
+    float* ang = reinterpret_cast<float*>(lds + ld.ang);
+    for (int x = tid; x < 16 * kDHead; x += kPagedThreads)
+      ang[(x & 15) * kPagedAngPitch + (x >> 4)] = kKeyScale * a.rope[rope_f32_index(x & 15, (x >> 4) & 63, x >> 10, kRopeTableStride)];
   }
-  w.rotate_queries<T>(lds + ld.q, ld.q_pitch, kPagedThreads);
+  w.rotate_queries<T, TURN>(lds + ld.q, ld.q_pitch, kPagedThreads);
 
   // weights.  FQ = 2: rotation pair fbase + 2 m + j is row m of tile j (low half) and 2 + j (high half); FQ = 4: pair fbase + m of tiles
   // 0 and 1.  A lane reads its features from eight rows of B_k and transposes them.  They stay in the accumulation registers, which the
@@ -143,27 +151,34 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   {
     const int width = w.per_group * kDHead;
     const uint16_t* B = a.Bk + w.weights_of(hh, hg) + fbase;
+    constexpr int AHEAD = KS < 4 ? KS : 4;                   // steps whose rows are in flight
+    uint32_t v[AHEAD][2][8];
+    auto fetch = [&](int ks) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint16_t* row = B + (size_t)min(32 * ks + 8 * kg + e, w.rk - 1) * width;
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+          v[ks % AHEAD][side][e] = FQ == 2 ? *reinterpret_cast<const uint32_t*>(row + side * kHalf + 2 * col) : (uint32_t)row[side * kHalf + col];
+      }
+    };
+#pragma unroll
+    for (int ks = 0; ks < AHEAD; ++ks) fetch(ks);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
+      const uint32_t keep = 32 * ks < w.rk ? 0xffffffffu : 0u;           // rows behind the rank: zero
 #pragma unroll
       for (int side = 0; side < 2; ++side) {
-        uint32_t v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] = 0;
-          if (32 * ks < w.rk) {
-            const uint16_t* row = B + (size_t)(32 * ks + 8 * kg + e) * width + side * kHalf;
-            v[e] = FQ == 2 ? *reinterpret_cast<const uint32_t*>(row + 2 * col) : (uint32_t)row[col];
-          }
-        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          W[ks][side * (FT / 2)][i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x05040100u);
-          if (FQ == 2) W[ks][side * (FT / 2) + FT / 2 - 1][i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x07060302u);
+          const uint32_t x = v[ks % AHEAD][side][2 * i], y = v[ks % AHEAD][side][2 * i + 1];
+          W[ks][side * (FT / 2)][i] = keep & __builtin_amdgcn_perm(y, x, 0x05040100u);
+          if (FQ == 2) W[ks][side * (FT / 2) + FT / 2 - 1][i] = keep & __builtin_amdgcn_perm(y, x, 0x07060302u);
         }
       }
 #pragma unroll
       for (int j = 0; j < FT; ++j) asm volatile("" : "+a"(W[ks][j]));
+      if (ks + AHEAD < KS) fetch(ks + AHEAD);
     }
   }
 
@@ -177,12 +192,28 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   float run_max = -INFINITY, run_sum = 0.f;
   const int limit = srow < n_packed ? w.limit_of(srow % nr) : w.L;
 
+  // The queries turned back to the first position of every sub-tile of tile j, [turned slot][packed row][hi | lo][feature]: with them, a
+  // sub-tile's keys are rotated by the angles of 0 .. 15, which are the same for all.
+  auto turned_slot = [&](int j, int sub) __attribute__((always_inline)) { return ld.turned + (sub == 0 ? j & 1 : 2 + (j + 3) % 3) * n_packed * ld.q_pitch; };
+  auto turn_queries = [&](int j) __attribute__((always_inline)) {
+    const float* base = reinterpret_cast<const float*>(lds + ld.base) + j % kPagedBaseSlots * (kPagedTile / 16) * kDHead + lane;
+    for (int x = wave; x < 2 * n_packed; x += 8) {           // lane: rotation pair
+      const int sub = x >= n_packed, r = x - sub * n_packed;
+      const float* q = reinterpret_cast<const float*>(lds + ld.q) + r * kDHead + lane;
+      const float c = base[sub * kDHead], s = base[sub * kDHead + kHalf], x0 = q[0], x1 = q[kHalf];
+      paged_store_query<T>(lds + turned_slot(j, sub) + r * ld.q_pitch, lane, __builtin_fmaf(x0, c, x1 * s), __builtin_fmaf(x1, c, -(x0 * s)));
+    }
+  };
+  if (TURN) {
+    lds_barrier();
+    turn_queries(i0);
+  }
   wait_vm(0);
   lds_barrier();
   const int steady = (NB - 2) * per_interval;
 
   const int my_row = works && col < nr ? hh * nr + col : n_packed;       // where this lane's scores go; of no row: behind the last
-  const unsigned char* const q_row = lds + ld.q + (hh * nr + min(col, nr - 1)) * ld.q_pitch + 2 * (fbase + NP * kg);
+  const int q_lane = (hh * nr + min(col, nr - 1)) * ld.q_pitch + 2 * (fbase + NP * kg);
   const int h_key = paged_key_swizzle(tok);
   const int h_lane = tok * ld.k_pieces * 16 + hg * KS * 64, off0 = h_lane + (kg ^ h_key) * 16, off1 = h_lane + ((4 + kg) ^ h_key) * 16;
   const int v_lane = kg * ld.v_pieces * 16 + (col & 3) * 4, v_pitch16 = 4 * ld.v_pieces * 16;
@@ -194,7 +225,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   for (int j = 0; j < FT; ++j) acc[0][j] = acc[1][j] = float4v{0, 0, 0, 0};
 
   // Keys of sub-tile `sub` of the tile staged at k_stage into acc[sub]; between their matrix instructions the previous sub-tile's, of tile
-  // `np` with its angles at b_stage, are rotated, split and multiplied by the queries.  The vector work is 8 steps of about three
+  // `np` with its angles at b_stage, are rotated, split and multiplied by the queries.  The vector work is 8 steps of two or three
   // instructions for every two pairs (a matrix instruction takes the issue slots of four).
   auto keys = [&](auto sub_c, int k_stage, int np, int b_stage) __attribute__((always_inline)) {
     constexpr int sub = decltype(sub_c)::value, old = 1 - sub;
@@ -202,59 +233,57 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     const unsigned char* h0p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off0;
     const unsigned char* h1p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off1;
     const float* bas = reinterpret_cast<const float*>(lds + b_stage) + old * kDHead + fbase + NP * kg;
+    const float* ang = reinterpret_cast<const float*>(lds + ld.ang) + tok * kPagedAngPitch + fbase + NP * kg;
+    const unsigned char* q_row = lds + (TURN ? turned_slot(np, old) : ld.q) + q_lane;
     uint4v af[3];
     af[0] = *reinterpret_cast<const uint4v*>(h0p);
     af[1] = *reinterpret_cast<const uint4v*>(h1p);
-    float4v bc[NT], bs[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      bc[t] = *reinterpret_cast<const float4v*>(bas + 4 * t);
-      bs[t] = *reinterpret_cast<const float4v*>(bas + 4 * t + kHalf);
-    }
     uint32_t khi[4], klo[4];                                 // of a contraction step: low halves of four pairs, high halves
     float4v dot = {0, 0, 0, 0};
     uint2v ql[2], qh[2];
-    float t1, t2, c, s, lo[2], hi[2], l0, l1, l2;
+    float4v c4, s4;                                          // cos and sin of a step's pairs
+    float t1, t2, lo[2], hi[2], l0, l1, l2, l3;
     uint32_t x, y;
     auto step = [&](int e) __attribute__((always_inline)) {
       const int pa = 2 * (e >> 3), pb = pa + 1, t = pa >> 2, at = (e >> 3) & 1;   // pairs pa and pb
       auto low = [&](int p) { return FQ == 2 ? acc[old][p & 1][p >> 1] : acc[old][0][p]; };
       auto high = [&](int p) { return FQ == 2 ? acc[old][FT / 2 + (p & 1)][p >> 1] : acc[old][1][p]; };
+      auto cosine = [&](int p) { return TURN ? ang_c[p] : c4[p & 3]; };
+      auto sine = [&](int p) { return TURN ? ang_s[p] : s4[p & 3]; };
       switch (e & 7) {
         case 0:
-          if (at == 0) {                                     // the step's queries
+          if (at == 0) {                                     // the step's queries and angles
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               qh[u] = *reinterpret_cast<const uint2v*>(q_row + u * 128 + 8 * t);
               if (PAIR) ql[u] = *reinterpret_cast<const uint2v*>(q_row + 256 + u * 128 + 8 * t);
             }
+            if (!TURN) {
+              const float4v c0 = *reinterpret_cast<const float4v*>(bas + 4 * t), s0 = *reinterpret_cast<const float4v*>(bas + 4 * t + kHalf);
+              const float4v c1 = *reinterpret_cast<const float4v*>(ang + 4 * t), s1 = *reinterpret_cast<const float4v*>(ang + 4 * t + kHalf);
+#pragma unroll
+              for (int p = 0; p < 4; ++p) {
+                c4[p] = __builtin_fmaf(c1[p], c0[p], -(s1[p] * s0[p]));
+                s4[p] = __builtin_fmaf(s1[p], c0[p], c1[p] * s0[p]);
+              }
+            }
           }
-          t1 = ang_s[pa] * bs[t][pa & 3];
-          t2 = ang_c[pa] * bs[t][pa & 3];
-          c = __builtin_fmaf(ang_c[pa], bc[t][pa & 3], -t1);
+          t1 = high(pa) * sine(pa);
+          t2 = low(pa) * sine(pa);
           break;
         case 1:
-          s = __builtin_fmaf(ang_s[pa], bc[t][pa & 3], t2);
-          t1 = high(pa) * s;
-          t2 = low(pa) * s;
+          lo[0] = __builtin_fmaf(low(pa), cosine(pa), -t1);
+          hi[0] = __builtin_fmaf(high(pa), cosine(pa), t2);
           break;
         case 2:
-          lo[0] = __builtin_fmaf(low(pa), c, -t1);
-          hi[0] = __builtin_fmaf(high(pa), c, t2);
-          t1 = ang_s[pb] * bs[t][pb & 3];
+          t1 = high(pb) * sine(pb);
+          t2 = low(pb) * sine(pb);
           break;
         case 3:
-          t2 = ang_c[pb] * bs[t][pb & 3];
-          c = __builtin_fmaf(ang_c[pb], bc[t][pb & 3], -t1);
-          s = __builtin_fmaf(ang_s[pb], bc[t][pb & 3], t2);
+          lo[1] = __builtin_fmaf(low(pb), cosine(pb), -t1);
+          hi[1] = __builtin_fmaf(high(pb), cosine(pb), t2);
           break;
         case 4:
-          t1 = high(pb) * s;
-          t2 = low(pb) * s;
-          lo[1] = __builtin_fmaf(low(pb), c, -t1);
-          break;
-        case 5:
-          hi[1] = __builtin_fmaf(high(pb), c, t2);
           // (the empty statements: a product and its rounding stay two instructions.  As one, they would round the exact product to hi
           // where lo is measured from the float32 one, and take one instruction per number instead of one per two.)
           asm("" : "+v"(lo[0]), "+v"(lo[1]), "+v"(hi[0]), "+v"(hi[1]));
@@ -264,17 +293,22 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
           khi[at] = x;
           khi[2 + at] = y;
           break;
-        case 6:
+        case 5:
           if (PAIR) {
             l0 = less<F16>(lo[0], x, minus_one);
             l1 = less<F16>(lo[1], x >> 16, minus_one);
+          }
+          break;
+        case 6:
+          if (PAIR) {
             l2 = less<F16>(hi[0], y, minus_one);
+            l3 = less<F16>(hi[1], y >> 16, minus_one);
           }
           break;
         case 7:
           if (PAIR) {
             klo[at] = pack2<F16>(l0, l1);
-            klo[2 + at] = pack2<F16>(l2, less<F16>(hi[1], y >> 16, minus_one));
+            klo[2 + at] = pack2<F16>(l2, l3);
           }
           if (at == 1) {
             const uint4v h = {khi[0], khi[1], khi[2], khi[3]}, q = {qh[0].x, qh[0].y, qh[1].x, qh[1].y};
@@ -360,16 +394,28 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   };
 
   for (int n = i0; n < i1 + 3; ++n) {
-    if (n + NB - 1 < i1) request_keys(n + NB - 1, ring_k.before(k_at));
-    if (n + NB - 4 >= i0 && n + NB - 4 < i1) request_values(n + NB - 4, ring_v.before(v_at));
+    const bool more_k = n + NB - 1 < i1, more_v = n + NB - 4 >= i0 && n + NB - 4 < i1;
+    // (the wavefronts of a SIMD take requests and values at different times, beside the other's matrix instructions)
+    if (wave < 4) {
+      if (more_k) request_keys(n + NB - 1, ring_k.before(k_at));
+      if (n >= i0 + 3) values(n - 3, v_at);
+    } else {
+      if (more_v) request_values(n + NB - 4, ring_v.before(v_at));
+      if (4 * (wave & 3) < n_packed && n >= i0 + 2 && n < i1 + 2) softmax(n - 2);
+    }
     request_entries(n);
     if (wave == 3) {
-      angles.request(n + NB);
-      if (n + 1 < i1) angles.make(n + 1);
+      angles.request(n + NB + (TURN ? 1 : 0));
+      if (n + 1 + (TURN ? 1 : 0) < i1) angles.make(n + 1 + (TURN ? 1 : 0));
     }
-    if (wave >= 4 && 4 * (wave & 3) < n_packed && n >= i0 + 2 && n < i1 + 2) softmax(n - 2);
+    if (TURN && n + 1 < i1) turn_queries(n + 1);
     if (n <= i1) keys(IntC<0>(), k_at, n - 1, b_old);        // (behind the last tile, and of the one before the first: nothing that is used)
-    if (n >= i0 + 3) values(n - 3, v_at);
+    if (wave < 4) {
+      if (more_v) request_values(n + NB - 4, ring_v.before(v_at));
+    } else {
+      if (more_k) request_keys(n + NB - 1, ring_k.before(k_at));
+      if (n >= i0 + 3) values(n - 3, v_at);
+    }
     if (n < i1) keys(IntC<1>(), k_at, n, b_at);
     k_at = ring_k.behind(k_at);
     v_at = ring_v.behind(v_at);
@@ -398,17 +444,20 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 
 namespace {
 template <typename T, int FQ, int KS>
-PagedFn pick(int vb) { return vb == 1 ? paged_kernel<T, FQ, KS, 1> : paged_kernel<T, FQ, KS, 2>; }
+PagedFn pick(const PagedForm& f) {
+  if (f.turned) return f.vb == 1 ? paged_kernel<T, FQ, KS, 1, true> : paged_kernel<T, FQ, KS, 2, true>;
+  return f.vb == 1 ? paged_kernel<T, FQ, KS, 1, false> : paged_kernel<T, FQ, KS, 2, false>;
+}
 }  // namespace
 
 template <typename T> PagedFn paged_form(const PagedForm& f) {
   switch (f.ks) {
-    case 2: return pick<T, 2, 2>(f.vb);
-    case 4: return pick<T, 2, 4>(f.vb);
-    case 6: return pick<T, 2, 6>(f.vb);
-    case 8: return pick<T, 2, 8>(f.vb);
-    case 12: return pick<T, 4, 12>(f.vb);
-    default: return pick<T, 4, 16>(f.vb);
+    case 2: return pick<T, 2, 2>(f);
+    case 4: return pick<T, 2, 4>(f);
+    case 6: return pick<T, 2, 6>(f);
+    case 8: return pick<T, 2, 8>(f);
+    case 12: return pick<T, 4, 12>(f);
+    default: return pick<T, 4, 16>(f);
   }
 }
 template PagedFn paged_form<PALU_PAGED_ACT>(const PagedForm&);

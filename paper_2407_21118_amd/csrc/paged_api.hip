@@ -71,7 +71,7 @@ int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, 
     for (int j = 0; j < m.n_groups; ++j) any += in_class(j);
     if (!any) continue;
     PagedClass& c = p->cls[p->n_cls++];
-    c.form = PagedForm{ks, vb, false};
+    c.form = PagedForm{ks, vb, false, false};
     // Units: whole adjacent groups of equal ranks and size side by side, as far as 256 columns and the heads go (ranks in whole 64s:
     // the staged rows' layout), else parts of one group.  A unit of more heads reads its latents once for all of them.
     const int unit_heads = c.form.unit_heads();
@@ -100,11 +100,13 @@ int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, 
     c.form.many = ks <= 8 && most * rows > 16;
     auto lds_bytes = [&](int stages) {
       const int packed = most * c.block_rows;
-      return paged_lds(k_groups, ks, v_cols, packed, c.form.many ? c.form.max_rows() / 16 : 1, c.form.many ? 0 : c.form.parts(), act == PALU_F16, stages).total;
+      return paged_lds(k_groups, ks, v_cols, packed, c.form.many ? c.form.max_rows() / 16 : 1, c.form.many ? 0 : c.form.parts(), c.form.turned,
+                       act == PALU_F16, stages).total;
     };
     for (int limit = std::min(16, c.form.max_rows() / most); limit > 0; --limit) {   // (fewer where two stages leave no more LDS)
       c.n_row_blocks = ceil_div(rows, limit);
       c.block_rows = ceil_div(rows, c.n_row_blocks);
+      c.form.turned = !c.form.many && most * c.block_rows <= 8;
       if (lds_bytes(2) <= kPagedLdsBytes) break;
     }
     if (lds_bytes(2) > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;

@@ -84,6 +84,19 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// features f and f + 64 of a query as an operand of the score product
+template <typename T> __device__ __forceinline__ void paged_store_query(unsigned char* row, int f, float y0, float y1) {
+  uint32_t hi, lo;
+  split2<F16>(y0, y1, &hi, &lo);
+  uint16_t* y = reinterpret_cast<uint16_t*>(row) + f;
+  y[0] = (uint16_t)hi;
+  y[kHalf] = (uint16_t)(hi >> 16);
+  if (__is_same(T, F16)) {
+    y[kDHead] = (uint16_t)lo;
+    y[kDHead + kHalf] = (uint16_t)(lo >> 16);
+  }
+}
+
 // What a workgroup does.
 struct PagedWork {
   const PagedArgs& a;
@@ -158,8 +171,9 @@ struct PagedWork {
     const int ohead = a.meta.o_off[g] + (h0 + h - a.meta.head_off[g]) * rv;
     *reinterpret_cast<float2*>(a.o_part + slot() * a.o_stride + (size_t)a.rows * ohead + (size_t)(row0 + r) * rv + c - cg * rv) = make_float2(x, y);
   }
-  // rotated and scaled queries as pairs (bfloat16 layers: single numbers) of float16: [packed row][hi | lo][feature]
-  template <typename T> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch, int threads) const {
+  // rotated and scaled queries: float32 numbers [packed row][feature], or pairs (bfloat16 layers: single numbers) of float16
+  // [packed row][hi | lo][feature]
+  template <typename T, bool FLOAT> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch, int threads) const {
     for (int x = threadIdx.x; x < n_packed * kHalf; x += threads) {
       const int f = x & 63, pr = x >> 6, h = pr / nr, r = pr - h * nr;
       const int b = sequence_of(r), qh = shared ? row0 + r - b * a.meta.qpk : row0 + r;
@@ -169,14 +183,12 @@ struct PagedWork {
       pos = max(0, min(pos, a.rope_len - 1));
       const float k = a.scale / kKeyScale;
       const float c = a.rope[rope_f32_index(pos, f, 0, kRopeTableStride)] * k, s = a.rope[rope_f32_index(pos, f, 1, kRopeTableStride)] * k;
-      uint32_t hi, lo;
-      split2<F16>(x0 * c - x1 * s, x1 * c + x0 * s, &hi, &lo);
-      uint16_t* y = reinterpret_cast<uint16_t*>(q + pr * pitch) + f;
-      y[0] = (uint16_t)hi;
-      y[kHalf] = (uint16_t)(hi >> 16);
-      if (__is_same(T, F16)) {
-        y[kDHead] = (uint16_t)lo;
-        y[kDHead + kHalf] = (uint16_t)(lo >> 16);
+      if (FLOAT) {
+        float* y = reinterpret_cast<float*>(q) + pr * kDHead + f;
+        y[0] = x0 * c - x1 * s;
+        y[kHalf] = x1 * c + x0 * s;
+      } else {
+        paged_store_query<T>(q + pr * pitch, f, x0 * c - x1 * s, x1 * c + x0 * s);
       }
     }
   }
@@ -219,13 +231,13 @@ struct PagedAngles {
   }
   __device__ __forceinline__ void request(int j) const {
     if (!anchor(j)) return;
-    const uint32_t at = lds0 + anchors + j % kPagedMaxStages * (kDHead * 4);
+    const uint32_t at = lds0 + anchors + j % kPagedAnchorSlots * (kDHead * 4);
     load_to_lds4(table(w.tile_pos(j), 0), at);
     load_to_lds4(table(w.tile_pos(j), 1), at + kHalf * 4);
   }
   __device__ __forceinline__ void make(int j) {
     if (anchor(j)) {
-      const float* at = reinterpret_cast<const float*>(lds + anchors + j % kPagedMaxStages * (kDHead * 4));
+      const float* at = reinterpret_cast<const float*>(lds + anchors + j % kPagedAnchorSlots * (kDHead * 4));
       c = at[lane];
       s = at[kHalf + lane];
     }
@@ -239,16 +251,18 @@ struct PagedAngles {
       c = next;
     }
   }
-  // angles of the first two tiles, and anchors up to tile i0 + stages - 1
-  __device__ __forceinline__ void begin(int stages) {
+  // angles of the first tile and state for the second, from the table; anchors before tile i0 + ahead
+  __device__ __forceinline__ void begin(int ahead) {
+    const int next = w.tile_pos(min(w.i0 + 1, w.i1 - 1));
     turn_c = *table(16, 0);
     turn_s = *table(16, 1);
-    for (int j = w.i0; j <= w.i0 + 1 && j < w.i1; ++j) {
-      c = *table(w.tile_pos(j), 0);
-      s = *table(w.tile_pos(j), 1);
-      if (j == w.i0) make(j);
-    }
-    for (int j = w.i0 + 2; j < w.i0 + stages; ++j) request(j);
+    c = *table(w.tile_pos(w.i0), 0);
+    s = *table(w.tile_pos(w.i0), 1);
+    const float c1 = *table(next, 0), s1 = *table(next, 1);
+    make(w.i0);
+    c = c1;
+    s = s1;
+    for (int j = w.i0 + 2; j < w.i0 + ahead; ++j) request(j);
   }
 };
 

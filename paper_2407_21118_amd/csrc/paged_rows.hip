@@ -26,7 +26,7 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
   if (w.idle()) return;
   const int i0 = w.i0, i1 = w.i1, nr = w.nr, n_packed = w.n_packed;
   const int NB = a.n_stages;
-  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, n_packed, PT, 0, PAIR, NB);
+  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, n_packed, PT, 0, false, PAIR, NB);
   const uint32_t lds0 = lds_addr(lds);
   const bool works = wave < w.nh;                            // else: the same instructions, results nowhere
   const int hh = works ? wave : 0;
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
     ang_c[p] = kKeyScale * a.rope[rope_f32_index(tok, 16 * kg + p, 0, kRopeTableStride)];
     ang_s[p] = kKeyScale * a.rope[rope_f32_index(tok, 16 * kg + p, 1, kRopeTableStride)];
   }
-  w.rotate_queries<T>(lds + ld.q, ld.q_pitch, kPagedRowsThreads);
+  w.rotate_queries<T, false>(lds + ld.q, ld.q_pitch, kPagedRowsThreads);
 
   // weights: feature 4 m + j (j < 4) or 64 + 4 m + j - 4 is row m of tile j, so that a lane holds both features of a rotation
   // pair.  A lane reads its four features of either half from eight rows of B_k and transposes them.  They stay in the
@@ -128,27 +128,30 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
   {
     const int width = w.per_group * kDHead;
     const uint16_t* B = a.Bk + w.weights_of(hh, hg) + 4 * col;
+    constexpr int AHEAD = KS < 3 ? KS : 3;                   // steps whose rows are in flight
+    uint2v v[AHEAD][2][8];
+    auto fetch = [&](int ks) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint16_t* row = B + (size_t)min(32 * ks + 8 * kg + e, w.rk - 1) * width;
+        v[ks % AHEAD][0][e] = *reinterpret_cast<const uint2v*>(row);
+        v[ks % AHEAD][1][e] = *reinterpret_cast<const uint2v*>(row + kHalf);
+      }
+    };
+#pragma unroll
+    for (int ks = 0; ks < AHEAD; ++ks) fetch(ks);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      uint2v v[2][8];
-      if (32 * ks < w.rk) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint16_t* row = B + (size_t)(32 * ks + 8 * kg + e) * width;
-          v[0][e] = *reinterpret_cast<const uint2v*>(row);
-          v[1][e] = *reinterpret_cast<const uint2v*>(row + kHalf);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[0][e] = v[1][e] = uint2v{0, 0};
-      }
+      const uint32_t keep = 32 * ks < w.rk ? 0xffffffffu : 0u;           // rows behind the rank: zero
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          W[ks][j][i] = __builtin_amdgcn_perm(v[j >> 2][2 * i + 1][(j >> 1) & 1], v[j >> 2][2 * i][(j >> 1) & 1], (j & 1) ? 0x07060302u : 0x05040100u);
+          W[ks][j][i] = keep & __builtin_amdgcn_perm(v[ks % AHEAD][j >> 2][2 * i + 1][(j >> 1) & 1], v[ks % AHEAD][j >> 2][2 * i][(j >> 1) & 1],
+                                                     (j & 1) ? 0x07060302u : 0x05040100u);
         asm volatile("" : "+a"(W[ks][j]));
       }
+      if (ks + AHEAD < KS) fetch(ks + AHEAD);
     }
   }
 
