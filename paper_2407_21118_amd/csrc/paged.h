@@ -6,8 +6,7 @@
 namespace palu {
 
 constexpr int kPagedTile = 32;                 // tokens per tile: positions 32 i .. 32 i + 31
-constexpr int kPagedThreads = 512;             // paged_kernel: eight wavefronts, two per SIMD
-constexpr int kPagedRowsThreads = 256;         // paged_rows_kernel: four
+constexpr int kPagedThreads = 512;             // eight wavefronts, two per SIMD
 
 // Layer metadata; heads are KEY/VALUE heads here.  Everything indexed by the group is 32 bits wide: beside an array of 16-bit
 // numbers with the same index the compiler addresses these from a base that lies on no whole word, and scalar loads drop its low bits.
@@ -70,15 +69,15 @@ struct PagedLds {
   int k, v, base, anchors, entries, rows, q, turned, ang, s, p, alpha, total;
 };
 constexpr int kPagedScorePitch = 36;           // floats per row of scores: a tile and 16 bytes
+constexpr int kPagedHalfPitch = 20;            // ... of a sub-tile of 16 tokens
 constexpr int kPagedScoreSlots = 3;            // tiles whose scores are held
 constexpr int kPagedBaseSlots = 3;             // ... and whose first angles
 constexpr int kPagedAnchorSlots = 8;
 constexpr int kPagedTurnedSlots = 5;           // sub-tiles whose turned queries are held: the first of two tiles, the second of three
 constexpr int kPagedAngPitch = kDHead + 4;     // floats per token of the angles of the first 16 positions
 constexpr int kPagedAnchorTiles = 8;           // every so many tiles their angles come from the table
-// n_groups groups of the unit, ks steps of 32 key channels each; rows: packed query rows, in row_tiles tiles of 16; planes: partial
-// scores that are added up (0: none go through LDS); turned: queries are turned to every sub-tile's first position, else keys by its angle
-__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, int planes, bool turned, bool pairs, int n_stages) {
+// n_groups groups of the unit, ks steps of 32 key channels each; what both kernels have
+__host__ __device__ __forceinline__ PagedLds paged_lds_head(int n_groups, int ks, int v_cols, bool pairs, int n_stages) {
   PagedLds l;
   const int k_pieces = n_groups * ks * 4;
   l.k_pieces = k_pieces <= 8 ? 8 : (k_pieces <= 16 ? 16 : (k_pieces <= 32 ? 32 : 64));
@@ -88,17 +87,37 @@ __host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int
   l.stage_v = kPagedTile * l.v_pieces * 16;
   l.k = 0;
   l.v = l.k + n_stages * l.stage_k;
-  l.base = l.v + n_stages * l.stage_v;
-  l.anchors = l.base + kPagedBaseSlots * (kPagedTile / 16) * kDHead * 4;
+  l.anchors = l.v + n_stages * l.stage_v;
   l.entries = l.anchors + kPagedAnchorSlots * kDHead * 4;
   l.rows = l.entries + kPagedEntrySlots * kPagedTile * 4;
-  l.q = l.rows + kPagedRowSlots * kPagedTile * 4;
+  return l;
+}
+// of paged_kernel: rows packed query rows; parts: partial scores that are added up; turned: queries are turned to every sub-tile's
+// first position, else keys by its angle
+__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int parts, bool turned, bool pairs, int n_stages) {
+  PagedLds l = paged_lds_head(n_groups, ks, v_cols, pairs, n_stages);
+  l.base = l.rows + kPagedRowSlots * kPagedTile * 4;
+  l.q = l.base + kPagedBaseSlots * (kPagedTile / 16) * kDHead * 4;
   l.turned = l.q + rows * (turned ? kDHead * 4 : l.q_pitch);                   // (float32 numbers to be turned)
   l.ang = l.turned + (turned ? kPagedTurnedSlots * rows * l.q_pitch : 0);
-  l.s = l.ang + (planes && !turned ? 16 * kPagedAngPitch * 4 : 0);
-  l.p = l.s + kPagedScoreSlots * planes * (rows + 1) * kPagedScorePitch * 4;
-  l.alpha = l.p + 2 * (row_tiles * 16 + 1) * kPagedProbPitch;
-  l.total = l.alpha + 2 * (row_tiles * 16 + 4) * 4;
+  l.s = l.ang + (turned ? 0 : 16 * kPagedAngPitch * 4);
+  l.p = l.s + kPagedScoreSlots * parts * (rows + 1) * kPagedScorePitch * 4;
+  l.alpha = l.p + 2 * 17 * kPagedProbPitch;
+  l.total = l.alpha + 2 * 20 * 4;
+  return l;
+}
+// of paged_rows_kernel: packed query rows in row_tiles tiles of 16.  Queries lie where scores and probabilities come later.
+__host__ __device__ __forceinline__ PagedLds paged_rows_lds(int n_groups, int ks, int v_cols, int row_tiles, bool pairs, int n_stages) {
+  PagedLds l = paged_lds_head(n_groups, ks, v_cols, pairs, n_stages);
+  l.base = l.turned = 0;
+  l.ang = l.rows + kPagedRowSlots * kPagedTile * 4;
+  l.alpha = l.ang + 2 * 16 * kPagedAngPitch * 4;
+  l.s = l.alpha + row_tiles * 16 * 4;
+  l.p = l.s + 3 * 2 * (row_tiles * 16 + 1) * kPagedHalfPitch * 4;
+  l.q = l.s;
+  l.total = l.p + (row_tiles * 16 + 1) * kPagedProbPitch;
+  const int q_end = l.q + row_tiles * 16 * l.q_pitch;
+  if (l.total < q_end) l.total = q_end;
   return l;
 }
 

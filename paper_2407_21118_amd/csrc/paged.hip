@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   if (w.idle()) return;
   const int i0 = w.i0, i1 = w.i1, nr = w.nr, n_packed = w.n_packed;
   const int NB = a.n_stages;
-  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, n_packed, 1, FQ, TURN, PAIR, NB);
+  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, n_packed, FQ, TURN, PAIR, NB);
   const uint32_t lds0 = lds_addr(lds);
   const bool works = wave % NH < w.nh;                       // else: the same instructions, results nowhere
   const int hh = works ? wave % NH : 0, fq = wave / NH;
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     }
     request_entries(n);
     if (wave == 3) {
-      angles.request(n + NB + (TURN ? 1 : 0));
+      angles.request(n + NB + (TURN ? 1 : 0), i0 + 1);
       if (n + 1 + (TURN ? 1 : 0) < i1) angles.make(n + 1 + (TURN ? 1 : 0));
     }
     if (TURN && n + 1 < i1) turn_queries(n + 1);

@@ -99,9 +99,8 @@ int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, 
     // Query rows: 16 in all, or 16 per head and as many as accumulators go where there are more; as many blocks of them as it takes
     c.form.many = ks <= 8 && most * rows > 16;
     auto lds_bytes = [&](int stages) {
-      const int packed = most * c.block_rows;
-      return paged_lds(k_groups, ks, v_cols, packed, c.form.many ? c.form.max_rows() / 16 : 1, c.form.many ? 0 : c.form.parts(), c.form.turned,
-                       act == PALU_F16, stages).total;
+      return c.form.many ? paged_rows_lds(k_groups, ks, v_cols, c.form.max_rows() / 16, act == PALU_F16, stages).total
+                         : paged_lds(k_groups, ks, v_cols, most * c.block_rows, c.form.parts(), c.form.turned, act == PALU_F16, stages).total;
     };
     for (int limit = std::min(16, c.form.max_rows() / most); limit > 0; --limit) {   // (fewer where two stages leave no more LDS)
       c.n_row_blocks = ceil_div(rows, limit);
@@ -198,7 +197,7 @@ int launch_paged(const PagedPlan& p, PagedArgs& a, int act, int n_seq, bool shar
                                        : (c.form.many ? paged_rows_form<BF16>(c.form) : paged_form<BF16>(c.form));
     int st = allow_lds(fn, (size_t)c.lds_bytes);
     if (st != PALU_OK) return st;
-    hipLaunchKernelGGL(fn, dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)), dim3(c.form.many ? kPagedRowsThreads : kPagedThreads),
+    hipLaunchKernelGGL(fn, dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)), dim3(kPagedThreads),
                        (unsigned)c.lds_bytes, s, a);
     if ((st = launch_ok()) != PALU_OK) return st;
   }

@@ -23,6 +23,7 @@ template <typename T> __device__ __forceinline__ uint32_t pack2(float x, float y
 template <> __device__ __forceinline__ uint32_t pack2<F16>(float x, float y) {
   return __builtin_bit_cast(uint32_t, half2v{(_Float16)x, (_Float16)y});
 }
+typedef float float2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <> __device__ __forceinline__ uint32_t pack2<BF16>(float x, float y) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
@@ -48,7 +49,7 @@ __device__ __forceinline__ void load_to_lds(const void* g, uint32_t m0) {
 __device__ __forceinline__ void load_to_lds4(const void* g, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(m0), "v"(g) : "memory");
 }
-// Waits until at most n of this wavefront's vector-memory operations are outstanding, or fewer: 16, 8, 4 or none.  (A branch for every
+// Waits until at most n of this wavefront's vector-memory operations are outstanding, or fewer: 16, 8, 4, 2 or none.  (A branch for every
 // number took 400 cycles a tile.)
 __device__ __forceinline__ void wait_vm(int n) {
   if (n >= 8) {
@@ -56,29 +57,19 @@ __device__ __forceinline__ void wait_vm(int n) {
     else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
   } else {
     if (n >= 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    else if (n >= 2) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 }
-// the larger of x over 16 lanes
-__device__ __forceinline__ float max_of_row(float x) {
-  auto other = [&](auto ctrl) __attribute__((always_inline)) {
-    const int u = __builtin_bit_cast(int, x);
-    x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, decltype(ctrl)::value, 0xf, 0xf, false)));
-  };
-  other(IntC<0xB1>());                         // lane ^ 1, ^ 2 in a quad, mirrored in 8 lanes, mirrored in 16
-  other(IntC<0x4E>());
-  other(IntC<0x141>());
-  other(IntC<0x140>());
-  return x;
+// the larger of x over 8 and 16 lanes
+template <int CTRL> __device__ __forceinline__ float max_with(float x) {
+  const int u = __builtin_bit_cast(int, x);
+  return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, CTRL, 0xf, 0xf, false)));
 }
-// the larger of x over the four lanes that differ in lane bits 4 and 5
-__device__ __forceinline__ float max_of_4(float x) {
-  uint32_t u = __builtin_bit_cast(uint32_t, x);
-  auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  u = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1])));
-  auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+__device__ __forceinline__ float max_of_8(float x) {           // lane ^ 1, ^ 2 in a quad, mirrored in 8 lanes
+  return max_with<0x141>(max_with<0x4E>(max_with<0xB1>(x)));
 }
+__device__ __forceinline__ float max_of_row(float x) { return max_with<0x140>(max_of_8(x)); }   // mirrored in 16
 // This wavefront's LDS operations are done, and so are the other wavefronts'; loads to LDS go on.
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -225,44 +216,55 @@ struct PagedAngles {
   int base, anchors, lane;
   float c, s, turn_c, turn_s;                  // of the next tile; of 16 positions
 
-  __device__ __forceinline__ bool anchor(int j) const { return j > w.i0 + 1 && j < w.i1 && ((j - w.i0) % kPagedAnchorTiles == 0 || j == w.span.sink_tiles); }
+  // (last: the last tile that does not take its angles from there)
+  __device__ __forceinline__ bool anchor(int j, int last) const { return j > last && j < w.i1 && ((j - w.i0) % kPagedAnchorTiles == 0 || j == w.span.sink_tiles); }
   __device__ __forceinline__ const float* table(int pos, int cs) const {
     return w.a.rope + rope_f32_index(min(pos, w.a.rope_len - 1), lane, cs, kRopeTableStride);
   }
-  __device__ __forceinline__ void request(int j) const {
-    if (!anchor(j)) return;
+  __device__ __forceinline__ void request(int j, int last) const {
+    if (!anchor(j, last)) return;
     const uint32_t at = lds0 + anchors + j % kPagedAnchorSlots * (kDHead * 4);
     load_to_lds4(table(w.tile_pos(j), 0), at);
     load_to_lds4(table(w.tile_pos(j), 1), at + kHalf * 4);
   }
+  // at tile j
+  __device__ __forceinline__ void reach(int j, int last) {
+    if (!anchor(j, last)) return;
+    const float* at = reinterpret_cast<const float*>(lds + anchors + j % kPagedAnchorSlots * (kDHead * 4));
+    c = at[lane];
+    s = at[kHalf + lane];
+  }
+  __device__ __forceinline__ void turn() {
+    const float next = __builtin_fmaf(c, turn_c, -(s * turn_s));
+    s = __builtin_fmaf(s, turn_c, c * turn_s);
+    c = next;
+  }
+  __device__ __forceinline__ void start() {
+    turn_c = *table(16, 0);
+    turn_s = *table(16, 1);
+    c = *table(w.tile_pos(w.i0), 0);
+    s = *table(w.tile_pos(w.i0), 1);
+  }
+  // paged_kernel: the angles of tile j's sub-tiles
   __device__ __forceinline__ void make(int j) {
-    if (anchor(j)) {
-      const float* at = reinterpret_cast<const float*>(lds + anchors + j % kPagedAnchorSlots * (kDHead * 4));
-      c = at[lane];
-      s = at[kHalf + lane];
-    }
+    reach(j, w.i0 + 1);
     float* at = reinterpret_cast<float*>(lds + base + j % kPagedBaseSlots * (kPagedTile / 16) * kDHead * 4);
 #pragma unroll
     for (int sub = 0; sub < kPagedTile / 16; ++sub) {
       at[sub * kDHead + lane] = c;
       at[sub * kDHead + kHalf + lane] = s;
-      const float next = __builtin_fmaf(c, turn_c, -(s * turn_s));
-      s = __builtin_fmaf(s, turn_c, c * turn_s);
-      c = next;
+      turn();
     }
   }
   // angles of the first tile and state for the second, from the table; anchors before tile i0 + ahead
   __device__ __forceinline__ void begin(int ahead) {
     const int next = w.tile_pos(min(w.i0 + 1, w.i1 - 1));
-    turn_c = *table(16, 0);
-    turn_s = *table(16, 1);
-    c = *table(w.tile_pos(w.i0), 0);
-    s = *table(w.tile_pos(w.i0), 1);
+    start();
     const float c1 = *table(next, 0), s1 = *table(next, 1);
     make(w.i0);
     c = c1;
     s = s1;
-    for (int j = w.i0 + 2; j < w.i0 + ahead; ++j) request(j);
+    for (int j = w.i0 + 2; j < w.i0 + ahead; ++j) request(j, w.i0 + 1);
   }
 };
 

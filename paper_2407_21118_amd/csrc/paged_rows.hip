@@ -1,21 +1,28 @@
 // Decode attention over a paged latent cache with many query rows per key/value head: a prefix that a batch shares, large groups of
 // query heads.  The arithmetic is paged.hip's; up to 16 rows per head and 64 in all share a key.
 //
-// Four wavefronts, one per SIMD and one per head, whose 128 x r weights stay in the accumulation registers.
+// Eight wavefronts, two per SIMD; the two of a SIMD share a head: each has 32 of its rotation pairs, the weights for which stay in up to
+// 128 accumulation registers.
 //   keys    K^T = B_k^T H_k^T of 16 tokens at a time, from latents in LDS; rotated in float32 and multiplied by the
-//           rotated queries on the matrix cores, both between the matrix instructions of the next 16 tokens' keys.
-//   softmax in the wavefront: a lane holds one row's scores of 8 of the tile's tokens, four lanes the row.
+//           rotated queries on the matrix cores, both between the matrix instructions of the next 16 tokens' keys.  The
+//           scores over a wavefront's features go to LDS.
+//   softmax eight lanes per row, eight rows per wavefront.
 //   values  every wavefront contracts the probabilities of all heads' rows (through LDS) with its share of the value columns.
-// One barrier per tile: in interval n are the keys of tile n, the softmax of n - 1 and the values of n - 2.
+//   angles  of every token of 16, a 512th part by every lane: all heads' keys are rotated by them.
+// Two barriers per tile: the first half of interval n has the keys of the tile's first 16 tokens and the softmax of n - 1, the second
+// half the other keys and the values of n - 1.  One wavefront of a SIMD begins with the keys, the other ends with them: the matrix
+// instructions of one run beside the vector instructions of the other.
 
 #include "paged_dev.h"
 
 namespace palu {
 
 template <typename T, int KS, int PT, int VB>
-__global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs a) {
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs a) {
   constexpr bool PAIR = __is_same(T, F16);     // queries and keys as pairs hi + lo
-  constexpr int NB_V = 2 * VB;                 // blocks of 32 value columns per wavefront
+  constexpr int FT = 4;                        // tiles of 16 features per wavefront: low halves of the rotation pairs, then high halves
+  constexpr int NP = 8;                        // rotation pairs per lane
+  constexpr int kPlane = (PT * 16 + 1) * kPagedHalfPitch;    // floats: a wavefront's part of 16 tokens' scores, of all rows and none
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -26,10 +33,11 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
   if (w.idle()) return;
   const int i0 = w.i0, i1 = w.i1, nr = w.nr, n_packed = w.n_packed;
   const int NB = a.n_stages;
-  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, n_packed, PT, 0, false, PAIR, NB);
+  const PagedLds ld = paged_rows_lds(w.un.n_groups(), KS, w.v_cols, PT, PAIR, NB);
   const uint32_t lds0 = lds_addr(lds);
-  const bool works = wave < w.nh;                            // else: the same instructions, results nowhere
-  const int hh = works ? wave : 0;
+  const bool works = (wave & 3) < w.nh;                      // else: the same instructions, results nowhere
+  const int hh = works ? wave & 3 : 0, fq = wave >> 2;
+  const int fbase = 32 * fq;                                 // first rotation pair of this wavefront
   const int hg = w.un.n_groups() > 1 ? hh / w.per_group : 0; // the head's group inside the unit
   const int E = 2 * NB - 1;                                  // entries are requested so many tiles ahead: early enough to be there when rows are made of them
   int* const entries = reinterpret_cast<int*>(lds + ld.entries);
@@ -38,66 +46,47 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
     rows[(i % kPagedRowSlots) * kPagedTile + x] = w.row_of(i, x, entries[(i % kPagedEntrySlots) * kPagedTile + x]);
   };
 
-  // ---- requests of interval n: keys of tile n + NB - 1, values of n + NB - 3, entries of n + E; the rows of tile
-  // n + NB.  An operation moves 64 16-byte pieces, lane i the i-th of them; a wavefront takes every fourth.
-  const int ops_k = ld.k_pieces / 8, ops_v = ld.v_pieces / 8;   // per wavefront, each 256 / pieces tokens on
+  // ---- requests of interval n: keys of tile n + NB - 1, values of n + NB - 2, entries of n + E; the rows of tile n + NB.  An operation
+  // moves 64 16-byte pieces, lane i the i-th of them; a wavefront takes every eighth.
   const int id0 = wave * 64 + lane, x_k = id0 / ld.k_pieces, x_v = id0 / ld.v_pieces;
-  const int p_k = (id0 % ld.k_pieces) ^ paged_key_swizzle(x_k);
-  const unsigned char* const src_k0 = paged_source(a.hk, a.meta.k_off[w.g], w.k_cols, p_k);
-  const unsigned char* const src_k1 = paged_source(a.hk, a.meta.k_off[w.g], w.k_cols, p_k ^ 2);    // (32 pieces: eight tokens on)
+  const unsigned char* const src_k = paged_source(a.hk, a.meta.k_off[w.g], w.k_cols, (id0 % ld.k_pieces) ^ paged_key_swizzle(x_k));
   const unsigned char* const src_v = paged_source(a.hv, a.meta.v_off[w.g], w.v_cols, (id0 % ld.v_pieces) ^ paged_value_swizzle(x_v));
   const uint32_t k_pitch = (uint32_t)a.R_k * 2, v_pitch = (uint32_t)a.R_v * 2;
   auto request_keys = [&](int j, int stage) __attribute__((always_inline)) {
     const int* r = rows + (j % kPagedRowSlots) * kPagedTile + x_k;
     const uint32_t dst = lds0 + stage + wave * 1024;
-    if (ops_k == 4) {
-      const uint32_t r0 = r[0], r1 = r[8], r2 = r[16], r3 = r[24];
-      load_to_lds(src_k0 + (uint64_t)r0 * k_pitch, dst);
-      load_to_lds(src_k1 + (uint64_t)r1 * k_pitch, dst + 4096);
-      load_to_lds(src_k0 + (uint64_t)r2 * k_pitch, dst + 8192);
-      load_to_lds(src_k1 + (uint64_t)r3 * k_pitch, dst + 12288);
-    } else if (ops_k == 2) {
+    if (ld.k_pieces == 32) {
       const uint32_t r0 = r[0], r1 = r[16];
-      load_to_lds(src_k0 + (uint64_t)r0 * k_pitch, dst);
-      load_to_lds(src_k0 + (uint64_t)r1 * k_pitch, dst + 4096);
-    } else {
-      load_to_lds(src_k0 + (uint64_t)(uint32_t)r[0] * k_pitch, dst);
+      load_to_lds(src_k + (uint64_t)r0 * k_pitch, dst);
+      load_to_lds(src_k + (uint64_t)r1 * k_pitch, dst + 8192);
+    } else if (ld.k_pieces == 16 || wave < 4) {
+      load_to_lds(src_k + (uint64_t)(uint32_t)r[0] * k_pitch, dst);
     }
   };
   auto request_values = [&](int j, int stage) __attribute__((always_inline)) {
     const int* r = rows + (j % kPagedRowSlots) * kPagedTile + x_v;
     const uint32_t dst = lds0 + stage + wave * 1024;
     if (VB == 2) {                                           // rows of 64 pieces
-      uint32_t y[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = r[4 * k];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) load_to_lds(src_v + (uint64_t)y[k] * v_pitch, dst + 4096 * k);
-    } else if (ops_v == 4) {
       const uint32_t r0 = r[0], r1 = r[8], r2 = r[16], r3 = r[24];
       load_to_lds(src_v + (uint64_t)r0 * v_pitch, dst);
-      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 4096);
-      load_to_lds(src_v + (uint64_t)r2 * v_pitch, dst + 8192);
-      load_to_lds(src_v + (uint64_t)r3 * v_pitch, dst + 12288);
-    } else {
+      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 8192);
+      load_to_lds(src_v + (uint64_t)r2 * v_pitch, dst + 16384);
+      load_to_lds(src_v + (uint64_t)r3 * v_pitch, dst + 24576);
+    } else if (ld.v_pieces == 32) {
       const uint32_t r0 = r[0], r1 = r[16];
       load_to_lds(src_v + (uint64_t)r0 * v_pitch, dst);
-      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 4096);
+      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 8192);
+    } else {
+      load_to_lds(src_v + (uint64_t)(uint32_t)r[0] * v_pitch, dst);
     }
   };
-  auto request_entries = [&](int n) __attribute__((always_inline)) {
-    const int je = n + E;
-    if (wave == 3 && je < i1 && lane < kPagedTile)
-      load_to_lds4(w.entry_of(je, lane), lds0 + ld.entries + (je % kPagedEntrySlots) * (kPagedTile * 4));
-    if (wave == 2 && n >= i0 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
-  };
-  const int per_interval = ops_k + ops_v;
-  // Stages in use, as LDS offsets: keys of tile n and values of tile n - 2 (the stage before is requested into), angles of n and n - 1.
-  const PagedRing ring_k{ld.k, ld.stage_k, NB}, ring_v{ld.v, ld.stage_v, NB}, ring_b{ld.base, (kPagedTile / 16) * kDHead * 4, kPagedBaseSlots};
-  int k_at = ring_k.stage(i0), v_at = ring_v.stage(i0 + 2 * NB - 2), b_at = ring_b.stage(i0), b_old = ring_b.before(b_at);
+  const int per_k = (ld.k_pieces / 2 + 7 - wave) / 8, per_v = ld.v_pieces / 16;    // operations of this wavefront
+  // Stages in use, as LDS offsets: keys of tile n and values of tile n - 1 (the stage before is requested into).
+  const PagedRing ring_k{ld.k, ld.stage_k, NB}, ring_v{ld.v, ld.stage_v, NB};
+  int k_at = ring_k.stage(i0), v_at = ring_v.stage(i0 + NB - 1);
 
   // ---- prologue
-  for (int x = tid; x < kPagedTile * E; x += kPagedRowsThreads) {   // entries of the first tiles, and rows of those that are requested at once
+  for (int x = tid; x < kPagedTile * E; x += kPagedThreads) {   // entries of the first tiles, and rows of those that are requested at once
     const int i = i0 + x / kPagedTile;
     if (i < i1) {
       entries[(i % kPagedEntrySlots) * kPagedTile + x % kPagedTile] = *w.entry_of(i, x % kPagedTile);
@@ -106,36 +95,42 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
   }
   lds_barrier();
   for (int j = i0; j < min(i0 + NB - 1, i1); ++j) request_keys(j, ring_k.stage(j));
-  for (int j = i0; j < min(i0 + NB - 3, i1); ++j) request_values(j, ring_v.stage(j));
+  for (int j = i0; j < min(i0 + NB - 2, i1); ++j) request_values(j, ring_v.stage(j));
 
-  PagedAngles angles{w, lds, lds0, ld.base, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
-  if (wave == 1) angles.begin(NB);
+  // angles: this lane makes those of rotation pair `lane` of tokens wave and wave + 8
+  PagedAngles angles{w, lds, lds0, 0, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
+  if (wave == 1)
+    for (int j = i0 + 1; j < i0 + NB; ++j) angles.request(j, i0);
+  angles.start();
+  const float in_c0 = kKeyScale * *angles.table(wave, 0), in_s0 = kKeyScale * *angles.table(wave, 1);
+  const float in_c1 = kKeyScale * *angles.table(wave + 8, 0), in_s1 = kKeyScale * *angles.table(wave + 8, 1);
+  auto make_angles = [&](int sub) __attribute__((always_inline)) {
+    float* at = reinterpret_cast<float*>(lds + ld.ang) + (16 * sub + wave) * kPagedAngPitch + lane;
+    const float c = angles.c, s = angles.s;
+    at[0] = __builtin_fmaf(in_c0, c, -(in_s0 * s));
+    at[kHalf] = __builtin_fmaf(in_s0, c, in_c0 * s);
+    at[8 * kPagedAngPitch] = __builtin_fmaf(in_c1, c, -(in_s1 * s));
+    at[8 * kPagedAngPitch + kHalf] = __builtin_fmaf(in_s1, c, in_c1 * s);
+    angles.turn();
+  };
+  make_angles(0);
 
-  const int tok = paged_token(col);
-  // angles of position tok, of this lane's 16 rotation pairs 16 kg ..; scaled
-  float ang_c[16], ang_s[16];
-#pragma unroll
-  for (int p = 0; p < 16; ++p) {
-    ang_c[p] = kKeyScale * a.rope[rope_f32_index(tok, 16 * kg + p, 0, kRopeTableStride)];
-    ang_s[p] = kKeyScale * a.rope[rope_f32_index(tok, 16 * kg + p, 1, kRopeTableStride)];
-  }
-  w.rotate_queries<T, false>(lds + ld.q, ld.q_pitch, kPagedRowsThreads);
+  w.rotate_queries<T, false>(lds + ld.q, ld.q_pitch, kPagedThreads);
 
-  // weights: feature 4 m + j (j < 4) or 64 + 4 m + j - 4 is row m of tile j, so that a lane holds both features of a rotation
-  // pair.  A lane reads its four features of either half from eight rows of B_k and transposes them.  They stay in the
-  // accumulation registers, which the matrix instructions read as they are.
-  uint4v W[KS][8];
+  // weights: rotation pair fbase + 2 m + j is row m of tile j (low half) and 2 + j (high half).  A lane reads its features from eight
+  // rows of B_k and transposes them.  They stay in the accumulation registers, which the matrix instructions read as they are.
+  uint4v W[KS][FT];
   {
     const int width = w.per_group * kDHead;
-    const uint16_t* B = a.Bk + w.weights_of(hh, hg) + 4 * col;
-    constexpr int AHEAD = KS < 3 ? KS : 3;                   // steps whose rows are in flight
-    uint2v v[AHEAD][2][8];
+    const uint16_t* B = a.Bk + w.weights_of(hh, hg) + fbase + 2 * col;
+    constexpr int AHEAD = KS < 4 ? KS : 4;                   // steps whose rows are in flight
+    uint32_t v[AHEAD][2][8];
     auto fetch = [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint16_t* row = B + (size_t)min(32 * ks + 8 * kg + e, w.rk - 1) * width;
-        v[ks % AHEAD][0][e] = *reinterpret_cast<const uint2v*>(row);
-        v[ks % AHEAD][1][e] = *reinterpret_cast<const uint2v*>(row + kHalf);
+        v[ks % AHEAD][0][e] = *reinterpret_cast<const uint32_t*>(row);
+        v[ks % AHEAD][1][e] = *reinterpret_cast<const uint32_t*>(row + kHalf);
       }
     };
 #pragma unroll
@@ -144,209 +139,166 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
     for (int ks = 0; ks < KS; ++ks) {
       const uint32_t keep = 32 * ks < w.rk ? 0xffffffffu : 0u;           // rows behind the rank: zero
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int side = 0; side < 2; ++side) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          W[ks][j][i] = keep & __builtin_amdgcn_perm(v[ks % AHEAD][j >> 2][2 * i + 1][(j >> 1) & 1], v[ks % AHEAD][j >> 2][2 * i][(j >> 1) & 1],
-                                                     (j & 1) ? 0x07060302u : 0x05040100u);
-        asm volatile("" : "+a"(W[ks][j]));
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = v[ks % AHEAD][side][2 * i], y = v[ks % AHEAD][side][2 * i + 1];
+          W[ks][2 * side][i] = keep & __builtin_amdgcn_perm(y, x, 0x05040100u);
+          W[ks][2 * side + 1][i] = keep & __builtin_amdgcn_perm(y, x, 0x07060302u);
+        }
       }
+#pragma unroll
+      for (int j = 0; j < FT; ++j) asm volatile("" : "+a"(W[ks][j]));
       if (ks + AHEAD < KS) fetch(ks + AHEAD);
     }
   }
 
-  const int n_blocks = w.v_cols / 32;                          // of 32 value columns: block wave + 4 v is this wavefront's
+  const int n_blocks = w.v_cols / 32;                        // of 32 value columns: block wave + 8 v is this wavefront's
   const int n_pt = (n_packed + 15) / 16;
-  float4v O[NB_V][PT][2];
+  float4v O[VB][PT][2];
 #pragma unroll
-  for (int v = 0; v < NB_V; ++v)
+  for (int v = 0; v < VB; ++v)
 #pragma unroll
     for (int p = 0; p < PT; ++p) O[v][p][0] = O[v][p][1] = float4v{0, 0, 0, 0};
 
-  // softmax state of row col (the sum: over this lane's tokens); rows of the cache it may see
+  // softmax: this lane has tokens 16 stile + squad + 4 i of packed row srow; its state (the sum: over these tokens)
+  const int srow = 8 * wave + (lane >> 3), stile = lane >> 2 & 1, squad = lane & 3;
   float run_max = -INFINITY, run_sum = 0.f;
-  const bool live = works && col < nr;
-  const int limit = live ? w.limit_of(col) : w.L;
+  const int limit = srow < n_packed ? w.limit_of(srow % nr) : w.L;       // rows of the cache that it may see
   int all_see = limit;                                       // rows that every row of the wavefront sees
 #pragma unroll
-  for (int d = 1; d < 16; d *= 2) all_see = min(all_see, __shfl_xor(all_see, d));
+  for (int d = 8; d < 64; d *= 2) all_see = min(all_see, __shfl_xor(all_see, d));
   all_see = __builtin_amdgcn_readfirstlane(all_see);
-  const int prow = live ? hh * nr + col : PT * 16;           // where its probabilities go; of no row: behind the last
 
   wait_vm(0);
   lds_barrier();
-  const int steady = (NB - 2) * per_interval;
+  const int steady = (NB - 2) * (per_k + per_v);
 
-  const unsigned char* const q_row = lds + ld.q + (hh * nr + min(col, nr - 1)) * ld.q_pitch + 32 * kg;
+  // queries of row col: of two contraction steps, low halves of four pairs, high halves
+  uint4v qh[2], ql[2];
+  {
+    const unsigned char* q = lds + ld.q + (hh * nr + min(col, nr - 1)) * ld.q_pitch + 2 * (fbase + NP * kg);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint2v x = *reinterpret_cast<const uint2v*>(q + 8 * t), y = *reinterpret_cast<const uint2v*>(q + 128 + 8 * t);
+      qh[t] = uint4v{x.x, x.y, y.x, y.y};
+      if (PAIR) {
+        const uint2v z = *reinterpret_cast<const uint2v*>(q + 256 + 8 * t), u = *reinterpret_cast<const uint2v*>(q + 384 + 8 * t);
+        ql[t] = uint4v{z.x, z.y, u.x, u.y};
+      }
+    }
+  }
+  lds_barrier();                                             // (scores and probabilities take their place)
+
+  const int my_row = works && col < nr ? hh * nr + col : PT * 16;        // where this lane's scores go; of no row: behind the last
+  const int tok = paged_token(col);
   const int h_key = paged_key_swizzle(tok);
   const int h_lane = tok * ld.k_pieces * 16 + hg * KS * 64, off0 = h_lane + (kg ^ h_key) * 16, off1 = h_lane + ((4 + kg) ^ h_key) * 16;
-  const int v_lane = kg * ld.v_pieces * 16, v_pitch16 = 4 * ld.v_pieces * 16;
-
+  const int v_lane = kg * ld.v_pieces * 16 + (col & 3) * 4, v_pitch16 = 4 * ld.v_pieces * 16;
+  const float* const my_ang = reinterpret_cast<const float*>(lds + ld.ang) + tok * kPagedAngPitch + fbase + NP * kg;
+  float* const my_score = reinterpret_cast<float*>(lds + ld.s) + fq * kPlane + my_row * kPagedHalfPitch + 4 * kg;
+  // scores of a tile's first 16 tokens: of two tiles, in turn; of the others: of one
+  auto score_slot = [&](int n, int sub) __attribute__((always_inline)) { return (sub == 0 ? n & 1 : 2) * 2 * kPlane; };
   float minus_one = -1.f;                                    // (not a constant to the compiler, which would make a conversion and a subtraction of `less`)
   asm("" : "+s"(minus_one));
-  float4v acc[2][8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) acc[0][j] = acc[1][j] = float4v{0, 0, 0, 0};
-  float4v score[2];
 
-  // Keys of sub-tile `sub` of the tile staged at k_stage into acc[sub]; between their matrix instructions the previous sub-tile's, whose
-  // tile has its angles at b_stage, are rotated, split and multiplied by the queries into score[1 - sub].  The vector work is 64 steps of
-  // about three instructions (a matrix instruction takes the issue slots of four), a step or more behind every matrix instruction.
-  auto keys = [&](auto sub_c, int k_stage, int b_stage) __attribute__((always_inline)) {
-    constexpr int sub = decltype(sub_c)::value, old = 1 - sub;
-    constexpr int kSlots = KS * 8;
+  // Keys of sub-tile `sub` of tile n, staged at k_stage; rotated, split and multiplied by the queries.
+  auto keys = [&](auto sub_c, int n, int k_stage) __attribute__((always_inline)) {
+    constexpr int sub = decltype(sub_c)::value;
     const unsigned char* h0p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off0;
     const unsigned char* h1p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off1;
-    const float* bas = reinterpret_cast<const float*>(lds + b_stage) + old * kDHead + 16 * kg;
+    float4v acc[FT];
     uint4v af[3];
     af[0] = *reinterpret_cast<const uint4v*>(h0p);
     af[1] = *reinterpret_cast<const uint4v*>(h1p);
-    float4v bc[2], bs[2];                                    // angles of four pairs, and of the next four
-    bc[0] = *reinterpret_cast<const float4v*>(bas);
-    bs[0] = *reinterpret_cast<const float4v*>(bas + kHalf);
-    uint32_t khi[4][4], klo[4][4];                           // [2 side + half][pairs]: contraction steps, feature 64 side + 16 kg + 8 half + ..
-    float4v dot[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    float t1, t2, c, s, lo[2], hi[2], l0, l1, l2;
-    uint32_t x, y;
-    auto step = [&](int e) __attribute__((always_inline)) {
-      const int pa = 2 * (e >> 3), pb = pa + 1, q4 = pa >> 2, at = (e >> 3) & 3, half = e >> 5;   // pairs pa and pb
-      const float4v c0 = bc[q4 & 1], s0 = bs[q4 & 1];
-      if ((e & 15) == 0 && q4 + 1 < 4) {
-        bc[(q4 + 1) & 1] = *reinterpret_cast<const float4v*>(bas + 4 * (q4 + 1));
-        bs[(q4 + 1) & 1] = *reinterpret_cast<const float4v*>(bas + 4 * (q4 + 1) + kHalf);
-      }
-      const float kl0 = acc[old][pa & 3][pa >> 2], kh0 = acc[old][4 + (pa & 3)][pa >> 2], kl1 = acc[old][pb & 3][pb >> 2], kh1 = acc[old][4 + (pb & 3)][pb >> 2];
-      switch (e & 7) {
-        case 0:
-          t1 = ang_s[pa] * s0[pa & 3];
-          t2 = ang_c[pa] * s0[pa & 3];
-          c = __builtin_fmaf(ang_c[pa], c0[pa & 3], -t1);
-          break;
-        case 1:
-          s = __builtin_fmaf(ang_s[pa], c0[pa & 3], t2);
-          t1 = kh0 * s;
-          t2 = kl0 * s;
-          break;
-        case 2:
-          lo[0] = __builtin_fmaf(kl0, c, -t1);
-          hi[0] = __builtin_fmaf(kh0, c, t2);
-          t1 = ang_s[pb] * s0[pb & 3];
-          break;
-        case 3:
-          t2 = ang_c[pb] * s0[pb & 3];
-          c = __builtin_fmaf(ang_c[pb], c0[pb & 3], -t1);
-          s = __builtin_fmaf(ang_s[pb], c0[pb & 3], t2);
-          break;
-        case 4:
-          t1 = kh1 * s;
-          t2 = kl1 * s;
-          lo[1] = __builtin_fmaf(kl1, c, -t1);
-          break;
-        case 5:
-          hi[1] = __builtin_fmaf(kh1, c, t2);
-          // (the empty statements: a product and its rounding stay two instructions.  As one, they would round the exact product to hi
-          // where lo is measured from the float32 one, and take one instruction per number instead of one per two.)
-          asm("" : "+v"(lo[0]), "+v"(lo[1]), "+v"(hi[0]), "+v"(hi[1]));
-          x = pack2<F16>(lo[0], lo[1]);
-          y = pack2<F16>(hi[0], hi[1]);
-          if (PAIR) asm("" : "+v"(x), "+v"(y));
-          khi[half][at] = x;
-          khi[2 + half][at] = y;
-          break;
-        case 6:
-          if (PAIR) {
-            l0 = less<F16>(lo[0], x, minus_one);
-            l1 = less<F16>(lo[1], x >> 16, minus_one);
-            l2 = less<F16>(hi[0], y, minus_one);
-          }
-          break;
-        case 7:
-          if (PAIR) {
-            klo[half][at] = pack2<F16>(l0, l1);
-            klo[2 + half][at] = pack2<F16>(l2, less<F16>(hi[1], y >> 16, minus_one));
-          }
-          break;
-      }
-    };
-    auto products = [&](int half) __attribute__((always_inline)) {
-#pragma unroll
-      for (int side = 0; side < 2; ++side) {
-        const int k = 2 * side + half;
-        const uint4v kh = {khi[k][0], khi[k][1], khi[k][2], khi[k][3]};
-        const uint4v qh = *reinterpret_cast<const uint4v*>(q_row + side * 128 + half * 16);
-        dot[side] = mma<F16>(kh, qh, dot[side]);
-        if (PAIR) {
-          const uint4v kl = {klo[k][0], klo[k][1], klo[k][2], klo[k][3]};
-          const uint4v ql = *reinterpret_cast<const uint4v*>(q_row + 256 + side * 128 + half * 16);
-          dot[side] = mma<F16>(kh, ql, dot[side]);
-          dot[side] = mma<F16>(kl, qh, dot[side]);
-        }
-      }
-    };
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       if (ks + 2 < KS) af[(ks + 2) % 3] = *reinterpret_cast<const uint4v*>(((ks & 1) ? h1p : h0p) + ((ks + 2) >> 1) * 128);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int slot = ks * 8 + j;
-        acc[sub][j] = mma<T>(W[ks][j], af[ks % 3], ks == 0 ? float4v{0, 0, 0, 0} : acc[sub][j]);
+      for (int j = 0; j < FT; ++j) acc[j] = mma<T>(W[ks][j], af[ks % 3], ks == 0 ? float4v{0, 0, 0, 0} : acc[j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float* ang = my_ang + 16 * sub * kPagedAngPitch;
+    float4v dot = {0, 0, 0, 0};
 #pragma unroll
-        for (int e = slot * 64 / kSlots; e < (slot + 1) * 64 / kSlots; ++e) {
-          step(e);
-          if (e == 31) products(0);
+    for (int t = 0; t < 2; ++t) {                            // contraction steps: low halves of four pairs, high halves
+      const float4v c4 = *reinterpret_cast<const float4v*>(ang + 4 * t), s4 = *reinterpret_cast<const float4v*>(ang + 4 * t + kHalf);
+      uint4v hi, lo;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float x[2], y[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int p = 4 * t + 2 * u + i;
+          const float l = acc[p & 1][p >> 1], h = acc[2 + (p & 1)][p >> 1], c = c4[2 * u + i], sn = s4[2 * u + i];
+          x[i] = __builtin_fmaf(l, c, -(h * sn));
+          y[i] = __builtin_fmaf(h, c, l * sn);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        // (the empty statements: a product and its rounding stay two instructions.  As one, they would round the exact product to hi
+        // where lo is measured from the float32 one, and take one instruction per number instead of one per two.)
+        asm("" : "+v"(x[0]), "+v"(x[1]), "+v"(y[0]), "+v"(y[1]));
+        uint32_t xh = pack2<F16>(x[0], x[1]), yh = pack2<F16>(y[0], y[1]);
+        if (PAIR) {
+          asm("" : "+v"(xh), "+v"(yh));
+          lo[u] = pack2<F16>(less<F16>(x[0], xh, minus_one), less<F16>(x[1], xh >> 16, minus_one));
+          lo[2 + u] = pack2<F16>(less<F16>(y[0], yh, minus_one), less<F16>(y[1], yh >> 16, minus_one));
+        }
+        hi[u] = xh;
+        hi[2 + u] = yh;
+      }
+      dot = mma<F16>(hi, qh[t], dot);
+      if (PAIR) {
+        dot = mma<F16>(hi, ql[t], dot);
+        dot = mma<F16>(lo, qh[t], dot);
       }
     }
-    products(1);
-    score[old] = dot[0] + dot[1];
+    *reinterpret_cast<float4v*>(my_score + score_slot(n, sub)) = dot;   // lane: query row col, tokens kg + 4 i
   };
 
-  // ---- softmax of tile n: this lane has tokens kg + 4 i and 16 + kg + 4 i of row col
+  // ---- softmax of tile n
   auto softmax = [&](int n) __attribute__((always_inline)) {
-    const int buf = n & 1, t0 = w.tile_pos(n);
-    float s[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = score[e >> 2][e & 3];
+    if (8 * wave >= n_packed) return;
+    const int t0 = w.tile_pos(n);
+    const float* row = reinterpret_cast<const float*>(lds + ld.s) + score_slot(n, 0) + (stile ? score_slot(n, 1) - score_slot(n, 0) : 0) +
+                       srow * kPagedHalfPitch + 4 * squad;
+    float4v s = *reinterpret_cast<const float4v*>(row) + *reinterpret_cast<const float4v*>(row + kPlane);
     const bool whole = t0 + kPagedTile <= all_see && (t0 + kPagedTile <= w.span.sink || t0 >= w.span.lo);
     if (!whole) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int t = t0 + 4 * e + kg;
+      for (int e = 0; e < 4; ++e) {
+        const int t = t0 + 16 * stile + squad + 4 * e;
         if (t >= limit || (t >= w.span.sink && t < w.span.lo)) s[e] = -INFINITY;
       }
     }
-    float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    top = max_of_4(top);
-    const float now = fmaxf(run_max, top);
+    const float now = fmaxf(run_max, max_of_8(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
     const float zero = now == -INFINITY ? 0.f : now;         // no row seen yet: exp2(-inf) = 0 below
     const float alpha = __builtin_amdgcn_exp2f(run_max - zero);
-    float sum = 0.f;
-    uint32_t ph[4], pl[4];
+    float p[4];
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(s[e] - zero), p1 = __builtin_amdgcn_exp2f(s[e + 1] - zero);
-      sum += p0 + p1;
-      split2<T>(p0, p1, &ph[e / 2], &pl[e / 2]);
-    }
+    for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(s[e] - zero);
+    uint2v hi, lo;
+    uint32_t h0, l0, h1, l1;
+    split2<T>(p[0], p[1], &h0, &l0);
+    split2<T>(p[2], p[3], &h1, &l1);
+    hi = uint2v{h0, h1};
+    lo = uint2v{l0, l1};
     run_max = now;
-    run_sum = run_sum * alpha + sum;
-    // in the order of the value product's contraction: lane group kg, token kg + 4 i
-    unsigned char* P = lds + ld.p + (buf * (PT * 16 + 1) + prow) * kPagedProbPitch + 16 * kg;
-    *reinterpret_cast<uint4v*>(P) = uint4v{ph[0], ph[1], ph[2], ph[3]};
-    *reinterpret_cast<uint4v*>(P + 64) = uint4v{pl[0], pl[1], pl[2], pl[3]};
-    reinterpret_cast<float*>(lds + ld.alpha)[buf * (PT * 16 + 4) + prow] = alpha;
+    run_sum = run_sum * alpha + ((p[0] + p[1]) + (p[2] + p[3]));
+    // in the order of the value product's contraction: lane group squad, tokens squad + 4 e
+    unsigned char* P = lds + ld.p + min(srow, PT * 16) * kPagedProbPitch + 16 * squad + 8 * stile;
+    *reinterpret_cast<uint2v*>(P) = hi;
+    *reinterpret_cast<uint2v*>(P + 64) = lo;
+    reinterpret_cast<float*>(lds + ld.alpha)[srow] = alpha;
   };
 
-  // ---- values of tile n, staged at v_stage
-  auto values = [&](int n, int v_stage) __attribute__((always_inline)) {
-    const int buf = n & 1;
+  // ---- values of a tile, staged at v_stage
+  auto values = [&](int v_stage) __attribute__((always_inline)) {
 #pragma unroll
-    for (int v = 0; v < NB_V; ++v) {
-      if (v > 0 && 4 * v >= n_blocks) break;                 // (a block behind the last, of a wavefront whose neighbours have one: nothing that is stored)
-      const int block = wave + 4 * v;
+    for (int v = 0; v < VB; ++v) {
+      const int block = wave + 8 * v;
+      if (block >= n_blocks) break;
       uint32_t x[8];                                         // tokens kg + 4 e
-      const unsigned char* row = lds + v_stage + v_lane + ((block * 4 + (col >> 2)) ^ (4 * kg)) * 16 + (col & 3) * 4;
+      const unsigned char* row = lds + v_stage + v_lane + ((block * 4 + (col >> 2)) ^ (4 * kg)) * 16;
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = *reinterpret_cast<const uint32_t*>(row + e * v_pitch16);
       uint4v f0, f1;
@@ -355,36 +307,43 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
         f0[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x05040100u);
         f1[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x07060302u);
       }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int p = 0; p < PT; ++p) {
         if (p > 0 && p >= n_pt) break;
-        const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (buf * (PT * 16 + 4) + 16 * p + 4 * kg) * 4);
-        const unsigned char* P = lds + ld.p + (buf * (PT * 16 + 1) + 16 * p + col) * kPagedProbPitch + 16 * kg;
+        const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (16 * p + 4 * kg) * 4);
+        const unsigned char* P = lds + ld.p + (16 * p + col) * kPagedProbPitch + 16 * kg;
         const uint4v hi = *reinterpret_cast<const uint4v*>(P), lo = *reinterpret_cast<const uint4v*>(P + 64);
         O[v][p][0] = mma<T>(hi, f0, O[v][p][0] * al);
         O[v][p][1] = mma<T>(hi, f1, O[v][p][1] * al);
         O[v][p][0] = mma<T>(lo, f0, O[v][p][0]);
         O[v][p][1] = mma<T>(lo, f1, O[v][p][1]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
 
-  for (int n = i0; n < i1 + 2; ++n) {
+  for (int n = i0; n <= i1; ++n) {
+    // (the wavefronts of a SIMD take softmax and values at different times, beside the other's matrix instructions)
     if (n + NB - 1 < i1) request_keys(n + NB - 1, ring_k.before(k_at));
-    if (n + NB - 3 >= i0 && n + NB - 3 < i1) request_values(n + NB - 3, ring_v.before(v_at));
-    request_entries(n);
-    if (wave == 1) {
-      angles.request(n + NB);
-      if (n + 1 < i1) angles.make(n + 1);
+    if (n + NB - 2 >= i0 && n + NB - 2 < i1) request_values(n + NB - 2, ring_v.before(v_at));
+    if (wave == 3 && n + E < i1 && lane < kPagedTile) load_to_lds4(w.entry_of(n + E, lane), lds0 + ld.entries + ((n + E) % kPagedEntrySlots) * (kPagedTile * 4));
+    if (wave == 2 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
+    if (wave == 1) angles.request(n + NB, i0);
+    if (n < i1) make_angles(1);
+    if (fq == 0 && n > i0) softmax(n - 1);
+    if (n < i1) keys(IntC<0>(), n, k_at);
+    if (fq == 1 && n > i0) softmax(n - 1);
+    lds_barrier();
+    if (n + 1 < i1) {
+      angles.reach(n + 1, i0);
+      make_angles(0);
     }
-    if (n <= i1) keys(IntC<0>(), k_at, b_old);               // (behind the last tile, and of the one before the first: nothing that is used)
-    if (n >= i0 + 2) values(n - 2, v_at);
-    if (n > i0 && n <= i1) softmax(n - 1);
-    if (n < i1) keys(IntC<1>(), k_at, b_at);
+    if (fq == 0 && n > i0) values(v_at);
+    if (n < i1) keys(IntC<1>(), n, k_at);
+    if (fq == 1 && n > i0) values(v_at);
     k_at = ring_k.behind(k_at);
     v_at = ring_v.behind(v_at);
-    b_old = b_at;
-    b_at = ring_b.behind(b_at);
     // what interval n + 1 reads was requested in n - NB + 2; the NB - 2 intervals since then may be outstanding where all of them
     // requested whole tiles
     if (n + NB - 1 < i1) wait_vm(steady);
@@ -393,12 +352,12 @@ __global__ __launch_bounds__(kPagedRowsThreads) void paged_rows_kernel(PagedArgs
   }
 
   // ---- partial results
-  run_sum += __shfl_xor(run_sum, 16);
-  run_sum += __shfl_xor(run_sum, 32);
-  if (live && kg == 0) w.store_ml(hh, col, run_max, run_sum);
 #pragma unroll
-  for (int v = 0; v < NB_V; ++v) {
-    const int block = wave + 4 * v;
+  for (int d = 1; d < 8; d *= 2) run_sum += __shfl_xor(run_sum, d);
+  if (srow < n_packed && (lane & 7) == 0) w.store_ml(srow / nr, srow % nr, run_max, run_sum);
+#pragma unroll
+  for (int v = 0; v < VB; ++v) {
+    const int block = wave + 8 * v;
     if (block >= n_blocks) continue;
 #pragma unroll
     for (int p = 0; p < PT; ++p)
