@@ -165,21 +165,40 @@ struct PagedWork {
   // rotated and scaled queries: float32 numbers [packed row][feature], or pairs (bfloat16 layers: single numbers) of float16
   // [packed row][hi | lo][feature]
   template <typename T, bool FLOAT> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch, int threads) const {
-    for (int x = threadIdx.x; x < n_packed * kHalf; x += threads) {
-      const int f = x & 63, pr = x >> 6, h = pr / nr, r = pr - h * nr;
-      const int b = sequence_of(r), qh = shared ? row0 + r - b * a.meta.qpk : row0 + r;
-      const uint16_t* qp = a.q + ((size_t)b * a.meta.n_heads * a.meta.qpk + (h0 + h) * a.meta.qpk + qh) * kDHead;
-      const float x0 = T::to_float(qp[f]), x1 = T::to_float(qp[f + kHalf]);
-      int pos = a.q_pos ? a.q_pos[b] : (a.seq_lens ? a.seq_lens[b] : a.pos_len) - 1;
-      pos = max(0, min(pos, a.rope_len - 1));
-      const float k = a.scale / kKeyScale;
-      const float c = a.rope[rope_f32_index(pos, f, 0, kRopeTableStride)] * k, s = a.rope[rope_f32_index(pos, f, 1, kRopeTableStride)] * k;
-      if (FLOAT) {
-        float* y = reinterpret_cast<float*>(q) + pr * kDHead + f;
-        y[0] = x0 * c - x1 * s;
-        y[kHalf] = x1 * c + x0 * s;
-      } else {
-        paged_store_query<T>(q + pr * pitch, f, x0 * c - x1 * s, x1 * c + x0 * s);
+    constexpr int AHEAD = 4;                                 // rows of a wavefront whose loads are in flight
+    const int f = threadIdx.x & 63, step = threads / 64;
+    const float k = a.scale / kKeyScale;
+    for (int first = threadIdx.x >> 6; first < n_packed; first += AHEAD * step) {
+      int b[AHEAD], pos[AHEAD];
+      float x0[AHEAD], x1[AHEAD], c[AHEAD], s[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int pr = min(first + i * step, n_packed - 1), h = pr / nr, r = pr - h * nr;
+        b[i] = sequence_of(r);
+        const int qh = shared ? row0 + r - b[i] * a.meta.qpk : row0 + r;
+        const uint16_t* qp = a.q + ((size_t)b[i] * a.meta.n_heads * a.meta.qpk + (h0 + h) * a.meta.qpk + qh) * kDHead;
+        x0[i] = T::to_float(qp[f]);
+        x1[i] = T::to_float(qp[f + kHalf]);
+        pos[i] = a.q_pos ? a.q_pos[b[i]] : (a.seq_lens ? a.seq_lens[b[i]] : a.pos_len) - 1;
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        pos[i] = max(0, min(pos[i], a.rope_len - 1));
+        c[i] = a.rope[rope_f32_index(pos[i], f, 0, kRopeTableStride)] * k;
+        s[i] = a.rope[rope_f32_index(pos[i], f, 1, kRopeTableStride)] * k;
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int pr = first + i * step;
+        if (pr >= n_packed) break;
+        const float y0 = x0[i] * c[i] - x1[i] * s[i], y1 = x1[i] * c[i] + x0[i] * s[i];
+        if (FLOAT) {
+          float* y = reinterpret_cast<float*>(q) + pr * kDHead + f;
+          y[0] = y0;
+          y[kHalf] = y1;
+        } else {
+          paged_store_query<T>(q + pr * pitch, f, y0, y1);
+        }
       }
     }
   }

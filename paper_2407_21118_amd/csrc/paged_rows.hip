@@ -307,7 +307,6 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
         f0[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x05040100u);
         f1[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x07060302u);
       }
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int p = 0; p < PT; ++p) {
         if (p > 0 && p >= n_pt) break;
@@ -318,30 +317,35 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
         O[v][p][1] = mma<T>(hi, f1, O[v][p][1] * al);
         O[v][p][0] = mma<T>(lo, f0, O[v][p][0]);
         O[v][p][1] = mma<T>(lo, f1, O[v][p][1]);
-        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
 
   for (int n = i0; n <= i1; ++n) {
-    // (the wavefronts of a SIMD take softmax and values at different times, beside the other's matrix instructions)
-    if (n + NB - 1 < i1) request_keys(n + NB - 1, ring_k.before(k_at));
-    if (n + NB - 2 >= i0 && n + NB - 2 < i1) request_values(n + NB - 2, ring_v.before(v_at));
+    // (the wavefronts of a SIMD take requests, softmax and values at different times, beside the other's matrix instructions)
+    auto first_half = [&]() __attribute__((always_inline)) {
+      if (n + NB - 1 < i1) request_keys(n + NB - 1, ring_k.before(k_at));
+      if (n > i0) softmax(n - 1);
+    };
+    auto second_half = [&]() __attribute__((always_inline)) {
+      if (n + NB - 2 >= i0 && n + NB - 2 < i1) request_values(n + NB - 2, ring_v.before(v_at));
+      if (n > i0) values(v_at);
+    };
     if (wave == 3 && n + E < i1 && lane < kPagedTile) load_to_lds4(w.entry_of(n + E, lane), lds0 + ld.entries + ((n + E) % kPagedEntrySlots) * (kPagedTile * 4));
     if (wave == 2 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
     if (wave == 1) angles.request(n + NB, i0);
     if (n < i1) make_angles(1);
-    if (fq == 0 && n > i0) softmax(n - 1);
+    if (fq == 0) first_half();
     if (n < i1) keys(IntC<0>(), n, k_at);
-    if (fq == 1 && n > i0) softmax(n - 1);
+    if (fq == 1) first_half();
     lds_barrier();
     if (n + 1 < i1) {
       angles.reach(n + 1, i0);
       make_angles(0);
     }
-    if (fq == 0 && n > i0) values(v_at);
+    if (fq == 0) second_half();
     if (n < i1) keys(IntC<1>(), n, k_at);
-    if (fq == 1 && n > i0) values(v_at);
+    if (fq == 1) second_half();
     k_at = ring_k.behind(k_at);
     v_at = ring_v.behind(v_at);
     // what interval n + 1 reads was requested in n - NB + 2; the NB - 2 intervals since then may be outstanding where all of them
