@@ -163,9 +163,8 @@ struct PagedWork {
     *reinterpret_cast<float2*>(a.o_part + slot() * a.o_stride + (size_t)a.rows * ohead + (size_t)(row0 + r) * rv + c - cg * rv) = make_float2(x, y);
   }
   // rotated and scaled queries: float32 numbers [packed row][feature], or pairs (bfloat16 layers: single numbers) of float16
-  // [packed row][hi | lo][feature]
-  template <typename T, bool FLOAT> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch, int threads) const {
-    constexpr int AHEAD = 4;                                 // rows of a wavefront whose loads are in flight
+  // [packed row][hi | lo][feature]; AHEAD: rows of a wavefront whose loads are in flight
+  template <typename T, bool FLOAT, int AHEAD> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch, int threads) const {
     const int f = threadIdx.x & 63, step = threads / 64;
     const float k = a.scale / kKeyScale;
     for (int first = threadIdx.x >> 6; first < n_packed; first += AHEAD * step) {

@@ -113,10 +113,6 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
     at[8 * kPagedAngPitch + kHalf] = __builtin_fmaf(in_s1, c, in_c1 * s);
     angles.turn();
   };
-  make_angles(0);
-
-  w.rotate_queries<T, false>(lds + ld.q, ld.q_pitch, kPagedThreads);
-
   // weights: rotation pair fbase + 2 m + j is row m of tile j (low half) and 2 + j (high half).  A lane reads its features from eight
   // rows of B_k and transposes them.  They stay in the accumulation registers, which the matrix instructions read as they are.
   uint4v W[KS][FT];
@@ -135,6 +131,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
     };
 #pragma unroll
     for (int ks = 0; ks < AHEAD; ++ks) fetch(ks);
+    w.rotate_queries<T, false, PT * 2>(lds + ld.q, ld.q_pitch, kPagedThreads);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const uint32_t keep = 32 * ks < w.rk ? 0xffffffffu : 0u;           // rows behind the rank: zero
@@ -152,6 +149,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
       if (ks + AHEAD < KS) fetch(ks + AHEAD);
     }
   }
+  make_angles(0);
 
   const int n_blocks = w.v_cols / 32;                        // of 32 value columns: block wave + 8 v is this wavefront's
   const int n_pt = (n_packed + 15) / 16;
@@ -161,8 +159,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
 #pragma unroll
     for (int p = 0; p < PT; ++p) O[v][p][0] = O[v][p][1] = float4v{0, 0, 0, 0};
 
-  // softmax: this lane has tokens 16 stile + squad + 4 i of packed row srow; its state (the sum: over these tokens)
-  const int srow = 8 * wave + (lane >> 3), stile = lane >> 2 & 1, squad = lane & 3;
+  // softmax: this lane has four tokens of packed row srow; its state (the sum: over these tokens)
+  const int srow = 8 * wave + (lane >> 3);
   float run_max = -INFINITY, run_sum = 0.f;
   const int limit = srow < n_packed ? w.limit_of(srow % nr) : w.L;       // rows of the cache that it may see
   int all_see = limit;                                       // rows that every row of the wavefront sees
@@ -207,22 +205,28 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
     constexpr int sub = decltype(sub_c)::value;
     const unsigned char* h0p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off0;
     const unsigned char* h1p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off1;
-    float4v acc[FT];
+    const float* ang = my_ang + 16 * sub * kPagedAngPitch;
+    float4v acc[FT], c4[2], s4[2];
     uint4v af[3];
     af[0] = *reinterpret_cast<const uint4v*>(h0p);
     af[1] = *reinterpret_cast<const uint4v*>(h1p);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      if (ks + 2 < KS) af[(ks + 2) % 3] = *reinterpret_cast<const uint4v*>(((ks & 1) ? h1p : h0p) + ((ks + 2) >> 1) * 128);
+      if (ks + 2 < KS) {
+        af[(ks + 2) % 3] = *reinterpret_cast<const uint4v*>(((ks & 1) ? h1p : h0p) + ((ks + 2) >> 1) * 128);
+      } else if (ks + 2 == KS) {
+        c4[0] = *reinterpret_cast<const float4v*>(ang);
+        s4[0] = *reinterpret_cast<const float4v*>(ang + kHalf);
+      }
 #pragma unroll
       for (int j = 0; j < FT; ++j) acc[j] = mma<T>(W[ks][j], af[ks % 3], ks == 0 ? float4v{0, 0, 0, 0} : acc[j]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    const float* ang = my_ang + 16 * sub * kPagedAngPitch;
     float4v dot = {0, 0, 0, 0};
+    c4[1] = *reinterpret_cast<const float4v*>(ang + 4);
+    s4[1] = *reinterpret_cast<const float4v*>(ang + 4 + kHalf);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {                            // contraction steps: low halves of four pairs, high halves
-      const float4v c4 = *reinterpret_cast<const float4v*>(ang + 4 * t), s4 = *reinterpret_cast<const float4v*>(ang + 4 * t + kHalf);
       uint4v hi, lo;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -230,7 +234,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int p = 4 * t + 2 * u + i;
-          const float l = acc[p & 1][p >> 1], h = acc[2 + (p & 1)][p >> 1], c = c4[2 * u + i], sn = s4[2 * u + i];
+          const float l = acc[p & 1][p >> 1], h = acc[2 + (p & 1)][p >> 1], c = c4[t][2 * u + i], sn = s4[t][2 * u + i];
           x[i] = __builtin_fmaf(l, c, -(h * sn));
           y[i] = __builtin_fmaf(h, c, l * sn);
         }
@@ -255,9 +259,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
     *reinterpret_cast<float4v*>(my_score + score_slot(n, sub)) = dot;   // lane: query row col, tokens kg + 4 i
   };
 
-  // ---- softmax of tile n
+  // ---- softmax of tile n: this lane has tokens 16 stile + squad + 4 i
   auto softmax = [&](int n) __attribute__((always_inline)) {
     if (8 * wave >= n_packed) return;
+    int at = lane;                                           // (addresses are made anew in every tile: kept, they take registers that spill)
+    asm volatile("" : "+v"(at));
+    const int srow = 8 * wave + (at >> 3), stile = at >> 2 & 1, squad = at & 3;
     const int t0 = w.tile_pos(n);
     const float* row = reinterpret_cast<const float*>(lds + ld.s) + score_slot(n, 0) + (stile ? score_slot(n, 1) - score_slot(n, 0) : 0) +
                        srow * kPagedHalfPitch + 4 * squad;
