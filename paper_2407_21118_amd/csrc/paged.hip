@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     for (int x = tid; x < 16 * kDHead; x += kPagedThreads)
       ang[(x & 15) * kPagedAngPitch + (x >> 4)] = kKeyScale * a.rope[rope_f32_index(x & 15, (x >> 4) & 63, x >> 10, kRopeTableStride)];
   }
-  w.rotate_queries<T, TURN, TURN ? 1 : 2>(lds + ld.q, ld.q_pitch, kPagedThreads);
+  w.rotate_queries<T, TURN, 1>(lds + ld.q, ld.q_pitch);
 
   // weights.  FQ = 2: rotation pair fbase + 2 m + j is row m of tile j (low half) and 2 + j (high half); FQ = 4: pair fbase + m of tiles
   // 0 and 1.  A lane reads its features from eight rows of B_k and transposes them.  They stay in the accumulation registers, which the

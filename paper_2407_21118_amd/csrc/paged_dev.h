@@ -162,41 +162,48 @@ struct PagedWork {
     const int ohead = a.meta.o_off[g] + (h0 + h - a.meta.head_off[g]) * rv;
     *reinterpret_cast<float2*>(a.o_part + slot() * a.o_stride + (size_t)a.rows * ohead + (size_t)(row0 + r) * rv + c - cg * rv) = make_float2(x, y);
   }
-  // rotated and scaled queries: float32 numbers [packed row][feature], or pairs (bfloat16 layers: single numbers) of float16
-  // [packed row][hi | lo][feature]; AHEAD: rows of a wavefront whose loads are in flight
-  template <typename T, bool FLOAT, int AHEAD> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch, int threads) const {
-    const int f = threadIdx.x & 63, step = threads / 64;
+  // Rotated and scaled queries: float32 numbers [packed row][feature], or pairs (bfloat16 layers: single numbers) of float16
+  // [packed row][hi | lo][feature].  A wavefront takes a row of all heads, which has one position (whose angles lie in 128 cache lines), and
+  // has ROWS of them in flight.
+  template <typename T, bool FLOAT, int ROWS> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch) const {
+    constexpr int kWaves = kPagedThreads / 64, kHeads = 4;
+    const int f = threadIdx.x & 63;
     const float k = a.scale / kKeyScale;
-    for (int first = threadIdx.x >> 6; first < n_packed; first += AHEAD * step) {
-      int b[AHEAD], pos[AHEAD];
-      float x0[AHEAD], x1[AHEAD], c[AHEAD], s[AHEAD];
+    for (int first = threadIdx.x >> 6; first < nr; first += kWaves * ROWS) {
+      int pos[ROWS];
+      float x0[ROWS][kHeads], x1[ROWS][kHeads], c[ROWS], s[ROWS];
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const int pr = min(first + i * step, n_packed - 1), h = pr / nr, r = pr - h * nr;
-        b[i] = sequence_of(r);
-        const int qh = shared ? row0 + r - b[i] * a.meta.qpk : row0 + r;
-        const uint16_t* qp = a.q + ((size_t)b[i] * a.meta.n_heads * a.meta.qpk + (h0 + h) * a.meta.qpk + qh) * kDHead;
-        x0[i] = T::to_float(qp[f]);
-        x1[i] = T::to_float(qp[f + kHalf]);
-        pos[i] = a.q_pos ? a.q_pos[b[i]] : (a.seq_lens ? a.seq_lens[b[i]] : a.pos_len) - 1;
+      for (int i = 0; i < ROWS; ++i) {
+        const int r = min(first + i * kWaves, nr - 1), b = sequence_of(r), qh = shared ? row0 + r - b * a.meta.qpk : row0 + r;
+        pos[i] = a.q_pos ? a.q_pos[b] : (a.seq_lens ? a.seq_lens[b] : a.pos_len) - 1;
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h) {
+          const uint16_t* qp = a.q + ((size_t)b * a.meta.n_heads * a.meta.qpk + (h0 + min(h, nh - 1)) * a.meta.qpk + qh) * kDHead;
+          x0[i][h] = T::to_float(qp[f]);
+          x1[i][h] = T::to_float(qp[f + kHalf]);
+        }
       }
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
+      for (int i = 0; i < ROWS; ++i) {
         pos[i] = max(0, min(pos[i], a.rope_len - 1));
         c[i] = a.rope[rope_f32_index(pos[i], f, 0, kRopeTableStride)] * k;
         s[i] = a.rope[rope_f32_index(pos[i], f, 1, kRopeTableStride)] * k;
       }
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const int pr = first + i * step;
-        if (pr >= n_packed) break;
-        const float y0 = x0[i] * c[i] - x1[i] * s[i], y1 = x1[i] * c[i] + x0[i] * s[i];
-        if (FLOAT) {
-          float* y = reinterpret_cast<float*>(q) + pr * kDHead + f;
-          y[0] = y0;
-          y[kHalf] = y1;
-        } else {
-          paged_store_query<T>(q + pr * pitch, f, y0, y1);
+      for (int i = 0; i < ROWS; ++i) {
+        if (first + i * kWaves >= nr) break;
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h) {
+          if (h >= nh) break;
+          const int pr = h * nr + first + i * kWaves;
+          const float y0 = x0[i][h] * c[i] - x1[i][h] * s[i], y1 = x1[i][h] * c[i] + x0[i][h] * s[i];
+          if (FLOAT) {
+            float* y = reinterpret_cast<float*>(q) + pr * kDHead + f;
+            y[0] = y0;
+            y[kHalf] = y1;
+          } else {
+            paged_store_query<T>(q + pr * pitch, f, y0, y1);
+          }
         }
       }
     }
@@ -239,16 +246,18 @@ struct PagedAngles {
   __device__ __forceinline__ const float* table(int pos, int cs) const {
     return w.a.rope + rope_f32_index(min(pos, w.a.rope_len - 1), lane, cs, kRopeTableStride);
   }
+  __device__ __forceinline__ int slot(int j) const { return anchors + j % kPagedAnchorSlots * (kDHead * 4); }
+  __device__ __forceinline__ void fetch(int pos, int at) const {
+    load_to_lds4(table(pos, 0), lds0 + at);
+    load_to_lds4(table(pos, 1), lds0 + at + kHalf * 4);
+  }
   __device__ __forceinline__ void request(int j, int last) const {
-    if (!anchor(j, last)) return;
-    const uint32_t at = lds0 + anchors + j % kPagedAnchorSlots * (kDHead * 4);
-    load_to_lds4(table(w.tile_pos(j), 0), at);
-    load_to_lds4(table(w.tile_pos(j), 1), at + kHalf * 4);
+    if (anchor(j, last)) fetch(w.tile_pos(j), slot(j));
   }
   // at tile j
   __device__ __forceinline__ void reach(int j, int last) {
     if (!anchor(j, last)) return;
-    const float* at = reinterpret_cast<const float*>(lds + anchors + j % kPagedAnchorSlots * (kDHead * 4));
+    const float* at = reinterpret_cast<const float*>(lds + slot(j));
     c = at[lane];
     s = at[kHalf + lane];
   }
@@ -256,12 +265,6 @@ struct PagedAngles {
     const float next = __builtin_fmaf(c, turn_c, -(s * turn_s));
     s = __builtin_fmaf(s, turn_c, c * turn_s);
     c = next;
-  }
-  __device__ __forceinline__ void start() {
-    turn_c = *table(16, 0);
-    turn_s = *table(16, 1);
-    c = *table(w.tile_pos(w.i0), 0);
-    s = *table(w.tile_pos(w.i0), 1);
   }
   // paged_kernel: the angles of tile j's sub-tiles
   __device__ __forceinline__ void make(int j) {
@@ -277,7 +280,10 @@ struct PagedAngles {
   // angles of the first tile and state for the second, from the table; anchors before tile i0 + ahead
   __device__ __forceinline__ void begin(int ahead) {
     const int next = w.tile_pos(min(w.i0 + 1, w.i1 - 1));
-    start();
+    turn_c = *table(16, 0);
+    turn_s = *table(16, 1);
+    c = *table(w.tile_pos(w.i0), 0);
+    s = *table(w.tile_pos(w.i0), 1);
     const float c1 = *table(next, 0), s1 = *table(next, 1);
     make(w.i0);
     c = c1;

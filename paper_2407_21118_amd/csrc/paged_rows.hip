@@ -94,25 +94,14 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
     }
   }
   lds_barrier();
+  PagedAngles angles{w, lds, lds0, 0, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
+  if (wave == 1) {
+    for (int j = i0; j < i0 + NB; ++j) angles.request(j, i0 - 1);
+    angles.fetch(16, angles.slot(i0 + kPagedAnchorSlots - 1));
+  }
   for (int j = i0; j < min(i0 + NB - 1, i1); ++j) request_keys(j, ring_k.stage(j));
   for (int j = i0; j < min(i0 + NB - 2, i1); ++j) request_values(j, ring_v.stage(j));
 
-  // angles: this lane makes those of rotation pair `lane` of tokens wave and wave + 8
-  PagedAngles angles{w, lds, lds0, 0, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
-  if (wave == 1)
-    for (int j = i0 + 1; j < i0 + NB; ++j) angles.request(j, i0);
-  angles.start();
-  const float in_c0 = kKeyScale * *angles.table(wave, 0), in_s0 = kKeyScale * *angles.table(wave, 1);
-  const float in_c1 = kKeyScale * *angles.table(wave + 8, 0), in_s1 = kKeyScale * *angles.table(wave + 8, 1);
-  auto make_angles = [&](int sub) __attribute__((always_inline)) {
-    float* at = reinterpret_cast<float*>(lds + ld.ang) + (16 * sub + wave) * kPagedAngPitch + lane;
-    const float c = angles.c, s = angles.s;
-    at[0] = __builtin_fmaf(in_c0, c, -(in_s0 * s));
-    at[kHalf] = __builtin_fmaf(in_s0, c, in_c0 * s);
-    at[8 * kPagedAngPitch] = __builtin_fmaf(in_c1, c, -(in_s1 * s));
-    at[8 * kPagedAngPitch + kHalf] = __builtin_fmaf(in_s1, c, in_c1 * s);
-    angles.turn();
-  };
   // weights: rotation pair fbase + 2 m + j is row m of tile j (low half) and 2 + j (high half).  A lane reads its features from eight
   // rows of B_k and transposes them.  They stay in the accumulation registers, which the matrix instructions read as they are.
   uint4v W[KS][FT];
@@ -131,7 +120,14 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
     };
 #pragma unroll
     for (int ks = 0; ks < AHEAD; ++ks) fetch(ks);
-    w.rotate_queries<T, false, PT * 2>(lds + ld.q, ld.q_pitch, kPagedThreads);
+    w.rotate_queries<T, false, PT / 2>(lds + ld.q, ld.q_pitch);
+    // angles of positions 0 .. 15, scaled, where those of a tile's other tokens come later
+    float* const in = reinterpret_cast<float*>(lds + ld.ang) + 16 * kPagedAngPitch;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = tid + i * kPagedThreads;
+      in[(x & 15) * kPagedAngPitch + (x >> 4)] = kKeyScale * a.rope[rope_f32_index(x & 15, (x >> 4) & 63, x >> 10, kRopeTableStride)];
+    }
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const uint32_t keep = 32 * ks < w.rk ? 0xffffffffu : 0u;           // rows behind the rank: zero
@@ -149,8 +145,6 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
       if (ks + AHEAD < KS) fetch(ks + AHEAD);
     }
   }
-  make_angles(0);
-
   const int n_blocks = w.v_cols / 32;                        // of 32 value columns: block wave + 8 v is this wavefront's
   const int n_pt = (n_packed + 15) / 16;
   float4v O[VB][PT][2];
@@ -186,7 +180,26 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
       }
     }
   }
-  lds_barrier();                                             // (scores and probabilities take their place)
+  // angles: this lane makes those of rotation pair `lane` of tokens wave and wave + 8 of 16
+  const float* const in = reinterpret_cast<const float*>(lds + ld.ang) + (16 + wave) * kPagedAngPitch + lane;
+  const float in_c0 = in[0], in_s0 = in[kHalf], in_c1 = in[8 * kPagedAngPitch], in_s1 = in[8 * kPagedAngPitch + kHalf];
+  auto make_angles = [&](int sub) __attribute__((always_inline)) {
+    float* at = reinterpret_cast<float*>(lds + ld.ang) + (16 * sub + wave) * kPagedAngPitch + lane;
+    const float c = angles.c, s = angles.s;
+    at[0] = __builtin_fmaf(in_c0, c, -(in_s0 * s));
+    at[kHalf] = __builtin_fmaf(in_s0, c, in_c0 * s);
+    at[8 * kPagedAngPitch] = __builtin_fmaf(in_c1, c, -(in_s1 * s));
+    at[8 * kPagedAngPitch + kHalf] = __builtin_fmaf(in_s1, c, in_c1 * s);
+    angles.turn();
+  };
+  {
+    const float* turn = reinterpret_cast<const float*>(lds + angles.slot(i0 + kPagedAnchorSlots - 1));
+    angles.turn_c = turn[lane];
+    angles.turn_s = turn[kHalf + lane];
+  }
+  angles.reach(i0, i0 - 1);
+  make_angles(0);
+  lds_barrier();                                             // (scores and probabilities take the queries' place, other angles that of the first 16)
 
   const int my_row = works && col < nr ? hh * nr + col : PT * 16;        // where this lane's scores go; of no row: behind the last
   const int tok = paged_token(col);
@@ -340,14 +353,14 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_rows_kernel(PagedArgs 
     };
     if (wave == 3 && n + E < i1 && lane < kPagedTile) load_to_lds4(w.entry_of(n + E, lane), lds0 + ld.entries + ((n + E) % kPagedEntrySlots) * (kPagedTile * 4));
     if (wave == 2 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
-    if (wave == 1) angles.request(n + NB, i0);
+    if (wave == 1) angles.request(n + NB, i0 - 1);
     if (n < i1) make_angles(1);
     if (fq == 0) first_half();
     if (n < i1) keys(IntC<0>(), n, k_at);
     if (fq == 1) first_half();
     lds_barrier();
     if (n + 1 < i1) {
-      angles.reach(n + 1, i0);
+      angles.reach(n + 1, i0 - 1);
       make_angles(0);
     }
     if (fq == 0) second_half();
