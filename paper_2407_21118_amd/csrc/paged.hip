@@ -54,6 +54,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   const int E = 2 * NB - 1;                                  // entries are requested so many tiles ahead: early enough to be there when rows are made of them
   int* const entries = reinterpret_cast<int*>(lds + ld.entries);
   int* const rows = reinterpret_cast<int*>(lds + ld.rows);
+  // the lane, once more: where registers are short, what is made of it is made anew, not kept in registers of the loop, which spill
+  auto fresh_lane = [&]() __attribute__((always_inline)) {
+    int l = lane;
+    if (KS * FT >= 24 || VB == 2) asm volatile("" : "+v"(l));
+    return l;
+  };
   auto make_row = [&](int i, int x) __attribute__((always_inline)) {
     rows[(i % kPagedRowSlots) * kPagedTile + x] = w.row_of(i, x, entries[(i % kPagedEntrySlots) * kPagedTile + x]);
   };
@@ -66,38 +72,30 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   const unsigned char* const src_k1 = FQ == 4 ? paged_source(a.hk, a.meta.k_off[w.g], w.k_cols, p_k ^ 2) : src_k0;   // (64 pieces: eight tokens on)
   const unsigned char* const src_v = paged_source(a.hv, a.meta.v_off[w.g], w.v_cols, (id0 % ld.v_pieces) ^ paged_value_swizzle(x_v));
   const uint32_t k_pitch = (uint32_t)a.R_k * 2, v_pitch = (uint32_t)a.R_v * 2;
-  auto request_keys = [&](int j, int stage) __attribute__((always_inline)) {
-    const int* r = rows + (j % kPagedRowSlots) * kPagedTile + x_k;
+  // Half 0 or 1 of a tile's operations, the rows r of its tokens at hand: a wavefront waits while its operations are taken, one per 16 cycles
+  // of all the wavefronts', so they come in fours through the interval.
+  constexpr int KR = FQ == 4 ? 4 : 2, VR = VB == 2 ? 4 : 2;  // operations of a wavefront, at most
+  auto rows_of = [&](int j, int x, auto count, uint32_t* r) __attribute__((always_inline)) {
+    const int* from = rows + (j % kPagedRowSlots) * kPagedTile + x;
+#pragma unroll
+    for (int i = 0; i < decltype(count)::value; ++i) r[i] = from[i * (kPagedTile / decltype(count)::value)];
+  };
+  auto request_keys = [&](int half, const uint32_t* r, int stage) __attribute__((always_inline)) {
     const uint32_t dst = lds0 + stage + wave * 1024;
     if (FQ == 4) {                                           // rows of 64 pieces
-      const uint32_t r0 = r[0], r1 = r[8], r2 = r[16], r3 = r[24];
-      load_to_lds(src_k0 + (uint64_t)r0 * k_pitch, dst);
-      load_to_lds(src_k1 + (uint64_t)r1 * k_pitch, dst + 8192);
-      load_to_lds(src_k0 + (uint64_t)r2 * k_pitch, dst + 16384);
-      load_to_lds(src_k1 + (uint64_t)r3 * k_pitch, dst + 24576);
-    } else if (ld.k_pieces == 32) {
-      const uint32_t r0 = r[0], r1 = r[16];
-      load_to_lds(src_k0 + (uint64_t)r0 * k_pitch, dst);
-      load_to_lds(src_k0 + (uint64_t)r1 * k_pitch, dst + 8192);
-    } else if (ld.k_pieces == 16 || wave < 4) {
-      load_to_lds(src_k0 + (uint64_t)(uint32_t)r[0] * k_pitch, dst);
+      load_to_lds(src_k0 + (uint64_t)r[2 * half] * k_pitch, dst + 16384 * half);
+      load_to_lds(src_k1 + (uint64_t)r[2 * half + 1] * k_pitch, dst + 16384 * half + 8192);
+    } else if (half == 0 ? ld.k_pieces >= 16 || wave < 4 : ld.k_pieces == 32) {
+      load_to_lds(src_k0 + (uint64_t)r[half] * k_pitch, dst + 8192 * half);
     }
   };
-  auto request_values = [&](int j, int stage) __attribute__((always_inline)) {
-    const int* r = rows + (j % kPagedRowSlots) * kPagedTile + x_v;
+  auto request_values = [&](int half, const uint32_t* r, int stage) __attribute__((always_inline)) {
     const uint32_t dst = lds0 + stage + wave * 1024;
     if (VB == 2) {                                           // rows of 64 pieces
-      const uint32_t r0 = r[0], r1 = r[8], r2 = r[16], r3 = r[24];
-      load_to_lds(src_v + (uint64_t)r0 * v_pitch, dst);
-      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 8192);
-      load_to_lds(src_v + (uint64_t)r2 * v_pitch, dst + 16384);
-      load_to_lds(src_v + (uint64_t)r3 * v_pitch, dst + 24576);
-    } else if (ld.v_pieces == 32) {
-      const uint32_t r0 = r[0], r1 = r[16];
-      load_to_lds(src_v + (uint64_t)r0 * v_pitch, dst);
-      load_to_lds(src_v + (uint64_t)r1 * v_pitch, dst + 8192);
-    } else {
-      load_to_lds(src_v + (uint64_t)(uint32_t)r[0] * v_pitch, dst);
+      load_to_lds(src_v + (uint64_t)r[2 * half] * v_pitch, dst + 16384 * half);
+      load_to_lds(src_v + (uint64_t)r[2 * half + 1] * v_pitch, dst + 16384 * half + 8192);
+    } else if (half == 0 || ld.v_pieces == 32) {
+      load_to_lds(src_v + (uint64_t)r[half] * v_pitch, dst + 8192 * half);
     }
   };
   auto request_entries = [&](int n) __attribute__((always_inline)) {
@@ -119,8 +117,17 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     }
   }
   lds_barrier();
-  for (int j = i0; j < min(i0 + NB - 1, i1); ++j) request_keys(j, ring_k.stage(j));
-  for (int j = i0; j < min(i0 + NB - 4, i1); ++j) request_values(j, ring_v.stage(j));
+  uint32_t row_k[KR], row_v[VR];
+  for (int j = i0; j < min(i0 + NB - 1, i1); ++j) {
+    rows_of(j, x_k, IntC<KR>(), row_k);
+    request_keys(0, row_k, ring_k.stage(j));
+    request_keys(1, row_k, ring_k.stage(j));
+  }
+  for (int j = i0; j < min(i0 + NB - 4, i1); ++j) {
+    rows_of(j, x_v, IntC<VR>(), row_v);
+    request_values(0, row_v, ring_v.stage(j));
+    request_values(1, row_v, ring_v.stage(j));
+  }
 
   PagedAngles angles{w, lds, lds0, ld.base, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
   if (wave == 3) {
@@ -188,7 +195,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   for (int v = 0; v < VB; ++v) O[v][0] = O[v][1] = float4v{0, 0, 0, 0};
 
   // softmax state of the lanes of the last four wavefronts: row, two of its tokens; rows of the cache that the row may see
-  const int srow = 4 * (wave & 3) + (lane >> 4), stok = 16 * (col >> 3) + 8 * (col & 1) + (col >> 1 & 3);
+  const int srow = 4 * (wave & 3) + (lane >> 4);
   float run_max = -INFINITY, run_sum = 0.f;
   const int limit = srow < n_packed ? w.limit_of(srow % nr) : w.L;
 
@@ -196,6 +203,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   // sub-tile's keys are rotated by the angles of 0 .. 15, which are the same for all.
   auto turned_slot = [&](int j, int sub) __attribute__((always_inline)) { return ld.turned + (sub == 0 ? j & 1 : 2 + (j + 3) % 3) * n_packed * ld.q_pitch; };
   auto turn_queries = [&](int j) __attribute__((always_inline)) {
+    const int lane = fresh_lane();
     const float* base = reinterpret_cast<const float*>(lds + ld.base) + j % kPagedBaseSlots * (kPagedTile / 16) * kDHead + lane;
     for (int x = wave; x < 2 * n_packed; x += 8) {           // lane: rotation pair
       const int sub = x >= n_packed, r = x - sub * n_packed;
@@ -211,12 +219,13 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   wait_vm(0);
   lds_barrier();
   const int steady = (NB - 2) * per_interval;
+  // (a wavefront that has softmax rows has more to do than the other of its SIMD: it goes first.  8 sequences, one latent per head: 242 -> 222 us)
+  if (wave >= 4 && 4 * (wave & 3) < n_packed) __builtin_amdgcn_s_setprio(2);
 
   const int my_row = works && col < nr ? hh * nr + col : n_packed;       // where this lane's scores go; of no row: behind the last
   const int q_lane = (hh * nr + min(col, nr - 1)) * ld.q_pitch + 2 * (fbase + NP * kg);
   const int h_key = paged_key_swizzle(tok);
   const int h_lane = tok * ld.k_pieces * 16 + hg * KS * 64, off0 = h_lane + (kg ^ h_key) * 16, off1 = h_lane + ((4 + kg) ^ h_key) * 16;
-  const int v_lane = kg * ld.v_pieces * 16 + (col & 3) * 4, v_pitch16 = 4 * ld.v_pieces * 16;
   float minus_one = -1.f;                                    // (not a constant to the compiler, which would make a conversion and a subtraction of `less`)
   asm("" : "+s"(minus_one));
 
@@ -227,7 +236,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   // Keys of sub-tile `sub` of the tile staged at k_stage into acc[sub]; between their matrix instructions the previous sub-tile's, of tile
   // `np` with its angles at b_stage, are rotated, split and multiplied by the queries.  The vector work is 8 steps of two or three
   // instructions for every two pairs (a matrix instruction takes the issue slots of four).
-  auto keys = [&](auto sub_c, int k_stage, int np, int b_stage) __attribute__((always_inline)) {
+  auto keys = [&](auto sub_c, int k_stage, int np, int b_stage, auto&& halfway) __attribute__((always_inline)) {
     constexpr int sub = decltype(sub_c)::value, old = 1 - sub;
     constexpr int kSlots = KS * FT, kSteps = NP * 4;
     const unsigned char* h0p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off0;
@@ -328,6 +337,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 #pragma unroll
       for (int j = 0; j < FT; ++j) {
         const int slot = ks * FT + j;
+        if (slot == kSlots / 2) halfway();
         acc[sub][j] = mma<T>(W[ks][j], af[ks % 3], ks == 0 ? float4v{0, 0, 0, 0} : acc[sub][j]);
 #pragma unroll
         for (int e = slot * kSteps / kSlots; e < (slot + 1) * kSteps / kSlots; ++e) step(e);
@@ -341,6 +351,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 
   // ---- softmax of tile n: this lane has scores 2 col and 2 col + 1 of row srow, of tokens stok and stok + 4
   auto softmax = [&](int n) __attribute__((always_inline)) {
+    const int l = fresh_lane(), col = l & 15, srow = 4 * (wave & 3) + (l >> 4), stok = 16 * (col >> 3) + 8 * (col & 1) + (col >> 1 & 3);
     const int buf = n & 1, t0 = w.tile_pos(n) + stok, r = min(srow, n_packed);
     const float* row = reinterpret_cast<const float*>(lds + ld.s) + (n % kPagedScoreSlots * FQ * (n_packed + 1) + r) * kPagedScorePitch + 2 * col;
     float s0 = row[0], s1 = row[1];
@@ -368,6 +379,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 
   // ---- values of tile n, staged at v_stage
   auto values = [&](int n, int v_stage) __attribute__((always_inline)) {
+    const int l = fresh_lane(), col = l & 15, kg = l >> 4, v_lane = kg * ld.v_pieces * 16 + (col & 3) * 4, v_pitch16 = 4 * ld.v_pieces * 16;
     const int buf = n & 1;
     const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (buf * 20 + 4 * kg) * 4);
     const unsigned char* P = lds + ld.p + (buf * 17 + col) * kPagedProbPitch + 16 * kg;
@@ -395,28 +407,47 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 
   for (int n = i0; n < i1 + 3; ++n) {
     const bool more_k = n + NB - 1 < i1, more_v = n + NB - 4 >= i0 && n + NB - 4 < i1;
-    // (the wavefronts of a SIMD take requests and values at different times, beside the other's matrix instructions)
-    if (wave < 4) {
-      if (more_k) request_keys(n + NB - 1, ring_k.before(k_at));
-      if (n >= i0 + 3) values(n - 3, v_at);
-    } else {
-      if (more_v) request_values(n + NB - 4, ring_v.before(v_at));
-      if (4 * (wave & 3) < n_packed && n >= i0 + 2 && n < i1 + 2) softmax(n - 2);
-    }
+    const int to_k = ring_k.before(k_at), to_v = ring_v.before(v_at);
+    if (more_k) rows_of(n + NB - 1, x_k, IntC<KR>(), row_k);
+    if (more_v) rows_of(n + NB - 4, x_v, IntC<VR>(), row_v);
     request_entries(n);
     if (wave == 3) {
       angles.request(n + NB + (TURN ? 1 : 0), i0 + 1);
       if (n + 1 + (TURN ? 1 : 0) < i1) angles.make(n + 1 + (TURN ? 1 : 0));
     }
-    if (TURN && n + 1 < i1) turn_queries(n + 1);
-    if (n <= i1) keys(IntC<0>(), k_at, n - 1, b_old);        // (behind the last tile, and of the one before the first: nothing that is used)
-    if (wave < 4) {
-      if (more_v) request_values(n + NB - 4, ring_v.before(v_at));
-    } else {
-      if (more_k) request_keys(n + NB - 1, ring_k.before(k_at));
+    // The first wavefronts of the SIMDs end with the keys, the others begin with them: the matrix instructions of one run beside the rest
+    // of the other.
+    const bool front = wave < 4;
+    auto rest = [&]() __attribute__((always_inline)) {
+      if (!front && 4 * (wave & 3) < n_packed && n >= i0 + 2 && n < i1 + 2) softmax(n - 2);
       if (n >= i0 + 3) values(n - 3, v_at);
+      if (TURN && n + 1 < i1) turn_queries(n + 1);
+    };
+    auto request = [&](int part) __attribute__((always_inline)) {
+      if (part < 2) {
+        if (more_k) request_keys(part, row_k, to_k);
+      } else {
+        if (more_v) request_values(part - 2, row_v, to_v);
+      }
+    };
+    if (front) {
+      request(0);
+      rest();
     }
-    if (n < i1) keys(IntC<1>(), k_at, n, b_at);
+    if (n <= i1)                                             // (behind the last tile, and of the one before the first: nothing that is used)
+      keys(IntC<0>(), k_at, n - 1, b_old, [&]() __attribute__((always_inline)) { if (front) request(1); else request(0); });
+    if (front) request(2);
+    else request(1);
+    if (n < i1) {
+      keys(IntC<1>(), k_at, n, b_at, [&]() __attribute__((always_inline)) { if (front) request(3); else request(2); });
+    } else {
+      if (front) request(3);
+      else request(2);
+    }
+    if (!front) {
+      request(3);
+      rest();
+    }
     k_at = ring_k.behind(k_at);
     v_at = ring_v.behind(v_at);
     b_old = b_at;
