@@ -55,29 +55,26 @@ struct PagedUnit {
 };
 
 constexpr int kPagedProbPitch = 144;           // bytes per row of probabilities: a tile's hi, its lo and 16 bytes
+constexpr int kPagedScorePitch = 20;           // floats per row of scores: 16 tokens and 16 bytes
+constexpr int kPagedAngPitch = kDHead + 4;     // floats per token of angles
 constexpr int kPagedMaxStages = 6;
 constexpr int kPagedEntrySlots = 16;           // tiles whose page-table entries are held
 constexpr int kPagedRowSlots = 8;              // ... and whose tokens' rows of the cache
+constexpr int kPagedAnchorSlots = 8;           // ... and whose first angles
+constexpr int kPagedAnchorTiles = 8;           // every so many tiles the angles come from the table
 constexpr int kPagedLdsBytes = 160 * 1024;     // of a compute unit
 
 // LDS of a workgroup, in bytes from its start.  Tiles are staged n_stages deep, rows in 16-byte pieces, as many of them as a power
-// of two (at least 8, of values 16).
+// of two (at least 8, of values 16).  Queries lie where scores and probabilities come later.
 struct PagedLds {
   int k_pieces, v_pieces;
   int q_pitch;                                 // bytes per packed query row
   int stage_k, stage_v;                        // bytes per staged tile
-  int k, v, base, anchors, entries, rows, q, turned, ang, s, p, alpha, total;
+  int k, v, anchors, entries, rows, ang, alpha, s, p, q, total;
 };
-constexpr int kPagedScorePitch = 36;           // floats per row of scores: a tile and 16 bytes
-constexpr int kPagedHalfPitch = 20;            // ... of a sub-tile of 16 tokens
-constexpr int kPagedScoreSlots = 3;            // tiles whose scores are held
-constexpr int kPagedBaseSlots = 3;             // ... and whose first angles
-constexpr int kPagedAnchorSlots = 8;
-constexpr int kPagedTurnedSlots = 5;           // sub-tiles whose turned queries are held: the first of two tiles, the second of three
-constexpr int kPagedAngPitch = kDHead + 4;     // floats per token of the angles of the first 16 positions
-constexpr int kPagedAnchorTiles = 8;           // every so many tiles their angles come from the table
-// n_groups groups of the unit, ks steps of 32 key channels each; what both kernels have
-__host__ __device__ __forceinline__ PagedLds paged_lds_head(int n_groups, int ks, int v_cols, bool pairs, int n_stages) {
+// n_groups groups of the unit, ks steps of 32 key channels each; rows: packed query rows, in row_tiles tiles of 16; parts: partial scores
+// that are added up
+__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, int parts, bool pairs, int n_stages) {
   PagedLds l;
   const int k_pieces = n_groups * ks * 4;
   l.k_pieces = k_pieces <= 8 ? 8 : (k_pieces <= 16 ? 16 : (k_pieces <= 32 ? 32 : 64));
@@ -90,36 +87,29 @@ __host__ __device__ __forceinline__ PagedLds paged_lds_head(int n_groups, int ks
   l.anchors = l.v + n_stages * l.stage_v;
   l.entries = l.anchors + kPagedAnchorSlots * kDHead * 4;
   l.rows = l.entries + kPagedEntrySlots * kPagedTile * 4;
-  return l;
-}
-// of paged_kernel: rows packed query rows; parts: partial scores that are added up; turned: queries are turned to every sub-tile's
-// first position, else keys by its angle
-__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int parts, bool turned, bool pairs, int n_stages) {
-  PagedLds l = paged_lds_head(n_groups, ks, v_cols, pairs, n_stages);
-  l.base = l.rows + kPagedRowSlots * kPagedTile * 4;
-  l.q = l.base + kPagedBaseSlots * (kPagedTile / 16) * kDHead * 4;
-  l.turned = l.q + rows * (turned ? kDHead * 4 : l.q_pitch);                   // (float32 numbers to be turned)
-  l.ang = l.turned + (turned ? kPagedTurnedSlots * rows * l.q_pitch : 0);
-  l.s = l.ang + (turned ? 0 : 16 * kPagedAngPitch * 4);
-  l.p = l.s + kPagedScoreSlots * parts * (rows + 1) * kPagedScorePitch * 4;
-  l.alpha = l.p + 2 * 17 * kPagedProbPitch;
-  l.total = l.alpha + 2 * 20 * 4;
-  return l;
-}
-// of paged_rows_kernel: packed query rows in row_tiles tiles of 16.  Queries lie where scores and probabilities come later.
-__host__ __device__ __forceinline__ PagedLds paged_rows_lds(int n_groups, int ks, int v_cols, int row_tiles, bool pairs, int n_stages) {
-  PagedLds l = paged_lds_head(n_groups, ks, v_cols, pairs, n_stages);
-  l.base = l.turned = 0;
   l.ang = l.rows + kPagedRowSlots * kPagedTile * 4;
-  l.alpha = l.ang + 2 * 16 * kPagedAngPitch * 4;
-  l.s = l.alpha + row_tiles * 16 * 4;
-  l.p = l.s + 3 * 2 * (row_tiles * 16 + 1) * kPagedHalfPitch * 4;
-  l.q = l.s;
-  l.total = l.p + (row_tiles * 16 + 1) * kPagedProbPitch;
-  const int q_end = l.q + row_tiles * 16 * l.q_pitch;
+  l.alpha = l.ang + kPagedTile * kPagedAngPitch * 4;
+  l.p = l.alpha + row_tiles * 16 * 4;
+  l.s = l.p + (row_tiles * 16 + 1) * kPagedProbPitch;
+  l.total = l.s + 3 * parts * (rows + 1) * kPagedScorePitch * 4;
+  l.q = l.p;
+  const int q_end = l.q + rows * l.q_pitch;
   if (l.total < q_end) l.total = q_end;
   return l;
 }
+
+// Tokens that are attended in the same way: every sequence's own, or the shared prefix's.
+struct PagedPart {
+  float* o_part;                               // [slot][rows * sum of value ranks over the heads]: sums of exp2(score - max) * latent
+  float* ml_part;                              // [slot][head][row][2]: the maximum and the sum
+  long long o_stride;                          // floats of o_part per slot
+  int max_len, first, window, n_sink;
+  int shared;                                  // the tokens are those of the shared prefix
+  int rows;                                    // query rows per key/value head: qpk, or batch * qpk where the tokens are shared
+  int n_row_blocks, block_rows;
+  int chunk_tiles;                             // tiles per workgroup, at most
+  int n_slots;                                 // partial results per sequence, or of the shared tokens
+};
 
 struct PagedArgs {
   const uint16_t* hk;                          // [n_pages * page_rows, R_k]
@@ -129,23 +119,16 @@ struct PagedArgs {
   const float* rope;                           // angle table, layout in palu_dev.h
   const int32_t* q_pos;                        // [batch] or NULL: the newest row's
   const int32_t* page_table;                   // [batch, table_stride]
-  const int32_t* seq_lens;                     // [batch] or NULL: max_len
-  float* o_part;                               // [slot][rows * sum of value ranks over the heads]: sums of exp2(score - max) * latent
-  float* ml_part;                              // [slot][head][row][2]: the maximum and the sum
+  const int32_t* seq_lens;                     // [batch] or NULL: pos_len
   long long R_k, R_v;
   int n_pages, page_shift, table_stride, rope_len;
-  int max_len, first, window, n_sink;
-  int pos_len;                                 // rows of a sequence where seq_lens is NULL (max_len: those of the tokens in question)
-  int batch;
+  int pos_len;                                 // rows of a sequence where seq_lens is NULL
   int n_units;
-  int rows;                                    // query rows per key/value head: qpk, or batch * qpk where the tokens are shared
-  int n_row_blocks, block_rows;
-  int chunk_tiles;                             // tiles per workgroup, at most
   int n_stages;                                // tiles staged in LDS
-  int shared;                                  // the tokens are those of the shared prefix
-  int n_slots;                                 // partial results per sequence, or of the shared tokens
-  long long o_stride;                          // floats of o_part per slot
+  int max_packed;                              // packed query rows that LDS is laid out for (more than 16: as many as accumulators go)
+  int n_first;                                 // workgroups of part 0; those behind them are part 1's
   float scale;                                 // log2(e) / sqrt(128)
+  PagedPart part[2];
   PagedMeta meta;
   PagedUnit units[PALU_MAX_HEADS];
 };
@@ -167,18 +150,17 @@ struct PagedMergeArgs {
 };
 
 using PagedFn = void (*)(PagedArgs);
-// The instantiations: paged_kernel (up to 16 packed query rows) by ks: steps of 32 key channels, 2, 4, 6, 8 (units of up to four heads), 12
-// or 16 (of two), and vb: blocks of 256 value columns; paged_rows_kernel (many: up to 16 rows per head, ks up to 8) likewise
+// The instantiations, by ks: steps of 32 key channels, 2, 4, 6, 8 (units of up to four heads), 12 or 16 (of two); vb: blocks of 256 value
+// columns; many: more than 16 packed query rows, up to 16 per head
 struct PagedForm {
   int ks, vb;
-  bool many;                               // paged_rows_kernel
-  bool turned;                             // paged_kernel: queries are turned to the tiles, for up to 8 packed rows
-  int parts() const { return ks > 8 ? 4 : 2; }           // paged_kernel: wavefronts that share a head's features
+  bool many;
+  int parts() const { return ks > 8 ? 4 : 2; }           // wavefronts that share a head's features
   int unit_heads() const { return 8 / parts(); }
-  int max_rows() const { return many ? (vb == 1 ? 64 : 32) : 16; }   // packed
+  int row_tiles() const { return many ? (vb == 1 ? 4 : 2) : 1; }
+  int max_rows() const { return 16 * row_tiles(); }      // packed
 };
 template <typename T> PagedFn paged_form(const PagedForm& f);
-template <typename T> PagedFn paged_rows_form(const PagedForm& f);
 using PagedMergeFn = void (*)(PagedMergeArgs);
 // rows: of one key/value head per workgroup, 1, 2, 4 or 8
 template <typename T> PagedMergeFn paged_merge_form(int rows);

@@ -7,19 +7,23 @@ namespace {
 // Units that one launch takes: key/value heads of one rank class.
 struct PagedClass {
   PagedForm form;
-  int n_stages, lds_bytes;
-  int n_row_blocks, block_rows;
+  int n_stages, lds_bytes, max_packed;
+  int n_row_blocks[2], block_rows[2];          // of either part
   int n_units;
   PagedUnit units[PALU_MAX_HEADS];
 };
 constexpr int kPagedMaxClasses = 12;       // steps of key channels 2, 4, 6, 8, 12, 16, value columns up to 256 or above
-struct PagedPlan {
-  PagedMeta meta;
-  int rows;                                // query rows per key/value head
-  int n_cls;
-  PagedClass cls[kPagedMaxClasses];
+struct PagedPlanPart {
+  int rows, seqs, max_tiles;               // query rows per key/value head, sequences whose tokens are attended one by one, tiles of the longest
   int chunk_tiles, n_slots;                // 0 slots: nothing to attend
   long long o_stride, ml_stride;           // floats per slot
+};
+enum { kPagedOwn, kPagedShared };          // a sequence's own tokens, those of the prefix
+struct PagedPlan {
+  PagedMeta meta;
+  PagedPlanPart part[2];
+  int n_cls;
+  PagedClass cls[kPagedMaxClasses];
 };
 
 int check_paged_desc(const palu_layer_desc* desc, PagedMeta* pm) {
@@ -47,12 +51,32 @@ int check_paged_desc(const palu_layer_desc* desc, PagedMeta* pm) {
   return PALU_OK;
 }
 
-// batch: sequences whose tokens are attended one by one (1 where they are shared); max_tiles: tiles of the longest
-int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, PagedPlan* p) {
+// Time of n0 workgroups of length a followed by n1 of length b <= a on so many compute units, each of which takes the next when it is free
+double paged_makespan(long long n0, double a, long long n1, double b, int cus) {
+  const long long full = n0 / cus, rest = n0 - full * cus;
+  const double least = ((double)n0 * a + (double)n1 * b) / cus;
+  double best = 1e300;
+  for (int late = 0; late < 2; ++late) {       // it ends with a workgroup of a unit that has had `full` long ones, or one more
+    const double base = (full + late) * a;
+    const int from = (int)std::max(0.0, std::floor((least - base) / b));
+    for (int k = from; k <= from + 8; ++k) {
+      const double t = base + k * b;
+      if (t < (full + (rest > 0)) * a) continue;
+      if (t >= best) break;
+      const double fit = (cus - rest) * std::floor((t - full * a) / b + 1e-9) + (rest ? rest * std::floor((t - (full + 1) * a) / b + 1e-9) : 0.0);
+      if (fit < (double)n1) continue;
+      best = t;
+      break;
+    }
+  }
+  return best < 1e300 ? best : least + a;
+}
+
+// p->part: rows, seqs and max_tiles are set
+int plan_paged(const PagedMeta& m, int act, PagedPlan* p) {
   p->meta = m;
-  p->rows = rows;
   p->n_cls = 0;
-  long long wgs = 0;
+  long long wgs[2] = {0, 0};                   // workgroups per chunk
   int sum_rv = 0;
   auto rk = [&](int j) { return m.k_off[j + 1] - m.k_off[j]; };
   auto rv = [&](int j) { return m.v_off[j + 1] - m.v_off[j]; };
@@ -71,7 +95,7 @@ int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, 
     for (int j = 0; j < m.n_groups; ++j) any += in_class(j);
     if (!any) continue;
     PagedClass& c = p->cls[p->n_cls++];
-    c.form = PagedForm{ks, vb, false, false};
+    c.form = PagedForm{ks, vb, false};
     // Units: whole adjacent groups of equal ranks and size side by side, as far as 256 columns and the heads go (ranks in whole 64s:
     // the staged rows' layout), else parts of one group.  A unit of more heads reads its latents once for all of them.
     const int unit_heads = c.form.unit_heads();
@@ -97,42 +121,66 @@ int plan_paged(const PagedMeta& m, int act, int rows, int batch, int max_tiles, 
       if (!more) break;
     }
     // Query rows: 16 in all, or 16 per head and as many as accumulators go where there are more; as many blocks of them as it takes
-    c.form.many = ks <= 8 && most * rows > 16;
+    for (const PagedPlanPart& t : p->part) c.form.many = c.form.many || (t.max_tiles > 0 && ks <= 8 && most * t.rows > 16);
     auto lds_bytes = [&](int stages) {
-      return c.form.many ? paged_rows_lds(k_groups, ks, v_cols, c.form.max_rows() / 16, act == PALU_F16, stages).total
-                         : paged_lds(k_groups, ks, v_cols, most * c.block_rows, c.form.parts(), c.form.turned, act == PALU_F16, stages).total;
+      return paged_lds(k_groups, ks, v_cols, c.max_packed, c.form.row_tiles(), c.form.parts(), act == PALU_F16, stages).total;
     };
     for (int limit = std::min(16, c.form.max_rows() / most); limit > 0; --limit) {   // (fewer where two stages leave no more LDS)
-      c.n_row_blocks = ceil_div(rows, limit);
-      c.block_rows = ceil_div(rows, c.n_row_blocks);
-      c.form.turned = !c.form.many && most * c.block_rows <= 8;
+      c.max_packed = 0;
+      for (int i = 0; i < 2; ++i) {
+        c.n_row_blocks[i] = ceil_div(p->part[i].rows, limit);
+        c.block_rows[i] = ceil_div(p->part[i].rows, c.n_row_blocks[i]);
+        if (p->part[i].max_tiles > 0) c.max_packed = std::max(c.max_packed, most * c.block_rows[i]);
+      }
+      if (c.form.many) c.max_packed = c.form.max_rows();
       if (lds_bytes(2) <= kPagedLdsBytes) break;
     }
     if (lds_bytes(2) > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;
     c.n_stages = 2;
     while (c.n_stages < kPagedMaxStages && lds_bytes(c.n_stages + 1) <= kPagedLdsBytes) ++c.n_stages;
     c.lds_bytes = lds_bytes(c.n_stages);
-    wgs += (long long)c.n_units * c.n_row_blocks;
+    for (int i = 0; i < 2; ++i) wgs[i] += (long long)c.n_units * c.n_row_blocks[i] * p->part[i].seqs;
   }
-  wgs *= batch;
-  p->o_stride = (long long)rows * sum_rv;
-  p->ml_stride = (long long)rows * m.n_heads * 2;
-  p->chunk_tiles = 1;
-  p->n_slots = 0;
-  if (max_tiles <= 0) return PALU_OK;
-  // Tiles per workgroup: one workgroup is resident per compute unit, and loading its weights costs about as much as four tiles.
+  for (PagedPlanPart& t : p->part) {
+    t.o_stride = (long long)t.rows * sum_rv;
+    t.ml_stride = (long long)t.rows * m.n_heads * 2;
+    t.chunk_tiles = 1;
+    t.n_slots = 0;
+  }
+  // Tiles per workgroup: one workgroup is resident per compute unit, and its start and end cost about as much as four tiles; a slot more is
+  // merged in a twentieth.  The two parts' workgroups run together: of equal length, or one part's halves or quarters of the other's.
   const int cus = device_cu_count();
   double best = 1e300;
-  for (int n = 1; n <= max_tiles && n <= 1024; ++n) {
-    const int tiles = ceil_div(max_tiles, n);
-    const double rounds = (double)((wgs * ceil_div(max_tiles, tiles) + cus - 1) / cus);
-    const double cost = rounds * (4.0 + tiles) + 0.05 * n;
-    if (cost < best) {
-      best = cost;
-      p->chunk_tiles = tiles;
+  PagedPlanPart& own = p->part[kPagedOwn];
+  PagedPlanPart& shared = p->part[kPagedShared];
+  auto consider = [&](int tiles_own, int tiles_shared) {
+    const int n_own = own.max_tiles > 0 ? ceil_div(own.max_tiles, tiles_own) : 0, n_shared = shared.max_tiles > 0 ? ceil_div(shared.max_tiles, tiles_shared) : 0;
+    double a = 4.0 + (n_own ? ceil_div(own.max_tiles, n_own) : 0), b = 4.0 + (n_shared ? ceil_div(shared.max_tiles, n_shared) : 0);
+    long long na = wgs[kPagedOwn] * n_own, nb = wgs[kPagedShared] * n_shared;
+    if (a < b) {
+      std::swap(a, b);
+      std::swap(na, nb);
+    }
+    const double cost = paged_makespan(na, a, nb, b, cus) + 0.05 * (n_own + n_shared);
+    if (cost >= best) return;
+    best = cost;
+    own.n_slots = n_own;
+    own.chunk_tiles = std::max(1, n_own ? ceil_div(own.max_tiles, n_own) : 0);
+    shared.n_slots = n_shared;
+    shared.chunk_tiles = std::max(1, n_shared ? ceil_div(shared.max_tiles, n_shared) : 0);
+  };
+  const bool both = own.max_tiles > 0 && shared.max_tiles > 0;
+  for (const PagedPlanPart* t : {&own, &shared}) {
+    for (int n = 1; n <= std::min(t->max_tiles, both ? 64 : 1024); ++n) {
+      const int tiles = ceil_div(t->max_tiles, n);
+      consider(tiles, tiles);
+      if (!both) continue;
+      for (int f = 2; f <= 4; f *= 2) {
+        consider(ceil_div(tiles, f), tiles);
+        consider(tiles, ceil_div(tiles, f));
+      }
     }
   }
-  p->n_slots = ceil_div(max_tiles, p->chunk_tiles);
   return PALU_OK;
 }
 
@@ -143,62 +191,68 @@ int paged_max_tiles(int max_len, int first, int window, int n_sink) {
   return (int)std::min<long long>(all, ((long long)n_sink + kPagedTile - 1) / kPagedTile + ((long long)window + kPagedTile - 2) / kPagedTile + 1);
 }
 
-size_t paged_part_bytes(const PagedPlan& p, int batch, size_t* ml_offset) {
-  *ml_offset = align_up((size_t)batch * p.n_slots * p.o_stride * sizeof(float));
-  return *ml_offset + align_up((size_t)batch * p.n_slots * p.ml_stride * sizeof(float));
-}
-
 struct PagedCall {
-  int batch, prefix, max_len, window, n_sink;
-  PagedPlan own, shared;
-  size_t own_ml, shared_at, shared_ml, total;
+  PagedPlan plan;
+  int prefix, max_len, window, n_sink;
+  size_t o_at[2], ml_at[2], total;             // partial results in the workspace
 };
 
 int plan_paged_call(const palu_layer_desc* desc, int batch, int prefix, int max_len, int window, int n_sink, PagedCall* c) {
   PagedMeta m;
-  const int st = check_paged_desc(desc, &m);
+  int st = check_paged_desc(desc, &m);
   if (st != PALU_OK) return st;
   if (batch <= 0 || max_len <= 0 || prefix < 0 || prefix > max_len || window < 0 || n_sink < 0) return PALU_ERR_INVALID_ARG;
   if (batch > 65535) return PALU_ERR_UNSUPPORTED;
   if (max_len > (1 << 30)) return PALU_ERR_UNSUPPORTED;      // positions of the angle table
-  c->batch = batch;
   c->prefix = prefix;
   c->max_len = max_len;
   c->window = window;
   c->n_sink = window > 0 ? n_sink : 0;
-  int st2 = plan_paged(m, desc->act_dtype, m.qpk, batch, paged_max_tiles(max_len, prefix, window, c->n_sink), &c->own);
-  if (st2 == PALU_OK) st2 = plan_paged(m, desc->act_dtype, batch * m.qpk, 1, ceil_div(prefix, kPagedTile), &c->shared);
-  if (st2 != PALU_OK) return st2;
-  c->shared_at = paged_part_bytes(c->own, batch, &c->own_ml);
-  c->total = c->shared_at + paged_part_bytes(c->shared, 1, &c->shared_ml);
+  PagedPlan& p = c->plan;
+  p.part[kPagedOwn] = PagedPlanPart{m.qpk, batch, paged_max_tiles(max_len, prefix, window, c->n_sink)};
+  p.part[kPagedShared] = PagedPlanPart{batch * m.qpk, 1, ceil_div(prefix, kPagedTile)};
+  st = plan_paged(m, desc->act_dtype, &p);
+  if (st != PALU_OK) return st;
+  c->total = 0;
+  for (int i = 0; i < 2; ++i) {
+    const PagedPlanPart& t = p.part[i];
+    c->o_at[i] = c->total;
+    c->ml_at[i] = c->o_at[i] + align_up((size_t)t.seqs * t.n_slots * t.o_stride * sizeof(float));
+    c->total = c->ml_at[i] + align_up((size_t)t.seqs * t.n_slots * t.ml_stride * sizeof(float));
+  }
   if (c->total < kAlign) c->total = kAlign;
-  for (const PagedPlan* p : {&c->own, &c->shared})
-    for (int i = 0; i < p->n_cls; ++i)
-      if ((long long)p->cls[i].n_units * p->cls[i].n_row_blocks * p->n_slots * (p == &c->own ? batch : 1) > 0x7fffffffLL) return PALU_ERR_UNSUPPORTED;
+  for (int i = 0; i < p.n_cls; ++i) {
+    long long wgs = 0;
+    for (int k = 0; k < 2; ++k) wgs += (long long)p.cls[i].n_units * p.cls[i].n_row_blocks[k] * p.part[k].n_slots * p.part[k].seqs;
+    if (wgs > 0x7fffffffLL) return PALU_ERR_UNSUPPORTED;
+  }
   return PALU_OK;
 }
 
-int launch_paged(const PagedPlan& p, PagedArgs& a, int act, int n_seq, bool shared, hipStream_t s) {
-  if (p.n_slots == 0) return PALU_OK;
-  a.meta = p.meta;
-  a.rows = p.rows;
-  a.chunk_tiles = p.chunk_tiles;
-  a.n_slots = p.n_slots;
-  a.o_stride = p.o_stride;
+// a.part is that of kPagedOwn, kPagedShared, but for what the classes say
+int launch_paged(const PagedPlan& p, const PagedArgs& args, int act, hipStream_t s) {
+  const int first = p.part[kPagedShared].chunk_tiles > p.part[kPagedOwn].chunk_tiles ? kPagedShared : kPagedOwn;   // (the longer ones)
   for (int i = 0; i < p.n_cls; ++i) {
     const PagedClass& c = p.cls[i];
+    PagedArgs a = args;
     a.n_units = c.n_units;
-    a.n_row_blocks = c.n_row_blocks;
-    a.block_rows = c.block_rows;
     std::memcpy(a.units, c.units, sizeof(PagedUnit) * c.n_units);
     a.n_stages = c.n_stages;
-    a.shared = shared;
-    const PagedFn fn = act == PALU_F16 ? (c.form.many ? paged_rows_form<F16>(c.form) : paged_form<F16>(c.form))
-                                       : (c.form.many ? paged_rows_form<BF16>(c.form) : paged_form<BF16>(c.form));
+    a.max_packed = c.max_packed;
+    unsigned wgs[2];
+    for (int k = 0; k < 2; ++k) {
+      const int from = k == 0 ? first : 1 - first;
+      a.part[k] = args.part[from];
+      a.part[k].n_row_blocks = c.n_row_blocks[from];
+      a.part[k].block_rows = c.block_rows[from];
+      wgs[k] = (unsigned)(c.n_units * c.n_row_blocks[from] * p.part[from].n_slots * p.part[from].seqs);
+    }
+    if (wgs[0] + wgs[1] == 0) continue;
+    a.n_first = (int)wgs[0];
+    const PagedFn fn = act == PALU_F16 ? paged_form<F16>(c.form) : paged_form<BF16>(c.form);
     int st = allow_lds(fn, (size_t)c.lds_bytes);
     if (st != PALU_OK) return st;
-    hipLaunchKernelGGL(fn, dim3((unsigned)(c.n_units * c.n_row_blocks * p.n_slots * n_seq)), dim3(kPagedThreads),
-                       (unsigned)c.lds_bytes, s, a);
+    hipLaunchKernelGGL(fn, dim3(wgs[0] + wgs[1]), dim3(kPagedThreads), (unsigned)c.lds_bytes, s, a);
     if ((st = launch_ok()) != PALU_OK) return st;
   }
   return PALU_OK;
@@ -214,16 +268,17 @@ int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32
   if (!q || !hk || !hv || !page_table || !Bk || !Bv || !rope_table || !out || !workspace) return PALU_ERR_INVALID_ARG;
   if (n_pages <= 0 || page_rows <= 0 || table_stride <= 0) return PALU_ERR_INVALID_ARG;
   if ((long long)table_stride * page_rows < max_len || rope_table_len < max_len) return PALU_ERR_INVALID_ARG;
-  for (const void* p : {q, hk, hv, Bk, Bv, rope_table, (const void*)out, (const void*)workspace})
-    if (reinterpret_cast<uintptr_t>(p) & 15) return PALU_ERR_INVALID_ARG;
-  for (const void* p : {(const void*)q_pos, (const void*)page_table, (const void*)seq_lens})
-    if (reinterpret_cast<uintptr_t>(p) & 3) return PALU_ERR_INVALID_ARG;
+  for (const void* x : {q, hk, hv, Bk, Bv, rope_table, (const void*)out, (const void*)workspace})
+    if (reinterpret_cast<uintptr_t>(x) & 15) return PALU_ERR_INVALID_ARG;
+  for (const void* x : {(const void*)q_pos, (const void*)page_table, (const void*)seq_lens})
+    if (reinterpret_cast<uintptr_t>(x) & 3) return PALU_ERR_INVALID_ARG;
   if ((page_rows & (page_rows - 1)) != 0 || (long long)n_pages * page_rows > 0x7fffffffLL) return PALU_ERR_UNSUPPORTED;
   if (workspace_bytes < c.total) return PALU_ERR_WORKSPACE_TOO_SMALL;
 
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const PagedMeta& m = c.own.meta;
+  const PagedPlan& p = c.plan;
+  const PagedMeta& m = p.meta;
   PagedArgs a;
   std::memset(&a, 0, sizeof(a));
   a.hk = static_cast<const uint16_t*>(hk);
@@ -241,28 +296,32 @@ int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32
   a.table_stride = table_stride;
   a.rope_len = rope_table_len;
   a.pos_len = max_len;
-  a.batch = batch;
+  a.meta = m;
   a.scale = (float)(1.4426950408889634 / std::sqrt((double)PALU_D_HEAD));
+
+  for (int i = 0; i < 2; ++i) {
+    PagedPart& t = a.part[i];
+    t.o_part = reinterpret_cast<float*>(ws + c.o_at[i]);
+    t.ml_part = reinterpret_cast<float*>(ws + c.ml_at[i]);
+    t.o_stride = p.part[i].o_stride;
+    t.rows = p.part[i].rows;
+    t.chunk_tiles = p.part[i].chunk_tiles;
+    t.n_slots = p.part[i].n_slots;
+  }
+  a.part[kPagedOwn].max_len = max_len;
+  a.part[kPagedOwn].first = prefix;
+  a.part[kPagedOwn].window = c.window;
+  a.part[kPagedOwn].n_sink = c.n_sink;
+  a.part[kPagedShared].max_len = prefix;       // nothing of the shared tokens is before, and no window
+  a.part[kPagedShared].shared = 1;
+  if ((st = launch_paged(p, a, desc->act_dtype, s)) != PALU_OK) return st;
 
   PagedMergeArgs e;
   std::memset(&e, 0, sizeof(e));
-  e.o_part = reinterpret_cast<const float*>(ws);
-  e.ml_part = reinterpret_cast<const float*>(ws + c.own_ml);
-  e.o_shared = reinterpret_cast<const float*>(ws + c.shared_at);
-  e.ml_shared = reinterpret_cast<const float*>(ws + c.shared_at + c.shared_ml);
-
-  a.max_len = prefix;                          // shared tokens: nothing of them is before, and no window
-  a.o_part = const_cast<float*>(e.o_shared);
-  a.ml_part = const_cast<float*>(e.ml_shared);
-  if ((st = launch_paged(c.shared, a, desc->act_dtype, 1, true, s)) != PALU_OK) return st;
-  a.max_len = max_len;
-  a.first = prefix;
-  a.window = c.window;
-  a.n_sink = c.n_sink;
-  a.o_part = const_cast<float*>(e.o_part);
-  a.ml_part = const_cast<float*>(e.ml_part);
-  if ((st = launch_paged(c.own, a, desc->act_dtype, batch, false, s)) != PALU_OK) return st;
-
+  e.o_part = a.part[kPagedOwn].o_part;
+  e.ml_part = a.part[kPagedOwn].ml_part;
+  e.o_shared = a.part[kPagedShared].o_part;
+  e.ml_shared = a.part[kPagedShared].ml_part;
   e.Bv = static_cast<const uint16_t*>(Bv);
   e.seq_lens = seq_lens;
   e.out = static_cast<uint16_t*>(out);
@@ -271,11 +330,11 @@ int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32
   e.window = c.window;
   e.n_sink = c.n_sink;
   e.batch = batch;
-  e.chunk_tiles = c.own.chunk_tiles;
-  e.n_slots = c.own.n_slots;
-  e.o_stride = c.own.o_stride;
-  e.n_shared = c.shared.n_slots;
-  e.o_shared_stride = c.shared.o_stride;
+  e.chunk_tiles = p.part[kPagedOwn].chunk_tiles;
+  e.n_slots = p.part[kPagedOwn].n_slots;
+  e.o_stride = p.part[kPagedOwn].o_stride;
+  e.n_shared = p.part[kPagedShared].n_slots;
+  e.o_shared_stride = p.part[kPagedShared].o_stride;
   e.meta = m;
   int per_wg = 8;                              // rows of a head per workgroup: fewer until there are two workgroups per compute unit
   while (per_wg > 1 && (long long)ceil_div(batch * m.qpk, per_wg) * m.n_heads < 2 * device_cu_count()) per_wg /= 2;

@@ -61,7 +61,7 @@ __device__ __forceinline__ void wait_vm(int n) {
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 }
-// the larger of x over 8 and 16 lanes
+// the larger of x over 8 lanes
 template <int CTRL> __device__ __forceinline__ float max_with(float x) {
   const int u = __builtin_bit_cast(int, x);
   return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, CTRL, 0xf, 0xf, false)));
@@ -69,28 +69,15 @@ template <int CTRL> __device__ __forceinline__ float max_with(float x) {
 __device__ __forceinline__ float max_of_8(float x) {           // lane ^ 1, ^ 2 in a quad, mirrored in 8 lanes
   return max_with<0x141>(max_with<0x4E>(max_with<0xB1>(x)));
 }
-__device__ __forceinline__ float max_of_row(float x) { return max_with<0x140>(max_of_8(x)); }   // mirrored in 16
 // This wavefront's LDS operations are done, and so are the other wavefronts'; loads to LDS go on.
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// features f and f + 64 of a query as an operand of the score product
-template <typename T> __device__ __forceinline__ void paged_store_query(unsigned char* row, int f, float y0, float y1) {
-  uint32_t hi, lo;
-  split2<F16>(y0, y1, &hi, &lo);
-  uint16_t* y = reinterpret_cast<uint16_t*>(row) + f;
-  y[0] = (uint16_t)hi;
-  y[kHalf] = (uint16_t)(hi >> 16);
-  if (__is_same(T, F16)) {
-    y[kDHead] = (uint16_t)lo;
-    y[kDHead + kHalf] = (uint16_t)(lo >> 16);
-  }
-}
-
 // What a workgroup does.
 struct PagedWork {
   const PagedArgs& a;
+  const PagedPart t;
   PagedUnit un;
   bool shared;
   int rb, seq, chunk, L;
@@ -99,19 +86,19 @@ struct PagedWork {
   int g, nh, h0, rk, rv, per_group, k_cols, v_cols;
   int row0, nr, n_packed;                      // query rows per head and in all
 
-  __device__ __forceinline__ PagedWork(const PagedArgs& args) : a(args) {
-    const int bid = blockIdx.x;
+  __device__ __forceinline__ PagedWork(const PagedArgs& args) : a(args), t((int)blockIdx.x < args.n_first ? args.part[0] : args.part[1]) {
+    const int bid = (int)blockIdx.x >= a.n_first ? blockIdx.x - a.n_first : blockIdx.x;
     un = a.units[bid % a.n_units];
     int rest = bid / a.n_units;
-    rb = rest % a.n_row_blocks;
-    rest /= a.n_row_blocks;
-    shared = a.shared != 0;
-    seq = shared ? 0 : rest / a.n_slots;
-    chunk = rest - seq * a.n_slots;
-    L = shared || !a.seq_lens ? a.max_len : a.seq_lens[seq];
-    L = __builtin_amdgcn_readfirstlane(max(0, min(L, a.max_len)));
-    span = paged_span(L, a.first, a.window, a.n_sink);
-    const int n_chunks = (span.n_tiles + a.chunk_tiles - 1) / a.chunk_tiles;
+    rb = rest % t.n_row_blocks;
+    rest /= t.n_row_blocks;
+    shared = t.shared != 0;
+    seq = shared ? 0 : rest / t.n_slots;
+    chunk = rest - seq * t.n_slots;
+    L = shared || !a.seq_lens ? t.max_len : a.seq_lens[seq];
+    L = __builtin_amdgcn_readfirstlane(max(0, min(L, t.max_len)));
+    span = paged_span(L, t.first, t.window, t.n_sink);
+    const int n_chunks = (span.n_tiles + t.chunk_tiles - 1) / t.chunk_tiles;
     i0 = i1 = 0;
     if (chunk >= n_chunks) return;
     i0 = (int)((long long)span.n_tiles * chunk / n_chunks);
@@ -125,16 +112,16 @@ struct PagedWork {
     per_group = m.head_off[g + 1] - m.head_off[g];           // a unit of several groups takes whole ones
     k_cols = un.n_groups() * rk;
     v_cols = un.n_groups() * rv;
-    row0 = rb * a.block_rows;
-    nr = min(a.block_rows, a.rows - row0);
+    row0 = rb * t.block_rows;
+    nr = min(t.block_rows, t.rows - row0);
     n_packed = nh * nr;
   }
   __device__ __forceinline__ bool idle() const { return i0 >= i1; }
   // position of tile i, and the position whose row its token x reads (a masked token: the first attended one's)
   __device__ __forceinline__ int tile_pos(int i) const { return kPagedTile * (i < span.sink_tiles ? i : span.tile0 + i - span.sink_tiles); }
   __device__ __forceinline__ int token_of(int t0, int x) const {
-    const int t = t0 + x, head = t0 < span.sink ? t0 : max(t0, span.lo);
-    return t >= L || (t >= span.sink && t < span.lo) ? head : t;
+    const int pos = t0 + x, head = t0 < span.sink ? t0 : max(t0, span.lo);
+    return pos >= L || (pos >= span.sink && pos < span.lo) ? head : pos;
   }
   __device__ __forceinline__ const int32_t* entry_of(int i, int x) const {
     return a.page_table + (size_t)seq * a.table_stride + (token_of(tile_pos(i), x) >> a.page_shift);
@@ -151,21 +138,20 @@ struct PagedWork {
     const int width = per_group * kDHead;
     return a.meta.bk_off[g] + (size_t)hg * rk * width + (size_t)(hh + h0 - a.meta.head_off[g] - hg * per_group) * kDHead;
   }
-  __device__ __forceinline__ size_t slot() const { return shared ? (size_t)chunk : (size_t)seq * a.n_slots + chunk; }
+  __device__ __forceinline__ size_t slot() const { return shared ? (size_t)chunk : (size_t)seq * t.n_slots + chunk; }
   __device__ __forceinline__ void store_ml(int hh, int r, float top, float sum) const {
-    reinterpret_cast<float2*>(a.ml_part)[slot() * a.meta.n_heads * a.rows + (size_t)(h0 + hh) * a.rows + row0 + r] = make_float2(top, sum);
+    reinterpret_cast<float2*>(t.ml_part)[slot() * a.meta.n_heads * t.rows + (size_t)(h0 + hh) * t.rows + row0 + r] = make_float2(top, sum);
   }
   // packed row pr, value columns c and c + 1 of the unit; rows of other groups than the columns' are dropped
   __device__ __forceinline__ void store_o(int pr, int c, float x, float y) const {
     const int h = pr / nr, r = pr - h * nr, cg = c / rv;
     if (un.n_groups() > 1 && h / per_group != cg) return;
     const int ohead = a.meta.o_off[g] + (h0 + h - a.meta.head_off[g]) * rv;
-    *reinterpret_cast<float2*>(a.o_part + slot() * a.o_stride + (size_t)a.rows * ohead + (size_t)(row0 + r) * rv + c - cg * rv) = make_float2(x, y);
+    *reinterpret_cast<float2*>(t.o_part + slot() * t.o_stride + (size_t)t.rows * ohead + (size_t)(row0 + r) * rv + c - cg * rv) = make_float2(x, y);
   }
-  // Rotated and scaled queries: float32 numbers [packed row][feature], or pairs (bfloat16 layers: single numbers) of float16
-  // [packed row][hi | lo][feature].  A wavefront takes a row of all heads, which has one position (whose angles lie in 128 cache lines), and
+  // Rotated and scaled queries as pairs (bfloat16 layers: single numbers) of float16, [packed row][hi | lo][feature].  A wavefront takes a row of all heads, which has one position (whose angles lie in 128 cache lines), and
   // has ROWS of them in flight.
-  template <typename T, bool FLOAT, int ROWS> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch) const {
+  template <typename T, int ROWS> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch) const {
     constexpr int kWaves = kPagedThreads / 64, kHeads = 4;
     const int f = threadIdx.x & 63;
     const float k = a.scale / kKeyScale;
@@ -197,12 +183,14 @@ struct PagedWork {
           if (h >= nh) break;
           const int pr = h * nr + first + i * kWaves;
           const float y0 = x0[i][h] * c[i] - x1[i][h] * s[i], y1 = x1[i][h] * c[i] + x0[i][h] * s[i];
-          if (FLOAT) {
-            float* y = reinterpret_cast<float*>(q) + pr * kDHead + f;
-            y[0] = y0;
-            y[kHalf] = y1;
-          } else {
-            paged_store_query<T>(q + pr * pitch, f, y0, y1);
+          uint32_t hi, lo;
+          split2<F16>(y0, y1, &hi, &lo);
+          uint16_t* y = reinterpret_cast<uint16_t*>(q + pr * pitch) + f;
+          y[0] = (uint16_t)hi;
+          y[kHalf] = (uint16_t)(hi >> 16);
+          if (__is_same(T, F16)) {
+            y[kDHead] = (uint16_t)lo;
+            y[kDHead + kHalf] = (uint16_t)(lo >> 16);
           }
         }
       }
@@ -230,33 +218,41 @@ __device__ __forceinline__ const unsigned char* paged_source(const uint16_t* bas
   return reinterpret_cast<const unsigned char*>(base + col0 + (p * 8 < cols ? p * 8 : 0));
 }
 
-// Angles of every 16 tokens' first position, [sub-tile][cos 64 | sin 64] in LDS: one wavefront makes them, a lane per rotation pair, a tile
-// ahead, by turning those before by 16 positions, from anchors every kPagedAnchorTiles tiles (and where positions jump) that come
-// from the table, whose rows of one position lie in 128 cache lines: every tile's from there took a quarter of the time.  A turn rounds twice at
-// 2^-24: 1e-7 or so, as the table.
+// Angles of the first position of every 16 tokens, a lane per rotation pair: those before, turned by 16 positions, from anchors every
+// kPagedAnchorTiles tiles (and where positions jump) that come from the table, whose rows of one position lie in 128 cache lines:
+// every tile's from there took a quarter of the time.  A turn rounds twice at 2^-24: 1e-7 or so, as the table.
 struct PagedAngles {
   const PagedWork& w;
   unsigned char* lds;
   uint32_t lds0;
-  int base, anchors, lane;
-  float c, s, turn_c, turn_s;                  // of the next tile; of 16 positions
+  int anchors, lane;
+  float c, s, turn_c, turn_s;                  // of the next 16 tokens; of 16 positions
 
-  // (last: the last tile that does not take its angles from there)
-  __device__ __forceinline__ bool anchor(int j, int last) const { return j > last && j < w.i1 && ((j - w.i0) % kPagedAnchorTiles == 0 || j == w.span.sink_tiles); }
-  __device__ __forceinline__ const float* table(int pos, int cs) const {
-    return w.a.rope + rope_f32_index(min(pos, w.a.rope_len - 1), lane, cs, kRopeTableStride);
-  }
+  __device__ __forceinline__ bool anchor(int j) const { return j < w.i1 && ((j - w.i0) % kPagedAnchorTiles == 0 || j == w.span.sink_tiles); }
   __device__ __forceinline__ int slot(int j) const { return anchors + j % kPagedAnchorSlots * (kDHead * 4); }
   __device__ __forceinline__ void fetch(int pos, int at) const {
-    load_to_lds4(table(pos, 0), lds0 + at);
-    load_to_lds4(table(pos, 1), lds0 + at + kHalf * 4);
+    const int p = min(pos, w.a.rope_len - 1);
+    load_to_lds4(w.a.rope + rope_f32_index(p, lane, 0, kRopeTableStride), lds0 + at);
+    load_to_lds4(w.a.rope + rope_f32_index(p, lane, 1, kRopeTableStride), lds0 + at + kHalf * 4);
   }
-  __device__ __forceinline__ void request(int j, int last) const {
-    if (anchor(j, last)) fetch(w.tile_pos(j), slot(j));
+  __device__ __forceinline__ void request(int j) const {
+    if (anchor(j)) fetch(w.tile_pos(j), slot(j));
+  }
+  // by one wavefront: anchors before tile i0 + ahead, and the angles of 16 positions in a slot that none of these has
+  __device__ __forceinline__ void begin(int ahead) const {
+    for (int j = w.i0; j < w.i0 + ahead; ++j) request(j);
+    fetch(16, slot(w.i0 + kPagedAnchorSlots - 1));
+  }
+  // when these are there
+  __device__ __forceinline__ void start() {
+    const float* at = reinterpret_cast<const float*>(lds + slot(w.i0 + kPagedAnchorSlots - 1));
+    turn_c = at[lane];
+    turn_s = at[kHalf + lane];
+    reach(w.i0);
   }
   // at tile j
-  __device__ __forceinline__ void reach(int j, int last) {
-    if (!anchor(j, last)) return;
+  __device__ __forceinline__ void reach(int j) {
+    if (!anchor(j)) return;
     const float* at = reinterpret_cast<const float*>(lds + slot(j));
     c = at[lane];
     s = at[kHalf + lane];
@@ -265,30 +261,6 @@ struct PagedAngles {
     const float next = __builtin_fmaf(c, turn_c, -(s * turn_s));
     s = __builtin_fmaf(s, turn_c, c * turn_s);
     c = next;
-  }
-  // paged_kernel: the angles of tile j's sub-tiles
-  __device__ __forceinline__ void make(int j) {
-    reach(j, w.i0 + 1);
-    float* at = reinterpret_cast<float*>(lds + base + j % kPagedBaseSlots * (kPagedTile / 16) * kDHead * 4);
-#pragma unroll
-    for (int sub = 0; sub < kPagedTile / 16; ++sub) {
-      at[sub * kDHead + lane] = c;
-      at[sub * kDHead + kHalf + lane] = s;
-      turn();
-    }
-  }
-  // angles of the first tile and state for the second, from the table; anchors before tile i0 + ahead
-  __device__ __forceinline__ void begin(int ahead) {
-    const int next = w.tile_pos(min(w.i0 + 1, w.i1 - 1));
-    turn_c = *table(16, 0);
-    turn_s = *table(16, 1);
-    c = *table(w.tile_pos(w.i0), 0);
-    s = *table(w.tile_pos(w.i0), 1);
-    const float c1 = *table(next, 0), s1 = *table(next, 1);
-    make(w.i0);
-    c = c1;
-    s = s1;
-    for (int j = w.i0 + 2; j < w.i0 + ahead; ++j) request(j, w.i0 + 1);
   }
 };
 
