@@ -88,10 +88,11 @@ __host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int
   l.entries = l.anchors + kPagedAnchorSlots * kDHead * 4;
   l.rows = l.entries + kPagedEntrySlots * kPagedTile * 4;
   l.ang = l.rows + kPagedRowSlots * kPagedTile * 4;
-  l.alpha = l.ang + kPagedTile * kPagedAngPitch * 4;
-  l.p = l.alpha + row_tiles * 16 * 4;
-  l.s = l.p + (row_tiles * 16 + 1) * kPagedProbPitch;
-  l.total = l.s + 3 * parts * (rows + 1) * kPagedScorePitch * 4;
+  const int held = row_tiles == 1 && parts == 2 ? 2 : 1;    // tiles whose angles and probabilities are held: one where halves of tiles are between barriers
+  l.alpha = l.ang + held * kPagedTile * kPagedAngPitch * 4;
+  l.p = l.alpha + held * row_tiles * 16 * 4;
+  l.s = l.p + held * (row_tiles * 16 + 1) * kPagedProbPitch;
+  l.total = l.s + (held == 2 ? 4 : 3) * parts * (rows + 1) * kPagedScorePitch * 4;
   l.q = l.p;
   const int q_end = l.q + rows * l.q_pitch;
   if (l.total < q_end) l.total = q_end;

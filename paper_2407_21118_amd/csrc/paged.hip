@@ -37,6 +37,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   constexpr bool PAIR = __is_same(T, F16);     // queries and keys as pairs hi + lo
   constexpr int NH = 8 / FQ;
   constexpr int FT = 8 / FQ;                   // tiles of 16 features per wavefront: low halves of the rotation pairs, then high halves
+  constexpr bool WHOLE = PT == 1 && FQ == 2;   // one barrier per tile
   constexpr int NP = 16 / FQ, NT = NP / 4;     // rotation pairs per lane, contraction steps of the score product
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
 
@@ -55,7 +56,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   const bool works = wave % NH < w.nh;                       // else: the same instructions, results nowhere
   const int hh = works ? wave % NH : 0, fq = wave / NH;
   const int fbase = (64 / FQ) * fq;                          // first rotation pair of this wavefront
-  const bool front = wave < 4;                               // of the two of a SIMD: the one that ends with the keys
+  const bool front = wave >= 4;                              // of the two of a SIMD: the one that ends with the keys (not that with rows
+                                                             // of the softmax, where there are few)
   const int hg = w.un.n_groups() > 1 ? hh / w.per_group : 0; // the head's group inside the unit
   const int E = 2 * NB - 1;                                  // entries are requested so many tiles ahead: early enough to be there when rows are made of them
   // the lane, once more: where accumulators take the registers, what is made of it is made anew, not kept in registers of the loop, which spill
@@ -113,9 +115,9 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     }
   };
   const int per_k = (ld.k_pieces / 2 + 7 - wave) / 8, per_v = ld.v_pieces / 16;    // operations of this wavefront
-  // Stages in use, as LDS offsets: keys of tile n and values of tile n - 1 (the stage before is requested into).
+  // Stages in use, as LDS offsets: keys of tile n and values of tile n - LAG (the stage before is requested into).
   const PagedRing ring_k{ld.k, ld.stage_k, NB}, ring_v{ld.v, ld.stage_v, NB};
-  int k_at = ring_k.stage(i0), v_at = ring_v.stage(i0 + NB - 1);
+  int k_at = ring_k.stage(i0), v_at = ring_v.stage(i0 + 2 * NB - (WHOLE ? 2 : 1));
 
   // ---- prologue
   for (int x = tid; x < kPagedTile * E; x += kPagedThreads) {   // entries of the first tiles, and rows of those that are requested at once
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   PagedAngles angles{w, lds, lds0, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
   if (wave == 1) angles.begin(NB);
   for (int j = i0; j < min(i0 + NB - 1, i1); ++j) request_keys(j, ring_k.stage(j));
-  for (int j = i0; j < min(i0 + NB - 2, i1); ++j) request_values(j, ring_v.stage(j));
+  for (int j = i0; j < min(i0 + NB - (WHOLE ? 3 : 2), i1); ++j) request_values(j, ring_v.stage(j));
 
   // weights.  FQ = 2: rotation pair fbase + 2 m + j is row m of tile j (low half) and 2 + j (high half); FQ = 4: pair fbase + m of tiles
   // 0 and 1.  A lane reads its features from eight rows of B_k and transposes them.  They stay in the accumulation registers, which the matrix instructions read as they are.
@@ -152,7 +154,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     for (int ks = 0; ks < AHEAD; ++ks) fetch(ks);
     w.rotate_queries<T, PT == 4 ? 2 : 1>(lds + ld.q, ld.q_pitch);
     // angles of positions 0 .. 15, scaled, where those of a tile's other tokens come later
-    float* const in = reinterpret_cast<float*>(lds + ld.ang) + 16 * kPagedAngPitch;
+    float* const in = reinterpret_cast<float*>(lds + ld.ang) + (WHOLE ? 3 : 1) * 16 * kPagedAngPitch;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int x = tid + i * kPagedThreads;
@@ -211,11 +213,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     }
   }
   // angles: this lane makes those of rotation pair `lane` of tokens wave and wave + 8 of 16
-  const float* const in = reinterpret_cast<const float*>(lds + ld.ang) + (16 + wave) * kPagedAngPitch + lane;
+  const float* const in = reinterpret_cast<const float*>(lds + ld.ang) + ((WHOLE ? 48 : 16) + wave) * kPagedAngPitch + lane;
   const float in_c0 = in[0], in_s0 = in[kHalf], in_c1 = in[8 * kPagedAngPitch], in_s1 = in[8 * kPagedAngPitch + kHalf];
-  auto make_angles = [&](int sub) __attribute__((always_inline)) {
+  auto ang_slot = [&](int n, int sub) __attribute__((always_inline)) { return (WHOLE ? 2 * ((n - i0) & 1) + sub : sub) * 16; };
+  auto make_angles = [&](int n, int sub) __attribute__((always_inline)) {
     const int lane = fresh_lane();
-    float* at = reinterpret_cast<float*>(lds + ld.ang) + (16 * sub + wave) * kPagedAngPitch + lane;
+    float* at = reinterpret_cast<float*>(lds + ld.ang) + (ang_slot(n, sub) + wave) * kPagedAngPitch + lane;
     const float c = angles.c, s = angles.s;
     at[0] = __builtin_fmaf(in_c0, c, -(in_s0 * s));
     at[kHalf] = __builtin_fmaf(in_s0, c, in_c0 * s);
@@ -224,7 +227,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     angles.turn();
   };
   angles.start();
-  make_angles(0);
+  make_angles(i0, 0);
+  if (WHOLE) make_angles(i0, 1);
   lds_barrier();                                             // (scores and probabilities take the queries' place, other angles that of the first 16)
 
   const int my_row = works && col < nr ? hh * nr + col : max_packed;   // where this lane's scores go; of no row: behind the last
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   const float* const my_ang = reinterpret_cast<const float*>(lds + ld.ang) + tok * kPagedAngPitch + fbase + NP * kg;
   float* const my_score = reinterpret_cast<float*>(lds + ld.s) + fq * plane + my_row * kPagedScorePitch + 4 * kg;
   // scores of a tile's first 16 tokens: of two tiles, in turn; of the others: of one
-  auto score_slot = [&](int n, int sub) __attribute__((always_inline)) { return (sub == 0 ? n & 1 : 2) * FQ * plane; };
+  auto score_slot = [&](int n, int sub) __attribute__((always_inline)) { return (WHOLE ? 2 * (n & 1) + sub : (sub == 0 ? n & 1 : 2)) * FQ * plane; };
   float minus_one = -1.f;                                    // (not a constant to the compiler, which would make a conversion and a subtraction of `less`)
   asm("" : "+s"(minus_one));
 
@@ -243,7 +247,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     constexpr int sub = decltype(sub_c)::value;
     const unsigned char* h0p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off0;
     const unsigned char* h1p = lds + k_stage + 16 * sub * ld.k_pieces * 16 + off1;
-    const float* ang = my_ang + 16 * sub * kPagedAngPitch;
+    const float* ang = my_ang + ang_slot(n, sub) * kPagedAngPitch;
     float4v acc[FT], c4[NT], s4[NT];
     uint4v af[3];
     af[0] = *reinterpret_cast<const uint4v*>(h0p);
@@ -258,7 +262,6 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < FT; ++j) acc[j] = mma<T>(W[ks][j], af[ks % 3], ks == 0 ? float4v{0, 0, 0, 0} : acc[j]);
-      __builtin_amdgcn_sched_barrier(0);
     }
     float4v dot = {0, 0, 0, 0};
     if (NT > 1) {
@@ -333,14 +336,14 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     run_max = now;
     run_sum = run_sum * alpha + ((p[0] + p[1]) + (p[2] + p[3]));
     // in the order of the value product's contraction: lane group squad, tokens squad + 4 e
-    unsigned char* P = lds + ld.p + min(srow, PT * 16) * kPagedProbPitch + 16 * squad + 8 * stile;
+    unsigned char* P = lds + ld.p + ((WHOLE ? (n & 1) * 17 : 0) + min(srow, PT * 16)) * kPagedProbPitch + 16 * squad + 8 * stile;
     *reinterpret_cast<uint2v*>(P) = hi;
     *reinterpret_cast<uint2v*>(P + 64) = lo;
-    reinterpret_cast<float*>(lds + ld.alpha)[srow] = alpha;
+    reinterpret_cast<float*>(lds + ld.alpha)[(WHOLE ? (n & 1) * 16 : 0) + srow] = alpha;
   };
 
-  // ---- values of a tile, staged at v_stage
-  auto values = [&](int v_stage) __attribute__((always_inline)) {
+  // ---- values of tile n, staged at v_stage
+  auto values = [&](int n, int v_stage) __attribute__((always_inline)) {
     const int l = fresh_lane(), col = l & 15, kg = l >> 4, v_lane = kg * ld.v_pieces * 16 + (col & 3) * 4, v_pitch16 = 4 * ld.v_pieces * 16;
 #pragma unroll
     for (int v = 0; v < VB; ++v) {
@@ -359,8 +362,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 #pragma unroll
       for (int p = 0; p < PT; ++p) {
         if (p > 0 && p >= n_pt) break;
-        const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (16 * p + 4 * kg) * 4);
-        const unsigned char* P = lds + ld.p + (16 * p + col) * kPagedProbPitch + 16 * kg;
+        const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + ((WHOLE ? (n & 1) * 16 : 0) + 16 * p + 4 * kg) * 4);
+        const unsigned char* P = lds + ld.p + ((WHOLE ? (n & 1) * 17 : 0) + 16 * p + col) * kPagedProbPitch + 16 * kg;
         const uint4v hi = *reinterpret_cast<const uint4v*>(P), lo = *reinterpret_cast<const uint4v*>(P + 64);
         O[v][p][0] = mma<T>(hi, f0, O[v][p][0] * al);
         O[v][p][1] = mma<T>(hi, f1, O[v][p][1] * al);
@@ -370,30 +373,52 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     }
   };
 
-  for (int n = i0; n <= i1; ++n) {
+  constexpr int LAG = WHOLE ? 2 : 1;                         // values follow the keys so many intervals later
+  for (int n = i0; n < i1 + LAG; ++n) {
     auto first_half = [&]() __attribute__((always_inline)) {
       if (n + NB - 1 < i1) request_keys(n + NB - 1, ring_k.before(k_at));
-      if (n > i0) softmax(n - 1);
+      if (n > i0 && n <= i1) softmax(n - 1);
     };
     auto second_half = [&]() __attribute__((always_inline)) {
-      if (n + NB - 2 >= i0 && n + NB - 2 < i1) request_values(n + NB - 2, ring_v.before(v_at));
-      if (n > i0) values(v_at);
+      const int j = n + NB - 1 - LAG;
+      if (j >= i0 && j < i1) request_values(j, ring_v.before(v_at));
+      if (n >= i0 + LAG) values(n - LAG, v_at);
     };
     if (wave == 3 && n + E < i1 && lane < kPagedTile) load_to_lds4(w.entry_of(n + E, lane), lds0 + ld.entries + ((n + E) % kPagedEntrySlots) * (kPagedTile * 4));
     if (wave == 2 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
     if (wave == 1) angles.request(n + NB);
-    if (n < i1) make_angles(1);
-    if (front) first_half();
-    if (n < i1) keys(IntC<0>(), n, k_at);
-    if (!front) first_half();
-    lds_barrier();
-    if (n + 1 < i1) {
-      angles.reach(n + 1);
-      make_angles(0);
+    if (WHOLE) {
+      if (n + 1 < i1) {
+        angles.reach(n + 1);
+        make_angles(n + 1, 0);
+        make_angles(n + 1, 1);
+      }
+      if (front) {
+        first_half();
+        second_half();
+      }
+      if (n < i1) {
+        keys(IntC<0>(), n, k_at);
+        keys(IntC<1>(), n, k_at);
+      }
+      if (!front) {
+        first_half();
+        second_half();
+      }
+    } else {
+      if (n < i1) make_angles(n, 1);
+      if (front) first_half();
+      if (n < i1) keys(IntC<0>(), n, k_at);
+      if (!front) first_half();
+      lds_barrier();
+      if (n + 1 < i1) {
+        angles.reach(n + 1);
+        make_angles(n + 1, 0);
+      }
+      if (front) second_half();
+      if (n < i1) keys(IntC<1>(), n, k_at);
+      if (!front) second_half();
     }
-    if (front) second_half();
-    if (n < i1) keys(IntC<1>(), n, k_at);
-    if (!front) second_half();
     k_at = ring_k.behind(k_at);
     v_at = ring_v.behind(v_at);
     // what interval n + 1 reads was requested in n - NB + 2; the NB - 2 intervals since then may be outstanding where all of them
