@@ -58,16 +58,17 @@ constexpr int kPagedProbPitch = 144;           // bytes per row of probabilities
 constexpr int kPagedScorePitch = 20;           // floats per row of scores: 16 tokens and 16 bytes
 constexpr int kPagedAngPitch = kDHead + 4;     // floats per token of angles
 constexpr int kPagedMaxStages = 6;
-constexpr int kPagedEntrySlots = 16;           // tiles whose page-table entries are held
-constexpr int kPagedRowSlots = 8;              // ... and whose tokens' rows of the cache
-constexpr int kPagedAnchorSlots = 8;           // ... and whose first angles
 constexpr int kPagedAnchorTiles = 8;           // every so many tiles the angles come from the table
 constexpr int kPagedLdsBytes = 160 * 1024;     // of a compute unit
+
+// One barrier per tile, or one per half of a tile where two tiles' scores, angles and probabilities leave no LDS for two stages of wide rows
+__host__ __device__ constexpr bool paged_whole(int parts, int row_tiles) { return parts == 2 && row_tiles != 2; }
 
 // LDS of a workgroup, in bytes from its start.  Tiles are staged n_stages deep, rows in 16-byte pieces, as many of them as a power
 // of two (at least 8, of values 16).  Queries lie where scores and probabilities come later.
 struct PagedLds {
   int k_pieces, v_pieces;
+  int slots;                                   // tiles whose tokens' rows of the cache and whose first angles are held; of page-table entries: twice as many
   int q_pitch;                                 // bytes per packed query row
   int stage_k, stage_v;                        // bytes per staged tile
   int k, v, anchors, entries, rows, ang, alpha, s, p, q, total;
@@ -82,13 +83,14 @@ __host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int
   l.q_pitch = kDHead * 2 * (pairs ? 2 : 1) + 16;
   l.stage_k = kPagedTile * l.k_pieces * 16;
   l.stage_v = kPagedTile * l.v_pieces * 16;
+  l.slots = n_stages <= 3 ? 4 : 8;
   l.k = 0;
   l.v = l.k + n_stages * l.stage_k;
   l.anchors = l.v + n_stages * l.stage_v;
-  l.entries = l.anchors + kPagedAnchorSlots * kDHead * 4;
-  l.rows = l.entries + kPagedEntrySlots * kPagedTile * 4;
-  l.ang = l.rows + kPagedRowSlots * kPagedTile * 4;
-  const int held = row_tiles == 1 && parts == 2 ? 2 : 1;    // tiles whose angles and probabilities are held: one where halves of tiles are between barriers
+  l.entries = l.anchors + l.slots * kDHead * 4;
+  l.rows = l.entries + 2 * l.slots * kPagedTile * 4;
+  l.ang = l.rows + l.slots * kPagedTile * 4;
+  const int held = paged_whole(parts, row_tiles) ? 2 : 1;    // tiles whose angles and probabilities are held
   l.alpha = l.ang + held * kPagedTile * kPagedAngPitch * 4;
   l.p = l.alpha + held * row_tiles * 16 * 4;
   l.s = l.p + held * (row_tiles * 16 + 1) * kPagedProbPitch;

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   constexpr bool PAIR = __is_same(T, F16);     // queries and keys as pairs hi + lo
   constexpr int NH = 8 / FQ;
   constexpr int FT = 8 / FQ;                   // tiles of 16 features per wavefront: low halves of the rotation pairs, then high halves
-  constexpr bool WHOLE = PT == 1 && FQ == 2;   // one barrier per tile
+  constexpr bool WHOLE = paged_whole(FQ, PT);  // one barrier per tile
   constexpr int NP = 16 / FQ, NT = NP / 4;     // rotation pairs per lane, contraction steps of the score product
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
 
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   int* const entries = reinterpret_cast<int*>(lds + ld.entries);
   int* const rows = reinterpret_cast<int*>(lds + ld.rows);
   auto make_row = [&](int i, int x) __attribute__((always_inline)) {
-    rows[(i % kPagedRowSlots) * kPagedTile + x] = w.row_of(i, x, entries[(i % kPagedEntrySlots) * kPagedTile + x]);
+    rows[(i & (ld.slots - 1)) * kPagedTile + x] = w.row_of(i, x, entries[(i & (2 * ld.slots - 1)) * kPagedTile + x]);
   };
 
   // ---- requests of interval n: keys of tile n + NB - 1, values of n + NB - 2, entries of n + E; the rows of tile n + NB.  An operation
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   const unsigned char* const src_v = paged_source(a.hv, a.meta.v_off[w.g], w.v_cols, (id0 % ld.v_pieces) ^ paged_value_swizzle(x_v));
   const uint32_t k_pitch = (uint32_t)a.R_k * 2, v_pitch = (uint32_t)a.R_v * 2;
   auto request_keys = [&](int j, int stage) __attribute__((always_inline)) {
-    const int* r = rows + (j % kPagedRowSlots) * kPagedTile + x_k;
+    const int* r = rows + (j & (ld.slots - 1)) * kPagedTile + x_k;
     const uint32_t dst = lds0 + stage + wave * 1024;
     if (FQ == 4) {                                           // rows of 64 pieces
       const uint32_t r0 = r[0], r1 = r[8], r2 = r[16], r3 = r[24];
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     }
   };
   auto request_values = [&](int j, int stage) __attribute__((always_inline)) {
-    const int* r = rows + (j % kPagedRowSlots) * kPagedTile + x_v;
+    const int* r = rows + (j & (ld.slots - 1)) * kPagedTile + x_v;
     const uint32_t dst = lds0 + stage + wave * 1024;
     if (VB == 2) {                                           // rows of 64 pieces
       const uint32_t r0 = r[0], r1 = r[8], r2 = r[16], r3 = r[24];
@@ -123,12 +123,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   for (int x = tid; x < kPagedTile * E; x += kPagedThreads) {   // entries of the first tiles, and rows of those that are requested at once
     const int i = i0 + x / kPagedTile;
     if (i < i1) {
-      entries[(i % kPagedEntrySlots) * kPagedTile + x % kPagedTile] = *w.entry_of(i, x % kPagedTile);
+      entries[(i & (2 * ld.slots - 1)) * kPagedTile + x % kPagedTile] = *w.entry_of(i, x % kPagedTile);
       if (i < i0 + NB) make_row(i, x % kPagedTile);
     }
   }
   lds_barrier();
-  PagedAngles angles{w, lds, lds0, ld.anchors, lane, 0.f, 0.f, 0.f, 0.f};
+  PagedAngles angles{w, lds, lds0, ld.anchors, ld.slots, lane, 0.f, 0.f, 0.f, 0.f};
   if (wave == 1) angles.begin(NB);
   for (int j = i0; j < min(i0 + NB - 1, i1); ++j) request_keys(j, ring_k.stage(j));
   for (int j = i0; j < min(i0 + NB - (WHOLE ? 3 : 2), i1); ++j) request_values(j, ring_v.stage(j));
@@ -336,10 +336,10 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     run_max = now;
     run_sum = run_sum * alpha + ((p[0] + p[1]) + (p[2] + p[3]));
     // in the order of the value product's contraction: lane group squad, tokens squad + 4 e
-    unsigned char* P = lds + ld.p + ((WHOLE ? (n & 1) * 17 : 0) + min(srow, PT * 16)) * kPagedProbPitch + 16 * squad + 8 * stile;
+    unsigned char* P = lds + ld.p + ((WHOLE ? (n & 1) * (PT * 16 + 1) : 0) + min(srow, PT * 16)) * kPagedProbPitch + 16 * squad + 8 * stile;
     *reinterpret_cast<uint2v*>(P) = hi;
     *reinterpret_cast<uint2v*>(P + 64) = lo;
-    reinterpret_cast<float*>(lds + ld.alpha)[(WHOLE ? (n & 1) * 16 : 0) + srow] = alpha;
+    reinterpret_cast<float*>(lds + ld.alpha)[(WHOLE ? (n & 1) * (PT * 16) : 0) + srow] = alpha;
   };
 
   // ---- values of tile n, staged at v_stage
@@ -362,8 +362,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 #pragma unroll
       for (int p = 0; p < PT; ++p) {
         if (p > 0 && p >= n_pt) break;
-        const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + ((WHOLE ? (n & 1) * 16 : 0) + 16 * p + 4 * kg) * 4);
-        const unsigned char* P = lds + ld.p + ((WHOLE ? (n & 1) * 17 : 0) + 16 * p + col) * kPagedProbPitch + 16 * kg;
+        const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + ((WHOLE ? (n & 1) * (PT * 16) : 0) + 16 * p + 4 * kg) * 4);
+        const unsigned char* P = lds + ld.p + ((WHOLE ? (n & 1) * (PT * 16 + 1) : 0) + 16 * p + col) * kPagedProbPitch + 16 * kg;
         const uint4v hi = *reinterpret_cast<const uint4v*>(P), lo = *reinterpret_cast<const uint4v*>(P + 64);
         O[v][p][0] = mma<T>(hi, f0, O[v][p][0] * al);
         O[v][p][1] = mma<T>(hi, f1, O[v][p][1] * al);
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
       if (j >= i0 && j < i1) request_values(j, ring_v.before(v_at));
       if (n >= i0 + LAG) values(n - LAG, v_at);
     };
-    if (wave == 3 && n + E < i1 && lane < kPagedTile) load_to_lds4(w.entry_of(n + E, lane), lds0 + ld.entries + ((n + E) % kPagedEntrySlots) * (kPagedTile * 4));
+    if (wave == 3 && n + E < i1 && lane < kPagedTile) load_to_lds4(w.entry_of(n + E, lane), lds0 + ld.entries + ((n + E) & (2 * ld.slots - 1)) * (kPagedTile * 4));
     if (wave == 2 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
     if (wave == 1) angles.request(n + NB);
     if (WHOLE) {

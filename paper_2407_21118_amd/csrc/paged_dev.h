@@ -225,11 +225,11 @@ struct PagedAngles {
   const PagedWork& w;
   unsigned char* lds;
   uint32_t lds0;
-  int anchors, lane;
+  int anchors, slots, lane;
   float c, s, turn_c, turn_s;                  // of the next 16 tokens; of 16 positions
 
   __device__ __forceinline__ bool anchor(int j) const { return j < w.i1 && ((j - w.i0) % kPagedAnchorTiles == 0 || j == w.span.sink_tiles); }
-  __device__ __forceinline__ int slot(int j) const { return anchors + j % kPagedAnchorSlots * (kDHead * 4); }
+  __device__ __forceinline__ int slot(int j) const { return anchors + (j & (slots - 1)) * (kDHead * 4); }
   __device__ __forceinline__ void fetch(int pos, int at) const {
     const int p = min(pos, w.a.rope_len - 1);
     load_to_lds4(w.a.rope + rope_f32_index(p, lane, 0, kRopeTableStride), lds0 + at);
@@ -241,11 +241,11 @@ struct PagedAngles {
   // by one wavefront: anchors before tile i0 + ahead, and the angles of 16 positions in a slot that none of these has
   __device__ __forceinline__ void begin(int ahead) const {
     for (int j = w.i0; j < w.i0 + ahead; ++j) request(j);
-    fetch(16, slot(w.i0 + kPagedAnchorSlots - 1));
+    fetch(16, slot(w.i0 + slots - 1));
   }
   // when these are there
   __device__ __forceinline__ void start() {
-    const float* at = reinterpret_cast<const float*>(lds + slot(w.i0 + kPagedAnchorSlots - 1));
+    const float* at = reinterpret_cast<const float*>(lds + slot(w.i0 + slots - 1));
     turn_c = at[lane];
     turn_s = at[kHalf + lane];
     reach(w.i0);
