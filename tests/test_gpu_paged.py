@@ -333,3 +333,59 @@ def test_append_then_attend_then_share():
                                     Bk.double().cpu().numpy(), Bv.double().cpu().numpy(), layer.group_head_off, layer.k_rank_off,
                                     layer.v_rank_off, 128, layer.rope_theta, sel.astype(np.int32))
                 hold(got[b:b + 1], ref, "f16")
+
+
+@pytest.mark.parametrize("name,dtype", [("4x256", "f16"), ("gqa4", "bf16"), ("wide values", "f16"), ("wide keys", "bf16")])
+def test_shared_and_own_rows_in_many_splits(name, dtype):
+    """Sequences of very different lengths behind a prefix of many tiles: splits of both kinds, in one launch, by up to 64 query rows."""
+    layer = {"wide values": lambda: synth.uniform_layer(8, 4, 256, 384), "wide keys": lambda: synth.uniform_layer(4, 2, 512, 256)}.get(name, LAYERS.get(name))()
+    lens = [2500 + (137 * i * i) % 701 for i in range(18)] + [0, 1, 1300]
+    say(f"[prefix] {name} {dtype}: 21 sequences behind 2500 rows")
+    check(Pool(layer, dtype, lens, 32, seed=15, prefix=2500, max_len=3300))
+
+
+def test_many_query_rows_over_a_window_with_sinks_far_apart():
+    """The jump from the sinks to the window lies inside a workgroup's run of tiles, for 20 and 70 query rows per head."""
+    for name in ("gqa20", "gqa70"):
+        say(f"[paged] {name}, window 700 of 3000 rows")
+        check(Pool(LAYERS[name](), "f16", [3000, 2999, 31, 740], 16, seed=16), window=700, n_sink=100)
+
+
+def test_queries_of_one_sequence_as_entries_of_the_batch():
+    """A speculative-decoding check: three entries with one page-table row and lengths of their own; as one by one."""
+    pool = Pool(synth.uniform_layer(8, 4, 128), "f16", [400, 400, 400], 16, seed=17)
+    pool.put(0, 0)
+    d = pool.device()
+    d["page_table"][1:] = d["page_table"][0]
+    d["seq_lens"] = torch.tensor([400, 399, 398], dtype=torch.int32, device="cuda")
+    got = pool.call(d, 90, 4)
+    pool.rows[1], pool.rows[2], pool.lens = pool.rows[0], pool.rows[0], [400, 399, 398]
+    hold(got, pool.reference(90, 4), "f16")
+
+
+def test_lengths_left_out():
+    """Without seq_lens every sequence has max_len rows, its query the position of the last."""
+    for prefix in (0, 100):
+        pool = Pool(synth.uniform_layer(8, 4, 128), "bf16", [260, 260], 16, seed=18, prefix=prefix)
+        pool.put(0, 0)
+        d = pool.device()
+        d["seq_lens"] = None
+        hold(pool.call(d), pool.reference(), "bf16")
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Workspaces of their own; each as when it runs alone."""
+    pools = [Pool(synth.uniform_layer(8, 4, 256), "f16", [2000, 1500, 1777], 64, seed=19 + p, prefix=p) for p in (0, 1400)]
+    runs = []
+    for pool in pools:
+        pool.put(0, 0)
+        d = pool.device()
+        runs.append((pool, d, pool.call(d), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for k in range(3):
+        for pool, d, alone, stream in runs:
+            with torch.cuda.stream(stream):
+                got.append((alone, pool.call(d)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in got)
