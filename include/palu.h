@@ -482,7 +482,7 @@ int palu_attn_decode_staged(const palu_layer_desc* desc, int32_t batch, int32_t 
  *
  * Arithmetic.  Keys are rebuilt and rotated in float32.  A float16 layer's keys, queries and probabilities enter the
  * matrix instructions as pairs of float16 numbers (2^-21 relative), so that the error is that of the output's
- * rounding; a bfloat16 layer's keys and queries as one float16 number each (2^-11; the output is rounded to 2^-9),
+ * rounding; a bfloat16 layer's keys and queries as one float16 number each (2^-11; the output is rounded to 2^-8),
  * its probabilities as a pair of bfloat16 numbers.  Entries of rotated keys are right up to 5e5 in magnitude, of
  * queries up to 6e4.  Sums, maxima and merged results are float32.
  */

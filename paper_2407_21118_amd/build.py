@@ -39,7 +39,7 @@ def sources():
               ("attend16_forms.hip", VGPR_FORM + ["-DPALU_ATTEND_SHARED=2"], "_shared_few")]
     units += [("attend16_mixed_forms.hip", VGPR_FORM, "")]
     for act, suffix in (("F16", ""), ("BF16", "_bf16")):
-        units += [(f, VGPR_FORM + ["-DPALU_PAGED_ACT=" + act], suffix) for f in ("paged.hip",)]
+        units += [("paged.hip", VGPR_FORM + ["-DPALU_PAGED_ACT=" + act], suffix)]
     units += [("encode_gemm.hip", [], "")]
     return [(os.path.join(CSRC, f), extra, os.path.splitext(f)[0] + suffix + ".o") for f, extra, suffix in units]
 

@@ -4,7 +4,7 @@
 //   out = softmax_t( RoPE(q, p) . RoPE(H_k[t] B_k, t) / sqrt(d_h) ) H_v[t] B_v
 //
 // One workgroup takes a unit (up to four key/value heads, two where the key rank is above 256), up to 16 query rows of each
-// (heads of a group, and sequences where the tokens are shared) and a run of tiles of 32 tokens.
+// (query heads, and sequences where the tokens are shared) and a run of tiles of 32 tokens.
 // Eight wavefronts, two per SIMD; FQ of them share a head: each has 64 / FQ of its rotation pairs, the weights for which stay
 // in up to 128 accumulation registers.
 //   keys    K^T = B_k^T H_k^T of 16 tokens at a time, from latents in LDS; rotated in float32 and multiplied by the
@@ -13,16 +13,21 @@
 //           float32.
 //   values  every wavefront contracts the probabilities of all rows with its 32 columns of the value latents (read as two
 //           columns of eight tokens per lane: the transposition that the matrix operand wants is a byte permute).
-//   angles  of every token of 16, a 512th part by every lane, in LDS: all heads' keys are rotated by them.
-// Two barriers per tile: the first half of interval n has the keys of the tile's first 16 tokens and the softmax of n - 1, the second
-// half the other keys and the values of n - 1.  One wavefront of a SIMD begins with the keys, the other ends with them: the matrix
-// instructions of one run beside the vector instructions of the other.  Latents, page-table entries and the angles' anchors come by
-// loads that write to LDS directly, n_stages - 1 tiles ahead, counted and never drained while tiles follow: 5.3 TB/s at 2 us
-// latency take 40 KB in flight per compute unit.
+//   angles  of a tile's tokens, a 512th part by every lane, in LDS: all heads' keys are rotated by them.
+// One barrier per tile: in interval n are the keys of tile n, the softmax of n - 1 and the values of n - 2 (WHOLE), or two of them, one per
+// 16 tokens' keys, where LDS does not hold two tiles' scores, angles and probabilities.  With two, 16 sequences of 8192 rows took 400 us,
+// with one 362.  One wavefront of a SIMD begins with the keys, the other ends with them: the matrix instructions of one run beside
+// the vector instructions of the other.  Latents, page-table entries and the angles' anchors come by loads that write to LDS
+// directly, n_stages - 1 tiles ahead, counted and never drained while tiles follow: 5.3 TB/s at 2 us latency take 40 KB in flight
+// per compute unit.
+// What bounds it: rank 256 of 4 heads takes 2048 cycles of matrix instructions per SIMD and tile for the keys, about 400 for the scores, and
+// 500 vector instructions of 4 cycles; two wavefronts per SIMD leave half of either unused.  Measured, 32 heads in groups of 4, rank 256, float16:
+// 16 sequences of 8192 rows 362 us (3.0 TB/s; the loads alone 199 us); 8 sequences behind 16384 shared rows 79 us.
 // Partial results (unnormalised sums, maxima, row sums) are merged, normalised and multiplied by B_v in paged_merge_kernel.
 //
 // Rotation.  The angle of position t0 + i is that of t0 plus that of i: a lane keeps cos and sin of two i < 16 and one pair, and those of
-// each 16 tokens' first position follow from those before.  Products of numbers that are right to 1e-7.
+// each 16 tokens' first position follow from those before.  Products of numbers that are right to 1e-7.  Rotated keys are made once for
+// all query rows; turning the queries of few rows to the tiles instead was no faster.
 // Rounding.  The matrix instructions take 16-bit operands.  A float16 layer's output is rounded to 2^-11 relative, so
 // the rotated keys, the queries and the probabilities enter as pairs of float16 numbers hi + lo (2^-21).  A bfloat16
 // layer's output is rounded to 2^-8: keys and queries enter as one float16 number each (2^-11), probabilities as a pair
@@ -72,8 +77,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     rows[(i & (ld.slots - 1)) * kPagedTile + x] = w.row_of(i, x, entries[(i & (2 * ld.slots - 1)) * kPagedTile + x]);
   };
 
-  // ---- requests of interval n: keys of tile n + NB - 1, values of n + NB - 2, entries of n + E; the rows of tile n + NB.  An operation
-  // moves 64 16-byte pieces, lane i the i-th of them; a wavefront takes every eighth.
+  // ---- requests of interval n: keys of tile n + NB - 1, values of n + NB - 1 - LAG, entries of n + E; the rows of tile n + NB.  An
+  // operation moves 64 16-byte pieces, lane i the i-th of them; a wavefront takes every eighth.
   const int id0 = wave * 64 + lane, x_k = id0 / ld.k_pieces, x_v = id0 / ld.v_pieces;
   const int p_k = (id0 % ld.k_pieces) ^ paged_key_swizzle(x_k);
   const unsigned char* const src_k = paged_source(a.hk, a.meta.k_off[w.g], w.k_cols, p_k);
@@ -134,7 +139,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   for (int j = i0; j < min(i0 + NB - (WHOLE ? 3 : 2), i1); ++j) request_values(j, ring_v.stage(j));
 
   // weights.  FQ = 2: rotation pair fbase + 2 m + j is row m of tile j (low half) and 2 + j (high half); FQ = 4: pair fbase + m of tiles
-  // 0 and 1.  A lane reads its features from eight rows of B_k and transposes them.  They stay in the accumulation registers, which the matrix instructions read as they are.
+  // 0 and 1.  A lane reads its features from eight rows of B_k and transposes them.  They stay in the accumulation registers, which the
+  // matrix instructions read as they are.
   uint4v W[KS][FT];
   {
     const int width = w.per_group * kDHead;
@@ -384,7 +390,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
       if (j >= i0 && j < i1) request_values(j, ring_v.before(v_at));
       if (n >= i0 + LAG) values(n - LAG, v_at);
     };
-    if (wave == 3 && n + E < i1 && lane < kPagedTile) load_to_lds4(w.entry_of(n + E, lane), lds0 + ld.entries + ((n + E) & (2 * ld.slots - 1)) * (kPagedTile * 4));
+    if (wave == 3 && n + E < i1 && lane < kPagedTile)
+      load_to_lds4(w.entry_of(n + E, lane), lds0 + ld.entries + ((n + E) & (2 * ld.slots - 1)) * (kPagedTile * 4));
     if (wave == 2 && n + NB < i1 && lane < kPagedTile) make_row(n + NB, lane);
     if (wave == 1) angles.request(n + NB);
     if (WHOLE) {
