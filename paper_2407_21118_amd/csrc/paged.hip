@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   const int NB = a.n_stages;
   const int max_packed = PT > 1 ? PT * 16 : a.max_packed;    // rows that LDS is laid out for
   const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, max_packed, PT, FQ, PAIR, NB);
-  const int plane = (max_packed + 1) * kPagedScorePitch;   // floats: a wavefront's part of 16 tokens' scores, of all rows and none
+  const int plane = (max_packed + 1) * kPagedScorePitch;     // floats: a wavefront's part of 16 tokens' scores, of all rows and none
   const uint32_t lds0 = lds_addr(lds);
   const bool works = wave % NH < w.nh;                       // else: the same instructions, results nowhere
   const int hh = works ? wave % NH : 0, fq = wave / NH;
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   {
     const int width = w.per_group * kDHead;
     const uint16_t* B = a.Bk + w.weights_of(hh, hg) + fbase;
-    constexpr int AHEAD = KS < 4 ? KS : (PT > 1 ? 3 : 4);                 // steps whose rows are in flight
+    constexpr int AHEAD = KS < 4 ? KS : (PT > 1 ? 3 : 4);    // steps whose rows are in flight (of many query rows fewer: registers)
     uint32_t v[AHEAD][2][8];
     auto fetch = [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
@@ -183,6 +183,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
       if (ks + AHEAD < KS) fetch(ks + AHEAD);
     }
   }
+
   const int n_blocks = w.v_cols / 32;                        // of 32 value columns: block wave + 8 v is this wavefront's
   const int n_pt = (n_packed + 15) / 16;
   float4v O[VB][PT][2];
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   const int h_lane = tok * ld.k_pieces * 16 + hg * KS * 64, off0 = h_lane + (kg ^ h_key) * 16, off1 = h_lane + ((4 + kg) ^ h_key) * 16;
   const float* const my_ang = reinterpret_cast<const float*>(lds + ld.ang) + tok * kPagedAngPitch + fbase + NP * kg;
   float* const my_score = reinterpret_cast<float*>(lds + ld.s) + fq * plane + my_row * kPagedScorePitch + 4 * kg;
-  // scores of a tile's first 16 tokens: of two tiles, in turn; of the others: of one
+  // scores of 16 tokens: of two tiles, in turn; with two barriers per tile, of its last 16 tokens those of one
   auto score_slot = [&](int n, int sub) __attribute__((always_inline)) { return (WHOLE ? 2 * (n & 1) + sub : (sub == 0 ? n & 1 : 2)) * FQ * plane; };
   float minus_one = -1.f;                                    // (not a constant to the compiler, which would make a conversion and a subtraction of `less`)
   asm("" : "+s"(minus_one));
@@ -283,7 +284,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int p = 4 * t + 2 * u + i;
-          const float l = FQ == 2 ? acc[p & 1][p >> 1] : acc[0][p], h = FQ == 2 ? acc[FT / 2 + (p & 1)][p >> 1] : acc[1][p], c = c4[t][2 * u + i], sn = s4[t][2 * u + i];
+          const float l = FQ == 2 ? acc[p & 1][p >> 1] : acc[0][p], h = FQ == 2 ? acc[FT / 2 + (p & 1)][p >> 1] : acc[1][p];
+          const float c = c4[t][2 * u + i], sn = s4[t][2 * u + i];
           x[i] = __builtin_fmaf(l, c, -(h * sn));
           y[i] = __builtin_fmaf(h, c, l * sn);
         }

@@ -23,7 +23,6 @@ template <typename T> __device__ __forceinline__ uint32_t pack2(float x, float y
 template <> __device__ __forceinline__ uint32_t pack2<F16>(float x, float y) {
   return __builtin_bit_cast(uint32_t, half2v{(_Float16)x, (_Float16)y});
 }
-typedef float float2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <> __device__ __forceinline__ uint32_t pack2<BF16>(float x, float y) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
