@@ -171,7 +171,9 @@ int plan_paged(const PagedMeta& m, int act, PagedPlan* p) {
   };
   const bool both = own.max_tiles > 0 && shared.max_tiles > 0;
   for (const PagedPlanPart* t : {&own, &shared}) {
-    for (int n = 1; n <= std::min(t->max_tiles, both ? 64 : 1024); ++n) {
+    // (more than a few workgroups per compute unit would be starts and little else)
+    const long long most = std::min<long long>(both ? 64 : 1024, std::max<long long>(16, 4LL * cus / std::max<long long>(1, wgs[t == &own ? kPagedOwn : kPagedShared])));
+    for (int n = 1; n <= std::min<long long>(t->max_tiles, most); ++n) {
       const int tiles = ceil_div(t->max_tiles, n);
       consider(tiles, tiles);
       if (!both) continue;
