@@ -120,7 +120,8 @@ int plan_paged(const PagedMeta& m, int act, PagedPlan* p) {
       }
       if (!more) break;
     }
-    // Query rows: 16 in all, or 16 per head and as many as accumulators go where there are more; as many blocks of them as it takes
+    // Query rows: 16 in all, or 16 per head and as many as accumulators go where there are more; as many blocks of them as it takes.
+    // (32 sequences behind 8192 rows, ranks 128 / 384: blocks of 32 packed rows 132 us, of 16 172; 8 sequences: one block 57, two 64.)
     for (const PagedPlanPart& t : p->part) c.form.many = c.form.many || (t.max_tiles > 0 && ks <= 8 && most * t.rows > 16);
     auto lds_bytes = [&](int stages) {
       return paged_lds(k_groups, ks, v_cols, c.max_packed, c.form.row_tiles(), c.form.parts(), act == PALU_F16, stages).total;
@@ -147,8 +148,8 @@ int plan_paged(const PagedMeta& m, int act, PagedPlan* p) {
     t.chunk_tiles = 1;
     t.n_slots = 0;
   }
-  // Tiles per workgroup: one workgroup is resident per compute unit, and its start and end cost about as much as four tiles; a slot more is
-  // merged in a twentieth.  The two parts' workgroups run together: of equal length, or one part's halves or quarters of the other's.
+  // Tiles per workgroup: one workgroup is resident per compute unit, and its start and end cost about as much as four tiles (11 us; 24 sequences
+  // with a window of 1024: 94 us, at 2.5 tiles 107); a slot more is merged in a twentieth.  The two parts' workgroups run together: of equal length, or one part's halves or quarters of the other's.
   const int cus = device_cu_count();
   double best = 1e300;
   PagedPlanPart& own = p->part[kPagedOwn];
@@ -338,7 +339,9 @@ int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32
   e.n_shared = p.part[kPagedShared].n_slots;
   e.o_shared_stride = p.part[kPagedShared].o_stride;
   e.meta = m;
-  int per_wg = 8;                              // rows of a head per workgroup: fewer until there are two workgroups per compute unit
+  // rows of a head per workgroup: fewer until there are two workgroups per compute unit (48 grouped-query sequences: 119 us a call; until
+  // one 120, until four 126)
+  int per_wg = 8;
   while (per_wg > 1 && (long long)ceil_div(batch * m.qpk, per_wg) * m.n_heads < 2 * device_cu_count()) per_wg /= 2;
   hipLaunchKernelGGL(desc->act_dtype == PALU_F16 ? paged_merge_form<F16>(per_wg) : paged_merge_form<BF16>(per_wg),
                      dim3((unsigned)ceil_div(batch * m.qpk, per_wg), (unsigned)m.n_heads), dim3(256), 0, s, e);
