@@ -149,7 +149,7 @@ int plan_paged(const PagedMeta& m, int act, PagedPlan* p) {
     t.n_slots = 0;
   }
   // Tiles per workgroup: one workgroup is resident per compute unit, and its start and end cost about as much as four tiles (11 us; 24 sequences
-  // with a window of 1024: 94 us, at 2.5 tiles 107); a slot more is merged in a twentieth.  The two parts' workgroups run together: of equal length, or one part's halves or quarters of the other's.
+  // with a window of 1024: 103 us, priced at 2.5 tiles 117); a slot more is merged in a twentieth.  The two parts' workgroups run together: of equal length, or one part's halves or quarters of the other's.
   const int cus = device_cu_count();
   double best = 1e300;
   PagedPlanPart& own = p->part[kPagedOwn];
