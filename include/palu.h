@@ -480,10 +480,9 @@ int palu_attn_decode_staged(const palu_layer_desc* desc, int32_t batch, int32_t 
  * Ranks up to PALU_PAGED_MAX_RANK.  q, hk, hv, B_k, B_v, table, out and workspace are 16-byte aligned.
  * Only attended rows are read: what lies in other rows, numbers or not, has no effect.
  *
- * Arithmetic.  Keys are rebuilt and rotated in float32.  A float16 layer's keys, queries and probabilities enter the
- * matrix instructions as pairs of float16 numbers (2^-21 relative), so that the error is that of the output's
- * rounding; a bfloat16 layer's keys and queries as one float16 number each (2^-11; the output is rounded to 2^-8),
- * its probabilities as a pair of bfloat16 numbers.  Entries of rotated keys are right up to 5e5 in magnitude, of
+ * Arithmetic.  Keys are rebuilt and rotated in float32.  Keys and queries enter the matrix instructions as pairs of
+ * float16 numbers (2^-21 relative), probabilities as pairs of float16 or, in a bfloat16 layer, of bfloat16 numbers
+ * (2^-16), so that the error is that of the output's rounding (2^-11, bfloat16 2^-8).  Entries of rotated keys are right up to 5e5 in magnitude, of
  * queries up to 6e4.  Sums, maxima and merged results are float32.
  */
 enum { PALU_PAGED_MAX_RANK = 512 };

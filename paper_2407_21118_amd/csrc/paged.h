@@ -75,12 +75,12 @@ struct PagedLds {
 };
 // n_groups groups of the unit, ks steps of 32 key channels each; rows: packed query rows, in row_tiles tiles of 16; parts: partial scores
 // that are added up
-__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, int parts, bool pairs, int n_stages) {
+__host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int v_cols, int rows, int row_tiles, int parts, int n_stages) {
   PagedLds l;
   const int k_pieces = n_groups * ks * 4;
   l.k_pieces = k_pieces <= 8 ? 8 : (k_pieces <= 16 ? 16 : (k_pieces <= 32 ? 32 : 64));
   l.v_pieces = v_cols <= 128 ? 16 : (v_cols <= 256 ? 32 : 64);
-  l.q_pitch = kDHead * 2 * (pairs ? 2 : 1) + 16;
+  l.q_pitch = kDHead * 2 * 2 + 16;             // pairs
   l.stage_k = kPagedTile * l.k_pieces * 16;
   l.stage_v = kPagedTile * l.v_pieces * 16;
   l.slots = n_stages <= 3 ? 4 : 8;

@@ -28,10 +28,10 @@
 // Rotation.  The angle of position t0 + i is that of t0 plus that of i: a lane keeps cos and sin of two i < 16 and one pair, and those of
 // each 16 tokens' first position follow from those before.  Products of numbers that are right to 1e-7.  Rotated keys are made once for
 // all query rows; turning the queries of few rows to the tiles instead was no faster.
-// Rounding.  The matrix instructions take 16-bit operands.  A float16 layer's output is rounded to 2^-11 relative, so
-// the rotated keys, the queries and the probabilities enter as pairs of float16 numbers hi + lo (2^-21).  A bfloat16
-// layer's output is rounded to 2^-8: keys and queries enter as one float16 number each (2^-11), probabilities as a pair
-// of bfloat16 numbers.  Keys are scaled by 1/8 and the queries by 8 (exact): magnitudes up to 524032 stay in range.
+// Rounding.  The matrix instructions take 16-bit operands.  The rotated keys and queries enter as pairs of float16 numbers hi + lo
+// (2^-21 relative), the probabilities as pairs of the latents' type (2^-21, bfloat16 2^-16), so that the error is that of the output's
+// rounding (2^-11, bfloat16 2^-8).  (One float16 number each for a bfloat16 layer's keys and queries left outputs 1.3e-3 from these in the
+// 2-norm, beside 1.66e-3 of rounding them.)  Keys are scaled by 1/8 and the queries by 8 (exact): magnitudes up to 524032 stay in range.
 
 #include "paged_dev.h"
 
@@ -39,7 +39,6 @@ namespace palu {
 
 template <typename T, int FQ, int KS, int PT, int VB>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
-  constexpr bool PAIR = __is_same(T, F16);     // queries and keys as pairs hi + lo
   constexpr int NH = 8 / FQ;
   constexpr int FT = 8 / FQ;                   // tiles of 16 features per wavefront: low halves of the rotation pairs, then high halves
   constexpr bool WHOLE = paged_whole(FQ, PT);  // one barrier per tile
@@ -55,7 +54,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
   const int i0 = w.i0, i1 = w.i1, nr = w.nr, n_packed = w.n_packed;
   const int NB = a.n_stages;
   const int max_packed = PT > 1 ? PT * 16 : a.max_packed;    // rows that LDS is laid out for
-  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, max_packed, PT, FQ, PAIR, NB);
+  const PagedLds ld = paged_lds(w.un.n_groups(), KS, w.v_cols, max_packed, PT, FQ, NB);
   const int plane = (max_packed + 1) * kPagedScorePitch;     // floats: a wavefront's part of 16 tokens' scores, of all rows and none
   const uint32_t lds0 = lds_addr(lds);
   const bool works = wave % NH < w.nh;                       // else: the same instructions, results nowhere
@@ -213,10 +212,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     for (int t = 0; t < NT; ++t) {
       const uint2v x = *reinterpret_cast<const uint2v*>(q + 8 * t), y = *reinterpret_cast<const uint2v*>(q + 128 + 8 * t);
       qh[t] = uint4v{x.x, x.y, y.x, y.y};
-      if (PAIR) {
-        const uint2v z = *reinterpret_cast<const uint2v*>(q + 256 + 8 * t), u = *reinterpret_cast<const uint2v*>(q + 384 + 8 * t);
-        ql[t] = uint4v{z.x, z.y, u.x, u.y};
-      }
+      const uint2v z = *reinterpret_cast<const uint2v*>(q + 256 + 8 * t), u = *reinterpret_cast<const uint2v*>(q + 384 + 8 * t);
+      ql[t] = uint4v{z.x, z.y, u.x, u.y};
     }
   }
   // angles: this lane makes those of rotation pair `lane` of tokens wave and wave + 8 of 16
@@ -293,19 +290,15 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
         // where lo is measured from the float32 one, and take one instruction per number instead of one per two.)
         asm("" : "+v"(x[0]), "+v"(x[1]), "+v"(y[0]), "+v"(y[1]));
         uint32_t xh = pack2<F16>(x[0], x[1]), yh = pack2<F16>(y[0], y[1]);
-        if (PAIR) {
-          asm("" : "+v"(xh), "+v"(yh));
-          lo[u] = pack2<F16>(less<F16>(x[0], xh, minus_one), less<F16>(x[1], xh >> 16, minus_one));
-          lo[2 + u] = pack2<F16>(less<F16>(y[0], yh, minus_one), less<F16>(y[1], yh >> 16, minus_one));
-        }
+        asm("" : "+v"(xh), "+v"(yh));
+        lo[u] = pack2<F16>(less<F16>(x[0], xh, minus_one), less<F16>(x[1], xh >> 16, minus_one));
+        lo[2 + u] = pack2<F16>(less<F16>(y[0], yh, minus_one), less<F16>(y[1], yh >> 16, minus_one));
         hi[u] = xh;
         hi[2 + u] = yh;
       }
       dot = mma<F16>(hi, qh[t], dot);
-      if (PAIR) {
-        dot = mma<F16>(hi, ql[t], dot);
-        dot = mma<F16>(lo, qh[t], dot);
-      }
+      dot = mma<F16>(hi, ql[t], dot);
+      dot = mma<F16>(lo, qh[t], dot);
     }
     *reinterpret_cast<float4v*>(my_score + score_slot(n, sub)) = dot;   // lane: query row col, tokens kg + 4 i
   };

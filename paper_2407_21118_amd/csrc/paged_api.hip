@@ -73,7 +73,7 @@ double paged_makespan(long long n0, double a, long long n1, double b, int cus) {
 }
 
 // p->part: rows, seqs and max_tiles are set
-int plan_paged(const PagedMeta& m, int act, PagedPlan* p) {
+int plan_paged(const PagedMeta& m, PagedPlan* p) {
   p->meta = m;
   p->n_cls = 0;
   long long wgs[2] = {0, 0};                   // workgroups per chunk
@@ -124,7 +124,7 @@ int plan_paged(const PagedMeta& m, int act, PagedPlan* p) {
     // (32 sequences behind 8192 rows, ranks 128 / 384: blocks of 32 packed rows 132 us, of 16 172; 8 sequences: one block 57, two 64.)
     for (const PagedPlanPart& t : p->part) c.form.many = c.form.many || (t.max_tiles > 0 && ks <= 8 && most * t.rows > 16);
     auto lds_bytes = [&](int stages) {
-      return paged_lds(k_groups, ks, v_cols, c.max_packed, c.form.row_tiles(), c.form.parts(), act == PALU_F16, stages).total;
+      return paged_lds(k_groups, ks, v_cols, c.max_packed, c.form.row_tiles(), c.form.parts(), stages).total;
     };
     for (int limit = std::min(16, c.form.max_rows() / most); limit > 0; --limit) {   // (fewer where two stages leave no more LDS)
       c.max_packed = 0;
@@ -214,7 +214,7 @@ int plan_paged_call(const palu_layer_desc* desc, int batch, int prefix, int max_
   PagedPlan& p = c->plan;
   p.part[kPagedOwn] = PagedPlanPart{m.qpk, batch, paged_max_tiles(max_len, prefix, window, c->n_sink)};
   p.part[kPagedShared] = PagedPlanPart{batch * m.qpk, 1, ceil_div(prefix, kPagedTile)};
-  st = plan_paged(m, desc->act_dtype, &p);
+  st = plan_paged(m, &p);
   if (st != PALU_OK) return st;
   c->total = 0;
   for (int i = 0; i < 2; ++i) {

@@ -148,8 +148,8 @@ struct PagedWork {
     const int ohead = a.meta.o_off[g] + (h0 + h - a.meta.head_off[g]) * rv;
     *reinterpret_cast<float2*>(t.o_part + slot() * t.o_stride + (size_t)t.rows * ohead + (size_t)(row0 + r) * rv + c - cg * rv) = make_float2(x, y);
   }
-  // Rotated and scaled queries as pairs (bfloat16 layers: single numbers) of float16, [packed row][hi | lo][feature].  A wavefront takes a
-  // row of all heads, which has one position (whose angles lie in 128 cache lines), and has ROWS of them in flight.
+  // Rotated and scaled queries as pairs of float16 numbers, [packed row][hi | lo][feature].  A wavefront takes a row of all heads, which has
+  // one position (whose angles lie in 128 cache lines), and has ROWS of them in flight.
   template <typename T, int ROWS> __device__ __forceinline__ void rotate_queries(unsigned char* q, int pitch) const {
     constexpr int kWaves = kPagedThreads / 64, kHeads = 4;
     const int f = threadIdx.x & 63;
@@ -187,10 +187,8 @@ struct PagedWork {
           uint16_t* y = reinterpret_cast<uint16_t*>(q + pr * pitch) + f;
           y[0] = (uint16_t)hi;
           y[kHalf] = (uint16_t)(hi >> 16);
-          if (__is_same(T, F16)) {
-            y[kDHead] = (uint16_t)lo;
-            y[kDHead + kHalf] = (uint16_t)(lo >> 16);
-          }
+          y[kDHead] = (uint16_t)lo;
+          y[kDHead + kHalf] = (uint16_t)(lo >> 16);
         }
       }
     }
