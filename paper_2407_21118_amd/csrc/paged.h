@@ -103,8 +103,8 @@ __host__ __device__ __forceinline__ PagedLds paged_lds(int n_groups, int ks, int
 
 // Tokens that are attended in the same way: every sequence's own, or the shared prefix's.
 struct PagedPart {
-  float* o_part;                               // [slot][rows * sum of value ranks over the heads]: sums of exp2(score - max) * latent
-  float* ml_part;                              // [slot][head][row][2]: the maximum and the sum
+  float* o_part;                               // [slot][rows * sum of value ranks over the heads]: sums of exp2(score - max) * latent, times kProbScale
+  float* ml_part;                              // [slot][head][row][2]: the maximum and the sum, times kProbScale
   long long o_stride;                          // floats of o_part per slot
   int max_len, first, window, n_sink;
   int shared;                                  // the tokens are those of the shared prefix

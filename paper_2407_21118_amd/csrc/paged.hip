@@ -29,7 +29,7 @@
 // each 16 tokens' first position follow from those before.  Products of numbers that are right to 1e-7.  Rotated keys are made once for
 // all query rows; turning the queries of few rows to the tiles instead was no faster.
 // Rounding.  The matrix instructions take 16-bit operands.  The rotated keys and queries enter as pairs of float16 numbers hi + lo
-// (2^-21 relative), the probabilities as pairs of the latents' type (2^-21, bfloat16 2^-16), so that the error is that of the output's
+// (2^-21 relative), the probabilities as pairs of the latents' type (2^-21 or 2^-40 of the largest, bfloat16 2^-16), so that the error is that of the output's
 // rounding (2^-11, bfloat16 2^-8).  (One float16 number each for a bfloat16 layer's keys and queries left outputs 1.3e-3 from these in the
 // 2-norm, beside 1.66e-3 of rounding them.)  Keys are scaled by 1/8 and the queries by 8 (exact): magnitudes up to 524032 stay in range.
 
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_kernel(PagedArgs a) {
     const float alpha = __builtin_amdgcn_exp2f(run_max - zero);
     float p[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(s[e] - zero);
+    for (int e = 0; e < 4; ++e) p[e] = kProbScale<T> * __builtin_amdgcn_exp2f(s[e] - zero);
     uint2v hi, lo;
     uint32_t h0, l0, h1, l1;
     split2<T>(p[0], p[1], &h0, &l0);

@@ -8,6 +8,10 @@ namespace palu {
 namespace {
 
 constexpr float kKeyScale = 0.125f;
+// Probabilities, exp2(score - running maximum) <= 1, are held times this (so are their sums and those of the latents, whose quotient is
+// what counts): a pair of float16 numbers has steps of 2^-24, so that those of rows that one row outweighs are right to 2^-40 of the
+// largest and not to 2^-25, which was 4 % of e^-14.  bfloat16 pairs are as exact at any size.
+template <typename T> constexpr float kProbScale = __is_same(T, F16) ? 32768.f : 1.f;
 template <int N> struct IntC { static constexpr int value = N; };
 
 template <typename T> __device__ __forceinline__ float4v mma(uint4v a, uint4v b, float4v c);

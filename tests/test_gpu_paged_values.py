@@ -34,3 +34,46 @@ def test_a_bfloat16_layer_rounds_its_output_alone(name, prefix):
     beyond = np.maximum(off - half, 0) / np.abs(ref).max(-1, keepdims=True)
     say(f"[paged] {name}, prefix {prefix}: beyond half a step by at most {beyond.max():.2e} of the row's largest")
     assert (off <= room).all(), beyond.max()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("q_per_kv", [1, 5])
+@pytest.mark.parametrize("at", [0, 2000])
+def test_rows_that_one_row_outweighs(at, q_per_kv, dtype):
+    """4000 rows of one score under one row whose score is larger by up to 20 (2^-28.9 of its probability) and whose values are zero,
+    as a first row may have them: the output is the 4000 rows' alone.  All lie in one split, which shares one running maximum.
+
+    A pair of float16 numbers of probabilities scaled by 2^15 is right to 2^-22 relative or 2^-40 of the largest, whichever is more:
+    exp(gap) * 2^-40 of these rows', all of them in the same direction.  Beside it, of the row's largest output: the score's products of
+    one sign (gap * 2^-20.5 = 2^-16.2), the float32 sum of 126 tiles (2^-17), and the merged latents, pairs of numbers of which
+    the second has steps of 2^-24 (64 of 2^-25 times |B_v| < 0.4 against outputs of 8e-3: 2^-13.4 at their worst, with random signs
+    2^-16.4).  Together 2^-14.  bfloat16 pairs keep 2^-16 relative at every size: 2^-14 with the merged latents', too."""
+    gaps = [0.0, 5.0, 10.0, 14.0, 16.0, 17.4, 19.0, 20.0]
+    layer = synth.uniform_layer(4, 4, 64, rope_theta=0.0, q_per_kv=q_per_kv)     # (no rotation: rows of equal latents score alike)
+    desc, n, batch, page = make_desc(layer, dtype), 4001, 256, 64
+    assert P.palu_attn_paged_workspace_bytes(desc, batch, n) == P.palu_attn_paged_workspace_bytes(desc, batch, 32)   # one split
+    rng = np.random.default_rng(31)
+    draw = lambda *s: rng.standard_normal(s)  # noqa: E731
+    Bk, Bv = (synth.round_to(draw(64 * 4 * 128) / 8, dtype) for _ in range(2))
+    pages = -(-n // page)
+    hk, hv = np.full((2, pages * page, 64), np.nan)
+    hk[:n], hv[:n] = 0.0, synth.round_to(1000 * (1 + 0.25 * draw(n, 64)), dtype)
+    hk[at], hv[at] = synth.round_to(draw(64), dtype), 0.0
+    key = (hk[at] @ Bk.reshape(64, 512)).reshape(4, 1, 128)
+    key = key * np.sqrt(128) / (key ** 2).sum(-1, keepdims=True)
+    q = np.stack([synth.round_to((key * np.array([gaps[(b + i) % 8] for i in range(q_per_kv)])[None, :, None]).reshape(-1, 128), dtype)
+                  for b in range(8)])
+    dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(torch_dtype(dtype)).cuda()  # noqa: E731
+    got = P.palu_attn_paged(desc, batch, n, dev(q).repeat(batch // 8, 1, 1), None, dev(hk.reshape(pages, page, 64)), dev(hv.reshape(pages, page, 64)),
+                            torch.arange(pages, dtype=torch.int32, device="cuda").repeat(batch, 1), None, dev(Bk), dev(Bv),
+                            P.palu_rope_table_init(0.0, 128, n), n)
+    assert torch.equal(got, got[:8].repeat(batch // 8, 1, 1))
+    got = got[:8].double().cpu().numpy()
+    both = lambda x: np.repeat(x[None, :n], 8, 0)  # noqa: E731
+    ref = O.attn_decode(q, np.full(8, n - 1), both(hk), both(hv), Bk, Bv, layer.group_head_off, layer.k_rank_off, layer.v_rank_off, 128, 0.0,
+                        np.arange(n, dtype=np.int32), None, q_per_kv)
+    gap = np.array([[gaps[(b + i) % 8] for _ in range(4) for i in range(q_per_kv)] for b in range(8)])
+    top = np.abs(ref).max(-1)
+    off = np.maximum(np.abs(got - ref) - np.abs(ref) * (2.0 ** -11 if dtype == "f16" else 2.0 ** -8), 0).max(-1) / top
+    say(f"[paged] {dtype}, {q_per_kv} queries a head, row {at}: beyond rounding " + " ".join(f"{g}: {off[gap == g].max():.1e}" for g in gaps))
+    assert (off <= 2.0 ** -14 + (2.0 ** -40 * np.exp(gap) if dtype == "f16" else 0)).all()
