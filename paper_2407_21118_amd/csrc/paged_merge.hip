@@ -47,7 +47,8 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
     return *reinterpret_cast<const float2*>(p);
   };
 
-  // maximum and sum of every row: 256 / R threads each
+  // maximum and sum of every row: 256 / R threads each.  A partial result that saw no row has the maximum -inf and the sum 0; one of
+  // nothing but NaN scores, which a maximum passes over, -inf and NaN: its sum counts all the same, and the row becomes NaN.
   constexpr int kPer = 256 / R < 64 ? 256 / R : 64;
   if (tid < kPer * R) {
     const int r = tid / kPer;
@@ -57,14 +58,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
       for (int s = tid % kPer; s < n_own + a.n_shared; s += kPer) {
         const float2 x = ml_of(row, b, n_own, s);
         const float now = fmaxf(top, x.x);
-        if (now > -INFINITY) sum = sum * __builtin_amdgcn_exp2f(top - now) + x.y * __builtin_amdgcn_exp2f(x.x - now);
+        sum = now > -INFINITY ? sum * __builtin_amdgcn_exp2f(top - now) + x.y * __builtin_amdgcn_exp2f(x.x - now) : sum + x.y;
         top = now;
       }
     }
 #pragma unroll
     for (int d = 1; d < kPer; d *= 2) {
       const float t2 = __shfl_xor(top, d), s2 = __shfl_xor(sum, d), now = fmaxf(top, t2);
-      if (now > -INFINITY) sum = sum * __builtin_amdgcn_exp2f(top - now) + s2 * __builtin_amdgcn_exp2f(t2 - now);
+      sum = now > -INFINITY ? sum * __builtin_amdgcn_exp2f(top - now) + s2 * __builtin_amdgcn_exp2f(t2 - now) : sum + s2;
       top = now;
     }
     if (tid % kPer == 0) {
@@ -90,7 +91,6 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
       if (s < n_own + a.n_shared) {
         const float top = ml_of(row, b, n_own, s).x;
         if (top > -INFINITY) w = __builtin_amdgcn_exp2f(top - Top[r]);
-        if (top != top) w = top;
       }
       Weight[r][s - s0] = w;
     }

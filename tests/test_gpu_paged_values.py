@@ -77,3 +77,74 @@ def test_rows_that_one_row_outweighs(at, q_per_kv, dtype):
     off = np.maximum(np.abs(got - ref) - np.abs(ref) * (2.0 ** -11 if dtype == "f16" else 2.0 ** -8), 0).max(-1) / top
     say(f"[paged] {dtype}, {q_per_kv} queries a head, row {at}: beyond rounding " + " ".join(f"{g}: {off[gap == g].max():.1e}" for g in gaps))
     assert (off <= 2.0 ** -14 + (2.0 ** -40 * np.exp(gap) if dtype == "f16" else 0)).all()
+
+
+def both_forms(dtype, lens, prefix, seed, layer="4x128", max_len=None):
+    pool = Pool(LAYERS[layer](), dtype, lens, 16, seed=seed, prefix=prefix, max_len=max_len)
+    pool.put(0, 0)
+    return pool, pool.device()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("layer", ["4x128", "gqa4", "8x512"])
+@pytest.mark.parametrize("prefix", [0, 300])
+def test_a_query_that_is_no_number_answers_none(layer, prefix, dtype):
+    """One NaN in the query of one head: that head's output is NaN, every other has the bits that it has without; an idle slot's is zeros."""
+    say(f"[nan] {layer} {dtype}, prefix {prefix}")
+    pool, d = both_forms(dtype, [700, 0, 333, 450], prefix, 32, layer)
+    clean = pool.call(d)
+    heads = pool.layer.n_q_heads
+    d["q"][0, 2, 5] = d["q"][1] = d["q"][3, heads - 1, 127] = float("nan")
+    got = pool.call(d)
+    lost = torch.zeros(4, heads, 1, dtype=torch.bool, device="cuda")
+    lost[0, 2] = lost[3, heads - 1] = True
+    assert torch.equal(got.isnan(), lost.expand_as(got))
+    assert torch.equal(got.masked_fill(lost, 0), clean.masked_fill(lost, 0)) and not got[1].any()
+
+
+@pytest.mark.parametrize("side", ["hk", "hv"])
+def test_attended_rows_that_are_no_numbers(side):
+    """NaN in five runs of 1 .. 8 tiles of 32 rows in the middle of a sequence, so that some splits hold nothing else whatever their length:
+    its outputs are NaN.  Another sequence's have the bits that they have without, and so has its own where a window or its length leaves
+    these rows out."""
+    pool, d = both_forms("f16", [4032, 3999], 0, 33)
+    clean, late, early = pool.call(d), pool.call(d, 500, 4), d["seq_lens"].clone()
+    early[0] = 150
+    short = pool.call({**d, "seq_lens": early})
+    whole = d[side]
+    for tiles in (1, 2, 3, 4, 5, 6, 8):
+        say(f"[nan] {side}, runs of {tiles} tiles")
+        d[side] = whole.clone()
+        d[side][d["page_table"][0, 10 * tiles: 20 * tiles].long()] = float("nan")
+        got = pool.call(d)
+        assert got[0].isnan().all() and torch.equal(got[1], clean[1])
+        assert torch.equal(pool.call(d, 500, 4), late)
+        if tiles == 1:
+            assert torch.equal(pool.call({**d, "seq_lens": early}), short)
+
+
+@pytest.mark.parametrize("side", ["hk", "hv"])
+def test_own_or_shared_rows_that_are_no_numbers(side):
+    """NaN in all of one sequence's rows behind the prefix: its outputs alone are NaN.  In the prefix: everyone's, but an idle slot's."""
+    pool, d = both_forms("f16", [3900, 3100, 0], 3008, 34)
+    clean, whole = pool.call(d), d[side].clone()
+    d[side][d["page_table"][0, 188:].long()] = float("nan")
+    got = pool.call(d)
+    assert got[0].isnan().all() and torch.equal(got[1:], clean[1:])
+    for tiles in (1, 2, 3, 4, 5):
+        d[side] = whole.clone()
+        d[side][d["page_table"][0, 20 * tiles: 30 * tiles].long()] = float("nan")
+        got = pool.call(d)
+        assert got[:2].isnan().all() and not got[2].any()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_query_beyond_the_range_does_not_answer_zeros(dtype):
+    """A rotated query above 65504 / (8 log2(e) / sqrt(128)) = 6.4e4 has no float16 pair: its head's output is NaN, not an idle slot's."""
+    pool, d = both_forms(dtype, [100, 200], 0, 34)
+    clean = pool.call(d)
+    d["q"][0, 1] = 6.0e4                                             # (turned by some angle, a pair of 6e4 has an entry of more than 6.4e4)
+    got = pool.call(d)
+    assert got[0, 1].isnan().all()
+    got[0, 1] = clean[0, 1]
+    assert torch.equal(got, clean)
