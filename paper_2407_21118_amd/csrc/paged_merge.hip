@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
     __syncthreads();
     for (int x = tid; x < n * kBlock; x += 256) {
       const int r = x / kBlock, s = s0 + x % kBlock, row = row0 + r, b = row / m.qpk, n_own = own_slots(b);
-      float w = 0.f;
+      float w = -1.f;                                        // a partial result that saw no row is none, whatever it holds
       if (s < n_own + a.n_shared) {
         const float top = ml_of(row, b, n_own, s).x;
         if (top > -INFINITY) w = __builtin_amdgcn_exp2f(top - Top[r]);
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
           const float w = Weight[r][k];
           const float4v p = *reinterpret_cast<const float4v*>(s < n_own ? own + (size_t)s * a.o_stride : shared + (size_t)(s - n_own) * a.o_shared_stride);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[i][e] += w == 0.f ? 0.f : w * p[e];     // (a partial result that saw no row is none)
+          for (int e = 0; e < 4; ++e) o[i][e] += w < 0.f ? 0.f : w * p[e];
         }
       }
     }

@@ -138,6 +138,21 @@ def test_own_or_shared_rows_that_are_no_numbers(side):
         assert got[:2].isnan().all() and not got[2].any()
 
 
+def test_values_that_are_no_numbers_under_a_weight_of_zero():
+    """A row whose score is 200 above the others', whose splits then weigh exp(-200) = 0 in float32: zero times a NaN among their values
+    is NaN, as in the sum that is not split."""
+    pool = Pool(LAYERS["norope"](), "f16", [4032], 16, seed=35)
+    pool.rows[0][1:, : pool.layer.R_k] = 0.0
+    key = np.concatenate([(pool.rows[0][0, 128 * j: 128 * j + 128] @ pool.Bk[j * 65536:(j + 1) * 65536].reshape(128, 512)).reshape(4, 128) for j in (0, 1)])
+    pool.q = synth.round_to(200 * np.sqrt(128) * key / (key ** 2).sum(-1, keepdims=True), "f16")[None]
+    pool.put(0, 0)
+    d = pool.device()
+    hold(pool.call(d), pool.reference(), "f16")
+    d["hv"][d["page_table"][0, 100: 180].long(), 3, 130] = float("nan")
+    got = pool.call(d)
+    assert torch.isfinite(got[0, :4]).all() and got[0, 4:].isnan().all()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_a_query_beyond_the_range_does_not_answer_zeros(dtype):
     """A rotated query above 65504 / (8 log2(e) / sqrt(128)) = 6.4e4 has no float16 pair: its head's output is NaN, not an idle slot's."""
