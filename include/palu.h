@@ -467,7 +467,7 @@ int palu_attn_decode_staged(const palu_layer_desc* desc, int32_t batch, int32_t 
  *
  *   max_len      upper bound of seq_lens (values are clamped to [0, max_len]); max_len <= table_stride * page_rows
  *   q            DEVICE [batch, n_heads*q_per_kv, d_head] act_dtype, before RoPE
- *   q_pos        DEVICE int32 [batch] position of each query, clamped to [0, rope_table_len), or NULL: seq_lens[b] - 1
+ *   q_pos        DEVICE int32 [batch] position of each query, clamped to [0, rope_table_len), or NULL: the newest row's
  *   hk, hv       DEVICE [n_pages, page_rows, R] act_dtype (quantized caches: PALU_ERR_UNSUPPORTED); page_rows is a power
  *                of two, n_pages * page_rows < 2^31
  *   page_table   DEVICE int32 [batch, table_stride].  Entries are clamped to [0, n_pages); those of pages

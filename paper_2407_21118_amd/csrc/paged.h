@@ -125,7 +125,7 @@ struct PagedArgs {
   const int32_t* seq_lens;                     // [batch] or NULL: pos_len
   long long R_k, R_v;
   int n_pages, page_shift, table_stride, rope_len;
-  int pos_len;                                 // rows of a sequence where seq_lens is NULL
+  int pos_len;                                 // rows of a sequence where seq_lens is NULL, else at most
   int n_units;
   int n_stages;                                // tiles staged in LDS
   int max_packed;                              // packed query rows that LDS is laid out for (more than 16: as many as accumulators go)

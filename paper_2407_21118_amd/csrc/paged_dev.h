@@ -164,7 +164,7 @@ struct PagedWork {
 #pragma unroll
       for (int i = 0; i < ROWS; ++i) {
         const int r = min(first + i * kWaves, nr - 1), b = sequence_of(r), qh = shared ? row0 + r - b * a.meta.qpk : row0 + r;
-        pos[i] = a.q_pos ? a.q_pos[b] : (a.seq_lens ? a.seq_lens[b] : a.pos_len) - 1;
+        pos[i] = a.q_pos ? a.q_pos[b] : (a.seq_lens ? max(0, min(a.seq_lens[b], a.pos_len)) : a.pos_len) - 1;
 #pragma unroll
         for (int h = 0; h < kHeads; ++h) {
           const uint16_t* qp = a.q + ((size_t)b * a.meta.n_heads * a.meta.qpk + (h0 + min(h, nh - 1)) * a.meta.qpk + qh) * kDHead;

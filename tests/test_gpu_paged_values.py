@@ -163,3 +163,17 @@ def test_a_query_beyond_the_range_does_not_answer_zeros(dtype):
     assert got[0, 1].isnan().all()
     got[0, 1] = clean[0, 1]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("prefix", [0, 100])
+def test_lengths_beyond_their_bound(prefix):
+    """seq_lens above max_len count as max_len, for the rows and for the query's position, also where the angle table goes on; below 0 as 0."""
+    pool, d = both_forms("f16", [260, 260, 200], prefix, 36)
+    d["rope_table"], d["rope_table_len"] = P.palu_rope_table_init(pool.layer.rope_theta, 128, 1000), 1000
+    right = pool.call(d)
+    d["seq_lens"][:2] = torch.tensor([267, 2 ** 31 - 1])
+    assert torch.equal(pool.call(d), right)
+    hold(right, pool.reference(), "f16")
+    d["seq_lens"][1] = -5
+    got = pool.call(d)
+    assert torch.equal(got[[0, 2]], right[[0, 2]]) and not got[1].any()
