@@ -140,6 +140,9 @@ class LayerDesc:
         self.rope_theta = float(rope_theta)
         self.q_per_kv = int(q_per_kv)
         self.n_q_heads = self.n_heads * max(self.q_per_kv, 1)
+        # elements of B_k and B_v
+        self.b_elems = tuple(self.d_head * sum((off[j + 1] - off[j]) * (self._gho[j + 1] - self._gho[j]) for j in range(n_groups))
+                             for off in (self._kro, self._vro))
         self.c = _Desc(self.n_heads, self.d_head, n_groups, self._gho, self._kro, self._vro, act_dtype,
                        self.k_latent_dtype, self.v_latent_dtype, quant_block, self.rope_theta, self.q_per_kv)
 
@@ -435,10 +438,6 @@ def _paged_call(fn, where, desc, sizes, q, q_pos, hk, hv, page_table, seq_lens, 
                 workspace, stream):
     """hk, hv: [n_pages, page_rows, R]; page_table: [batch, pages per sequence]."""
     import torch
-    _need_cuda(q, q_pos, hk, hv, page_table, seq_lens, Bk, Bv, rope_table, out, workspace)
-    n_pages, page_rows = int(hk.shape[0]), int(hk.shape[1])
-    if tuple(hv.shape[:2]) != (n_pages, page_rows):
-        raise ValueError("hk and hv need the same pages")
     act = torch.float16 if desc.act_dtype == PALU_F16 else torch.bfloat16
     if any(t.dtype != act for t in (q, hk, hv, Bk, Bv, out)):
         raise ValueError(f"q, hk, hv, Bk, Bv and out need dtype {act}")
@@ -448,6 +447,14 @@ def _paged_call(fn, where, desc, sizes, q, q_pos, hk, hv, page_table, seq_lens, 
             or page_table.shape[0] != sizes[0] or any(t.numel() != sizes[0] * desc.n_q_heads * desc.d_head for t in (q, out))
             or any(t is not None and t.numel() != sizes[0] for t in (q_pos, seq_lens))):
         raise ValueError("shapes do not fit the layer and the batch")
+    n_pages, page_rows = int(hk.shape[0]), int(hk.shape[1])
+    if tuple(hv.shape[:2]) != (n_pages, page_rows):
+        raise ValueError("hk and hv need the same pages")
+    if (Bk.numel(), Bv.numel()) != desc.b_elems:
+        raise ValueError("Bk or Bv does not fit the layer's ranks")
+    if rope_table.numel() * rope_table.element_size() < palu_rope_table_bytes(desc.d_head, int(rope_table_len)):
+        raise ValueError("rope_table holds fewer than rope_table_len positions")
+    _need_cuda(q, q_pos, hk, hv, page_table, seq_lens, Bk, Bv, rope_table, out, workspace)
     _check(fn(desc.ref(), *sizes, _ptr(q), _ptr(q_pos), _ptr(hk), _ptr(hv), n_pages, page_rows, _ptr(page_table),
               int(page_table.shape[1]), _ptr(seq_lens), _ptr(Bk), _ptr(Bv), _ptr(rope_table), int(rope_table_len), _ptr(out),
               _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), where)

@@ -177,3 +177,25 @@ def test_lengths_beyond_their_bound(prefix):
     d["seq_lens"][1] = -5
     got = pool.call(d)
     assert torch.equal(got[[0, 2]], right[[0, 2]]) and not got[1].any()
+
+
+def test_device_tensors_that_do_not_fit_are_refused():
+    """Before anything is launched: strides, types, shapes, sizes."""
+    for prefix in (0, 32):
+        pool, d = both_forms("f16", [100, 60], prefix, 37)
+        bad = {name: torch.zeros(*d[name].shape[:-1], 2 * d[name].shape[-1], dtype=d[name].dtype, device="cuda")[..., ::2]
+               for name in ("q", "hk", "hv", "page_table", "Bk", "Bv", "seq_lens")}
+        bad["rope_table"] = d["rope_table"][:-16].clone()
+        for name, x in bad.items():
+            with pytest.raises(ValueError):
+                pool.call({**d, name: x})
+        for name in ("q", "hk", "Bv", "page_table", "seq_lens"):
+            for x in (d[name].float(), d[name][:1].clone()):
+                with pytest.raises(ValueError):
+                    pool.call({**d, name: x})
+        for kw in (dict(out=d["q"][:1].clone()), dict(out=torch.empty(2, 8, 256, dtype=torch.float16, device="cuda")[..., ::2])):
+            with pytest.raises(ValueError):
+                pool.call(d, **kw)
+        with pytest.raises(P.PaluError):
+            pool.call(d, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        hold(pool.call(d), pool.reference(), "f16")
