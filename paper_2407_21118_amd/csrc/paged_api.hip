@@ -227,7 +227,7 @@ int plan_paged_call(const palu_layer_desc* desc, int batch, int prefix, int max_
   for (int i = 0; i < p.n_cls; ++i) {
     long long wgs = 0;
     for (int k = 0; k < 2; ++k) wgs += (long long)p.cls[i].n_units * p.cls[i].n_row_blocks[k] * p.part[k].n_slots * p.part[k].seqs;
-    if (wgs > 0x7fffffffLL) return PALU_ERR_UNSUPPORTED;
+    if (wgs * kPagedThreads > 0xffffffffLL) return PALU_ERR_UNSUPPORTED;     // (what a launch takes)
   }
   return PALU_OK;
 }

@@ -71,3 +71,12 @@ def test_angle_tables_too_short(call):
     for table in (good()["rope_table"].view(torch.float32), torch.zeros(P.palu_rope_table_bytes(128, 500), dtype=torch.uint8)):
         with pytest.raises(ValueError, match="device"):
             call(**{**good(), "rope_table": table})
+
+
+def test_batches_of_more_work_items_than_a_launch_takes():
+    """A launch has fewer than 2^32 work items: 128 units of 65535 sequences and blocks of the prefix's rows are more, without these they are not."""
+    wide = P.LayerDesc(256, 128, [4 * j for j in range(65)], [512 * j for j in range(65)], [32 * j for j in range(65)])
+    with pytest.raises(P.PaluError) as e:
+        P.palu_attn_prefix_workspace_bytes(wide, 65535, 32, 64)
+    assert e.value.status == -2
+    assert P.palu_attn_paged_workspace_bytes(wide, 65535, 32) > 0
