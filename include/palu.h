@@ -471,7 +471,7 @@ int palu_attn_decode_staged(const palu_layer_desc* desc, int32_t batch, int32_t 
  *   hk, hv       DEVICE [n_pages, page_rows, R] act_dtype (quantized caches: PALU_ERR_UNSUPPORTED); page_rows is a power
  *                of two, n_pages * page_rows < 2^31
  *   page_table   DEVICE int32 [batch, table_stride].  Entries are clamped to [0, n_pages); those of pages
- *                without an attended row are not read
+ *                without an attended row are not read (for a shared prefix: see there)
  *   seq_lens     DEVICE int32 [batch], or NULL (all max_len).  0: an idle slot, whose output is zeros
  *   rope_table   as for palu_attn_decode; rope_table_len >= max_len
  *   out          DEVICE [batch, n_heads*q_per_kv, d_head] act_dtype (what the output projection takes)
@@ -502,8 +502,9 @@ int palu_attn_paged(const palu_layer_desc* desc, int32_t batch, int32_t max_len,
  * whole batch, and their keys are rebuilt once for all queries.  Rows from prefix_len on are each sequence's own,
  * through its own page table (of which entries for whole shared pages are not read; a page that the prefix ends
  * in is read from sequence 0's for rows before prefix_len, from the sequence's own for rows behind).  No window.
- * A sequence shorter than the prefix attends its first seq_lens[b] rows; the latents of shared rows have to be finite
- * numbers then (of rows that a sequence does not attend, zero times the latent enters its sum).
+ * All prefix_len shared rows are read whatever the lengths, also where sequence 0 is an idle slot: its page-table row goes
+ * on naming them.  A sequence shorter than the prefix attends its first seq_lens[b] rows; the latents of shared rows have
+ * to be finite numbers then (of rows that a sequence does not attend, zero times the latent enters its sum).
  *   prefix_len   0 <= prefix_len <= max_len
  * Everything else as for palu_attn_paged; workspace of palu_attn_prefix_workspace_bytes(...) bytes.
  */

@@ -199,3 +199,44 @@ def test_device_tensors_that_do_not_fit_are_refused():
         with pytest.raises(P.PaluError):
             pool.call(d, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
         hold(pool.call(d), pool.reference(), "f16")
+
+
+@pytest.mark.parametrize("entry,page", [(60, 59), (2 ** 31 - 1, 59), (-1, 0), (-2 ** 31, 0)])
+def test_page_entries_out_of_range_are_the_nearest_page(entry, page):
+    """Against the oracle over the rows of the first or the last page, which hold numbers of their own."""
+    pool = Pool(LAYERS["4x128"](), "f16", [300, 40, 0], 16, seed=38)
+    rng = np.random.default_rng(39)
+    pool.table = 1 + rng.permutation(58)[:57].reshape(3, 19).astype(np.int32)    # (not the first of the 60 pages, nor the last)
+    pool.put(0, 0)
+    for x in (pool.hk, pool.hv):
+        for p in (0, 59):
+            x[p] = synth.round_to(rng.standard_normal(x[p].shape), "f16")
+    pool.table[1, 1] = entry
+    d = pool.device()
+    got = pool.call(d)
+    pool.rows[1][16:32] = np.concatenate([pool.hk[page], pool.hv[page]], -1)
+    hold(got, pool.reference(), "f16")
+
+
+@pytest.mark.parametrize("batch", [3, 40])
+def test_the_first_slot_of_a_batch_idle_behind_its_prefix(batch):
+    """Sequence 0 has ended: its page table goes on naming the shared pages, its output is zeros, and the others' are as with it."""
+    pool, d = both_forms("f16", [290 + (7 * i) % 90 for i in range(batch)], 275, 40)
+    whole = pool.call(d)
+    d["seq_lens"][0] = 0
+    got = pool.call(d)
+    assert not got[0].any() and torch.equal(got[1:], whole[1:])
+    hold(whole, pool.reference(), "f16")
+
+
+def test_queries_of_one_sequence_behind_a_prefix():
+    """A speculative-decoding check: three entries each of two sequences, with one page-table row and lengths of their own."""
+    pool = Pool(LAYERS["4x128"](), "f16", [400, 400, 400, 330, 330, 330], 16, seed=41, prefix=300)
+    pool.put(0, 0)
+    d = pool.device()
+    d["page_table"][1:3], d["page_table"][4:] = d["page_table"][0], d["page_table"][3]
+    pool.rows[1] = pool.rows[2] = pool.rows[0]
+    pool.rows[4] = pool.rows[5] = pool.rows[3]
+    pool.lens = [400, 399, 398, 330, 329, 301]
+    d["seq_lens"] = torch.tensor(pool.lens, dtype=torch.int32, device="cuda")
+    hold(pool.call(d), pool.reference(), "f16")
