@@ -480,12 +480,13 @@ int palu_attn_decode_staged(const palu_layer_desc* desc, int32_t batch, int32_t 
  * Ranks up to PALU_PAGED_MAX_RANK.  q, hk, hv, B_k, B_v, table, out and workspace are 16-byte aligned.
  * Only attended rows are read: what lies in other rows, numbers or not, has no effect.
  *
- * Arithmetic.  Keys are rebuilt and rotated in float32.  Keys and queries enter the matrix instructions as pairs of
- * float16 numbers (2^-21 relative), probabilities as pairs of float16 (2^-21, or 2^-40 of the largest) or, in a
- * bfloat16 layer, of bfloat16 numbers (2^-16), so that the error is that of the output's rounding (2^-11, bfloat16
- * 2^-8).  Entries of rotated keys are right up to 5e5 in magnitude, of queries up to 6e4; beyond,
- * and where a query or an attended row is not finite, the head's output is NaN.  Sums, maxima and merged results are
- * float32.
+ * Arithmetic.  Keys are rebuilt and rotated in float32, by angles right to 1e-6.  Keys and queries enter the matrix
+ * instructions as pairs of float16 numbers (2^-21 relative; keys below 1 are right to 2^-22, queries below 1/8 to
+ * 2^-25), probabilities as pairs of float16 (2^-21, or 2^-40 of the largest) or, in a bfloat16 layer, of bfloat16 numbers
+ * (2^-16), and so do the merged latents before B_v (float16 below 1/8: 2^-25), so that the error is that of the output's
+ * rounding (2^-11, bfloat16 2^-8).  Entries of rotated keys are right up to 5e5 in magnitude, of queries up to 6e4;
+ * beyond, and where a query or an attended row is not finite, the head's output is NaN.  Sums, maxima and merged results
+ * are float32.
  */
 enum { PALU_PAGED_MAX_RANK = 512 };
 int palu_attn_paged_workspace_bytes(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window,

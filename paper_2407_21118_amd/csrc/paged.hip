@@ -15,23 +15,25 @@
 //           columns of eight tokens per lane: the transposition that the matrix operand wants is a byte permute).
 //   angles  of a tile's tokens, a 512th part by every lane, in LDS: all heads' keys are rotated by them.
 // One barrier per tile: in interval n are the keys of tile n, the softmax of n - 1 and the values of n - 2 (WHOLE), or two of them, one per
-// 16 tokens' keys, where LDS does not hold two tiles' scores, angles and probabilities.  With two, 16 sequences of 8192 rows took 400 us,
-// with one 362.  One wavefront of a SIMD begins with the keys, the other ends with them: the matrix instructions of one run beside
+// 16 tokens' keys, where LDS does not hold two tiles' scores, angles and probabilities.  With two, 16 sequences of 8192 rows take 390 us,
+// with one 374.  One wavefront of a SIMD begins with the keys, the other ends with them: the matrix instructions of one run beside
 // the vector instructions of the other.  Latents, page-table entries and the angles' anchors come by loads that write to LDS
 // directly, n_stages - 1 tiles ahead, counted and never drained while tiles follow: 5.3 TB/s at 2 us latency take 40 KB in flight
 // per compute unit.
 // What bounds it: rank 256 of 4 heads takes 2048 cycles of matrix instructions per SIMD and tile for the keys, about 400 for the scores, and
 // 500 vector instructions of 4 cycles; two wavefronts per SIMD leave half of either unused.  Measured, 32 heads in groups of 4, rank 256, float16:
-// 16 sequences of 8192 rows 362 us (3.0 TB/s; the loads alone 199 us); 8 sequences behind 16384 shared rows 79 us.
+// 16 sequences of 8192 rows 374 us (2.9 TB/s; the loads alone 199 us); 8 sequences behind 16384 shared rows 81 us.
 // Partial results (unnormalised sums, maxima, row sums) are merged, normalised and multiplied by B_v in paged_merge_kernel.
 //
 // Rotation.  The angle of position t0 + i is that of t0 plus that of i: a lane keeps cos and sin of two i < 16 and one pair, and those of
-// each 16 tokens' first position follow from those before.  Products of numbers that are right to 1e-7.  Rotated keys are made once for
-// all query rows; turning the queries of few rows to the tiles instead was no faster.
+// each 16 tokens' first position follow from those before.  These products are right to 8e-7 (PagedAngles), which moves a logit by as
+// much of sum(|q k|) / sqrt(d_h).  Rotated keys are made once for all query rows; turning the queries of few rows to the tiles instead
+// was no faster.
 // Rounding.  The matrix instructions take 16-bit operands.  The rotated keys and queries enter as pairs of float16 numbers hi + lo
-// (2^-21 relative), the probabilities as pairs of the latents' type (2^-21 or 2^-40 of the largest, bfloat16 2^-16), so that the error is that of the output's
-// rounding (2^-11, bfloat16 2^-8).  (One float16 number each for a bfloat16 layer's keys and queries left outputs 1.3e-3 from these in the
-// 2-norm, beside 1.66e-3 of rounding them.)  Keys are scaled by 1/8 and the queries by 8 (exact): magnitudes up to 524032 stay in range.
+// (2^-21 relative; the second has steps of 2^-24, so keys below 1 to 2^-22 and queries below 1/8 to 2^-25), the probabilities as pairs of
+// the latents' type (2^-21 or 2^-40 of the largest, bfloat16 2^-16), so that the error is that of the output's rounding (2^-11, bfloat16
+// 2^-8).  (One float16 number each for a bfloat16 layer's keys and queries left outputs 1.3e-3 from these in the 2-norm, beside 1.66e-3
+// of rounding them.)  Keys are scaled by 1/8 and the queries by 8 (exact): magnitudes up to 524032 stay in range.
 
 #include "paged_dev.h"
 

@@ -121,7 +121,7 @@ int plan_paged(const PagedMeta& m, PagedPlan* p) {
       if (!more) break;
     }
     // Query rows: 16 in all, or 16 per head and as many as accumulators go where there are more; as many blocks of them as it takes.
-    // (32 sequences behind 8192 rows, ranks 128 / 384: blocks of 32 packed rows 132 us, of 16 172; 8 sequences: one block 57, two 64.)
+    // (32 sequences behind 8192 rows, ranks 128 / 384: blocks of 32 packed rows 129 us, of 16 176; 8 sequences: one block 57, two 63.)
     for (const PagedPlanPart& t : p->part) c.form.many = c.form.many || (t.max_tiles > 0 && ks <= 8 && most * t.rows > 16);
     auto lds_bytes = [&](int stages) {
       return paged_lds(k_groups, ks, v_cols, c.max_packed, c.form.row_tiles(), c.form.parts(), stages).total;
@@ -149,7 +149,8 @@ int plan_paged(const PagedMeta& m, PagedPlan* p) {
     t.n_slots = 0;
   }
   // Tiles per workgroup: one workgroup is resident per compute unit, and its start and end cost about as much as four tiles (11 us; 24 sequences
-  // with a window of 1024: 103 us, priced at 2.5 tiles 117); a slot more is merged in a twentieth.  The two parts' workgroups run together: of equal length, or one part's halves or quarters of the other's.
+  // with a window of 1024: 100 us, priced at 2.5 tiles 114); a slot more is merged in a twentieth.  The two parts' workgroups run together: of equal
+  // length, or one part's halves or quarters of the other's.
   const int cus = device_cu_count();
   double best = 1e300;
   PagedPlanPart& own = p->part[kPagedOwn];
@@ -339,8 +340,8 @@ int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32
   e.n_shared = p.part[kPagedShared].n_slots;
   e.o_shared_stride = p.part[kPagedShared].o_stride;
   e.meta = m;
-  // rows of a head per workgroup: fewer until there are two workgroups per compute unit (48 grouped-query sequences: 119 us a call; until
-  // one 120, until four 126)
+  // rows of a head per workgroup: fewer until there are two workgroups per compute unit (48 grouped-query sequences: 118 us a call; until
+  // one 126, until four 132)
   int per_wg = 8;
   while (per_wg > 1 && (long long)ceil_div(batch * m.qpk, per_wg) * m.n_heads < 2 * device_cu_count()) per_wg /= 2;
   hipLaunchKernelGGL(desc->act_dtype == PALU_F16 ? paged_merge_form<F16>(per_wg) : paged_merge_form<BF16>(per_wg),

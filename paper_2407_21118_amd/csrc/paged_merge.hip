@@ -5,8 +5,9 @@
 namespace palu {
 
 // A workgroup takes R rows (sequence, query head) of one key/value head: weights exp2(max - largest max) of their partial results, the
-// weighted sums of the latents, normalised and split into pairs of 16-bit numbers hi + lo, times the head's 128 columns of B_v (a
-// wavefront makes 32; its weights are requested first, and arrive meanwhile).  grid (blocks of R rows, key/value heads), 256 threads.
+// weighted sums of the latents, normalised and split into pairs of 16-bit numbers hi + lo (float16: 2^-21, or 2^-25 absolute below
+// 1/8), times the head's 128 columns of B_v (a wavefront makes 32; its weights are requested first, and arrive meanwhile).
+// grid (blocks of R rows, key/value heads), 256 threads.
 // Bound by the latency of its few dependent steps where there are few rows, else by reading the partial results: R is as
 // small as it takes for a workgroup or two per compute unit.
 template <typename T, int R>
