@@ -477,7 +477,8 @@ int palu_attn_decode_staged(const palu_layer_desc* desc, int32_t batch, int32_t 
  *   out          DEVICE [batch, n_heads*q_per_kv, d_head] act_dtype (what the output projection takes)
  *   workspace    DEVICE, palu_attn_paged_workspace_bytes(...) bytes for the same desc, batch, max_len, window, n_sink.
  *                Calls sharing a workspace must be ordered on one stream
- * Ranks up to PALU_PAGED_MAX_RANK.  q, hk, hv, B_k, B_v, table, out and workspace are 16-byte aligned.
+ * Ranks up to PALU_PAGED_MAX_RANK, batch up to 65535 and max_len up to 2^30 (more: PALU_ERR_UNSUPPORTED, as is a call of 2^32
+ * work items in one launch).  q, hk, hv, B_k, B_v, table, out and workspace are 16-byte aligned.
  * Only attended rows are read: what lies in other rows, numbers or not, has no effect.
  *
  * Arithmetic.  Keys are rebuilt and rotated in float32, by angles right to 1e-6.  Keys and queries enter the matrix
