@@ -518,6 +518,70 @@ int palu_attn_prefix(const palu_layer_desc* desc, int32_t batch, int32_t prefix_
                      const void* Bk, const void* Bv, const void* rope_table, int32_t rope_table_len,
                      void* out, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Rows of a quantized latent cache: quantized as they are written, and read back.  Both sides in one launch; a cache of
+ * pages is its rows, page by page, so row t of sequence b is dst_row = page_table[b][t / page_rows]*page_rows + t % page_rows.
+ * Each side holds B = 4, 3 or 2 bits as its latent dtype says; a side that is not quantized takes no part (its arguments
+ * are not looked at; where neither is, PALU_ERR_INVALID_ARG).  float16 and bfloat16 layers.
+ *   palu_quant_latent_kv    the codes, scales and zero-points are those of palu_quant_latent
+ *   palu_dequant_latent_kv  (code - zero) * scale, rounded once to act_dtype
+ *   hk, hv        DEVICE act_dtype, latent row i at hk + i*hk_row_stride_elems, R contiguous elements, 2-byte aligned, any
+ *                 stride >= R (16-byte aligned rows are moved in wide pieces)
+ *   n_tok         latent rows, >= 0
+ *   *_codes       DEVICE uint8 [n_rows, R*B/8], 4-byte aligned, layouts as under palu_quant_latent
+ *   *_scale, *_zero   DEVICE float16 [n_rows, R/128]
+ *   n_rows        rows of either cache, < 2^31
+ *   dst_row, src_row  DEVICE int32 [n_tok]: the cache's row of latent row i, or NULL for row i.  Where it is not in [0, n_rows), as
+ *                 -1 for the padding of a batch, latent row i is left out: nothing of it is read or written.  Rows written
+ *                 in one call have to be distinct
+ */
+int palu_quant_latent_kv(const palu_layer_desc* desc, const void* hk, int64_t hk_row_stride_elems,
+                         const void* hv, int64_t hv_row_stride_elems, int64_t n_tok,
+                         uint8_t* k_codes, void* k_scale, void* k_zero, uint8_t* v_codes, void* v_scale, void* v_zero,
+                         int64_t n_rows, const int32_t* dst_row, void* stream);
+int palu_dequant_latent_kv(const palu_layer_desc* desc, const uint8_t* k_codes, const void* k_scale, const void* k_zero,
+                           const uint8_t* v_codes, const void* v_scale, const void* v_zero, int64_t n_rows,
+                           const int32_t* src_row, int64_t n_tok, void* hk, int64_t hk_row_stride_elems,
+                           void* hv, int64_t hv_row_stride_elems, void* stream);
+
+/*
+ * palu_encode_kv_t from weights held in 4 bits (h = x A of Sec. 3.1 for both sides): every latent channel's
+ * n_heads*q_per_kv*d_head weights are one row, quantized like a latent row (palu_quant_latent with a row of that many channels,
+ * or any other quantizer of the format): a weight is (code - zero) * scale, with one float16 scale and zero-point per 128
+ * inputs.  One launch, no workspace, one token or many.
+ *   x            DEVICE [n_tok, d] act_dtype, d = n_heads*q_per_kv*d_head, 16-byte aligned
+ *   Akt, Avt     DEVICE uint8 [R_k, d/2], [R_v, d/2], 16-byte aligned, even input in the low half of a byte
+ *   A*_scale, A*_zero   DEVICE float16 [R, d/128]
+ *   hk, hv       DEVICE act_dtype; token t is written to hk + dst_row[t]*hk_row_stride_elems, R elements (whatever the sides'
+ *                latent dtypes: the rows of a quantized cache are then written with palu_quant_latent_kv)
+ *   dst_row      DEVICE int32 [n_tok], or NULL for row t; tokens with a negative row are not written
+ *   n_tok        >= 0
+ * Products are exact, sums float32 (of 128 products, then scaled and added up), rounded once to act_dtype.
+ */
+int palu_encode_kv_w4(const palu_layer_desc* desc, const void* x, int32_t n_tok,
+                      const uint8_t* Akt, const void* Ak_scale, const void* Ak_zero,
+                      const uint8_t* Avt, const void* Av_scale, const void* Av_zero,
+                      void* hk, int64_t hk_row_stride_elems, void* hv, int64_t hv_row_stride_elems,
+                      const int32_t* dst_row, void* stream);
+
+/*
+ * palu_attn_paged over pages held in 4 bits: both sides PALU_I4 (other latent dtypes: PALU_ERR_UNSUPPORTED), float16 and
+ * bfloat16 layers.  Rows are written with palu_quant_latent_kv, palu_quant_latent or palu_encode_quant.
+ *   hk, hv       DEVICE uint8 [n_pages, page_rows, R/2], 16-byte aligned, layout as under palu_quant_latent
+ *   h*_scale, h*_zero   DEVICE float16 [n_pages, page_rows, R/128]
+ *   workspace    DEVICE, palu_attn_paged_quant_workspace_bytes(...) bytes for the same desc, batch, max_len, window, n_sink
+ * Everything else as for palu_attn_paged.  A row stands for (code - zero) * scale, unrounded.
+ */
+int palu_attn_paged_quant_workspace_bytes(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window,
+                                          int32_t n_sink, size_t* out_bytes);
+int palu_attn_paged_quant(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window, int32_t n_sink,
+                          const void* q, const int32_t* q_pos,
+                          const uint8_t* hk, const void* hk_scale, const void* hk_zero,
+                          const uint8_t* hv, const void* hv_scale, const void* hv_zero, int32_t n_pages, int32_t page_rows,
+                          const int32_t* page_table, int32_t table_stride, const int32_t* seq_lens,
+                          const void* Bk, const void* Bv, const void* rope_table, int32_t rope_table_len,
+                          void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -50,8 +50,9 @@ int device_cu_count() {
 inline int latent_bits(int dtype) { return dtype == PALU_I4 ? 4 : (dtype == PALU_I3 ? 3 : (dtype == PALU_I2 ? 2 : 0)); }
 
 // ---- descriptor validation -------------------------------------------------
-// nq: queries per sequence of the call; the kernels then see q_per_kv * nq heads per key/value head
-int check_desc(const palu_layer_desc* d, Meta* m, int nq = 1) {
+// nq: queries per sequence of the call; the kernels then see q_per_kv * nq heads per key/value head; quantized_bf16: for calls that
+// take quantized latents of bfloat16 layers too
+int check_desc(const palu_layer_desc* d, Meta* m, int nq = 1, bool quantized_bf16 = false) {
   if (!d || !d->group_head_off || !d->k_rank_off || !d->v_rank_off) return PALU_ERR_INVALID_ARG;
   if (d->n_heads <= 0 || d->n_groups <= 0 || d->d_head <= 0) return PALU_ERR_INVALID_ARG;
   if (d->act_dtype != PALU_F16 && d->act_dtype != PALU_BF16) return PALU_ERR_INVALID_ARG;
@@ -84,7 +85,7 @@ int check_desc(const palu_layer_desc* d, Meta* m, int nq = 1) {
   // limits of this build
   if (d->d_head != PALU_D_HEAD) return PALU_ERR_UNSUPPORTED;
   if (d->n_heads > PALU_MAX_HEADS / qpk || d->n_groups > PALU_MAX_GROUPS) return PALU_ERR_UNSUPPORTED;
-  if (any_i4 && (d->quant_block != 128 || d->act_dtype != PALU_F16)) return PALU_ERR_UNSUPPORTED;
+  if (any_i4 && (d->quant_block != 128 || (d->act_dtype != PALU_F16 && !quantized_bf16))) return PALU_ERR_UNSUPPORTED;
   for (int j = 0; j < d->n_groups; ++j) {
     if (d->k_rank_off[j + 1] - d->k_rank_off[j] > PALU_MAX_RANK) return PALU_ERR_UNSUPPORTED;
     if (d->v_rank_off[j + 1] - d->v_rank_off[j] > PALU_MAX_RANK) return PALU_ERR_UNSUPPORTED;
@@ -2035,3 +2036,4 @@ int palu_decode_step_t(const palu_layer_desc* desc, int32_t batch, int32_t seq_l
 }  // extern "C"
 
 #include "paged_api.hip"
+#include "quant_api.hip"

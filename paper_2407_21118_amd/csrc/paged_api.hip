@@ -26,11 +26,13 @@ struct PagedPlan {
   PagedClass cls[kPagedMaxClasses];
 };
 
-int check_paged_desc(const palu_layer_desc* desc, PagedMeta* pm) {
+// quantized: both sides are held in 4 bits, else neither is quantized
+int check_paged_desc(const palu_layer_desc* desc, PagedMeta* pm, bool quantized = false) {
   Meta m;
-  const int st = check_desc(desc, &m);
+  const int st = check_desc(desc, &m, 1, quantized);
   if (st != PALU_OK) return st;
-  if (latent_bits(desc->k_latent_dtype) || latent_bits(desc->v_latent_dtype)) return PALU_ERR_UNSUPPORTED;
+  for (const int dtype : {desc->k_latent_dtype, desc->v_latent_dtype})
+    if (latent_bits(dtype) != (quantized ? 4 : 0)) return PALU_ERR_UNSUPPORTED;
   std::memset(pm, 0, sizeof(*pm));
   pm->n_heads = desc->n_heads;
   pm->n_groups = desc->n_groups;
@@ -262,6 +264,17 @@ int launch_paged(const PagedPlan& p, const PagedArgs& args, int act, hipStream_t
   return PALU_OK;
 }
 
+int launch_paged_merge(const PagedMergeArgs& e, int act, hipStream_t s) {
+  const int rows = e.batch * e.meta.qpk;
+  // rows of a head per workgroup: fewer until there are two workgroups per compute unit (48 grouped-query sequences: 118 us a call; until
+  // one 126, until four 132)
+  int per_wg = 8;
+  while (per_wg > 1 && (long long)ceil_div(rows, per_wg) * e.meta.n_heads < 2 * device_cu_count()) per_wg /= 2;
+  hipLaunchKernelGGL(act == PALU_F16 ? paged_merge_form<F16>(per_wg) : paged_merge_form<BF16>(per_wg),
+                     dim3((unsigned)ceil_div(rows, per_wg), (unsigned)e.meta.n_heads), dim3(256), 0, s, e);
+  return launch_ok();
+}
+
 int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32_t max_len, int32_t window, int32_t n_sink,
                const void* q, const int32_t* q_pos, const void* hk, const void* hv, int32_t n_pages, int32_t page_rows,
                const int32_t* page_table, int32_t table_stride, const int32_t* seq_lens, const void* Bk, const void* Bv,
@@ -340,13 +353,7 @@ int paged_impl(const palu_layer_desc* desc, int32_t batch, int32_t prefix, int32
   e.n_shared = p.part[kPagedShared].n_slots;
   e.o_shared_stride = p.part[kPagedShared].o_stride;
   e.meta = m;
-  // rows of a head per workgroup: fewer until there are two workgroups per compute unit (48 grouped-query sequences: 118 us a call; until
-  // one 126, until four 132)
-  int per_wg = 8;
-  while (per_wg > 1 && (long long)ceil_div(batch * m.qpk, per_wg) * m.n_heads < 2 * device_cu_count()) per_wg /= 2;
-  hipLaunchKernelGGL(desc->act_dtype == PALU_F16 ? paged_merge_form<F16>(per_wg) : paged_merge_form<BF16>(per_wg),
-                     dim3((unsigned)ceil_div(batch * m.qpk, per_wg), (unsigned)m.n_heads), dim3(256), 0, s, e);
-  return launch_ok();
+  return launch_paged_merge(e, desc->act_dtype, s);
 }
 
 }  // namespace

@@ -1,0 +1,200 @@
+// Host side of what a layer with a 4-bit paged cache and 4-bit projections takes beside the other entry points: rows quantized and read
+// back, the projection, attention (part of the translation unit api.hip).
+
+#include "cache_rows.h"
+#include "encode_w4.h"
+#include "pagedq.h"
+
+namespace {
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+int cache_rows_impl(const palu_layer_desc* desc, bool quantize, const void* hk, int64_t hk_stride, const void* hv, int64_t hv_stride, int64_t n_tok,
+                    const uint8_t* k_codes, const void* k_scale, const void* k_zero, const uint8_t* v_codes, const void* v_scale,
+                    const void* v_zero, int64_t n_rows, const int32_t* row, void* stream) {
+  Meta m;
+  const int st = check_desc(desc, &m, 1, true);
+  if (st != PALU_OK) return st;
+  if (n_tok < 0 || n_rows <= 0 || n_rows > 0x7fffffffLL || !aligned(row, 4)) return PALU_ERR_INVALID_ARG;
+  CacheRowsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  bool wide = true;
+  for (int s = 0; s < 2; ++s) {
+    const int bits = latent_bits(s ? desc->v_latent_dtype : desc->k_latent_dtype);
+    if (bits == 0) continue;
+    const int R = s ? m.v_off[m.n_groups] : m.k_off[m.n_groups];
+    const void *latent = s ? hv : hk, *codes = s ? v_codes : k_codes, *scale = s ? v_scale : k_scale, *zero = s ? v_zero : k_zero;
+    const int64_t stride = s ? hv_stride : hk_stride;
+    if ((!latent && n_tok > 0) || !codes || !scale || !zero || stride < R) return PALU_ERR_INVALID_ARG;   // (of no rows: whatever stands for them)
+    if (!aligned(latent, 2) || !aligned(codes, 4) || !aligned(scale, 2) || !aligned(zero, 2)) return PALU_ERR_INVALID_ARG;
+    wide = wide && aligned(latent, 16) && stride % 8 == 0;
+    a.side[s] = CacheSide{(uint16_t*)latent, (uint8_t*)codes, (uint16_t*)scale, (uint16_t*)zero, stride, R / 128, bits};
+  }
+  if (a.side[0].n_blocks + a.side[1].n_blocks == 0) return PALU_ERR_INVALID_ARG;
+  if (n_tok == 0) return PALU_OK;
+  a.row = row;
+  a.n = n_tok;
+  a.n_rows = n_rows;
+  const long long items = n_tok > (1LL << 32) ? 1LL << 62 : (long long)n_tok * (a.side[0].n_blocks + a.side[1].n_blocks);
+  if (items > (0xffffffffLL - 2 * kCacheRowsThreads) / 16) return PALU_ERR_UNSUPPORTED;      // work items of a launch
+  hipLaunchKernelGGL(cache_rows_form(desc->act_dtype, quantize, wide), dim3((unsigned)((items + kCacheRowsItems - 1) / kCacheRowsItems)),
+                     dim3(kCacheRowsThreads), 0, static_cast<hipStream_t>(stream), a);
+  return launch_ok();
+}
+
+struct PagedQCall {
+  PagedMeta meta;
+  int n_sink, max_tiles, chunk_tiles, n_slots;
+  long long o_stride;
+  size_t ml_at, total;
+};
+
+int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window, int n_sink, PagedQCall* c) {
+  int st = check_paged_desc(desc, &c->meta, true);
+  if (st != PALU_OK) return st;
+  if (batch <= 0 || max_len <= 0 || window < 0 || n_sink < 0) return PALU_ERR_INVALID_ARG;
+  if (batch > 65535 || max_len > (1 << 30)) return PALU_ERR_UNSUPPORTED;
+  c->n_sink = window > 0 ? n_sink : 0;
+  c->max_tiles = paged_max_tiles(max_len, 0, window, c->n_sink);
+  const PagedMeta& m = c->meta;
+  long long sum_rv = 0;
+  for (int j = 0; j < m.n_groups; ++j) sum_rv += (long long)(m.head_off[j + 1] - m.head_off[j]) * (m.v_off[j + 1] - m.v_off[j]);
+  c->o_stride = sum_rv * m.qpk;
+  const long long wgs = (long long)batch * m.n_heads;
+  const int slots = (int)std::max<long long>(1, std::min<long long>(c->max_tiles, 4LL * device_cu_count() / wgs));
+  c->chunk_tiles = ceil_div(c->max_tiles, slots);
+  c->n_slots = ceil_div(c->max_tiles, c->chunk_tiles);
+  c->ml_at = align_up((size_t)batch * c->n_slots * c->o_stride * sizeof(float));
+  c->total = c->ml_at + align_up((size_t)batch * c->n_slots * m.qpk * m.n_heads * 2 * sizeof(float));
+  if (wgs * c->n_slots * kPagedQThreads > 0xffffffffLL) return PALU_ERR_UNSUPPORTED;
+  return PALU_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int palu_quant_latent_kv(const palu_layer_desc* desc, const void* hk, int64_t hk_row_stride_elems, const void* hv, int64_t hv_row_stride_elems,
+                         int64_t n_tok, uint8_t* k_codes, void* k_scale, void* k_zero, uint8_t* v_codes, void* v_scale, void* v_zero,
+                         int64_t n_rows, const int32_t* dst_row, void* stream) {
+  return cache_rows_impl(desc, true, hk, hk_row_stride_elems, hv, hv_row_stride_elems, n_tok, k_codes, k_scale, k_zero, v_codes, v_scale,
+                         v_zero, n_rows, dst_row, stream);
+}
+
+int palu_dequant_latent_kv(const palu_layer_desc* desc, const uint8_t* k_codes, const void* k_scale, const void* k_zero, const uint8_t* v_codes,
+                           const void* v_scale, const void* v_zero, int64_t n_rows, const int32_t* src_row, int64_t n_tok, void* hk,
+                           int64_t hk_row_stride_elems, void* hv, int64_t hv_row_stride_elems, void* stream) {
+  return cache_rows_impl(desc, false, hk, hk_row_stride_elems, hv, hv_row_stride_elems, n_tok, k_codes, k_scale, k_zero, v_codes, v_scale,
+                         v_zero, n_rows, src_row, stream);
+}
+
+int palu_encode_kv_w4(const palu_layer_desc* desc, const void* x, int32_t n_tok, const uint8_t* Akt, const void* Ak_scale, const void* Ak_zero,
+                      const uint8_t* Avt, const void* Av_scale, const void* Av_zero, void* hk, int64_t hk_row_stride_elems, void* hv,
+                      int64_t hv_row_stride_elems, const int32_t* dst_row, void* stream) {
+  Meta m;
+  const int st = check_desc(desc, &m, 1, true);
+  if (st != PALU_OK) return st;
+  if (n_tok < 0 || !Akt || !Ak_scale || !Ak_zero || !Avt || !Av_scale || !Av_zero) return PALU_ERR_INVALID_ARG;
+  if (n_tok > 0 && (!x || !hk || !hv)) return PALU_ERR_INVALID_ARG;            // (of no tokens: whatever stands for them)
+  if (!aligned(x, 16) || !aligned(Akt, 16) || !aligned(Avt, 16) || !aligned(dst_row, 4)) return PALU_ERR_INVALID_ARG;
+  for (const void* p : {Ak_scale, Ak_zero, Av_scale, Av_zero, (const void*)hk, (const void*)hv})
+    if (!aligned(p, 2)) return PALU_ERR_INVALID_ARG;
+  const int Rk = m.k_off[m.n_groups], Rv = m.v_off[m.n_groups];
+  if (hk_row_stride_elems < Rk || hv_row_stride_elems < Rv) return PALU_ERR_INVALID_ARG;
+  if (n_tok == 0) return PALU_OK;
+  EncodeW4Args a;
+  std::memset(&a, 0, sizeof(a));
+  a.side[0] = EncodeW4Side{Akt, (const uint16_t*)Ak_scale, (const uint16_t*)Ak_zero, (uint16_t*)hk, hk_row_stride_elems, Rk / 16};
+  a.side[1] = EncodeW4Side{Avt, (const uint16_t*)Av_scale, (const uint16_t*)Av_zero, (uint16_t*)hv, hv_row_stride_elems, Rv / 16};
+  a.x = static_cast<const uint16_t*>(x);
+  a.dst_row = dst_row;
+  a.n_tok = n_tok;
+  a.d = m.n_heads * PALU_D_HEAD;
+  const int tiles = n_tok <= 16 ? 1 : (n_tok <= 32 ? 2 : 4), blocks = ceil_div(n_tok, 16 * tiles);
+  if (blocks > 65535) return PALU_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL(encode_w4_form(desc->act_dtype, tiles), dim3((unsigned)(a.side[0].tiles + a.side[1].tiles), (unsigned)blocks),
+                     dim3(kW4Threads), 0, static_cast<hipStream_t>(stream), a);
+  return launch_ok();
+}
+
+int palu_attn_paged_quant_workspace_bytes(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window, int32_t n_sink,
+                                          size_t* out_bytes) {
+  PagedQCall c;
+  const int st = plan_pagedq(desc, batch, max_len, window, n_sink, &c);
+  if (st != PALU_OK) return st;
+  if (!out_bytes) return PALU_ERR_INVALID_ARG;
+  *out_bytes = c.total;
+  return PALU_OK;
+}
+
+int palu_attn_paged_quant(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window, int32_t n_sink,
+                          const void* q, const int32_t* q_pos, const uint8_t* hk, const void* hk_scale, const void* hk_zero,
+                          const uint8_t* hv, const void* hv_scale, const void* hv_zero, int32_t n_pages, int32_t page_rows,
+                          const int32_t* page_table, int32_t table_stride, const int32_t* seq_lens, const void* Bk, const void* Bv,
+                          const void* rope_table, int32_t rope_table_len, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  PagedQCall c;
+  int st = plan_pagedq(desc, batch, max_len, window, n_sink, &c);
+  if (st != PALU_OK) return st;
+  if (!q || !hk || !hk_scale || !hk_zero || !hv || !hv_scale || !hv_zero || !page_table || !Bk || !Bv || !rope_table || !out || !workspace)
+    return PALU_ERR_INVALID_ARG;
+  if (n_pages <= 0 || page_rows <= 0 || table_stride <= 0) return PALU_ERR_INVALID_ARG;
+  if ((long long)table_stride * page_rows < max_len || rope_table_len < max_len) return PALU_ERR_INVALID_ARG;
+  for (const void* x : {q, (const void*)hk, (const void*)hv, Bk, Bv, rope_table, (const void*)out, (const void*)workspace})
+    if (!aligned(x, 16)) return PALU_ERR_INVALID_ARG;
+  for (const void* x : {(const void*)q_pos, (const void*)page_table, (const void*)seq_lens})
+    if (!aligned(x, 4)) return PALU_ERR_INVALID_ARG;
+  for (const void* x : {hk_scale, hk_zero, hv_scale, hv_zero})
+    if (!aligned(x, 2)) return PALU_ERR_INVALID_ARG;
+  if ((page_rows & (page_rows - 1)) != 0 || (long long)n_pages * page_rows > 0x7fffffffLL) return PALU_ERR_UNSUPPORTED;
+  if (workspace_bytes < c.total) return PALU_ERR_WORKSPACE_TOO_SMALL;
+
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const PagedMeta& m = c.meta;
+  PagedQArgs a;
+  std::memset(&a, 0, sizeof(a));
+  const int Rk = m.k_off[m.n_groups], Rv = m.v_off[m.n_groups];
+  a.k = PagedQSide{hk, (const uint16_t*)hk_scale, (const uint16_t*)hk_zero, Rk / 2, Rk / 128};
+  a.v = PagedQSide{hv, (const uint16_t*)hv_scale, (const uint16_t*)hv_zero, Rv / 2, Rv / 128};
+  a.q = static_cast<const uint16_t*>(q);
+  a.Bk = static_cast<const uint16_t*>(Bk);
+  a.rope = static_cast<const float*>(rope_table);
+  a.q_pos = q_pos;
+  a.page_table = page_table;
+  a.seq_lens = seq_lens;
+  a.o_part = reinterpret_cast<float*>(ws);
+  a.ml_part = reinterpret_cast<float*>(ws + c.ml_at);
+  a.o_stride = c.o_stride;
+  a.n_pages = n_pages;
+  a.page_shift = __builtin_ctz((unsigned)page_rows);
+  a.table_stride = table_stride;
+  a.rope_len = rope_table_len;
+  a.max_len = max_len;
+  a.window = window;
+  a.n_sink = c.n_sink;
+  a.chunk_tiles = c.chunk_tiles;
+  a.n_slots = c.n_slots;
+  a.scale = (float)(1.4426950408889634 / std::sqrt((double)PALU_D_HEAD));
+  a.meta = m;
+  hipLaunchKernelGGL(pagedq_plain_form(desc->act_dtype), dim3((unsigned)(batch * c.n_slots * m.n_heads)), dim3(kPagedQThreads), 0, s, a);
+  if ((st = launch_ok()) != PALU_OK) return st;
+
+  PagedMergeArgs e;
+  std::memset(&e, 0, sizeof(e));
+  e.o_part = a.o_part;
+  e.ml_part = a.ml_part;
+  e.Bv = static_cast<const uint16_t*>(Bv);
+  e.seq_lens = seq_lens;
+  e.out = static_cast<uint16_t*>(out);
+  e.max_len = max_len;
+  e.window = window;
+  e.n_sink = c.n_sink;
+  e.batch = batch;
+  e.chunk_tiles = c.chunk_tiles;
+  e.n_slots = c.n_slots;
+  e.o_stride = c.o_stride;
+  e.meta = m;
+  return launch_paged_merge(e, desc->act_dtype, s);
+}
+
+}  // extern "C"
