@@ -42,12 +42,30 @@ int cache_rows_impl(const palu_layer_desc* desc, bool quantize, const void* hk, 
   return launch_ok();
 }
 
+// Units that one launch takes: key/value heads whose keys have the same form.
+struct PagedQClass {
+  PagedQForm form;
+  int lds_bytes, n_units;
+  PagedUnit units[PALU_MAX_HEADS];
+};
 struct PagedQCall {
   PagedMeta meta;
   int n_sink, max_tiles, chunk_tiles, n_slots;
+  int span_steps;                              // 0: the plain kernel
+  int n_cls, n_row_blocks;
+  PagedQClass cls[3];                          // key ranks 128, 256, above
   long long o_stride;
   size_t ml_at, total;
 };
+
+// The largest span over which the folded pairs, of which the fastest turns theta^(-1/2) a position, turn by 1.3 radians either way from its middle
+// (their polynomials of degree 7 are then right to 2e-6); 0: not even one step's
+int pagedq_span_steps(float theta) {
+  const double w = theta > 0.f ? 1.0 / std::sqrt((double)theta) : 0.0;
+  for (int steps = kPagedQSpan / kPagedQStep; steps > 0; steps /= 2)
+    if (w * (0.5 * kPagedQStep * steps) <= 1.3) return steps;
+  return 0;
+}
 
 int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window, int n_sink, PagedQCall* c) {
   int st = check_paged_desc(desc, &c->meta, true);
@@ -57,16 +75,66 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
   c->n_sink = window > 0 ? n_sink : 0;
   c->max_tiles = paged_max_tiles(max_len, 0, window, c->n_sink);
   const PagedMeta& m = c->meta;
-  long long sum_rv = 0;
-  for (int j = 0; j < m.n_groups; ++j) sum_rv += (long long)(m.head_off[j + 1] - m.head_off[j]) * (m.v_off[j + 1] - m.v_off[j]);
+  auto rk = [&](int j) { return m.k_off[j + 1] - m.k_off[j]; };
+  auto rv = [&](int j) { return m.v_off[j + 1] - m.v_off[j]; };
+  auto heads = [&](int j) { return m.head_off[j + 1] - m.head_off[j]; };
+  long long sum_rv = 0, units = 0;
+  for (int j = 0; j < m.n_groups; ++j) sum_rv += (long long)heads(j) * rv(j);
   c->o_stride = sum_rv * m.qpk;
-  const long long wgs = (long long)batch * m.n_heads;
-  const int slots = (int)std::max<long long>(1, std::min<long long>(c->max_tiles, 4LL * device_cu_count() / wgs));
-  c->chunk_tiles = ceil_div(c->max_tiles, slots);
+  c->span_steps = pagedq_span_steps(desc->rope_theta);
+  c->n_cls = 0;
+  const int rows = m.qpk <= 2 ? m.qpk : 4;
+  c->n_row_blocks = ceil_div(m.qpk, rows);
+  for (int k = 0; k < 3 && c->span_steps > 0; ++k) {
+    auto in_class = [&](int j) { return k == 2 ? rk(j) > 256 : rk(j) == 128 * (k + 1); };
+    PagedQClass& cl = c->cls[c->n_cls];
+    cl.form = PagedQForm{k == 0 ? 4 : 8, k == 2 ? 2 : 1, rows};
+    cl.n_units = cl.lds_bytes = 0;
+    const int unit_heads = 4 / cl.form.slices;
+    for (int first = 0;; first += unit_heads) {              // as for unquantized latents: whole adjacent groups side by side, or parts of one
+      bool more = false;
+      for (int j = 0; j < m.n_groups; ++j) {
+        if (!in_class(j) || first >= heads(j)) continue;
+        int n = 1;
+        while (j + n < m.n_groups && rk(j + n) == rk(j) && rv(j + n) == rv(j) && heads(j + n) == heads(j) && (n + 1) * heads(j) <= unit_heads &&
+               (n + 1) * rk(j) <= 256 && (n + 1) * rv(j) <= 256)
+          ++n;
+        more = true;
+        const int nh = std::min(unit_heads, n * heads(j) - first);
+        cl.units[cl.n_units++].bits = (uint32_t)(m.head_off[j] + first) | (uint32_t)nh << 8 | (uint32_t)j << 16 | (uint32_t)n << 24;
+        cl.lds_bytes = std::max(cl.lds_bytes, pagedq_lds(n * rk(j), n * rv(j), cl.form.slices, rows).total);
+        j += n - 1;
+      }
+      if (!more) break;
+    }
+    if (cl.n_units == 0) continue;
+    if (cl.lds_bytes > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;
+    units += cl.n_units;
+    ++c->n_cls;
+  }
+  const int cus = device_cu_count();
+  if (c->span_steps == 0) {
+    const long long wgs = (long long)batch * m.n_heads;
+    const int slots = (int)std::max<long long>(1, std::min<long long>(c->max_tiles, 4LL * cus / wgs));
+    c->chunk_tiles = ceil_div(c->max_tiles, slots);
+  } else {
+    // Tiles per workgroup: one is resident per compute unit; its start and end are priced as eight tiles, a slot more is merged in a twentieth
+    const long long wgs = (long long)batch * units * c->n_row_blocks;
+    const long long most = std::min<long long>(1024, std::max<long long>(16, 4LL * cus / wgs));
+    double best = 1e300;
+    for (int n = 1; n <= std::min<long long>(ceil_div(c->max_tiles, 2), most); ++n) {
+      const int tiles = ceil_div(ceil_div(c->max_tiles, n), 2) * 2, used = ceil_div(c->max_tiles, tiles);
+      const double cost = paged_makespan(wgs * used, 8.0 + tiles, 0, 8.0 + tiles, cus) + 0.05 * used;
+      if (cost >= best) continue;
+      best = cost;
+      c->chunk_tiles = tiles;
+    }
+  }
   c->n_slots = ceil_div(c->max_tiles, c->chunk_tiles);
   c->ml_at = align_up((size_t)batch * c->n_slots * c->o_stride * sizeof(float));
   c->total = c->ml_at + align_up((size_t)batch * c->n_slots * m.qpk * m.n_heads * 2 * sizeof(float));
-  if (wgs * c->n_slots * kPagedQThreads > 0xffffffffLL) return PALU_ERR_UNSUPPORTED;
+  const long long launched = (long long)batch * c->n_slots * (c->span_steps ? units * c->n_row_blocks : m.n_heads);
+  if (launched * kPagedQThreads > 0xffffffffLL) return PALU_ERR_UNSUPPORTED;
   return PALU_OK;
 }
 
@@ -176,8 +244,23 @@ int palu_attn_paged_quant(const palu_layer_desc* desc, int32_t batch, int32_t ma
   a.n_slots = c.n_slots;
   a.scale = (float)(1.4426950408889634 / std::sqrt((double)PALU_D_HEAD));
   a.meta = m;
-  hipLaunchKernelGGL(pagedq_plain_form(desc->act_dtype), dim3((unsigned)(batch * c.n_slots * m.n_heads)), dim3(kPagedQThreads), 0, s, a);
-  if ((st = launch_ok()) != PALU_OK) return st;
+  if (c.span_steps == 0) {
+    hipLaunchKernelGGL(pagedq_plain_form(desc->act_dtype), dim3((unsigned)(batch * c.n_slots * m.n_heads)), dim3(kPagedQThreads), 0, s, a);
+    if ((st = launch_ok()) != PALU_OK) return st;
+  }
+  a.span_steps = c.span_steps;
+  a.n_row_blocks = c.n_row_blocks;
+  for (int i = 0; i < kDHead / 2 - kPagedQLow; ++i)
+    a.w_low[i] = desc->rope_theta > 0.f ? (float)std::pow((double)desc->rope_theta, -2.0 * (kPagedQLow + i) / kDHead) : 0.f;
+  for (int k = 0; k < c.n_cls; ++k) {
+    const PagedQClass& cl = c.cls[k];
+    const PagedQFn fn = pagedq_form(desc->act_dtype, cl.form);
+    if ((st = allow_lds(fn, (size_t)cl.lds_bytes)) != PALU_OK) return st;
+    a.n_units = cl.n_units;
+    std::memcpy(a.units, cl.units, sizeof(PagedUnit) * cl.n_units);
+    hipLaunchKernelGGL(fn, dim3((unsigned)((long long)batch * c.n_slots * c.n_row_blocks * cl.n_units)), dim3(kPagedQThreads), (unsigned)cl.lds_bytes, s, a);
+    if ((st = launch_ok()) != PALU_OK) return st;
+  }
 
   PagedMergeArgs e;
   std::memset(&e, 0, sizeof(e));
