@@ -32,7 +32,7 @@ FLAT = ["-DPALU_SCORE_FLAT=1"]
 
 def sources():
     """(source file, extra flags, object name) of every translation unit."""
-    vgpr = ["score16_shared_forms.hip", "score_forms.hip", "score_forms_lowbit.hip", "score16_forms.hip", "pv.hip", "api.hip", "paged_merge.hip", "pagedq.hip", "pagedq_fold.hip"]
+    vgpr = ["score16_shared_forms.hip", "score_forms.hip", "score_forms_lowbit.hip", "score16_forms.hip", "pv.hip", "api.hip", "paged_merge.hip", "pagedq.hip"]
     units = [(f, VGPR_FORM, "") for f in vgpr]
     units += [(f, VGPR_FORM + FLAT, "_flat") for f in ("score16_shared_forms.hip", "score16_forms.hip")]
     units += [("attend16_forms.hip", VGPR_FORM, ""), ("attend16_forms.hip", VGPR_FORM + FLAT, "_flat"), ("attend16_forms.hip", VGPR_FORM + ["-DPALU_ATTEND_SHARED=1"], "_shared"),
@@ -40,6 +40,8 @@ def sources():
     units += [("attend16_mixed_forms.hip", VGPR_FORM, "")]
     for act, suffix in (("F16", ""), ("BF16", "_bf16")):
         units += [("paged.hip", VGPR_FORM + ["-DPALU_PAGED_ACT=" + act], suffix)]
+    # (several query rows: more registers than there are ordinary ones, so accumulators take the accumulation registers too)
+    units += [("pagedq_fold.hip", (VGPR_FORM if rows == 1 else VGPR_FORM[2:]) + ["-DPALU_PAGEDQ_ROWS=%d" % rows], "_%d" % rows) for rows in (1, 2, 4)]
     units += [(f, [], "") for f in ("encode_gemm.hip", "cache_rows.hip", "encode_w4.hip")]
     return [(os.path.join(CSRC, f), extra, os.path.splitext(f)[0] + suffix + ".o") for f, extra, suffix in units]
 

@@ -42,11 +42,18 @@ using PagedQFn = void (*)(PagedQArgs);
 constexpr int kPagedQThreads = 256;
 PagedQFn pagedq_plain_form(int act);
 // The instantiations, by ks: steps of 32 key channels of a wavefront, 4 or 8; slices: wavefronts that share a head's channels (2: ranks above
-// 256); rows: query rows of a head, 1, 2 or 4
+// 256); rows: query rows of a head, 1, 2 or 4; piped: several steps at work at once, where LDS holds what that takes
 struct PagedQForm {
   int ks, slices, rows;
+  bool piped;
 };
-PagedQFn pagedq_form(int act, const PagedQForm& f);
+template <int ROWS> PagedQFn pagedq_rows_form(int act, const PagedQForm& f);
+template <> PagedQFn pagedq_rows_form<1>(int, const PagedQForm&);
+template <> PagedQFn pagedq_rows_form<2>(int, const PagedQForm&);
+template <> PagedQFn pagedq_rows_form<4>(int, const PagedQForm&);
+inline PagedQFn pagedq_form(int act, const PagedQForm& f) {
+  return f.rows == 1 ? pagedq_rows_form<1>(act, f) : (f.rows == 2 ? pagedq_rows_form<2>(act, f) : pagedq_rows_form<4>(act, f));
+}
 
 // LDS of a workgroup, in bytes from its start
 struct PagedQLds {
@@ -55,9 +62,9 @@ struct PagedQLds {
   int k, raw, v, p, p_cb, p_size, alpha, k_tok, v_tok, basis, anchors, rows, scores, flags, total;
 };
 constexpr int kPagedQProbPitch = kPagedQStep * 2 + 16;
-__host__ __device__ __forceinline__ PagedQLds pagedq_lds(int k_cols, int v_cols, int slices, int rows) {
+__host__ __device__ __forceinline__ PagedQLds pagedq_lds(int k_cols, int v_cols, int slices, int rows, bool piped) {
   PagedQLds l;
-  const int blocks = v_cols / 128, bufs = slices == 1 ? 2 : 1, p_rows = rows == 1 ? 8 : (slices == 1 ? 32 : 16);
+  const int blocks = v_cols / 128, bufs = piped ? 2 : 1, p_rows = rows == 1 ? 8 : (slices == 1 ? 32 : 16);
   l.k_pitch = k_cols * 2;
   l.k_size = kPagedQStep * l.k_pitch;
   l.raw_size = kPagedQStep * k_cols / 2;
@@ -65,13 +72,13 @@ __host__ __device__ __forceinline__ PagedQLds pagedq_lds(int k_cols, int v_cols,
   l.k = 0;
   l.raw = l.k + bufs * l.k_size;
   l.v = l.raw + bufs * l.raw_size;
-  l.p = l.v + (slices == 1 ? 3 : 2) * l.v_size;
+  l.p = l.v + (piped ? 3 : 2) * l.v_size;
   l.p_cb = p_rows * kPagedQProbPitch;          // probabilities of a block of value columns
   l.p_size = blocks * l.p_cb;
   l.alpha = l.p + 2 * l.p_size;                // [2][blocks][16]
-  l.k_tok = l.alpha + 2 * blocks * 16 * 4;     // [2][2][64]: ratio and scale, by slice or group; [2][4][64]: what is left of the zero-points
-  l.v_tok = l.k_tok + 2 * kPagedQStep * (2 * 8 + 4 * 4);
-  l.basis = l.v_tok + 2 * blocks * kPagedQStep * 8;    // [2][blocks][64]: scale, zero-point
+  l.k_tok = l.alpha + 2 * blocks * 16 * 4;     // [4][2][64]: ratio and scale, by slice or group; [2][4][64]: what is left of the zero-points
+  l.v_tok = l.k_tok + kPagedQStep * (4 * 2 * 8 + 2 * 4 * 4);
+  l.basis = l.v_tok + 4 * blocks * kPagedQStep * 8;    // [4][blocks][64]: scale, zero-point
   l.anchors = l.basis + kPagedQSpan * kPagedQNodes * 4;
   l.rows = l.anchors + 2 * kDHead * 4;
   l.scores = l.rows + 4 * kPagedQStep * 4;

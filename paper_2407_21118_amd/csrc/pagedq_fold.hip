@@ -18,7 +18,8 @@ namespace palu {
 namespace {
 
 constexpr int kSteps = kPagedQStep;
-constexpr float kWeightScale = 16384.f;        // of the values' weights in float16 pairs: 2^-39 of the largest is left of the others
+constexpr float kSlack = 4.f;                  // a running maximum rises when a score exceeds it by so much (base-2 logarithms)
+constexpr float kWeightScale = 2048.f;         // of the values' weights, up to 2^4, in float16 pairs: those of the others are right to 2^-36 of the largest
 
 // a and b with the upper half of a and the lower half of b exchanged; the same of odd and even rows of 16 lanes
 struct Swapped {
@@ -71,8 +72,8 @@ template <> __device__ __forceinline__ uint32_t to_f16<BF16>(uint32_t w, int shi
 
 }  // namespace
 
-// KS steps of 32 key channels per wavefront; SL wavefronts share a head's channels; NQ query rows of a head
-template <typename T, int KS, int SL, int NQ>
+// KS steps of 32 key channels per wavefront; SL wavefronts share a head's channels; NQ query rows of a head; PIPED: see the loop
+template <typename T, int KS, int SL, int NQ, bool PIPED>
 __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a) {
   constexpr int HEADS = 4 / SL;                // of a unit
   constexpr int NB = KS / 4;                   // blocks of 128 channels
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   const int rk = m.k_off[g + 1] - m.k_off[g], rv = m.v_off[g + 1] - m.v_off[g], per_group = m.head_off[g + 1] - m.head_off[g];
   const int k_cols = un.n_groups() * rk, v_cols = un.n_groups() * rv, CB = v_cols / 128;
   const int row0 = rb * NQ, nr = min(NQ, m.qpk - row0);      // query rows of a head
-  const PagedQLds ld = pagedq_lds(k_cols, v_cols, SL, NQ);
+  const PagedQLds ld = pagedq_lds(k_cols, v_cols, SL, NQ, PIPED);
   const uint32_t lds0 = lds_addr(lds);
 
   const int hw = wave % HEADS, slice = wave / HEADS;
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
       if (i * 128 >= k_cols) break;
       const int id = i * kPagedQThreads + tid, x = id / k_pieces, pc = id - x * k_pieces;
       const size_t row = r[x];
-      load_to_lds(a.k.codes + row * a.k.row_bytes + m.k_off[g] / 2 + pc * 16, lds0 + ld.raw + (SL == 1 ? (n & 1) * ld.raw_size : 0) + (i * kPagedQThreads + wave * 64) * 16);
+      load_to_lds(a.k.codes + row * a.k.row_bytes + m.k_off[g] / 2 + pc * 16, lds0 + ld.raw + (PIPED ? (n & 1) * ld.raw_size : 0) + (i * kPagedQThreads + wave * 64) * 16);
       zraw[i] = a.k.zero[row * a.k.n_blocks + k_block0 + (pc >> 2)];
     }
     if (wave < 2) {                            // scales and zero-points by token
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
       anchor_s = a.rope[rope_f32_index(pos_of(n), lane, 1, kRopeTableStride)];
     }
   };
-  constexpr int VBUFS = SL == 1 ? 3 : 2;
+  constexpr int VBUFS = PIPED ? 3 : 2;
   auto request_values = [&](int n) __attribute__((always_inline)) {
     const int* const r = rows + (n & 3) * kSteps;
 #pragma unroll
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   };
   // ---- what came of them: scales by token; keys as float16 numbers, code - zero where the zero-point is a small integer (else the code)
   float2* const k_tok = reinterpret_cast<float2*>(lds + ld.k_tok);
-  float* const k_left = reinterpret_cast<float*>(lds + ld.k_tok + 2 * kSteps * 2 * 8);
+  float* const k_left = reinterpret_cast<float*>(lds + ld.k_tok + 4 * kSteps * 2 * 8);
   float2* const v_tok = reinterpret_cast<float2*>(lds + ld.v_tok);
   float* const anchors = reinterpret_cast<float*>(lds + ld.anchors);
   int* const flags = reinterpret_cast<int*>(lds + ld.flags);
@@ -202,14 +203,14 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
           if (s1 == 0.f) s1 = 0x1p-60f;
           ratio = s0 / s1;
         }
-        k_tok[((n & 1) * 2 + s) * kSteps + lane] = make_float2(ratio, s1);
+        k_tok[((n & 3) * 2 + s) * kSteps + lane] = make_float2(ratio, s1);
       }
     }
     if (wave == 1) {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         if (b >= CB) break;
-        v_tok[((n & 1) * CB + b) * kSteps + lane] = make_float2(F16::to_float(tok_raw[b]), F16::to_float(tok_raw[4 + b]));
+        v_tok[((n & 3) * CB + b) * kSteps + lane] = make_float2(F16::to_float(tok_raw[b]), F16::to_float(tok_raw[4 + b]));
       }
     }
     if (wave == 2 && folds(n)) {
@@ -218,22 +219,36 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     }
   };
   const uint32_t k1024 = per_lane_constant(0x64006400u);
-  // piece i of this thread
+  // quarter c of piece i of this thread, whose codes are w: lane group c's channels, 4 c + u and 16 + 4 c + u of the step
+  auto minus_zero = [&](uint16_t z16) __attribute__((always_inline)) {
+    const float z = F16::to_float(z16), off = -1024.f - (small_integer(z) ? z : 0.f);
+    return half2v{(_Float16)off, (_Float16)off};
+  };
+  auto raw_codes = [&](int n, int i) __attribute__((always_inline)) {
+    return *reinterpret_cast<const uint4v*>(lds + ld.raw + (PIPED ? (n & 1) * ld.raw_size : 0) + (i * kPagedQThreads + tid) * 16);
+  };
+  auto quarter_codes = [&](uint4v w, int c) __attribute__((always_inline)) {
+    return __builtin_amdgcn_perm(w[2 + (c >> 1)], w[c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+  };
+  auto spread = [&](uint32_t both, half2v off, int u) __attribute__((always_inline)) {
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, ((both >> (4 * u)) & 0x000f000fu) | k1024) + off);
+  };
+  auto quarter = [&](uint4v w, half2v off, int c, unsigned char* to) __attribute__((always_inline)) {
+    const uint32_t both = quarter_codes(w, c);
+    uint4v out;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) out[u] = spread(both, off, u);
+    *reinterpret_cast<uint4v*>(to) = out;
+  };
   auto convert = [&](int n, int i, uint16_t z16) __attribute__((always_inline)) {
     const int id = i * kPagedQThreads + tid, x = id / k_pieces, pc = id - x * k_pieces;
-    const uint4v w = *reinterpret_cast<const uint4v*>(lds + ld.raw + (SL == 1 ? (n & 1) * ld.raw_size : 0) + id * 16);
-    const float z = F16::to_float(z16);
-    const half2v off = {(_Float16)(-1024.f - (small_integer(z) ? z : 0.f)), (_Float16)(-1024.f - (small_integer(z) ? z : 0.f))};
-    unsigned char* const row = lds + ld.k + (SL == 1 ? (n & 1) * ld.k_size : 0) + x * ld.k_pitch;
+    const uint4v w = raw_codes(n, i);
+    const half2v off = minus_zero(z16);
+    unsigned char* const row = lds + ld.k + (PIPED ? (n & 1) * ld.k_size : 0) + x * ld.k_pitch;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {              // lane group c's channels: 4 c + u and 16 + 4 c + u of the step
-      const uint32_t both = __builtin_amdgcn_perm(w[2 + (c >> 1)], w[c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
-      uint4v out;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        out[u] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, ((both >> (4 * u)) & 0x000f000fu) | k1024) + off);
+    for (int c = 0; c < 4; ++c) {
       const int p = 4 * pc + c;
-      *reinterpret_cast<uint4v*>(row + ((p & ~15) | ((p ^ x) & 15)) * 16) = out;
+      quarter(w, off, c, row + ((p & ~15) | ((p ^ x) & 15)) * 16);
     }
   };
 
@@ -274,7 +289,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   }
   lds_barrier();
   request_keys(0);
-  request_values(0);
+  if (!PIPED) request_values(0);
 
   // ---- weights, as operand rows.  W: tile j's row 2 x (+ 1) is feature 4 x + j (+ 64), x < 8; it stays in the accumulation registers, which
   // the matrix instructions read as they are.  Those to be folded: a channel's features 32 + 8 kg .. and 96 + 8 kg .., read for every span.
@@ -398,6 +413,10 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   // ---- the first step's keys
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   lds_barrier();                               // (with several query rows the queries reach into what follows)
+  if (PIPED) {                                 // the weights of values before the first step
+    for (int x = tid; x < 2 * ld.p_size / 16; x += kPagedQThreads) *reinterpret_cast<uint4v*>(lds + ld.p + x * 16) = uint4v{0, 0, 0, 0};
+    for (int x = tid; x < 2 * CB * 16; x += kPagedQThreads) reinterpret_cast<float*>(lds + ld.alpha)[x] = 1.f;
+  }
   put_tokens(0);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -407,15 +426,14 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   if (3 < n_steps && wave == 3) entry = entry_of(3);         // (its rows are there: the same again)
   lds_barrier();
 
-  float sc[8], ss[8];                          // cos and sin (one query row: a and b) of the next 16 tokens
+  float sc[8] = {}, ss[8] = {};                // cos and sin (one query row: a and b) of the next 16 tokens
   uint4v G[KS][NG];
-  // Folded weights from step n on
-  auto fold = [&](int n) __attribute__((always_inline)) {
-    const float* at = anchors + (n & 1) * kDHead;
-    auto four = [&](int f) __attribute__((always_inline)) { return *reinterpret_cast<const float4v*>(at + f); };
+  // angles of the first 16 tokens of step n
+  auto start = [&](int n) __attribute__((always_inline)) {
+    const float* at = anchors + (n & 1) * kDHead + 8 * kg;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const float4v c = four(8 * kg + 4 * half), s = four(kHalf + 8 * kg + 4 * half);
+      const float4v c = *reinterpret_cast<const float4v*>(at + 4 * half), s = *reinterpret_cast<const float4v*>(at + kHalf + 4 * half);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int p = 4 * half + e;
@@ -428,6 +446,11 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
         }
       }
     }
+  };
+  // Folded weights from step n on
+  auto fold = [&](int n) __attribute__((always_inline)) {
+    const float* at = anchors + (n & 1) * kDHead;
+    auto four = [&](int f) __attribute__((always_inline)) { return *reinterpret_cast<const float4v*>(at + f); };
     uint4v va[LG][2], vb[LG][2];               // a and b of the folded pairs at the nodes, hi and lo (one row: by lanes)
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -506,70 +529,115 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
 #pragma unroll
   for (int i = 0; i < 4; ++i) k_off[i] = k_at + (((4 * i + kg) ^ col) & 15) * 16;
   const int b_last = ks_here / 4 - 1;          // last block of this slice
-  auto keys = [&](int n, int sub, float (&part)[NQ]) __attribute__((always_inline)) {
-    const unsigned char* const k = lds + ld.k + (SL == 1 ? (n & 1) * ld.k_size : 0) + 16 * sub * ld.k_pitch;
+  struct Sums {
     float4v acc[4], low[LG];
+  };
+  auto clear = [&](Sums& a) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] = float4v{0, 0, 0, 0};
+    for (int j = 0; j < 4; ++j) a.acc[j] = float4v{0, 0, 0, 0};
 #pragma unroll
-    for (int l = 0; l < LG; ++l) low[l] = float4v{0, 0, 0, 0};
-    auto product = [&](int ks, uint4v h) __attribute__((always_inline)) {
+    for (int l = 0; l < LG; ++l) a.low[l] = float4v{0, 0, 0, 0};
+  };
+  auto product = [&](Sums& a, int ks, uint4v h) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = mma<F16>(W[ks][j], h, acc[j]);
+    for (int j = 0; j < 4; ++j) a.acc[j] = mma<F16>(W[ks][j], h, a.acc[j]);
 #pragma unroll
-      for (int l = 0; l < NG; ++l) low[NQ == 1 ? 0 : l / 2] = mma<F16>(G[ks][l], h, low[NQ == 1 ? 0 : l / 2]);
-    };
-    const float2 tok = k_tok[((n & 1) * 2 + (SL == 1 ? hg : slice)) * kSteps + 16 * sub + col];
+    for (int l = 0; l < NG; ++l) a.low[NQ == 1 ? 0 : l / 2] = mma<F16>(G[ks][l], h, a.low[NQ == 1 ? 0 : l / 2]);
+  };
+  auto scale_sums = [&](Sums& a, float x) __attribute__((always_inline)) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
+    for (int j = 0; j < 4; ++j) a.acc[j] *= x;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) product(4 * b + i, *reinterpret_cast<const uint4v*>(k + k_off[i] + (SL == 1 ? b : min(b, b_last)) * 256));
-      if (flags[n & 1]) {                      // zero-points that are no small integers: as operands of their own, the same for all channels
-        const int block = SL == 1 ? hg * NB + b : min(2 * slice + b, k_cols / 128 - 1);
-        const float left = k_left[((n & 1) * 4 + block) * kSteps + 16 * sub + col];
-        const uint32_t w = pack2<F16>(-left, -left);
+    for (int l = 0; l < LG; ++l) a.low[l] *= x;
+  };
+  auto tok_of = [&](int n, int sub) __attribute__((always_inline)) {
+    return k_tok[((n & 3) * 2 + (SL == 1 ? hg : slice)) * kSteps + 16 * sub + col];
+  };
+  auto operand = [&](int n, int sub, int ks) __attribute__((always_inline)) {
+    const unsigned char* const k = lds + ld.k + (PIPED ? (n & 1) * ld.k_size : 0) + 16 * sub * ld.k_pitch;
+    return *reinterpret_cast<const uint4v*>(k + k_off[ks & 3] + (SL == 1 ? ks >> 2 : min(ks >> 2, b_last)) * 256);
+  };
+  // zero-points that are no small integers: as operands of their own, the same for all channels of block b, times x
+  auto zero_points = [&](Sums& a, int n, int sub, int b, float x) __attribute__((always_inline)) {
+    const int block = SL == 1 ? hg * NB + b : min(2 * slice + b, k_cols / 128 - 1);
+    const float left = k_left[((n & 1) * 4 + block) * kSteps + 16 * sub + col];
+    const uint32_t w = pack2<F16>(-left, -left);
+    Sums more;
+    clear(more);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) product(4 * b + i, uint4v{w, w, w, w});
-      }
-      if (b + 1 < NB) {
+    for (int i = 0; i < 4; ++i) product(more, 4 * b + i, uint4v{w, w, w, w});
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] *= tok.x;
+    for (int j = 0; j < 4; ++j) a.acc[j] += more.acc[j] * x;
 #pragma unroll
-        for (int l = 0; l < LG; ++l) low[l] *= tok.x;
+    for (int l = 0; l < LG; ++l) a.low[l] += more.low[l] * x;
+  };
+  // What pair p of this lane adds to the scores; its angle (one query row: a and b) 16 tokens on.  (The empty statements keep both where they are.)
+  auto pair_adds = [&](const Sums& a, int p, float (&part)[NQ]) __attribute__((always_inline)) {
+    const float lo = a.acc[p & 3][2 * (p >> 2)], hi = a.acc[p & 3][2 * (p >> 2) + 1], c = sc[p], s = ss[p];
+    if (NQ == 1) {
+      part[0] = __builtin_fmaf(lo, c, part[0]);
+      part[0] = __builtin_fmaf(hi, s, part[0]);
+      asm volatile("" : "+v"(part[0]));
+    } else {
+      const float x = __builtin_fmaf(lo, c, -(hi * s)), y = __builtin_fmaf(hi, c, lo * s);
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) {
+        part[r] = __builtin_fmaf(x, qa[r][p], part[r]);
+        part[r] = __builtin_fmaf(y, qb[r][p], part[r]);
+        asm volatile("" : "+v"(part[r]));
       }
     }
-    const int t = pos_of(n) + 16 * sub + col;
-    const int first = n < steps_s ? kPagedTile * i0 : pos_w;
-    const float4v basis = *reinterpret_cast<const float4v*>(lds + ld.basis + (((t - first) & (kSteps * a.span_steps - 1)) * 8 + 4 * (kg & 1)) * 4);
-#pragma unroll
-    for (int r = 0; r < NQ; ++r) part[r] = 0.f;
-#pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      const float lo = acc[p & 3][2 * (p >> 2)], hi = acc[p & 3][2 * (p >> 2) + 1], c = sc[p], s = ss[p];
-      if (NQ == 1) {
-        part[0] = __builtin_fmaf(lo, c, part[0]);
-        part[0] = __builtin_fmaf(hi, s, part[0]);
-        sc[p] = __builtin_fmaf(c, tc[p], s * ts[p]);         // a and b, 16 positions on
-        ss[p] = __builtin_fmaf(s, tc[p], -(c * ts[p]));
-      } else {
-        const float x = __builtin_fmaf(lo, c, -(hi * s)), y = __builtin_fmaf(hi, c, lo * s);
-#pragma unroll
-        for (int r = 0; r < NQ; ++r) {
-          part[r] = __builtin_fmaf(x, qa[r][p], part[r]);
-          part[r] = __builtin_fmaf(y, qb[r][p], part[r]);
-        }
-        sc[p] = __builtin_fmaf(c, tc[p], -(s * ts[p]));
-        ss[p] = __builtin_fmaf(s, tc[p], c * ts[p]);
-      }
+  };
+  auto pair_turns = [&](int p) __attribute__((always_inline)) {
+    const float c = sc[p], s = ss[p];
+    if (NQ == 1) {
+      sc[p] = __builtin_fmaf(c, tc[p], s * ts[p]);
+      ss[p] = __builtin_fmaf(s, tc[p], -(c * ts[p]));
+    } else {
+      sc[p] = __builtin_fmaf(c, tc[p], -(s * ts[p]));
+      ss[p] = __builtin_fmaf(s, tc[p], c * ts[p]);
     }
+    asm volatile("" : "+v"(sc[p]), "+v"(ss[p]));
+  };
+  auto pair = [&](const Sums& a, int p, float (&part)[NQ]) __attribute__((always_inline)) {
+    pair_adds(a, p, part);
+    pair_turns(p);
+  };
+  auto basis_of = [&](int n, int sub) __attribute__((always_inline)) {
+    const int t = pos_of(n) + 16 * sub + col - (n < steps_s ? kPagedTile * i0 : pos_w);
+    return *reinterpret_cast<const float4v*>(lds + ld.basis + ((t & (kSteps * a.span_steps - 1)) * 8 + 4 * (kg & 1)) * 4);
+  };
+  auto folded = [&](const Sums& a, float4v basis, float scale, float (&part)[NQ]) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < NQ; ++r) {
-      const float4v x = low[NQ == 1 ? 0 : r / 2];
+      const float4v x = a.low[NQ == 1 ? 0 : r / 2];
       const float sum = __builtin_fmaf(x[0], basis[0], __builtin_fmaf(x[1], basis[1], __builtin_fmaf(x[2], basis[2], x[3] * basis[3])));
       const bool mine = NQ == 1 || (kg >> 1) == (r & 1);
       part[r] = mine ? __builtin_fmaf(sum, low_unit[r], part[r]) : part[r];
-      part[r] *= tok.y;
+      part[r] *= scale;
     }
+  };
+  auto keys = [&](int n, int sub, float (&part)[NQ]) __attribute__((always_inline)) {
+    Sums a;
+    clear(a);
+    const float2 tok = tok_of(n, sub);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) product(a, 4 * b + i, operand(n, sub, 4 * b + i));
+      if (flags[n & 1]) zero_points(a, n, sub, b, 1.f);
+      if (b + 1 < NB) scale_sums(a, tok.x);
+    }
+#pragma unroll
+    for (int r = 0; r < NQ; ++r) part[r] = 0.f;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) pair(a, p, part);
+    folded(a, basis_of(n, sub), tok.y, part);
+  };
+  // every query row's scores of step n, a token per lane, from the lane groups' parts of its sub-tiles
+  auto whole_scores = [&](const float (&part)[4][NQ], float (&x)[NQ]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < NQ; ++r) x[r] = add_swapped16(add_swapped32(part[0][r], part[2][r]), add_swapped32(part[1][r], part[3][r]));
   };
 
   // ---- softmax of step n, a token per lane
@@ -585,32 +653,77 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     }
   }
   float* const scores = reinterpret_cast<float*>(lds + ld.scores);
-  auto softmax = [&](int n, const float (&x_in)[NQ]) __attribute__((always_inline)) {
-    const bool seen = attended(n, pos_of(n) + lane);
+  struct Weights {                             // of step n's rows, on the way to LDS
+    float x[NQ], u[NQ][MAXCB];
+    float2 tok[MAXCB];
+    bool seen;
+  };
+  // Scores and what of them the blocks' values weigh, masked; running maxima
+  auto weigh = [&](int n, const float (&x)[NQ], Weights& w) __attribute__((always_inline)) {
+    w.seen = attended(n, pos_of(n) + lane);
+#pragma unroll
+    for (int b = 0; b < MAXCB; ++b)
+      if (b < 2 || b < CB) w.tok[b] = v_tok[((n & 3) * CB + min(b, CB - 1)) * kSteps + lane];
+    bool rises = false;
 #pragma unroll
     for (int r = 0; r < NQ; ++r) {
-      const float x = seen ? x_in[r] : -INFINITY;
-      const float now = fmaxf(run_max[r], max_of_wave(x)), zero = now == -INFINITY ? 0.f : now;
-      run_sum[r] = run_sum[r] * __builtin_amdgcn_exp2f(run_max[r] - zero) + __builtin_amdgcn_exp2f(x - zero);
-      run_max[r] = now;
-      const int row = hw * NQ + r;
+      w.x[r] = w.seen ? x[r] : -INFINITY;
+      rises = rises || w.x[r] > run_max[r] + kSlack;
 #pragma unroll
-      for (int b = 0; b < MAXCB; ++b) {
-        if (b >= CB) break;
-        const float2 tok = v_tok[((n & 1) * CB + b) * kSteps + lane];
-        const float u = x + (float)__builtin_amdgcn_frexp_expf(tok.x);
-        const float top = fmaxf(blk_max[r][b], max_of_wave(u)), base = top == -INFINITY ? 0.f : top;
-        const float alpha = __builtin_amdgcn_exp2f(blk_max[r][b] - base);
-        const float w = seen ? __builtin_amdgcn_frexp_mantf(tok.x) * __builtin_amdgcn_exp2f(u - base) : 0.f;
-        blk_max[r][b] = top;
-        z_sum[r][b] = z_sum[r][b] * alpha + (seen ? w * (tok.y - 8.f) : 0.f);
-        uint32_t hi, lo;
-        split2<F16>(w * kWeightScale, 0.f, &hi, &lo);
-        uint16_t* P = reinterpret_cast<uint16_t*>(lds + ld.p + (n & 1) * ld.p_size + b * ld.p_cb + row * kPagedQProbPitch) + lane;
-        P[0] = (uint16_t)hi;
-        P[kLoRows * (kPagedQProbPitch / 2)] = (uint16_t)lo;
-        if (lane == 0) reinterpret_cast<float*>(lds + ld.alpha)[((n & 1) * CB + b) * 16 + row] = alpha;
+      for (int b = 0; b < MAXCB; ++b)
+        if (b < 2 || b < CB) {
+          w.u[r][b] = w.x[r] + (float)__builtin_amdgcn_frexp_expf(w.tok[b].x);
+          rises = rises || w.u[r][b] > blk_max[r][b] + kSlack;
+        }
+    }
+    float* const alphas = reinterpret_cast<float*>(lds + ld.alpha) + (n & 1) * CB * 16 + hw * NQ;
+    if (__any(rises)) {                        // seldom behind the first steps
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) {
+        const float now = fmaxf(run_max[r], max_of_wave(w.x[r]));
+        run_sum[r] *= __builtin_amdgcn_exp2f(run_max[r] - (now == -INFINITY ? 0.f : now));
+        run_max[r] = now;
+#pragma unroll
+        for (int b = 0; b < MAXCB; ++b)
+          if (b < 2 || b < CB) {
+            const float top = fmaxf(blk_max[r][b], max_of_wave(w.u[r][b]));
+            const float alpha = __builtin_amdgcn_exp2f(blk_max[r][b] - (top == -INFINITY ? 0.f : top));
+            z_sum[r][b] *= alpha;
+            blk_max[r][b] = top;
+            if (lane == 0) alphas[min(b, CB - 1) * 16 + r] = alpha;
+          }
       }
+    } else if (lane < CB) {
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) alphas[lane * 16 + r] = 1.f;
+    }
+  };
+  auto add_sum = [&](const Weights& w, int r) __attribute__((always_inline)) {
+    run_sum[r] += __builtin_amdgcn_exp2f(w.x[r] - (run_max[r] == -INFINITY ? 0.f : run_max[r]));
+    asm volatile("" : "+v"(run_sum[r]));
+  };
+  auto weight = [&](const Weights& w, int r, int b) __attribute__((always_inline)) {
+    const float y = __builtin_amdgcn_frexp_mantf(w.tok[b].x) * kWeightScale * __builtin_amdgcn_exp2f(w.u[r][b] - (blk_max[r][b] == -INFINITY ? 0.f : blk_max[r][b]));
+    return w.seen ? y : 0.f;
+  };
+  auto put_weight = [&](int n, const Weights& w, int r, int b, float y) __attribute__((always_inline)) {
+    z_sum[r][b] += w.seen ? y * (w.tok[b].y - 8.f) : 0.f;
+    asm volatile("" : "+v"(z_sum[r][b]));
+    uint32_t hi, lo;
+    split2<F16>(y, 0.f, &hi, &lo);
+    uint16_t* P = reinterpret_cast<uint16_t*>(lds + ld.p + (n & 1) * ld.p_size + min(b, CB - 1) * ld.p_cb + (hw * NQ + r) * kPagedQProbPitch) + lane;
+    P[0] = (uint16_t)hi;
+    P[kLoRows * (kPagedQProbPitch / 2)] = (uint16_t)lo;
+  };
+  auto softmax = [&](int n, const float (&x)[NQ]) __attribute__((always_inline)) {
+    Weights w;
+    weigh(n, x, w);
+#pragma unroll
+    for (int r = 0; r < NQ; ++r) {
+      add_sum(w, r);
+#pragma unroll
+      for (int b = 0; b < MAXCB; ++b)
+        if (b < CB) put_weight(n, w, r, b, weight(w, r, b));
     }
   };
 
@@ -618,46 +731,211 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   float4v O[8];                                // column 8 col + u of rows 4 kg + e; odd columns in units of 2^-20, even ones of 2^-24
 #pragma unroll
   for (int u = 0; u < 8; ++u) O[u] = float4v{0, 0, 0, 0};
-  const int vb = CB <= 2 ? wave % CB : wave;
-  const int half0 = CB <= 2 ? wave / CB : 0, half1 = CB <= 2 ? min(half0 + 1, 2) : 2;
-  const bool has_values = CB <= 2 ? half0 < 2 : wave < CB;
+  const int vb = CB <= 2 ? wave % CB : min(wave, CB - 1);
+  const int half0 = CB <= 2 ? wave / CB : 0;
+  const bool has_values = CB <= 2 ? half0 < 2 : wave < CB;   // (the others do a part that another one does, results nowhere)
   // Codes enter as code - 8: most zero-points are near 8, and sums of codes and of zero-points, which all but cancel over many tokens, would leave their
   // rounding (4e-5 of the largest output at 3000 tokens, against 4e-6).
   const half2v minus8_even = __builtin_bit_cast(half2v, 0x80088008u), minus8_odd = __builtin_bit_cast(half2v, 0x80808080u);
-  auto values = [&](int n) __attribute__((always_inline)) {
-    if (!has_values) return;
+  struct Values {
+    uint32_t d[8];
+    uint4v hi, lo, even, odd;
+  };
+  auto rescale = [&](int n) __attribute__((always_inline)) {
     const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (((n & 1) * CB + vb) * 16 + (NQ == 1 ? 0 : 4 * kg)) * 4);
     if (__any(!(al[0] == 1.f && al[1] == 1.f && al[2] == 1.f && al[3] == 1.f)))
 #pragma unroll
       for (int u = 0; u < 8; ++u) O[u] *= al;
-    for (int half = half0; half < half1; ++half) {
-      uint32_t d[8];
-      const unsigned char* const v = lds + ld.v + (n % VBUFS) * ld.v_size + (32 * half + 8 * kg) * (v_cols / 2) + vb * 64 + col * 4;
+  };
+  auto fetch_values = [&](int n, int half, Values& v) __attribute__((always_inline)) {
+    const unsigned char* const at = lds + ld.v + ((n + VBUFS) % VBUFS) * ld.v_size + (32 * half + 8 * kg) * (v_cols / 2) + vb * 64 + col * 4;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] = *reinterpret_cast<const uint32_t*>(v + e * (v_cols / 2));
-      const unsigned char* const P = lds + ld.p + (n & 1) * ld.p_size + vb * ld.p_cb + (NQ == 1 || SL == 2 ? col & 7 : col) * kPagedQProbPitch + (32 * half + 8 * kg) * 2;
-      const uint4v hi = *reinterpret_cast<const uint4v*>(P);
-      uint4v lo = hi;
-      if (NQ > 1) lo = *reinterpret_cast<const uint4v*>(P + kLoRows * kPagedQProbPitch);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {            // byte j: channels 2 j and 2 j + 1
-        uint4v even, odd;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t x = __builtin_amdgcn_perm(d[2 * i + 1], d[2 * i], 0x0c040c00u + 0x00010001u * j);
-          even[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x & 0x000f000fu) + minus8_even);
-          odd[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x & 0x00f000f0u) + minus8_odd);
-        }
-        O[2 * j] = mma<F16>(hi, even, O[2 * j]);
-        O[2 * j + 1] = mma<F16>(hi, odd, O[2 * j + 1]);
-        if (NQ > 1) {
-          O[2 * j] = mma<F16>(lo, even, O[2 * j]);
-          O[2 * j + 1] = mma<F16>(lo, odd, O[2 * j + 1]);
-        }
-      }
+    for (int e = 0; e < 8; ++e) v.d[e] = *reinterpret_cast<const uint32_t*>(at + e * (v_cols / 2));
+    const unsigned char* const P = lds + ld.p + (n & 1) * ld.p_size + vb * ld.p_cb + (NQ == 1 || SL == 2 ? col & 7 : col) * kPagedQProbPitch + (32 * half + 8 * kg) * 2;
+    v.hi = *reinterpret_cast<const uint4v*>(P);
+    if (NQ > 1) v.lo = *reinterpret_cast<const uint4v*>(P + kLoRows * kPagedQProbPitch);
+  };
+  // byte j of the codes, channels 2 j and 2 j + 1: of tokens 2 i and 2 i + 1; its products
+  auto value_codes = [&](Values& v, int j, int i) __attribute__((always_inline)) {
+    const uint32_t x = __builtin_amdgcn_perm(v.d[2 * i + 1], v.d[2 * i], 0x0c040c00u + 0x00010001u * j);
+    v.even[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x & 0x000f000fu) + minus8_even);
+    v.odd[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x & 0x00f000f0u) + minus8_odd);
+  };
+  auto value_products = [&](const Values& v, int j) __attribute__((always_inline)) {
+    O[2 * j] = mma<F16>(v.hi, v.even, O[2 * j]);
+    O[2 * j + 1] = mma<F16>(v.hi, v.odd, O[2 * j + 1]);
+    if (NQ > 1) {
+      O[2 * j] = mma<F16>(v.lo, v.even, O[2 * j]);
+      O[2 * j + 1] = mma<F16>(v.lo, v.odd, O[2 * j + 1]);
     }
   };
+  auto value_half = [&](int n, int half) __attribute__((always_inline)) {
+    Values v;
+    fetch_values(n, half, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) value_codes(v, j, i);
+      value_products(v, j);
+    }
+  };
+  auto values = [&](int n) __attribute__((always_inline)) {
+    rescale(n);
+    value_half(n, half0 & 1);
+    if (CB > 2) value_half(n, 1);
+  };
 
+  if constexpr (PIPED) {
+    // Interval n: the matrix instructions of step n's four sub-tiles; between them, dealt out a few at a time, the scores of the sub-tile before (of
+    // step n - 1's last, of n's first three), the codes of step n + 1, the weights of n - 1, the values of n - 2.  One barrier.
+    const int x0 = tid / k_pieces, pc = tid - x0 * k_pieces; // first piece of this thread; the second (of 256 columns) lies 32 rows on
+    unsigned char* to[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) to[c] = lds + ld.k + x0 * ld.k_pitch + (((4 * pc) & ~15) | (((4 * pc + c) ^ x0) & 15)) * 16;
+    const bool two = k_cols > 128;
+    Sums sums[2];
+    clear(sums[0]);
+    clear(sums[1]);
+    float part[4][NQ];
+    constexpr int kPer = 4 + NG, kSlots = KS * kPer;         // matrix instructions of a step of channels, of a sub-tile
+    // products of sub-tile SUB of step n, the scores of the sub-tile before it and MORE pieces of something else between them
+    auto sub_tile = [&](auto sub_c, int n, bool left, auto more_c, auto&& more) __attribute__((always_inline)) {
+      constexpr int SUB = decltype(sub_c)::value, MORE = decltype(more_c)::value;
+      Sums& now = sums[SUB & 1];
+      const Sums& before = sums[(SUB + 1) & 1];
+      float (&scores_before)[NQ] = part[(SUB + 3) & 3];
+      const int n_before = SUB == 0 ? n - 1 : n;
+      uint4v h[3];
+      h[0] = operand(n, SUB, 0);
+      h[1] = operand(n, SUB, 1);
+      const float ratio = NB == 2 ? tok_of(n, SUB).x : 1.f;
+      const float scale_before = tok_of(n_before, (SUB + 3) & 3).y;
+      const float4v basis = basis_of(n_before, (SUB + 3) & 3);
+      clear(now);
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) scores_before[r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (ks + 2 < KS) h[(ks + 2) % 3] = operand(n, SUB, ks + 2);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          float4v& sum = j < 4 ? now.acc[j] : now.low[NQ == 1 ? 0 : (j - 4) / 2];
+          if (NB == 2 && ks == 4 && (j < 4 || NQ == 1 || j % 2 == 0)) sum *= ratio;
+          sum = mma<F16>(j < 4 ? W[ks][j] : G[ks][j - 4], h[ks % 3], sum);
+          const int slot = ks * kPer + j;
+#pragma unroll
+          for (int q = slot * 16 / kSlots; q < (slot + 1) * 16 / kSlots; ++q) {
+            if (q & 1) pair_turns(q >> 1);
+            else pair_adds(before, q >> 1, scores_before);
+          }
+#pragma unroll
+          for (int q = slot * MORE / kSlots; q < (slot + 1) * MORE / kSlots; ++q) more(q);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      folded(before, basis, scale_before, scores_before);
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) asm volatile("" : "+v"(scores_before[r]));
+      if (left) {
+        zero_points(now, n, SUB, 0, ratio);
+        if (NB == 2) zero_points(now, n, SUB, NB - 1, 1.f);
+      }
+    };
+    // the codes w of one piece, in sixteen pieces
+    uint32_t both = 0;
+    uint4v out;
+    auto conversion = [&](int q, uint4v w, half2v off, int shift_bytes) __attribute__((always_inline)) {
+      const int c = q >> 2, u = q & 3;
+      if (u == 0) both = quarter_codes(w, c);
+      out[u] = spread(both, off, u);
+      asm volatile("" : "+v"(out[u]));
+      if (u == 3) *reinterpret_cast<uint4v*>(to[c] + shift_bytes) = out;
+    };
+    for (int n = 0; n < n_steps; ++n) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what interval n - 1 requested
+      const half2v off0 = minus_zero(zraw[0]), off1 = minus_zero(zraw[1]);
+      const bool left = __builtin_amdgcn_readfirstlane(flags[n & 1]) != 0;
+      if (n + 1 < n_steps) put_tokens(n + 1);
+      if (wave == 3 && n + 3 < n_steps) put_rows(n + 3, entry);
+      if (n + 2 < n_steps) request_keys(n + 2);
+      request_values(n);
+      if (wave == 3 && n + 4 < n_steps) entry = entry_of(n + 4);
+      if (folds(n)) fold(n);
+      // (behind the last step: codes of the one before it, converted into a buffer that nobody reads)
+      const uint4v raw0 = raw_codes(n + 1, 0), raw1 = raw_codes(n + 1, two ? 1 : 0);
+      const int next = ((n + 1) & 1) * ld.k_size, next1 = two ? next + 32 * ld.k_pitch : next;
+      sub_tile(IntC<0>(), n, left, IntC<16>(), [&](int q) __attribute__((always_inline)) { conversion(q, raw0, off0, next); });
+      if (folds(n)) start(n);
+      Weights w;
+      if (n > 0) {
+        float x[NQ];
+        whole_scores(part, x);
+        weigh(n - 1, x, w);
+      } else {                                 // no step before: weights of zero
+        w.seen = false;
+#pragma unroll
+        for (int r = 0; r < NQ; ++r) {
+          w.x[r] = -INFINITY;
+#pragma unroll
+          for (int b = 0; b < MAXCB; ++b) w.u[r][b] = -INFINITY;
+        }
+#pragma unroll
+        for (int b = 0; b < MAXCB; ++b) w.tok[b] = make_float2(0.f, 0.f);
+      }
+      float y = 0.f;
+      constexpr int kWeights = NQ * 5;         // a row: its sum, two blocks' weights and their way to LDS
+      sub_tile(IntC<1>(), n, left, IntC<16 + kWeights>(), [&](int q) __attribute__((always_inline)) {
+        if (q >= kWeights) {
+          conversion(q - kWeights, raw1, two ? off1 : off0, next1);
+        } else {
+          const int r = q / 5, k = q % 5;
+          if (k == 0) {
+            add_sum(w, r);
+          } else if (k & 1) {
+            y = weight(w, r, k >> 1);
+            asm volatile("" : "+v"(y));
+          } else {
+            put_weight(n - 1, w, r, (k >> 1) - 1, y);
+          }
+        }
+      });
+      if (CB > 2 && n > 0) {
+#pragma unroll
+        for (int r = 0; r < NQ; ++r)
+#pragma unroll
+          for (int b = 2; b < MAXCB; ++b)
+            if (b < CB) put_weight(n - 1, w, r, b, weight(w, r, b));
+      }
+      rescale(n);                              // (of n - 2; in the first two intervals there are no weights and nothing to rescale)
+      Values v;
+      fetch_values(n - 2, half0 & 1, v);
+      sub_tile(IntC<2>(), n, left, IntC<20>(), [&](int q) __attribute__((always_inline)) {
+        if (q % 5 < 4) {
+          value_codes(v, q / 5, q % 5);
+          asm volatile("" : "+v"(v.even[q % 5 & 3]), "+v"(v.odd[q % 5 & 3]));
+        } else {
+          value_products(v, q / 5);
+        }
+      });
+      if (CB > 2) value_half(n - 2, 1);
+      sub_tile(IntC<3>(), n, left, IntC<0>(), [&](int) __attribute__((always_inline)) {});
+      lds_barrier();
+    }
+    {                                          // the last step's scores and values, and those of the one before it
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) part[3][r] = 0.f;
+#pragma unroll
+      for (int p = 0; p < 8; ++p) pair(sums[1], p, part[3]);
+      folded(sums[1], basis_of(n_steps - 1, 3), tok_of(n_steps - 1, 3).y, part[3]);
+      float x[NQ];
+      whole_scores(part, x);
+      softmax(n_steps - 1, x);
+      values(n_steps - 2);
+      lds_barrier();
+      values(n_steps - 1);
+    }
+  } else {
   for (int n = 0; n <= n_steps; ++n) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // what interval n - 1 requested
     uint16_t z_now[4];
@@ -665,36 +943,33 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     for (int i = 0; i < 4; ++i) z_now[i] = zraw[i];
     if (n + 1 < n_steps) put_tokens(n + 1);
     if (wave == 3 && n + 3 < n_steps) put_rows(n + 3, entry);
-    if (SL == 1 && n + 2 < n_steps) request_keys(n + 2);
-    if (SL == 1 && n + 1 < n_steps) request_values(n + 1);
     if (wave == 3 && n + 4 < n_steps) entry = entry_of(n + 4);
     if (n > 0) values(n - 1);
     if (n == n_steps) break;
-    if (folds(n)) fold(n);
+    if (folds(n)) {
+      fold(n);
+      start(n);
+    }
     float part[4][NQ], x[NQ];
 #pragma unroll
-    for (int sub = 0; sub < 4; ++sub) {
-      keys(n, sub, part[sub]);
-      if (SL == 1 && sub < 4 && n + 1 < n_steps && sub * 128 < k_cols) convert(n + 1, sub, z_now[sub]);
-    }
+    for (int sub = 0; sub < 4; ++sub) keys(n, sub, part[sub]);
+    whole_scores(part, x);
+    if (SL == 2 && slice == 1)
 #pragma unroll
-    for (int r = 0; r < NQ; ++r) x[r] = add_swapped16(add_swapped32(part[0][r], part[2][r]), add_swapped32(part[1][r], part[3][r]));
-    if (SL == 2) {
-      if (slice == 1)
+      for (int r = 0; r < NQ; ++r) scores[(hw * NQ + r) * kSteps + lane] = x[r];
+    lds_barrier();
+    if (n + 1 < n_steps) request_values(n + 1);
 #pragma unroll
-        for (int r = 0; r < NQ; ++r) scores[(hw * NQ + r) * kSteps + lane] = x[r];
-      lds_barrier();
-      if (n + 1 < n_steps) request_values(n + 1);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n + 1 < n_steps && i * 128 < k_cols) convert(n + 1, i, z_now[i]);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the raw codes have been read)
-      if (n + 2 < n_steps) request_keys(n + 2);
+    for (int i = 0; i < 4; ++i)
+      if (n + 1 < n_steps && i * 128 < k_cols) convert(n + 1, i, z_now[i]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the raw codes have been read)
+    if (n + 2 < n_steps) request_keys(n + 2);
+    if (SL == 2)
 #pragma unroll
       for (int r = 0; r < NQ; ++r) x[r] += scores[(hw * NQ + r) * kSteps + lane];
-    }
     if (slice == 0) softmax(n, x);
     lds_barrier();
+  }
   }
 
   // ---- partial results
@@ -736,7 +1011,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
       if (h >= nh || h >= HEADS || r >= nr || (NQ == 1 && kg != 0) || (un.n_groups() > 1 && h / per_group != vg)) continue;
       const float2 f = fin[row * MAXCB + vb];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) y[u] = (y[u] * ((u & 1 ? 1048576.f : 16777216.f) / kWeightScale) - f.x) * f.y;
+      for (int u = 0; u < 8; ++u) y[u] = (y[u] * ((u & 1 ? 1048576.f : 16777216.f)) - f.x) * (f.y / kWeightScale);
       const int ohead = m.o_off[g] + (h0 + h - m.head_off[g]) * rv;
       float* const o = a.o_part + slot * a.o_stride + (size_t)m.qpk * ohead + (size_t)(row0 + r) * rv + 128 * vb - vg * rv + 8 * col;
       *reinterpret_cast<float4v*>(o) = float4v{y[0], y[1], y[2], y[3]};
@@ -746,14 +1021,16 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
 }
 
 namespace {
-template <typename T, int KS, int SL> PagedQFn pick(int rows) {
-  return rows == 1 ? pagedq_kernel<T, KS, SL, 1> : (rows == 2 ? pagedq_kernel<T, KS, SL, 2> : pagedq_kernel<T, KS, SL, 4>);
-}
-template <typename T> PagedQFn pick(const PagedQForm& f) {
-  return f.slices == 2 ? pick<T, 8, 2>(f.rows) : (f.ks == 4 ? pick<T, 4, 1>(f.rows) : pick<T, 8, 1>(f.rows));
+template <typename T, int NQ> PagedQFn pick(const PagedQForm& f) {
+  if (f.slices == 2) return pagedq_kernel<T, 8, 2, NQ, false>;
+  if (f.piped) return f.ks == 4 ? pagedq_kernel<T, 4, 1, NQ, true> : pagedq_kernel<T, 8, 1, NQ, true>;
+  return f.ks == 4 ? pagedq_kernel<T, 4, 1, NQ, false> : pagedq_kernel<T, 8, 1, NQ, false>;
 }
 }  // namespace
 
-PagedQFn pagedq_form(int act, const PagedQForm& f) { return act == PALU_F16 ? pick<F16>(f) : pick<BF16>(f); }
+// (every number of rows is a translation unit of its own)
+template <> PagedQFn pagedq_rows_form<PALU_PAGEDQ_ROWS>(int act, const PagedQForm& f) {
+  return act == PALU_F16 ? pick<F16, PALU_PAGEDQ_ROWS>(f) : pick<BF16, PALU_PAGEDQ_ROWS>(f);
+}
 
 }  // namespace palu

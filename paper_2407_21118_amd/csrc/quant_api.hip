@@ -88,8 +88,9 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
   for (int k = 0; k < 3 && c->span_steps > 0; ++k) {
     auto in_class = [&](int j) { return k == 2 ? rk(j) > 256 : rk(j) == 128 * (k + 1); };
     PagedQClass& cl = c->cls[c->n_cls];
-    cl.form = PagedQForm{k == 0 ? 4 : 8, k == 2 ? 2 : 1, rows};
-    cl.n_units = cl.lds_bytes = 0;
+    cl.form = PagedQForm{k == 0 ? 4 : 8, k == 2 ? 2 : 1, rows, k < 2};
+    cl.n_units = 0;
+    int lds[2] = {0, 0};
     const int unit_heads = 4 / cl.form.slices;
     for (int first = 0;; first += unit_heads) {              // as for unquantized latents: whole adjacent groups side by side, or parts of one
       bool more = false;
@@ -102,12 +103,14 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
         more = true;
         const int nh = std::min(unit_heads, n * heads(j) - first);
         cl.units[cl.n_units++].bits = (uint32_t)(m.head_off[j] + first) | (uint32_t)nh << 8 | (uint32_t)j << 16 | (uint32_t)n << 24;
-        cl.lds_bytes = std::max(cl.lds_bytes, pagedq_lds(n * rk(j), n * rv(j), cl.form.slices, rows).total);
+        for (int piped = 0; piped < 2; ++piped) lds[piped] = std::max(lds[piped], pagedq_lds(n * rk(j), n * rv(j), cl.form.slices, rows, piped).total);
         j += n - 1;
       }
       if (!more) break;
     }
     if (cl.n_units == 0) continue;
+    cl.form.piped = cl.form.piped && lds[1] <= kPagedLdsBytes;
+    cl.lds_bytes = lds[cl.form.piped];
     if (cl.lds_bytes > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;
     units += cl.n_units;
     ++c->n_cls;

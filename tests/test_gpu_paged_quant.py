@@ -47,6 +47,9 @@ LAYERS = {
     "gqa2": lambda: synth.uniform_layer(8, 4, 256, rope_theta=500000.0, q_per_kv=2),
     "gqa4": lambda: synth.uniform_layer(8, 4, 256, rope_theta=500000.0, q_per_kv=4),
     "gqa8-2x128": lambda: synth.uniform_layer(4, 2, 128, q_per_kv=8),
+    "gqa4-256-384": lambda: synth.uniform_layer(8, 4, 256, 384, q_per_kv=4),
+    "gqa2-128-512": lambda: synth.uniform_layer(5, 5, 128, 512, q_per_kv=2),
+    "8x256-512": lambda: synth.uniform_layer(8, 8, 256, 512),
     "gqa20-512": lambda: synth.uniform_layer(4, 4, 512, q_per_kv=20),
     "gqa70": lambda: synth.uniform_layer(2, 2, 128, q_per_kv=70),
     "norope": lambda: synth.uniform_layer(8, 4, 128, rope_theta=0.0),
