@@ -42,11 +42,12 @@ using PagedQFn = void (*)(PagedQArgs);
 constexpr int kPagedQThreads = 256;
 PagedQFn pagedq_plain_form(int act);
 // The instantiations, by ks: steps of 32 key channels of a wavefront, 4 or 8; slices: wavefronts that share a head's channels (2: ranks above
-// 256); rows: query rows of a head, 1, 2 or 4; piped: several steps at work at once, where LDS holds what that takes
+// 256); rows: query rows of a head, 1, 2 or 4; piped: several steps at work at once, where LDS holds what that takes, for k_blocks and v_blocks blocks
+// of 128 key and value columns of a unit (else up to 2 * slices and 4)
 struct PagedQForm {
-  int ks, slices, rows;
-  bool piped;
+  int ks, slices, rows, k_blocks, v_blocks, piped;
 };
+constexpr int kPagedQPipedBlocks = 3, kPagedQPipedRows = 2;
 template <int ROWS> PagedQFn pagedq_rows_form(int act, const PagedQForm& f);
 template <> PagedQFn pagedq_rows_form<1>(int, const PagedQForm&);
 template <> PagedQFn pagedq_rows_form<2>(int, const PagedQForm&);
@@ -59,11 +60,11 @@ inline PagedQFn pagedq_form(int act, const PagedQForm& f) {
 struct PagedQLds {
   int k_pitch;               // bytes per staged key row: k_cols float16 numbers
   int k_size, raw_size, v_size;                // of a step's keys, raw key codes, raw value codes
-  int k, raw, v, p, p_cb, p_size, alpha, k_tok, v_tok, basis, anchors, rows, scores, flags, total;
+  int k, raw, v, p, p_cb, p_size, alpha, k_tok, k_zero, v_tok, basis, anchors, rows, scores, flags, total;
 };
 constexpr int kPagedQProbPitch = kPagedQStep * 2 + 16;
-__host__ __device__ __forceinline__ PagedQLds pagedq_lds(int k_cols, int v_cols, int slices, int rows, bool piped) {
-  PagedQLds l;
+__host__ __device__ constexpr PagedQLds pagedq_lds(int k_cols, int v_cols, int slices, int rows, bool piped) {
+  PagedQLds l = {};
   const int blocks = v_cols / 128, bufs = piped ? 2 : 1, p_rows = rows == 1 ? 8 : (slices == 1 ? 32 : 16);
   l.k_pitch = k_cols * 2;
   l.k_size = kPagedQStep * l.k_pitch;
@@ -76,15 +77,20 @@ __host__ __device__ __forceinline__ PagedQLds pagedq_lds(int k_cols, int v_cols,
   l.p_cb = p_rows * kPagedQProbPitch;          // probabilities of a block of value columns
   l.p_size = blocks * l.p_cb;
   l.alpha = l.p + 2 * l.p_size;                // [2][blocks][16]
-  l.k_tok = l.alpha + 2 * blocks * 16 * 4;     // [4][2][64]: ratio and scale, by slice or group; [2][4][64]: what is left of the zero-points
-  l.v_tok = l.k_tok + kPagedQStep * (4 * 2 * 8 + 2 * 4 * 4);
-  l.basis = l.v_tok + 4 * blocks * kPagedQStep * 8;    // [4][blocks][64]: scale, zero-point
-  l.anchors = l.basis + kPagedQSpan * kPagedQNodes * 4;
-  l.rows = l.anchors + 2 * kDHead * 4;
-  l.scores = l.rows + 4 * kPagedQStep * 4;
+  l.k_tok = l.alpha + 2 * blocks * 16 * 4;     // [4][2][64]: ratio and scale, by slice or group
+  l.k_zero = l.k_tok + kPagedQStep * 4 * 2 * 8;        // [4][4][64]: the zero-point for the codes, what is left of it
+  l.v_tok = l.k_zero + kPagedQStep * 4 * 4 * 4;        // [4][blocks][64]: scale, zero-point
+  l.basis = l.v_tok + kPagedQStep * 4 * blocks * 4;
+  l.anchors = l.basis + kPagedQSpan * kPagedQNodes * 4;        // [4]
+  l.rows = l.anchors + 4 * kDHead * 4;                 // [8][64]
+  l.scores = l.rows + 8 * kPagedQStep * 4;
   l.flags = l.scores + (slices == 1 ? 0 : 2 * rows * kPagedQStep * 4);
   l.total = l.flags + 16;
   return l;
+}
+
+__host__ __device__ constexpr PagedQLds pagedq_lds(int ks, int slices, int rows, int k_blocks, int v_blocks, bool piped) {
+  return pagedq_lds(128 * (piped ? k_blocks : 2 * slices), 128 * (piped ? v_blocks : 4), slices, rows, piped);
 }
 
 }  // namespace palu

@@ -72,14 +72,16 @@ template <> __device__ __forceinline__ uint32_t to_f16<BF16>(uint32_t w, int shi
 
 }  // namespace
 
-// KS steps of 32 key channels per wavefront; SL wavefronts share a head's channels; NQ query rows of a head; PIPED: see the loop
-template <typename T, int KS, int SL, int NQ, bool PIPED>
+// KS steps of 32 key channels per wavefront; SL wavefronts share a head's channels; NQ query rows of a head; PIPED: see the loop, for units of KB and
+// VB blocks of key and value columns
+template <typename T, int KS, int SL, int NQ, bool PIPED, int KB = 0, int VB = 0>
 __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a) {
   constexpr int HEADS = 4 / SL;                // of a unit
   constexpr int NB = KS / 4;                   // blocks of 128 channels
   constexpr int LG = NQ == 1 ? 1 : NQ / 2;     // folded query rows, 16 (row, node) a group
   constexpr int NG = NQ == 1 ? 1 : NQ;         // tiles of folded weights: of one row hi and lo in one tile, else apart
-  constexpr int MAXCB = 4;
+  constexpr int MAXCB = PIPED ? VB : 4;
+  constexpr PagedQLds ld = pagedq_lds(KS, SL, NQ, KB, VB, PIPED);
   constexpr int kLoRows = NQ == 1 ? 4 : (SL == 1 ? 16 : 8);  // rows of probabilities before those that the rounding left
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const PagedMeta& m = a.meta;
@@ -100,9 +102,8 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   const int i0 = (int)((long long)span.n_tiles * chunk / n_chunks), i1 = (int)((long long)span.n_tiles * (chunk + 1) / n_chunks);
   const int g = un.group(), nh = un.nh(), h0 = un.h0();
   const int rk = m.k_off[g + 1] - m.k_off[g], rv = m.v_off[g + 1] - m.v_off[g], per_group = m.head_off[g + 1] - m.head_off[g];
-  const int k_cols = un.n_groups() * rk, v_cols = un.n_groups() * rv, CB = v_cols / 128;
+  const int k_cols = PIPED ? 128 * KB : un.n_groups() * rk, v_cols = PIPED ? 128 * VB : un.n_groups() * rv, CB = v_cols / 128;
   const int row0 = rb * NQ, nr = min(NQ, m.qpk - row0);      // query rows of a head
-  const PagedQLds ld = pagedq_lds(k_cols, v_cols, SL, NQ, PIPED);
   const uint32_t lds0 = lds_addr(lds);
 
   const int hw = wave % HEADS, slice = wave / HEADS;
@@ -119,13 +120,18 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   auto pos_of = [&](int n) __attribute__((always_inline)) { return n < steps_s ? kPagedTile * i0 + kSteps * n : pos_w + kSteps * (n - steps_s); };
   auto end_of = [&](int n) __attribute__((always_inline)) { return min(L, n < steps_s ? kPagedTile * mid : pos_w + kPagedTile * (i1 - mid)); };
   auto attended = [&](int n, int t) __attribute__((always_inline)) { return t < end_of(n) && (t < span.sink || t >= span.lo); };
-  auto folds = [&](int n) __attribute__((always_inline)) { return (n < steps_s ? n : n - steps_s) % a.span_steps == 0; };
+  // spans: the first steps of either part, and every span_steps-th
+  const int span_log = __builtin_ctz(a.span_steps), spans_s = (steps_s + a.span_steps - 1) >> span_log;
+  auto folds = [&](int n) __attribute__((always_inline)) { return ((n < steps_s ? n : n - steps_s) & (a.span_steps - 1)) == 0; };
+  auto span_of = [&](int n) __attribute__((always_inline)) { return n < steps_s ? n >> span_log : spans_s + ((n - steps_s) >> span_log); };
+  auto span_step = [&](int k) __attribute__((always_inline)) { return k < spans_s ? k << span_log : steps_s + ((k - spans_s) << span_log); };
 
-  // ---- requests.  In interval n: keys, scales and angles of step n + 2, values of n + 1, page-table entries of n + 4.
+  // ---- requests.  In interval n: scales and zero-points of step n + 3, keys of n + 2, values (PIPED: of n, else n + 1), page-table entries of n + 5,
+  // the angles of the third span after one that begins.
   int* const rows = reinterpret_cast<int*>(lds + ld.rows);
   const int k_pieces = k_cols / 32, v_pieces = v_cols / 32;  // 16-byte pieces of a raw row
   const int k_block0 = m.k_off[g] / 128, v_block0 = m.v_off[g] / 128;
-  uint16_t zraw[4], tok_raw[8];
+  uint16_t tok_raw[8];
   int entry = 0;
   float anchor_c = 0.f, anchor_s = 0.f;
   auto token_of = [&](int n, int x) __attribute__((always_inline)) {       // the position whose row token x reads (a masked token: the first attended one's)
@@ -136,63 +142,89 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     return a.page_table[(size_t)seq * a.table_stride + (token_of(n, lane) >> a.page_shift)];
   };
   auto put_rows = [&](int n, int e) __attribute__((always_inline)) {
-    rows[(n & 3) * kSteps + lane] = (max(0, min(e, a.n_pages - 1)) << a.page_shift) + (token_of(n, lane) & ((1 << a.page_shift) - 1));
+    rows[(n & 7) * kSteps + lane] = (max(0, min(e, a.n_pages - 1)) << a.page_shift) + (token_of(n, lane) & ((1 << a.page_shift) - 1));
   };
+  const unsigned char* const k_src = a.k.codes + m.k_off[g] / 2 + (tid % k_pieces) * 16;
+  const int k_x = tid / k_pieces;              // (PIPED: row of the first piece; the second lies 32 on)
   auto request_keys = [&](int n) __attribute__((always_inline)) {
-    const int* const r = rows + (n & 3) * kSteps;
+    const int* const r = rows + (n & 7) * kSteps;
+    const uint32_t dst = lds0 + ld.raw + (PIPED ? (n & 1) * ld.raw_size : 0) + wave * 1024;
+    if (PIPED) {
+      const uint32_t r0 = r[k_x], r1 = r[(k_x + 32) & 63];
+      load_to_lds(k_src + (uint64_t)r0 * (uint32_t)a.k.row_bytes, dst);
+      if (k_cols > 128) load_to_lds(k_src + (uint64_t)r1 * (uint32_t)a.k.row_bytes, dst + kPagedQThreads * 16);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i * 128 >= k_cols) break;
-      const int id = i * kPagedQThreads + tid, x = id / k_pieces, pc = id - x * k_pieces;
-      const size_t row = r[x];
-      load_to_lds(a.k.codes + row * a.k.row_bytes + m.k_off[g] / 2 + pc * 16, lds0 + ld.raw + (PIPED ? (n & 1) * ld.raw_size : 0) + (i * kPagedQThreads + wave * 64) * 16);
-      zraw[i] = a.k.zero[row * a.k.n_blocks + k_block0 + (pc >> 2)];
-    }
-    if (wave < 2) {                            // scales and zero-points by token
-      const PagedQSide& s = wave == 0 ? a.k : a.v;
-      const int blocks = wave == 0 ? k_cols / 128 : CB;
-      const size_t at = (size_t)r[lane] * s.n_blocks + (wave == 0 ? k_block0 : v_block0);
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        if (b >= blocks) break;
-        tok_raw[b] = s.scale[at + b];
-        tok_raw[4 + b] = s.zero[at + b];
+      for (int i = 0; i < 4; ++i) {
+        if (i * 128 >= k_cols) break;
+        const int id = i * kPagedQThreads + tid, x = id / k_pieces, pc = id - x * k_pieces;
+        load_to_lds(a.k.codes + (size_t)r[x] * a.k.row_bytes + m.k_off[g] / 2 + pc * 16, dst + i * kPagedQThreads * 16);
       }
     }
-    if (wave == 2 && folds(n)) {
-      anchor_c = a.rope[rope_f32_index(pos_of(n), lane, 0, kRopeTableStride)];
-      anchor_s = a.rope[rope_f32_index(pos_of(n), lane, 1, kRopeTableStride)];
+  };
+  // role 0: keys', 1: values'; an even and an odd wavefront's, which keeps to its role
+  const PagedQSide& tok_side = wave & 1 ? a.v : a.k;
+  const uint16_t* const tok_scale = tok_side.scale + (wave & 1 ? v_block0 : k_block0);
+  const uint16_t* const tok_zero = tok_side.zero + (wave & 1 ? v_block0 : k_block0);
+  const uint32_t tok_blocks = tok_side.n_blocks;
+  auto request_tokens = [&](int n, int role) __attribute__((always_inline)) {
+    const int blocks = role == 0 ? k_cols / 128 : CB;
+    const uint64_t at = (uint64_t)(uint32_t)rows[(n & 7) * kSteps + lane] * tok_blocks;
+    const uint16_t *scale = tok_scale + at, *zero = tok_zero + at;
+    tok_raw[0] = scale[0];
+    tok_raw[4] = zero[0];
+    if (blocks > 1) {
+      tok_raw[1] = scale[1];
+      tok_raw[5] = zero[1];
+    }
+    if (blocks > 2) {
+#pragma unroll
+      for (int b = 2; b < 4; ++b) {
+        tok_raw[b] = scale[min(b, blocks - 1)];
+        tok_raw[4 + b] = zero[min(b, blocks - 1)];
+      }
     }
   };
+  auto request_anchors = [&](int k) __attribute__((always_inline)) {
+    anchor_c = a.rope[rope_f32_index(pos_of(span_step(k)), lane, 0, kRopeTableStride)];
+    anchor_s = a.rope[rope_f32_index(pos_of(span_step(k)), lane, 1, kRopeTableStride)];
+  };
   constexpr int VBUFS = PIPED ? 3 : 2;
+  int v_at[4];                                 // pieces of the values: column << 8 | row
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int id = i * kPagedQThreads + tid, x = (id / v_pieces) & 63;
+    v_at[i] = (id % v_pieces) << 12 | x;
+  }
+  const unsigned char* const v_src = a.v.codes + m.v_off[g] / 2;
   auto request_values = [&](int n) __attribute__((always_inline)) {
-    const int* const r = rows + (n & 3) * kSteps;
+    const int* const r = rows + (n & 7) * kSteps;
+    const uint32_t dst = lds0 + ld.v + (n % VBUFS) * ld.v_size + wave * 1024;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (i * 128 >= v_cols) break;
-      const int id = i * kPagedQThreads + tid, x = id / v_pieces, pc = id - x * v_pieces;
-      load_to_lds(a.v.codes + (size_t)r[x] * a.v.row_bytes + m.v_off[g] / 2 + pc * 16, lds0 + ld.v + (n % VBUFS) * ld.v_size + (i * kPagedQThreads + wave * 64) * 16);
+      load_to_lds(v_src + ((uint64_t)(uint32_t)r[v_at[i] & 63] * (uint32_t)a.v.row_bytes + (v_at[i] >> 8)), dst + i * kPagedQThreads * 16);
     }
   };
-  // ---- what came of them: scales by token; keys as float16 numbers, code - zero where the zero-point is a small integer (else the code)
+  // ---- what came of them
   float2* const k_tok = reinterpret_cast<float2*>(lds + ld.k_tok);
-  float* const k_left = reinterpret_cast<float*>(lds + ld.k_tok + 4 * kSteps * 2 * 8);
-  float2* const v_tok = reinterpret_cast<float2*>(lds + ld.v_tok);
+  uint32_t* const k_zero = reinterpret_cast<uint32_t*>(lds + ld.k_zero);
+  uint32_t* const v_tok = reinterpret_cast<uint32_t*>(lds + ld.v_tok);
   float* const anchors = reinterpret_cast<float*>(lds + ld.anchors);
   int* const flags = reinterpret_cast<int*>(lds + ld.flags);
-  auto put_tokens = [&](int n) __attribute__((always_inline)) {
-    if (wave == 0) {
+  auto put_tokens = [&](int n, int role) __attribute__((always_inline)) {
+    if (role == 0) {
       bool any = false;
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < 4; ++b) {            // codes take their zero-point where it is a small integer; what is left of it (with the other sign): see zero_points
         if (b * 128 >= k_cols) break;
         const float z = F16::to_float(tok_raw[4 + b]);
-        const float left = small_integer(z) ? 0.f : z;
-        any = any || !(left == 0.f);
-        k_left[((n & 1) * 4 + b) * kSteps + lane] = left;
+        const bool small = small_integer(z);
+        any = any || !small;
+        k_zero[((n & 3) * 4 + b) * kSteps + lane] = (uint32_t)F16::from_float(-1024.f - (small ? z : 0.f)) | (small ? 0u : (uint32_t)(tok_raw[4 + b] ^ 0x8000u) << 16);
       }
       const int some = __any(any) ? 1 : 0;
-      if (lane == 0) flags[n & 1] = some;
+      if (lane == 0) flags[n & 3] = some;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {            // blocks of a slice, or of a group: (first * ratio + second) * scale.  (A second scale of zero: so
         if (s * NB * 128 >= k_cols) break;     // small a number that nothing of the second block is left.)
@@ -201,28 +233,27 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
         if (NB == 2 && (2 * s + 1) * 128 < k_cols) {
           s1 = F16::to_float(tok_raw[2 * s + 1]);
           if (s1 == 0.f) s1 = 0x1p-60f;
-          ratio = s0 / s1;
+          ratio = s0 * __builtin_amdgcn_rcpf(s1);            // (right to 2^-22)
         }
         k_tok[((n & 3) * 2 + s) * kSteps + lane] = make_float2(ratio, s1);
       }
-    }
-    if (wave == 1) {
+    } else {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         if (b >= CB) break;
-        v_tok[((n & 3) * CB + b) * kSteps + lane] = make_float2(F16::to_float(tok_raw[b]), F16::to_float(tok_raw[4 + b]));
+        v_tok[((n & 3) * CB + b) * kSteps + lane] = (uint32_t)tok_raw[b] | (uint32_t)tok_raw[4 + b] << 16;
       }
     }
-    if (wave == 2 && folds(n)) {
-      anchors[(n & 1) * kDHead + lane] = anchor_c;
-      anchors[(n & 1) * kDHead + kHalf + lane] = anchor_s;
-    }
+  };
+  auto put_anchors = [&](int k) __attribute__((always_inline)) {
+    anchors[(k & 3) * kDHead + lane] = anchor_c;
+    anchors[(k & 3) * kDHead + kHalf + lane] = anchor_s;
   };
   const uint32_t k1024 = per_lane_constant(0x64006400u);
-  // quarter c of piece i of this thread, whose codes are w: lane group c's channels, 4 c + u and 16 + 4 c + u of the step
-  auto minus_zero = [&](uint16_t z16) __attribute__((always_inline)) {
-    const float z = F16::to_float(z16), off = -1024.f - (small_integer(z) ? z : 0.f);
-    return half2v{(_Float16)off, (_Float16)off};
+  // piece i of this thread: its codes; what is added to 1024 + code; quarter c of it, lane group c's channels, 4 c + u and 16 + 4 c + u of the step
+  auto zero_of = [&](int n, int x, int pc) __attribute__((always_inline)) {
+    const uint32_t z = k_zero[((n & 3) * 4 + (pc >> 2)) * kSteps + x];
+    return __builtin_bit_cast(half2v, __builtin_amdgcn_perm(z, z, 0x01000100u));
   };
   auto raw_codes = [&](int n, int i) __attribute__((always_inline)) {
     return *reinterpret_cast<const uint4v*>(lds + ld.raw + (PIPED ? (n & 1) * ld.raw_size : 0) + (i * kPagedQThreads + tid) * 16);
@@ -240,10 +271,10 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     for (int u = 0; u < 4; ++u) out[u] = spread(both, off, u);
     *reinterpret_cast<uint4v*>(to) = out;
   };
-  auto convert = [&](int n, int i, uint16_t z16) __attribute__((always_inline)) {
+  auto convert = [&](int n, int i) __attribute__((always_inline)) {
     const int id = i * kPagedQThreads + tid, x = id / k_pieces, pc = id - x * k_pieces;
     const uint4v w = raw_codes(n, i);
-    const half2v off = minus_zero(z16);
+    const half2v off = zero_of(n, x, pc);
     unsigned char* const row = lds + ld.k + (PIPED ? (n & 1) * ld.k_size : 0) + x * ld.k_pitch;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -290,6 +321,9 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   lds_barrier();
   request_keys(0);
   if (!PIPED) request_values(0);
+  const int token_step = min(wave >> 1, n_steps - 1);        // waves 0 and 1: of the first step, 2 and 3: of the second
+  request_tokens(token_step, wave & 1);
+  if (wave < 3 && span_step(wave) < n_steps) request_anchors(wave);
 
   // ---- weights, as operand rows.  W: tile j's row 2 x (+ 1) is feature 4 x + j (+ 64), x < 8; it stays in the accumulation registers, which
   // the matrix instructions read as they are.  Those to be folded: a channel's features 32 + 8 kg .. and 96 + 8 kg .., read for every span.
@@ -358,7 +392,6 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   float nc[LG][8], ns[LG][8];                  // a and b at the node, times 2^e of its row
   float qa[NQ == 1 ? 1 : NQ][8], qb[NQ == 1 ? 1 : NQ][8];    // several rows: the queries
   float low_unit[NQ];                          // what a folded row's sums are worth
-  float g_scale[LG];                           // ... and what its weights are multiplied by, by this lane's row
   {
     const float unit = __builtin_amdgcn_ldexpf(1.f, -shift);
 #pragma unroll
@@ -381,12 +414,12 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
         }
       }
     }
-    int ea[NQ], eg[NQ];
+    int ea[NQ];
 #pragma unroll
     for (int r = 0; r < NQ; ++r) {
-      ea[r] = 8 - __builtin_amdgcn_frexp_expf(q_max[r]);
-      eg[r] = 15 - __builtin_amdgcn_frexp_expf(__builtin_amdgcn_ldexpf(1.4143f * b_max * q_sum[r], ea[r]));
-      low_unit[r] = __builtin_amdgcn_ldexpf(1.f, -ea[r] - eg[r] - shift);
+      // a folded weight is at most b_max * sqrt(2) * q_sum, an a or b at most q_max: both times 2^e are float16 numbers
+      ea[r] = min(15 - __builtin_amdgcn_frexp_expf(1.4143f * b_max * q_sum[r]), 15 - __builtin_amdgcn_frexp_expf(q_max[r]));
+      low_unit[r] = __builtin_amdgcn_ldexpf(1.f, -ea[r] - shift);
     }
     const double T2 = 0.5 * kSteps * a.span_steps;
     constexpr float kNode[4] = {0.98078528040323044913f, 0.83146961230254523708f, 0.55557023301960222474f, 0.19509032201612826785f};
@@ -397,7 +430,6 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
 #pragma unroll
     for (int l = 0; l < LG; ++l) {
       const float scale = __builtin_amdgcn_ldexpf(1.f, NQ == 1 ? ea[0] : (upper ? ea[(2 * l + 1) % NQ] : ea[2 * l]));
-      g_scale[l] = __builtin_amdgcn_ldexpf(1.f, NQ == 1 ? eg[0] : (upper ? eg[(2 * l + 1) % NQ] : eg[2 * l]));
 #pragma unroll
       for (int p = 0; p < 8; ++p) {
         const int f = kPagedQLow + 8 * kg + p;
@@ -417,20 +449,42 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     for (int x = tid; x < 2 * ld.p_size / 16; x += kPagedQThreads) *reinterpret_cast<uint4v*>(lds + ld.p + x * 16) = uint4v{0, 0, 0, 0};
     for (int x = tid; x < 2 * CB * 16; x += kPagedQThreads) reinterpret_cast<float*>(lds + ld.alpha)[x] = 1.f;
   }
-  put_tokens(0);
+  put_tokens(token_step, wave & 1);
+  if (wave < 3 && span_step(wave) < n_steps) put_anchors(wave);
+  lds_barrier();
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (i * 128 < k_cols) convert(0, i, zraw[i]);
+    if (i * 128 < k_cols) convert(0, i);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (the raw codes have been read)
   if (n_steps > 1) request_keys(1);
-  if (3 < n_steps && wave == 3) entry = entry_of(3);         // (its rows are there: the same again)
+  if (n_steps > 2 && wave < 2) request_tokens(2, wave);
+  if (4 < n_steps && wave == 3) entry = entry_of(4);
   lds_barrier();
 
+  // What interval n - 1 requested goes to LDS, before anything is requested: the compiler waits for all loads that it does not know of, too
+  auto put = [&](int n) __attribute__((always_inline)) {
+    if (wave < 2) {
+      if (n + 2 < n_steps) put_tokens(n + 2, wave);
+    } else if (wave == 2) {
+      if (n > 0 && folds(n - 1) && span_step(span_of(n - 1) + 3) < n_steps) put_anchors(span_of(n - 1) + 3);
+    } else {
+      if (n + 4 < n_steps) put_rows(n + 4, entry);
+    }
+  };
+  auto request = [&](int n) __attribute__((always_inline)) {
+    if (wave < 2) {
+      if (n + 3 < n_steps) request_tokens(n + 3, wave);
+    } else if (wave == 2) {
+      if (folds(n) && span_step(span_of(n) + 3) < n_steps) request_anchors(span_of(n) + 3);
+    } else {
+      if (n + 5 < n_steps) entry = entry_of(n + 5);
+    }
+  };
   float sc[8] = {}, ss[8] = {};                // cos and sin (one query row: a and b) of the next 16 tokens
   uint4v G[KS][NG];
   // angles of the first 16 tokens of step n
   auto start = [&](int n) __attribute__((always_inline)) {
-    const float* at = anchors + (n & 1) * kDHead + 8 * kg;
+    const float* at = anchors + (span_of(n) & 3) * kDHead + 8 * kg;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const float4v c = *reinterpret_cast<const float4v*>(at + 4 * half), s = *reinterpret_cast<const float4v*>(at + kHalf + 4 * half);
@@ -447,14 +501,15 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
       }
     }
   };
-  // Folded weights from step n on
-  auto fold = [&](int n) __attribute__((always_inline)) {
-    const float* at = anchors + (n & 1) * kDHead;
-    auto four = [&](int f) __attribute__((always_inline)) { return *reinterpret_cast<const float4v*>(at + f); };
-    uint4v va[LG][2], vb[LG][2];               // a and b of the folded pairs at the nodes, hi and lo (one row: by lanes)
+  // a and b of the folded pairs at the nodes of span k, hi and lo (one row: by lanes)
+  struct Nodes {
+    uint4v a[LG][NQ == 1 ? 1 : 2], b[LG][NQ == 1 ? 1 : 2];
+  };
+  auto nodes_of = [&](int k, Nodes& v) __attribute__((always_inline)) {
+    const float* at = anchors + (k & 3) * kDHead + kPagedQLow + 8 * kg;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const float4v c = four(kPagedQLow + 8 * kg + 4 * half), s = four(kHalf + kPagedQLow + 8 * kg + 4 * half);
+      const float4v c = *reinterpret_cast<const float4v*>(at + 4 * half), s = *reinterpret_cast<const float4v*>(at + kHalf + 4 * half);
 #pragma unroll
       for (int l = 0; l < LG; ++l)
 #pragma unroll
@@ -468,56 +523,68 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
           }
           uint32_t h, lo;
           split2<F16>(x[0], x[1], &h, &lo);
-          va[l][0][2 * half + e / 2] = NQ == 1 && col >= 8 ? lo : h;
-          va[l][1][2 * half + e / 2] = lo;
+          v.a[l][0][2 * half + e / 2] = NQ == 1 && col >= 8 ? lo : h;
+          if (NQ > 1) v.a[l][NQ > 1][2 * half + e / 2] = lo;
           split2<F16>(y[0], y[1], &h, &lo);
-          vb[l][0][2 * half + e / 2] = NQ == 1 && col >= 8 ? lo : h;
-          vb[l][1][2 * half + e / 2] = lo;
+          v.b[l][0][2 * half + e / 2] = NQ == 1 && col >= 8 ? lo : h;
+          if (NQ > 1) v.b[l][NQ > 1][2 * half + e / 2] = lo;
         }
     }
+  };
+  // Folded weights of channel step ks, from its weights f
+  const float lo_part = NQ == 1 && col >= 8 ? -1.f : 0.f;    // one row: these lanes hold what the rounding leaves
+  auto fold_tile = [&](const uint4v (&f)[2], const Nodes& v, int l) __attribute__((always_inline)) {
+    float4v d = mma<F16>(f[0], v.a[l][0], float4v{0, 0, 0, 0});
+    d = mma<F16>(f[1], v.b[l][0], d);
+    if (NQ > 1) {
+      d = mma<F16>(f[0], v.a[l][NQ > 1], d);
+      d = mma<F16>(f[1], v.b[l][NQ > 1], d);
+    }
+    return d;
+  };
+  auto fold_pack = [&](float x, float y, uint32_t* hi, uint32_t* lo) __attribute__((always_inline)) {
+    if (NQ == 1) {
+      x = add_8_on(x);
+      y = add_8_on(y);
+      uint32_t h = pack2<F16>(x, y);
+      asm("" : "+v"(h));
+      *hi = pack2<F16>(less<F16>(x, h, lo_part), less<F16>(y, h >> 16, lo_part));
+    } else {
+      split2<F16>(x, y, hi, lo);
+    }
+  };
+  auto prepare_weights = [&](uint4v (&f)[2][2]) __attribute__((always_inline)) {
+    if (!__is_same(T, F16))
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) f[v][e][i] = to_f16<T>(f[v][e][i], shift);
+  };
+  auto fold = [&](int n) __attribute__((always_inline)) {
+    Nodes v;
+    nodes_of(span_of(n), v);
+    uint4v f[2][2][2];
+    fold_weights(0, f[0]);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
+      if (ks + 1 < KS && (SL == 1 || ks + 1 < ks_here)) fold_weights(ks + 1, f[(ks + 1) & 1]);
       if (SL == 2 && ks >= ks_here) {          // channels behind the rank
 #pragma unroll
         for (int l = 0; l < NG; ++l) G[ks][l] = uint4v{0, 0, 0, 0};
         continue;
       }
-      uint4v F[2][2];
-      fold_weights(ks, F);
-      if (!__is_same(T, F16))
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int v = 0; v < 2; ++v)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) F[v][e][i] = to_f16<T>(F[v][e][i], shift);
+      prepare_weights(f[ks & 1]);
 #pragma unroll
       for (int l = 0; l < LG; ++l) {
-        float4v d[2];
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          d[v] = mma<F16>(F[v][0], va[l][0], float4v{0, 0, 0, 0});
-          d[v] = mma<F16>(F[v][1], vb[l][0], d[v]);
-          if (NQ > 1) {
-            d[v] = mma<F16>(F[v][0], va[l][1], d[v]);
-            d[v] = mma<F16>(F[v][1], vb[l][1], d[v]);
-          }
-        }
+        const float4v d0 = fold_tile(f[ks & 1][0], v, l), d1 = fold_tile(f[ks & 1][1], v, l);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          float x = d[0][u], y = d[1][u];
-          if (NQ == 1) {
-            x = add_8_on(x);
-            y = add_8_on(y);
-          }
-          uint32_t h, lo;
-          split2<F16>(x * g_scale[l], y * g_scale[l], &h, &lo);
-          if (NQ == 1) {
-            G[ks][0][u] = col >= 8 ? lo : h;
-          } else {
-            G[ks][2 * l][u] = h;
-            G[ks][(2 * l + 1) % NG][u] = lo;
-          }
+          uint32_t hi, lo = 0;
+          fold_pack(d0[u], d1[u], &hi, &lo);
+          G[ks][NQ == 1 ? 0 : 2 * l][u] = hi;
+          if (NQ > 1) G[ks][(2 * l + 1) % NG][u] = lo;
         }
       }
     }
@@ -560,8 +627,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   // zero-points that are no small integers: as operands of their own, the same for all channels of block b, times x
   auto zero_points = [&](Sums& a, int n, int sub, int b, float x) __attribute__((always_inline)) {
     const int block = SL == 1 ? hg * NB + b : min(2 * slice + b, k_cols / 128 - 1);
-    const float left = k_left[((n & 1) * 4 + block) * kSteps + 16 * sub + col];
-    const uint32_t w = pack2<F16>(-left, -left);
+    const uint32_t z = k_zero[((n & 3) * 4 + block) * kSteps + 16 * sub + col], w = __builtin_amdgcn_perm(z, z, 0x03020302u);
     Sums more;
     clear(more);
 #pragma unroll
@@ -603,9 +669,10 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     pair_adds(a, p, part);
     pair_turns(p);
   };
+  const int my_basis = ld.basis + (col * 8 + 4 * (kg & 1)) * 4;
   auto basis_of = [&](int n, int sub) __attribute__((always_inline)) {
-    const int t = pos_of(n) + 16 * sub + col - (n < steps_s ? kPagedTile * i0 : pos_w);
-    return *reinterpret_cast<const float4v*>(lds + ld.basis + ((t & (kSteps * a.span_steps - 1)) * 8 + 4 * (kg & 1)) * 4);
+    const int step = (n < steps_s ? n : n - steps_s) & (a.span_steps - 1);
+    return *reinterpret_cast<const float4v*>(lds + my_basis + (step * kSteps + 16 * sub) * 32);
   };
   auto folded = [&](const Sums& a, float4v basis, float scale, float (&part)[NQ]) __attribute__((always_inline)) {
 #pragma unroll
@@ -625,7 +692,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) product(a, 4 * b + i, operand(n, sub, 4 * b + i));
-      if (flags[n & 1]) zero_points(a, n, sub, b, 1.f);
+      if (flags[n & 3]) zero_points(a, n, sub, b, 1.f);
       if (b + 1 < NB) scale_sums(a, tok.x);
     }
 #pragma unroll
@@ -655,7 +722,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   float* const scores = reinterpret_cast<float*>(lds + ld.scores);
   struct Weights {                             // of step n's rows, on the way to LDS
     float x[NQ], u[NQ][MAXCB];
-    float2 tok[MAXCB];
+    uint32_t tok[MAXCB];                       // scale, zero-point
     bool seen;
   };
   // Scores and what of them the blocks' values weigh, masked; running maxima
@@ -663,7 +730,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     w.seen = attended(n, pos_of(n) + lane);
 #pragma unroll
     for (int b = 0; b < MAXCB; ++b)
-      if (b < 2 || b < CB) w.tok[b] = v_tok[((n & 3) * CB + min(b, CB - 1)) * kSteps + lane];
+      if (b < CB) w.tok[b] = v_tok[((n & 3) * CB + b) * kSteps + lane];
     bool rises = false;
 #pragma unroll
     for (int r = 0; r < NQ; ++r) {
@@ -671,8 +738,8 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
       rises = rises || w.x[r] > run_max[r] + kSlack;
 #pragma unroll
       for (int b = 0; b < MAXCB; ++b)
-        if (b < 2 || b < CB) {
-          w.u[r][b] = w.x[r] + (float)__builtin_amdgcn_frexp_expf(w.tok[b].x);
+        if (b < CB) {
+          w.u[r][b] = w.x[r] + (float)__builtin_amdgcn_frexp_expf(F16::to_float((uint16_t)w.tok[b]));
           rises = rises || w.u[r][b] > blk_max[r][b] + kSlack;
         }
     }
@@ -685,12 +752,12 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
         run_max[r] = now;
 #pragma unroll
         for (int b = 0; b < MAXCB; ++b)
-          if (b < 2 || b < CB) {
+          if (b < CB) {
             const float top = fmaxf(blk_max[r][b], max_of_wave(w.u[r][b]));
             const float alpha = __builtin_amdgcn_exp2f(blk_max[r][b] - (top == -INFINITY ? 0.f : top));
             z_sum[r][b] *= alpha;
             blk_max[r][b] = top;
-            if (lane == 0) alphas[min(b, CB - 1) * 16 + r] = alpha;
+            if (lane == 0) alphas[b * 16 + r] = alpha;
           }
       }
     } else if (lane < CB) {
@@ -703,15 +770,15 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     asm volatile("" : "+v"(run_sum[r]));
   };
   auto weight = [&](const Weights& w, int r, int b) __attribute__((always_inline)) {
-    const float y = __builtin_amdgcn_frexp_mantf(w.tok[b].x) * kWeightScale * __builtin_amdgcn_exp2f(w.u[r][b] - (blk_max[r][b] == -INFINITY ? 0.f : blk_max[r][b]));
+    const float y = __builtin_amdgcn_frexp_mantf(F16::to_float((uint16_t)w.tok[b])) * kWeightScale * __builtin_amdgcn_exp2f(w.u[r][b] - (blk_max[r][b] == -INFINITY ? 0.f : blk_max[r][b]));
     return w.seen ? y : 0.f;
   };
   auto put_weight = [&](int n, const Weights& w, int r, int b, float y) __attribute__((always_inline)) {
-    z_sum[r][b] += w.seen ? y * (w.tok[b].y - 8.f) : 0.f;
+    z_sum[r][b] += w.seen ? y * (F16::to_float((uint16_t)(w.tok[b] >> 16)) - 8.f) : 0.f;
     asm volatile("" : "+v"(z_sum[r][b]));
     uint32_t hi, lo;
     split2<F16>(y, 0.f, &hi, &lo);
-    uint16_t* P = reinterpret_cast<uint16_t*>(lds + ld.p + (n & 1) * ld.p_size + min(b, CB - 1) * ld.p_cb + (hw * NQ + r) * kPagedQProbPitch) + lane;
+    uint16_t* P = reinterpret_cast<uint16_t*>(lds + ld.p + (n & 1) * ld.p_size + b * ld.p_cb + (hw * NQ + r) * kPagedQProbPitch) + lane;
     P[0] = (uint16_t)hi;
     P[kLoRows * (kPagedQProbPitch / 2)] = (uint16_t)lo;
   };
@@ -798,25 +865,38 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     clear(sums[1]);
     float part[4][NQ];
     constexpr int kPer = 4 + NG, kSlots = KS * kPer;         // matrix instructions of a step of channels, of a sub-tile
+    // What a sub-tile begins with: its first operands, its tokens' scales, the basis of the one before it; requested in the middle of that one
+    uint4v h[3];
+    float2 tok_now = {}, tok_before = {};
+    float4v basis = {};
+    auto first_operands = [&](int n) __attribute__((always_inline)) {
+      h[0] = operand(n, 0, 0);
+      h[1] = operand(n, 0, 1);
+      tok_now = tok_of(n, 0);
+      basis = basis_of(n - 1, 3);
+    };
+    float early[NQ];                           // the scores of the last sub-tile of step n - 1
     // products of sub-tile SUB of step n, the scores of the sub-tile before it and MORE pieces of something else between them
     auto sub_tile = [&](auto sub_c, int n, bool left, auto more_c, auto&& more) __attribute__((always_inline)) {
       constexpr int SUB = decltype(sub_c)::value, MORE = decltype(more_c)::value;
+      uint4v h_next[2] = {};
       Sums& now = sums[SUB & 1];
       const Sums& before = sums[(SUB + 1) & 1];
-      float (&scores_before)[NQ] = part[(SUB + 3) & 3];
-      const int n_before = SUB == 0 ? n - 1 : n;
-      uint4v h[3];
-      h[0] = operand(n, SUB, 0);
-      h[1] = operand(n, SUB, 1);
-      const float ratio = NB == 2 ? tok_of(n, SUB).x : 1.f;
-      const float scale_before = tok_of(n_before, (SUB + 3) & 3).y;
-      const float4v basis = basis_of(n_before, (SUB + 3) & 3);
+      float (&scores_before)[NQ] = *(SUB == 0 ? &early : &part[(SUB + 3) & 3]);
+      const float ratio = NB == 2 ? tok_now.x : 1.f, scale_before = tok_before.y;
+      const float4v basis_before = basis;
+      tok_before = tok_now;
       clear(now);
 #pragma unroll
       for (int r = 0; r < NQ; ++r) scores_before[r] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         if (ks + 2 < KS) h[(ks + 2) % 3] = operand(n, SUB, ks + 2);
+        if (SUB < 3 && ks + 2 >= KS) h_next[ks + 2 - KS] = operand(n, SUB < 3 ? SUB + 1 : SUB, ks + 2 - KS);
+        if (SUB < 3 && ks == KS / 2) {
+          tok_now = tok_of(n, SUB < 3 ? SUB + 1 : SUB);
+          basis = basis_of(n, SUB);
+        }
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
           float4v& sum = j < 4 ? now.acc[j] : now.low[NQ == 1 ? 0 : (j - 4) / 2];
@@ -833,9 +913,11 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      folded(before, basis, scale_before, scores_before);
+      folded(before, basis_before, scale_before, scores_before);
 #pragma unroll
       for (int r = 0; r < NQ; ++r) asm volatile("" : "+v"(scores_before[r]));
+      h[0] = h_next[0];
+      h[1] = h_next[1];
       if (left) {
         zero_points(now, n, SUB, 0, ratio);
         if (NB == 2) zero_points(now, n, SUB, NB - 1, 1.f);
@@ -851,25 +933,55 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
       asm volatile("" : "+v"(out[u]));
       if (u == 3) *reinterpret_cast<uint4v*>(to[c] + shift_bytes) = out;
     };
+    // One query row: a quarter of the next span's folded weights in every step of a span of four
+    constexpr bool AHEAD = NQ == 1;
+    constexpr int kAhead = KS / 4;             // steps of channels
+    uint4v H[AHEAD ? KS : 1];
+    Nodes nodes;
+    int ready = 0;                             // steps of channels that are folded
     for (int n = 0; n < n_steps; ++n) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what interval n - 1 requested
-      const half2v off0 = minus_zero(zraw[0]), off1 = minus_zero(zraw[1]);
-      const bool left = __builtin_amdgcn_readfirstlane(flags[n & 1]) != 0;
-      if (n + 1 < n_steps) put_tokens(n + 1);
-      if (wave == 3 && n + 3 < n_steps) put_rows(n + 3, entry);
-      if (n + 2 < n_steps) request_keys(n + 2);
-      request_values(n);
-      if (wave == 3 && n + 4 < n_steps) entry = entry_of(n + 4);
-      if (folds(n)) fold(n);
+      first_operands(n);
+      const bool left = __builtin_amdgcn_readfirstlane(flags[n & 3]) != 0;
       // (behind the last step: codes of the one before it, converted into a buffer that nobody reads)
       const uint4v raw0 = raw_codes(n + 1, 0), raw1 = raw_codes(n + 1, two ? 1 : 0);
+      const half2v off0 = zero_of(n + 1, x0, pc), off1 = zero_of(n + 1, two ? x0 + 32 : x0, pc);
+      put(n);
+      if (n + 2 < n_steps) request_keys(n + 2);
+      request_values(n);
+      request(n);
+      const int k = span_of(n);
+      const bool begins = folds(n), ahead = AHEAD && a.span_steps == 4 && span_step(k + 1) < n_steps;
+      const int quarter_of_span = (n < steps_s ? n : n - steps_s) & 3;
+      if (begins) {
+        if (AHEAD && ready == KS) {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) G[ks][0] = H[ks % (AHEAD ? KS : 1)];
+        } else {
+          fold(n);
+        }
+        ready = 0;
+        if (ahead) nodes_of(k + 1, nodes);
+      }
       const int next = ((n + 1) & 1) * ld.k_size, next1 = two ? next + 32 * ld.k_pitch : next;
       sub_tile(IntC<0>(), n, left, IntC<16>(), [&](int q) __attribute__((always_inline)) { conversion(q, raw0, off0, next); });
-      if (folds(n)) start(n);
+      if (begins) start(n);
       Weights w;
+      float x[NQ], half_sums[NQ][2], first[NQ];
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) first[r] = part[0][r];    // (sub-tile 1 makes another one)
+      constexpr int kScores = NQ * 3;          // a row: halves of its scores by lane groups, wholes
+      sub_tile(IntC<1>(), n, left, IntC<kScores + 16>(), [&](int q) __attribute__((always_inline)) {
+        if (q >= kScores) {
+          conversion(q - kScores, raw1, off1, next1);
+        } else {
+          const int r = q / 3;
+          if (q % 3 < 2) half_sums[r][q % 3 & 1] = q % 3 == 0 ? add_swapped32(first[r], part[2][r]) : add_swapped32(part[1][r], early[r]);
+          else x[r] = add_swapped16(half_sums[r][0], half_sums[r][1]);
+          if (q % 3 < 2) asm volatile("" : "+v"(half_sums[r][q % 3 & 1]));
+        }
+      });
       if (n > 0) {
-        float x[NQ];
-        whole_scores(part, x);
         weigh(n - 1, x, w);
       } else {                                 // no step before: weights of zero
         w.seen = false;
@@ -880,36 +992,30 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
           for (int b = 0; b < MAXCB; ++b) w.u[r][b] = -INFINITY;
         }
 #pragma unroll
-        for (int b = 0; b < MAXCB; ++b) w.tok[b] = make_float2(0.f, 0.f);
+        for (int b = 0; b < MAXCB; ++b) w.tok[b] = 0;
       }
-      float y = 0.f;
-      constexpr int kWeights = NQ * 5;         // a row: its sum, two blocks' weights and their way to LDS
-      sub_tile(IntC<1>(), n, left, IntC<16 + kWeights>(), [&](int q) __attribute__((always_inline)) {
-        if (q >= kWeights) {
-          conversion(q - kWeights, raw1, two ? off1 : off0, next1);
-        } else {
-          const int r = q / 5, k = q % 5;
-          if (k == 0) {
-            add_sum(w, r);
-          } else if (k & 1) {
-            y = weight(w, r, k >> 1);
-            asm volatile("" : "+v"(y));
-          } else {
-            put_weight(n - 1, w, r, (k >> 1) - 1, y);
-          }
-        }
-      });
-      if (CB > 2 && n > 0) {
+      uint4v f[kAhead][2][2];
+      if (ahead) {
 #pragma unroll
-        for (int r = 0; r < NQ; ++r)
-#pragma unroll
-          for (int b = 2; b < MAXCB; ++b)
-            if (b < CB) put_weight(n - 1, w, r, b, weight(w, r, b));
+        for (int i = 0; i < kAhead; ++i) fold_weights(quarter_of_span * kAhead + i, f[i]);
       }
-      rescale(n);                              // (of n - 2; in the first two intervals there are no weights and nothing to rescale)
       Values v;
       fetch_values(n - 2, half0 & 1, v);
-      sub_tile(IntC<2>(), n, left, IntC<20>(), [&](int q) __attribute__((always_inline)) {
+      float y = 0.f;
+      constexpr int kRow = 1 + 2 * MAXCB, kWeights = NQ * kRow;          // a row: its sum, the blocks' weights and their way to LDS
+      sub_tile(IntC<2>(), n, left, IntC<kWeights>(), [&](int q) __attribute__((always_inline)) {
+        const int r = q / kRow, k = q % kRow;
+        if (k == 0) {
+          add_sum(w, r);
+        } else if (k & 1) {
+          y = weight(w, r, k >> 1);
+          asm volatile("" : "+v"(y));
+        } else {
+          put_weight(n - 1, w, r, (k >> 1) - 1, y);
+        }
+      });
+      rescale(n);                              // (of n - 2; in the first two intervals there are no weights and nothing to rescale)
+      sub_tile(IntC<3>(), n, left, IntC<20>(), [&](int q) __attribute__((always_inline)) {
         if (q % 5 < 4) {
           value_codes(v, q / 5, q % 5);
           asm volatile("" : "+v"(v.even[q % 5 & 3]), "+v"(v.odd[q % 5 & 3]));
@@ -918,7 +1024,26 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
         }
       });
       if (CB > 2) value_half(n - 2, 1);
-      sub_tile(IntC<3>(), n, left, IntC<0>(), [&](int) __attribute__((always_inline)) {});
+      if (ahead) {
+        uint4v hi[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          prepare_weights(f[i]);
+          const float4v d0 = fold_tile(f[i][0], nodes, 0), d1 = fold_tile(f[i][1], nodes, 0);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            uint32_t h, lo = 0;
+            fold_pack(d0[u], d1[u], &h, &lo);
+            hi[i][u] = h;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (quarter_of_span == c)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) H[(c * kAhead + i) % (AHEAD ? KS : 1)] = hi[i];
+        ready += kAhead;
+      }
       lds_barrier();
     }
     {                                          // the last step's scores and values, and those of the one before it
@@ -938,12 +1063,8 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
   } else {
   for (int n = 0; n <= n_steps; ++n) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // what interval n - 1 requested
-    uint16_t z_now[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) z_now[i] = zraw[i];
-    if (n + 1 < n_steps) put_tokens(n + 1);
-    if (wave == 3 && n + 3 < n_steps) put_rows(n + 3, entry);
-    if (wave == 3 && n + 4 < n_steps) entry = entry_of(n + 4);
+    put(n);
+    request(n);
     if (n > 0) values(n - 1);
     if (n == n_steps) break;
     if (folds(n)) {
@@ -961,7 +1082,7 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
     if (n + 1 < n_steps) request_values(n + 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (n + 1 < n_steps && i * 128 < k_cols) convert(n + 1, i, z_now[i]);
+      if (n + 1 < n_steps && i * 128 < k_cols) convert(n + 1, i);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the raw codes have been read)
     if (n + 2 < n_steps) request_keys(n + 2);
     if (SL == 2)
@@ -1021,9 +1142,14 @@ __global__ __launch_bounds__(kPagedQThreads, 1) void pagedq_kernel(PagedQArgs a)
 }
 
 namespace {
+template <typename T, int NQ, int KS, int KB> PagedQFn pick_piped(int v_blocks) {
+  if constexpr (NQ <= kPagedQPipedRows)
+    return v_blocks == 1 ? pagedq_kernel<T, KS, 1, NQ, true, KB, 1> : (v_blocks == 2 ? pagedq_kernel<T, KS, 1, NQ, true, KB, 2> : pagedq_kernel<T, KS, 1, NQ, true, KB, 3>);
+  return nullptr;
+}
 template <typename T, int NQ> PagedQFn pick(const PagedQForm& f) {
   if (f.slices == 2) return pagedq_kernel<T, 8, 2, NQ, false>;
-  if (f.piped) return f.ks == 4 ? pagedq_kernel<T, 4, 1, NQ, true> : pagedq_kernel<T, 8, 1, NQ, true>;
+  if (f.piped) return f.ks == 8 ? pick_piped<T, NQ, 8, 2>(f.v_blocks) : (f.k_blocks == 2 ? pick_piped<T, NQ, 4, 2>(f.v_blocks) : pick_piped<T, NQ, 4, 1>(f.v_blocks));
   return f.ks == 4 ? pagedq_kernel<T, 4, 1, NQ, false> : pagedq_kernel<T, 8, 1, NQ, false>;
 }
 }  // namespace

@@ -48,12 +48,14 @@ struct PagedQClass {
   int lds_bytes, n_units;
   PagedUnit units[PALU_MAX_HEADS];
 };
+// (key ranks of 128, in one group or two, 256, in either number of value blocks; 256 and above, and what does not fit)
+constexpr int kPagedQMaxClasses = 3 * kPagedQPipedBlocks + 3;
 struct PagedQCall {
   PagedMeta meta;
   int n_sink, max_tiles, chunk_tiles, n_slots;
   int span_steps;                              // 0: the plain kernel
   int n_cls, n_row_blocks;
-  PagedQClass cls[3];                          // key ranks 128, 256, above
+  PagedQClass cls[kPagedQMaxClasses];
   long long o_stride;
   size_t ml_at, total;
 };
@@ -85,35 +87,39 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
   c->n_cls = 0;
   const int rows = m.qpk <= 2 ? m.qpk : 4;
   c->n_row_blocks = ceil_div(m.qpk, rows);
-  for (int k = 0; k < 3 && c->span_steps > 0; ++k) {
-    auto in_class = [&](int j) { return k == 2 ? rk(j) > 256 : rk(j) == 128 * (k + 1); };
-    PagedQClass& cl = c->cls[c->n_cls];
-    cl.form = PagedQForm{k == 0 ? 4 : 8, k == 2 ? 2 : 1, rows, k < 2};
-    cl.n_units = 0;
-    int lds[2] = {0, 0};
-    const int unit_heads = 4 / cl.form.slices;
-    for (int first = 0;; first += unit_heads) {              // as for unquantized latents: whole adjacent groups side by side, or parts of one
-      bool more = false;
-      for (int j = 0; j < m.n_groups; ++j) {
-        if (!in_class(j) || first >= heads(j)) continue;
-        int n = 1;
-        while (j + n < m.n_groups && rk(j + n) == rk(j) && rv(j + n) == rv(j) && heads(j + n) == heads(j) && (n + 1) * heads(j) <= unit_heads &&
-               (n + 1) * rk(j) <= 256 && (n + 1) * rv(j) <= 256)
-          ++n;
-        more = true;
-        const int nh = std::min(unit_heads, n * heads(j) - first);
-        cl.units[cl.n_units++].bits = (uint32_t)(m.head_off[j] + first) | (uint32_t)nh << 8 | (uint32_t)j << 16 | (uint32_t)n << 24;
-        for (int piped = 0; piped < 2; ++piped) lds[piped] = std::max(lds[piped], pagedq_lds(n * rk(j), n * rv(j), cl.form.slices, rows, piped).total);
-        j += n - 1;
+  // Units, as for unquantized latents: whole adjacent groups side by side, or parts of one
+  auto side_by_side = [&](int j, int unit_heads) {           // groups from j on
+    int n = 1;
+    while (j + n < m.n_groups && rk(j + n) == rk(j) && rv(j + n) == rv(j) && heads(j + n) == heads(j) && (n + 1) * heads(j) <= unit_heads &&
+           (n + 1) * rk(j) <= 256 && (n + 1) * rv(j) <= 256)
+      ++n;
+    return n;
+  };
+  for (int first = 0, more = c->span_steps > 0; more; first += 4) {      // heads of a group (or of groups side by side) from `first` on
+    more = 0;
+    for (int j = 0, n; j < m.n_groups; j += n) {
+      PagedQForm f{rk(j) == 128 ? 4 : 8, rk(j) > 256 ? 2 : 1, rows, 0, 0, 0};
+      n = side_by_side(j, 4 / f.slices);
+      f.k_blocks = n * rk(j) / 128;
+      f.v_blocks = n * rv(j) / 128;
+      f.piped = f.slices == 1 && f.v_blocks <= kPagedQPipedBlocks && rows <= kPagedQPipedRows;
+      if (!f.piped) f.k_blocks = f.v_blocks = 0;
+      PagedQClass* cl = nullptr;
+      for (int k = 0; k < c->n_cls; ++k)
+        if (std::memcmp(&c->cls[k].form, &f, sizeof(f)) == 0) cl = &c->cls[k];
+      for (int h = first; h < std::min(first + 4, n * heads(j)); h += 4 / f.slices) {
+        if (!cl) {
+          cl = &c->cls[c->n_cls++];
+          std::memset(cl, 0, sizeof(*cl));
+          std::memcpy(&cl->form, &f, sizeof(f));
+          cl->lds_bytes = pagedq_lds(f.ks, f.slices, f.rows, f.k_blocks, f.v_blocks, f.piped).total;
+        }
+        const int nh = std::min(4 / f.slices, n * heads(j) - h);
+        cl->units[cl->n_units++].bits = (uint32_t)(m.head_off[j] + h) | (uint32_t)nh << 8 | (uint32_t)j << 16 | (uint32_t)n << 24;
+        ++units;
       }
-      if (!more) break;
+      more = more || first + 4 < n * heads(j);
     }
-    if (cl.n_units == 0) continue;
-    cl.form.piped = cl.form.piped && lds[1] <= kPagedLdsBytes;
-    cl.lds_bytes = lds[cl.form.piped];
-    if (cl.lds_bytes > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;
-    units += cl.n_units;
-    ++c->n_cls;
   }
   const int cus = device_cu_count();
   if (c->span_steps == 0) {
