@@ -41,13 +41,12 @@ static_assert(sizeof(PagedQArgs) <= 4096, "kernel arguments");
 using PagedQFn = void (*)(PagedQArgs);
 constexpr int kPagedQThreads = 256;
 PagedQFn pagedq_plain_form(int act);
-// The instantiations, by ks: steps of 32 key channels of a wavefront, 4 or 8; slices: wavefronts that share a head's channels (2: ranks above
-// 256); rows: query rows of a head, 1, 2 or 4; piped: several steps at work at once, where LDS holds what that takes, for k_blocks and v_blocks blocks
-// of 128 key and value columns of a unit (else up to 2 * slices and 4)
+// The instantiations, by ks: steps of 32 key channels of a wavefront, 4 or 8; slices: parts of a head's channels (2: ranks above 256); rows: query
+// rows of a head, 1, 2 or 4; k_blocks, v_blocks: of 128 key and value columns of a unit, at most
 struct PagedQForm {
-  int ks, slices, rows, k_blocks, v_blocks, piped;
+  int ks, slices, rows, k_blocks, v_blocks;
 };
-constexpr int kPagedQPipedBlocks = 3, kPagedQPipedRows = 2;
+constexpr int kPagedQMaxClasses = 8;
 template <int ROWS> PagedQFn pagedq_rows_form(int act, const PagedQForm& f);
 template <> PagedQFn pagedq_rows_form<1>(int, const PagedQForm&);
 template <> PagedQFn pagedq_rows_form<2>(int, const PagedQForm&);
@@ -56,41 +55,48 @@ inline PagedQFn pagedq_form(int act, const PagedQForm& f) {
   return f.rows == 1 ? pagedq_rows_form<1>(act, f) : (f.rows == 2 ? pagedq_rows_form<2>(act, f) : pagedq_rows_form<4>(act, f));
 }
 
+constexpr int kPagedQFoldThreads = 512;        // of pagedq_kernel
+
+// Whether an interval has two parts with a barrier between: one step's keys in LDS at a time, weights and values a step earlier (pagedq_kernel)
+__host__ __device__ constexpr bool pagedq_two_phases(int slices, int rows, int v_blocks) { return slices == 2 || (rows > 1 && v_blocks == 4); }
+
+__host__ __device__ constexpr int pagedq_key_scales(int ks, int k_blocks) { return k_blocks * 4 / ks; }
+
 // LDS of a workgroup, in bytes from its start
 struct PagedQLds {
-  int k_pitch;               // bytes per staged key row: k_cols float16 numbers
-  int k_size, raw_size, v_size;                // of a step's keys, raw key codes, raw value codes
-  int k, raw, v, p, p_cb, p_size, alpha, k_tok, k_zero, v_tok, basis, anchors, rows, scores, flags, total;
+  int k_pitch;               // bytes per staged key row: float16 numbers
+  int k_size, v_size;        // of a step's keys, raw value codes
+  int k, v, p, p_cb, p_size, alpha, k_tok, k_zero, v_tok, basis, anchors, rows, scores, nodes, turns, q, stage, flags, total;
 };
-constexpr int kPagedQProbPitch = kPagedQStep * 2 + 16;
-__host__ __device__ constexpr PagedQLds pagedq_lds(int k_cols, int v_cols, int slices, int rows, bool piped) {
+constexpr int kPagedQProbPitch = kPagedQStep * 2 + 16, kPagedQTurnPitch = 2 * kPagedQLow * 4 + 16;
+__host__ __device__ constexpr PagedQLds pagedq_lds(const PagedQForm& f) {
   PagedQLds l = {};
-  const int blocks = v_cols / 128, bufs = piped ? 2 : 1, p_rows = rows == 1 ? 8 : (slices == 1 ? 32 : 16);
-  l.k_pitch = k_cols * 2;
+  const bool two = pagedq_two_phases(f.slices, f.rows, f.v_blocks);
+  const int p_rows = f.rows == 1 ? 8 : (f.slices == 1 ? 32 : 16);
+  l.k_pitch = 256 * f.k_blocks;
   l.k_size = kPagedQStep * l.k_pitch;
-  l.raw_size = kPagedQStep * k_cols / 2;
-  l.v_size = kPagedQStep * v_cols / 2;
-  l.k = 0;
-  l.raw = l.k + bufs * l.k_size;
-  l.v = l.raw + bufs * l.raw_size;
-  l.p = l.v + (piped ? 3 : 2) * l.v_size;
+  l.v_size = kPagedQStep * 64 * f.v_blocks;
   l.p_cb = p_rows * kPagedQProbPitch;          // probabilities of a block of value columns
-  l.p_size = blocks * l.p_cb;
-  l.alpha = l.p + 2 * l.p_size;                // [2][blocks][16]
-  l.k_tok = l.alpha + 2 * blocks * 16 * 4;     // [4][2][64]: ratio and scale, by slice or group
-  l.k_zero = l.k_tok + kPagedQStep * 4 * 2 * 8;        // [4][4][64]: the zero-point for the codes, what is left of it
-  l.v_tok = l.k_zero + kPagedQStep * 4 * 4 * 4;        // [4][blocks][64]: scale, zero-point
-  l.basis = l.v_tok + kPagedQStep * 4 * blocks * 4;
-  l.anchors = l.basis + kPagedQSpan * kPagedQNodes * 4;        // [4]
+  l.p_size = f.v_blocks * l.p_cb;
+  // (the small ones first, within the 64 KiB that an instruction's offset reaches)
+  l.alpha = 0;                                 // [2][blocks][16]
+  l.k_tok = l.alpha + 2 * f.v_blocks * 16 * 4; // [4][slices or groups][64]: ratio and scale
+  l.k_zero = l.k_tok + kPagedQStep * 4 * pagedq_key_scales(f.ks, f.k_blocks) * 8;      // [4][blocks][64]: the zero-point for the codes, what is left of it
+  l.v_tok = l.k_zero + kPagedQStep * 4 * f.k_blocks * 4;       // [4][blocks][64]: scale, zero-point
+  l.anchors = l.v_tok + kPagedQStep * 4 * f.v_blocks * 4;      // [4]
   l.rows = l.anchors + 4 * kDHead * 4;                 // [8][64]
-  l.scores = l.rows + 8 * kPagedQStep * 4;
-  l.flags = l.scores + (slices == 1 ? 0 : 2 * rows * kPagedQStep * 4);
-  l.total = l.flags + 16;
+  l.scores = l.rows + 8 * kPagedQStep * 4;             // [2 or 1][heads * rows][parts][64]
+  l.nodes = l.scores + (two ? 1 : 2) * (4 / f.slices) * f.rows * (2 * f.slices) * kPagedQStep * 4;
+  l.turns = l.nodes + kPagedQNodes * kPagedQTurnPitch; // cos and sin of the folded pairs from a span's begin to its nodes
+  l.q = l.turns + 16 * kPagedQTurnPitch;               // of the others from a sub-tile's begin to its tokens
+  l.stage = l.q + (4 / f.slices) * f.rows * kDHead * 4;        // [heads * rows][128]
+  l.flags = l.stage + (2 * f.k_blocks + 2 * f.v_blocks + 1) * kPagedQStep * 4;         // scales and zero-points, page entries on their way
+  l.basis = l.flags + 16;
+  l.p = l.basis + kPagedQSpan * kPagedQNodes * 4;
+  l.v = l.p + 2 * l.p_size;
+  l.k = l.v + (two ? 2 : 3) * l.v_size;
+  l.total = l.k + (two ? 1 : 2) * l.k_size;
   return l;
-}
-
-__host__ __device__ constexpr PagedQLds pagedq_lds(int ks, int slices, int rows, int k_blocks, int v_blocks, bool piped) {
-  return pagedq_lds(128 * (piped ? k_blocks : 2 * slices), 128 * (piped ? v_blocks : 4), slices, rows, piped);
 }
 
 }  // namespace palu

@@ -48,8 +48,8 @@ struct PagedQClass {
   int lds_bytes, n_units;
   PagedUnit units[PALU_MAX_HEADS];
 };
-// (key ranks of 128, in one group or two, 256, in either number of value blocks; 256 and above, and what does not fit)
-constexpr int kPagedQMaxClasses = 3 * kPagedQPipedBlocks + 3;
+// (key ranks of 128, in one group or two, 256, above; one or two, three or four value blocks)
+static_assert(kPagedQMaxClasses == 4 * 2, "classes");
 struct PagedQCall {
   PagedMeta meta;
   int n_sink, max_tiles, chunk_tiles, n_slots;
@@ -85,7 +85,9 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
   c->o_stride = sum_rv * m.qpk;
   c->span_steps = pagedq_span_steps(desc->rope_theta);
   c->n_cls = 0;
-  const int rows = m.qpk <= 2 ? m.qpk : 4;
+  bool sliced = false;
+  for (int j = 0; j < m.n_groups; ++j) sliced = sliced || rk(j) > 256;
+  const int rows = m.qpk <= 2 || sliced ? std::min(m.qpk, 2) : 4;       // (LDS does not hold four rows' parts of two slices)
   c->n_row_blocks = ceil_div(m.qpk, rows);
   // Units, as for unquantized latents: whole adjacent groups side by side, or parts of one
   auto side_by_side = [&](int j, int unit_heads) {           // groups from j on
@@ -98,12 +100,10 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
   for (int first = 0, more = c->span_steps > 0; more; first += 4) {      // heads of a group (or of groups side by side) from `first` on
     more = 0;
     for (int j = 0, n; j < m.n_groups; j += n) {
-      PagedQForm f{rk(j) == 128 ? 4 : 8, rk(j) > 256 ? 2 : 1, rows, 0, 0, 0};
+      PagedQForm f{rk(j) == 128 ? 4 : 8, rk(j) > 256 ? 2 : 1, rows, 0, 0};
       n = side_by_side(j, 4 / f.slices);
-      f.k_blocks = n * rk(j) / 128;
-      f.v_blocks = n * rv(j) / 128;
-      f.piped = f.slices == 1 && f.v_blocks <= kPagedQPipedBlocks && rows <= kPagedQPipedRows;
-      if (!f.piped) f.k_blocks = f.v_blocks = 0;
+      f.k_blocks = f.slices == 2 ? 4 : n * rk(j) / 128;
+      f.v_blocks = std::max(2, n * rv(j) / 128 + (n * rv(j) / 128 == 3));      // 2 or 4
       PagedQClass* cl = nullptr;
       for (int k = 0; k < c->n_cls; ++k)
         if (std::memcmp(&c->cls[k].form, &f, sizeof(f)) == 0) cl = &c->cls[k];
@@ -112,7 +112,8 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
           cl = &c->cls[c->n_cls++];
           std::memset(cl, 0, sizeof(*cl));
           std::memcpy(&cl->form, &f, sizeof(f));
-          cl->lds_bytes = pagedq_lds(f.ks, f.slices, f.rows, f.k_blocks, f.v_blocks, f.piped).total;
+          cl->lds_bytes = pagedq_lds(f).total;
+          if (cl->lds_bytes > kPagedLdsBytes) return PALU_ERR_UNSUPPORTED;
         }
         const int nh = std::min(4 / f.slices, n * heads(j) - h);
         cl->units[cl->n_units++].bits = (uint32_t)(m.head_off[j] + h) | (uint32_t)nh << 8 | (uint32_t)j << 16 | (uint32_t)n << 24;
@@ -143,7 +144,7 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
   c->ml_at = align_up((size_t)batch * c->n_slots * c->o_stride * sizeof(float));
   c->total = c->ml_at + align_up((size_t)batch * c->n_slots * m.qpk * m.n_heads * 2 * sizeof(float));
   const long long launched = (long long)batch * c->n_slots * (c->span_steps ? units * c->n_row_blocks : m.n_heads);
-  if (launched * kPagedQThreads > 0xffffffffLL) return PALU_ERR_UNSUPPORTED;
+  if (launched * kPagedQFoldThreads > 0xffffffffLL) return PALU_ERR_UNSUPPORTED;
   return PALU_OK;
 }
 
@@ -267,7 +268,7 @@ int palu_attn_paged_quant(const palu_layer_desc* desc, int32_t batch, int32_t ma
     if ((st = allow_lds(fn, (size_t)cl.lds_bytes)) != PALU_OK) return st;
     a.n_units = cl.n_units;
     std::memcpy(a.units, cl.units, sizeof(PagedUnit) * cl.n_units);
-    hipLaunchKernelGGL(fn, dim3((unsigned)((long long)batch * c.n_slots * c.n_row_blocks * cl.n_units)), dim3(kPagedQThreads), (unsigned)cl.lds_bytes, s, a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)((long long)batch * c.n_slots * c.n_row_blocks * cl.n_units)), dim3(kPagedQFoldThreads), (unsigned)cl.lds_bytes, s, a);
     if ((st = launch_ok()) != PALU_OK) return st;
   }
 
