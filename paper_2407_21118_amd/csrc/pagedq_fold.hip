@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   const PagedMeta& m = a.meta;
   const int tid = threadIdx.x;
   int lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int col = lane & 15, kg = lane >> 4;
   // ---- what this workgroup does
   const PagedUnit un = a.units[blockIdx.x % a.n_units];
@@ -111,12 +111,13 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   const int i0 = (int)((long long)span.n_tiles * chunk / n_chunks), i1 = (int)((long long)span.n_tiles * (chunk + 1) / n_chunks);
   const int g = un.group(), nh = un.nh(), h0 = un.h0();
   const int rk = m.k_off[g + 1] - m.k_off[g], rv = m.v_off[g + 1] - m.v_off[g], per_group = m.head_off[g + 1] - m.head_off[g];
-  const int k_cols = un.n_groups() * rk, v_cols = un.n_groups() * rv, CB = v_cols / 128;
+  int k_cols = un.n_groups() * rk, v_cols = un.n_groups() * rv, CB = v_cols / 128;
   const int row0 = rb * NQ, nr = min(NQ, m.qpk - row0);      // query rows of a head
   const uint32_t lds0 = lds_addr(lds);
 
-  const int hw = wave % HEADS, half = (wave / HEADS) & 1, slice = wave / (2 * HEADS);
-  const int member = wave / HEADS;                           // among a head's wavefronts
+  int hw = wave % HEADS;
+  const int half = (wave / HEADS) & 1, slice = wave / (2 * HEADS);
+  int member = wave / HEADS;                           // among a head's wavefronts
   const int hh = min(hw, nh - 1);                            // (a wavefront without a head does another one's work, results nowhere)
   const int hg = un.n_groups() > 1 ? hh / per_group : 0;     // the head's group in the unit
   const int width = per_group * kDHead;
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
 
   // ---- steps of 64 positions: those of the sinks' tiles first
   const int mid = max(i0, min(i1, span.sink_tiles));
-  const int steps_s = (mid - i0 + 1) / 2, n_steps = steps_s + (i1 - mid + 1) / 2;
+  int steps_s = (mid - i0 + 1) / 2, n_steps = steps_s + (i1 - mid + 1) / 2;
   const int pos_w = kPagedTile * (span.tile0 + mid - span.sink_tiles);     // (where mid < i1)
   auto pos_of = [&](int n) __attribute__((always_inline)) { return n < steps_s ? kPagedTile * i0 + kSteps * n : pos_w + kSteps * (n - steps_s); };
   auto end_of = [&](int n) __attribute__((always_inline)) { return min(L, n < steps_s ? kPagedTile * mid : pos_w + kPagedTile * (i1 - mid)); };
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   // third span after one that begins.
   constexpr int kMasked = 1 << 31;             // a masked token's row, with the number of an attended one's
   int* const rows = reinterpret_cast<int*>(lds + ld.rows);
-  const int k_pieces = k_cols / 32, v_pieces = v_cols / 32;  // 16-byte pieces of a raw row
+  int k_pieces = k_cols / 32, v_pieces = v_cols / 32;  // 16-byte pieces of a raw row
   const int k_block0 = m.k_off[g] / 128, v_block0 = m.v_off[g] / 128;
   // (What a wavefront requests for itself waits in LDS, not in registers, for which the compiler would wait where paths join.)
   auto stage = [&](int i) __attribute__((always_inline)) { return reinterpret_cast<uint32_t*>(lds + ld.stage) + i * kSteps; };
@@ -819,13 +820,13 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   float4v O[NO];                               // column 8 col + (4 quarter +) u of rows 4 kg + e; odd columns in units of 2^-20, even ones of 2^-24
 #pragma unroll
   for (int u = 0; u < NO; ++u) O[u] = float4v{0, 0, 0, 0};
-  const int vb0 = wave & (VB - 1), vb = min(vb0, CB - 1), half0 = VB == 2 ? (wave >> 1) & 1 : wave >> 2, quarter = VB == 2 ? wave >> 2 : 0;
-  const bool has_values = vb0 < CB;
+  int vb0 = wave & (VB - 1), half0 = VB == 2 ? (wave >> 1) & 1 : wave >> 2, quarter = VB == 2 ? wave >> 2 : 0;
   // Codes enter as code - 8: most zero-points are near 8, and sums of codes and of zero-points, which all but cancel over many tokens, would leave their
   // rounding (4e-5 of the largest output at 3000 tokens, against 4e-6).
   const half2v minus8_even = __builtin_bit_cast(half2v, 0x80088008u), minus8_odd = __builtin_bit_cast(half2v, 0x80808080u);
   auto values = [&](int n) __attribute__((always_inline)) {
-    if (!has_values) return;
+    const int vb = vb0;
+    if (vb >= CB) return;
     const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (((n & 1) * VB + vb) * 16 + (NQ == 1 ? 0 : 4 * kg)) * 4);
     const unsigned char* const at = lds + ld.v + n % VBUFS * ld.v_size + (32 * half0 + 8 * kg) * (v_cols / 2) + vb * 64 + col * 4;
     uint32_t d[8];
@@ -861,6 +862,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   uint4v now[KP];
   auto here = [&]() __attribute__((always_inline)) {         // addresses are made where they are used: kept over the loop they fill the registers
     asm volatile("" : "+v"(lane), "+v"(col), "+v"(kg));
+    asm volatile("" : "+s"(wave), "+s"(member), "+s"(hw), "+s"(k_cols), "+s"(v_cols), "+s"(CB), "+s"(k_pieces), "+s"(v_pieces), "+s"(steps_s), "+s"(n_steps), "+s"(vb0), "+s"(half0), "+s"(quarter));
 #pragma unroll
     for (int i = 0; i < KP; ++i) asm volatile("" : "+v"(k_x[i]), "+v"(k_pc[i]), "+v"(now[i]));
 #pragma unroll
@@ -930,7 +932,8 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
       reinterpret_cast<float2*>(a.ml_part)[(slot * m.n_heads + h0 + hw) * m.qpk + row0 + r] = make_float2(run_max[r], sum);
   }
   lds_barrier();
-  if (has_values && half0 == 0) {
+  const int vb = vb0;
+  if (vb < CB && half0 == 0) {
 #pragma unroll
     for (int u = 0; u < NO; ++u) O[u] += *reinterpret_cast<const float4v*>(halves + (u * 64 + lane) * 4);
     const int vg = 128 * vb / rv;              // the columns' group in the unit
