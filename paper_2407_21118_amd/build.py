@@ -40,8 +40,7 @@ def sources():
     units += [("attend16_mixed_forms.hip", VGPR_FORM, "")]
     for act, suffix in (("F16", ""), ("BF16", "_bf16")):
         units += [("paged.hip", VGPR_FORM + ["-DPALU_PAGED_ACT=" + act], suffix)]
-    # (several query rows: more registers than there are ordinary ones, so accumulators take the accumulation registers too)
-    units += [("pagedq_fold.hip", (VGPR_FORM if rows == 1 else VGPR_FORM[2:]) + ["-DPALU_PAGEDQ_ROWS=%d" % rows], "_%d" % rows) for rows in (1, 2, 4)]
+    units += [("pagedq_fold.hip", VGPR_FORM + ["-DPALU_PAGEDQ_ROWS=%d" % rows], "_%d" % rows) for rows in (1, 2)]
     units += [(f, [], "") for f in ("encode_gemm.hip", "cache_rows.hip", "encode_w4.hip")]
     return [(os.path.join(CSRC, f), extra, os.path.splitext(f)[0] + suffix + ".o") for f, extra, suffix in units]
 

@@ -42,7 +42,7 @@ using PagedQFn = void (*)(PagedQArgs);
 constexpr int kPagedQThreads = 256;
 PagedQFn pagedq_plain_form(int act);
 // The instantiations, by ks: steps of 32 key channels of a wavefront, 4 or 8; slices: parts of a head's channels (2: ranks above 256); rows: query
-// rows of a head, 1, 2 or 4; k_blocks, v_blocks: of 128 key and value columns of a unit, at most
+// rows of a head, 1 or 2; k_blocks, v_blocks: of 128 key and value columns of a unit, at most
 struct PagedQForm {
   int ks, slices, rows, k_blocks, v_blocks;
 };
@@ -50,9 +50,8 @@ constexpr int kPagedQMaxClasses = 8;
 template <int ROWS> PagedQFn pagedq_rows_form(int act, const PagedQForm& f);
 template <> PagedQFn pagedq_rows_form<1>(int, const PagedQForm&);
 template <> PagedQFn pagedq_rows_form<2>(int, const PagedQForm&);
-template <> PagedQFn pagedq_rows_form<4>(int, const PagedQForm&);
 inline PagedQFn pagedq_form(int act, const PagedQForm& f) {
-  return f.rows == 1 ? pagedq_rows_form<1>(act, f) : (f.rows == 2 ? pagedq_rows_form<2>(act, f) : pagedq_rows_form<4>(act, f));
+  return f.rows == 1 ? pagedq_rows_form<1>(act, f) : pagedq_rows_form<2>(act, f);
 }
 
 constexpr int kPagedQFoldThreads = 512;        // of pagedq_kernel
@@ -72,7 +71,7 @@ constexpr int kPagedQProbPitch = kPagedQStep * 2 + 16, kPagedQTurnPitch = 2 * kP
 __host__ __device__ constexpr PagedQLds pagedq_lds(const PagedQForm& f) {
   PagedQLds l = {};
   const bool two = pagedq_two_phases(f.slices, f.rows, f.v_blocks);
-  const int p_rows = f.rows == 1 ? 8 : (f.slices == 1 ? 32 : 16);
+  const int p_rows = 8 * f.rows;
   l.k_pitch = 256 * f.k_blocks;
   l.k_size = kPagedQStep * l.k_pitch;
   l.v_size = kPagedQStep * 64 * f.v_blocks;

@@ -82,10 +82,9 @@ template <typename T, int KS, int SL, int NQ, int KB, int VB>
 __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   constexpr int HEADS = 4 / SL;                // of a unit
   constexpr int NB = KS / 4;                   // blocks of 128 channels
-  constexpr int LG = NQ == 1 ? 1 : NQ / 2;     // folded query rows, 16 (row, node) a group
-  constexpr int NG = NQ == 1 ? 1 : NQ;         // their operands: with several rows hi and lo
+  constexpr int NG = NQ;                       // operands of the folded query rows, 16 (row, node): with two rows hi and lo
   constexpr int PARTS = 2 * SL;                // wavefronts whose scores of a head are added up
-  constexpr int kLoRows = NQ == 1 ? 4 : (SL == 1 ? 16 : 8);  // rows of probabilities before those that the rounding left
+  constexpr int kLoRows = 4 * NQ;              // rows of probabilities before those that the rounding left
   constexpr bool TWO = pagedq_two_phases(SL, NQ, VB);        // see below
   constexpr int KG = pagedq_key_scales(KS, KB);              // groups, or slices, with scales of their own
   constexpr int MB = VB < PARTS ? 1 : VB / PARTS;            // blocks of values whose weights a wavefront makes
@@ -473,7 +472,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   };
   // a and b of the folded pairs at the nodes of span k, hi and lo (one row: by lanes)
   struct Nodes {
-    uint4v a[LG][NQ == 1 ? 1 : 2], b[LG][NQ == 1 ? 1 : 2];
+    uint4v a[NG], b[NG];
   };
   uint4v G[KS / 2][NG];                        // the folded weights
   auto nodes_of = [&](int k, Nodes& v) __attribute__((always_inline)) {
@@ -484,39 +483,36 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     for (int q = 0; q < 2; ++q) {
       const float4v c0 = *reinterpret_cast<const float4v*>(at + 4 * q), s0 = *reinterpret_cast<const float4v*>(at + kHalf + 4 * q);
       const float4v c1 = *reinterpret_cast<const float4v*>(on + 4 * q), s1 = *reinterpret_cast<const float4v*>(on + kPagedQLow + 4 * q);
+      const float* const row = qs + upper * kDHead + kPagedQLow + f + 4 * q;
+      const float4v x = *reinterpret_cast<const float4v*>(row), y = *reinterpret_cast<const float4v*>(row + kHalf);
+      const int e = upper ? ea[NQ - 1] : ea[0];
+      float u[4], w[4];
 #pragma unroll
-      for (int l = 0; l < LG; ++l) {
-        const float* const row = qs + (2 * l + upper) * kDHead + kPagedQLow + f + 4 * q;
-        const float4v x = *reinterpret_cast<const float4v*>(row), y = *reinterpret_cast<const float4v*>(row + kHalf);
-        const int e = NQ == 1 ? ea[0] : (upper ? ea[(2 * l + 1) % NQ] : ea[2 * l]);
-        float u[4], w[4];
+      for (int i = 0; i < 4; ++i) {
+        const float c = __builtin_fmaf(c0[i], c1[i], -(s0[i] * s1[i])), s = __builtin_fmaf(c0[i], s1[i], s0[i] * c1[i]);
+        u[i] = __builtin_amdgcn_ldexpf(__builtin_fmaf(c, x[i], s * y[i]), e);
+        w[i] = __builtin_amdgcn_ldexpf(__builtin_fmaf(c, y[i], -(s * x[i])), e);
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float c = __builtin_fmaf(c0[i], c1[i], -(s0[i] * s1[i])), s = __builtin_fmaf(c0[i], s1[i], s0[i] * c1[i]);
-          u[i] = __builtin_amdgcn_ldexpf(__builtin_fmaf(c, x[i], s * y[i]), e);
-          w[i] = __builtin_amdgcn_ldexpf(__builtin_fmaf(c, y[i], -(s * x[i])), e);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t h, lo;
-          split2<F16>(u[2 * i], u[2 * i + 1], &h, &lo);
-          v.a[l][0][2 * q + i] = NQ == 1 && col >= 8 ? lo : h;
-          if (NQ > 1) v.a[l][NQ > 1][2 * q + i] = lo;
-          split2<F16>(w[2 * i], w[2 * i + 1], &h, &lo);
-          v.b[l][0][2 * q + i] = NQ == 1 && col >= 8 ? lo : h;
-          if (NQ > 1) v.b[l][NQ > 1][2 * q + i] = lo;
-        }
+      for (int i = 0; i < 2; ++i) {
+        uint32_t h, lo;
+        split2<F16>(u[2 * i], u[2 * i + 1], &h, &lo);
+        v.a[0][2 * q + i] = NQ == 1 && col >= 8 ? lo : h;
+        if (NQ > 1) v.a[NG - 1][2 * q + i] = lo;
+        split2<F16>(w[2 * i], w[2 * i + 1], &h, &lo);
+        v.b[0][2 * q + i] = NQ == 1 && col >= 8 ? lo : h;
+        if (NQ > 1) v.b[NG - 1][2 * q + i] = lo;
       }
     }
   };
   // Folded weights of channel step ks, from its weights f
   const float lo_part = NQ == 1 && col >= 8 ? -1.f : 0.f;    // one row: these lanes hold what the rounding leaves
-  auto fold_tile = [&](const uint4v (&f)[2], const Nodes& v, int l) __attribute__((always_inline)) {
-    float4v d = mma<F16>(f[0], v.a[l][0], float4v{0, 0, 0, 0});
-    d = mma<F16>(f[1], v.b[l][0], d);
-    if (NQ > 1) {
-      d = mma<F16>(f[0], v.a[l][NQ > 1], d);
-      d = mma<F16>(f[1], v.b[l][NQ > 1], d);
+  auto fold_tile = [&](const uint4v (&f)[2], const Nodes& v) __attribute__((always_inline)) {
+    float4v d = {0, 0, 0, 0};
+#pragma unroll
+    for (int l = 0; l < NG; ++l) {
+      d = mma<F16>(f[0], v.a[l], d);
+      d = mma<F16>(f[1], v.b[l], d);
     }
     return d;
   };
@@ -532,16 +528,13 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     }
   };
   auto fold_one = [&](const uint4v (&f)[2][2], const Nodes& v, uint4v (&g)[NG]) __attribute__((always_inline)) {
+    const float4v d0 = fold_tile(f[0], v), d1 = fold_tile(f[1], v);
 #pragma unroll
-    for (int l = 0; l < LG; ++l) {
-      const float4v d0 = fold_tile(f[0], v, l), d1 = fold_tile(f[1], v, l);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        uint32_t hi, lo = 0;
-        fold_pack(d0[u], d1[u], &hi, &lo);
-        g[NQ == 1 ? 0 : 2 * l][u] = hi;
-        if (NQ > 1) g[(2 * l + 1) % NG][u] = lo;
-      }
+    for (int u = 0; u < 4; ++u) {
+      uint32_t hi, lo = 0;
+      fold_pack(d0[u], d1[u], &hi, &lo);
+      g[0][u] = hi;
+      if (NQ > 1) g[NG - 1][u] = lo;
     }
   };
   auto fold = [&](int n) __attribute__((always_inline)) {
@@ -565,26 +558,24 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   for (int i = 0; i < 4; ++i) k_off[i] = (SL == 1 ? hg * KS * 64 : slice * 512) + col * ld.k_pitch + (((4 * step_of(i) + kg) ^ col) & 15) * 16;
   const int b_last = ks_here / 4 - 1;          // last block of this slice
   struct Sums {
-    float4v acc[2], low[LG];
+    float4v acc[2], low;
   };
   auto clear = [&](Sums& a) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) a.acc[j] = float4v{0, 0, 0, 0};
-#pragma unroll
-    for (int l = 0; l < LG; ++l) a.low[l] = float4v{0, 0, 0, 0};
+    a.low = float4v{0, 0, 0, 0};
   };
   auto product = [&](Sums& a, int i, uint4v h) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) a.acc[j] = mma<F16>(W[i][j], h, a.acc[j]);
     if (i % 2 == 0)
 #pragma unroll
-      for (int l = 0; l < NG; ++l) a.low[NQ == 1 ? 0 : l / 2] = mma<F16>(G[i / 2][l], h, a.low[NQ == 1 ? 0 : l / 2]);
+      for (int l = 0; l < NG; ++l) a.low = mma<F16>(G[i / 2][l], h, a.low);
   };
   auto scale_sums = [&](Sums& a, float x) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) a.acc[j] *= x;
-#pragma unroll
-    for (int l = 0; l < LG; ++l) a.low[l] *= x;
+    a.low *= x;
   };
   // zero-points that are no small integers: as operands of their own, the same for all channels of block b, times x
   auto zero_points = [&](Sums& a, int n, int sub, int b, float x) __attribute__((always_inline)) {
@@ -596,8 +587,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     for (int i = 0; i < 4; ++i) product(more, 4 * b + i, uint4v{w, w, w, w});
 #pragma unroll
     for (int j = 0; j < 2; ++j) a.acc[j] += more.acc[j] * x;
-#pragma unroll
-    for (int l = 0; l < LG; ++l) a.low[l] += more.low[l] * x;
+    a.low += more.low * x;
   };
   // What pair p of this lane adds to the scores; its angle (one query row: a and b) 16 tokens on
   auto pair = [&](const Sums& a, int p, const float4v (&qa)[NQ], const float4v (&qb)[NQ], float (&part)[NQ]) __attribute__((always_inline)) {
@@ -632,7 +622,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     for (int p = 0; p < 4; ++p) pair(z, p, qa, qb, part);
 #pragma unroll
     for (int r = 0; r < NQ; ++r) {
-      const float4v x = z.low[NQ == 1 ? 0 : r / 2];
+      const float4v x = z.low;
       const float sum = __builtin_fmaf(x[0], basis[0], __builtin_fmaf(x[1], basis[1], __builtin_fmaf(x[2], basis[2], x[3] * basis[3])));
       const bool mine = NQ == 1 || (kg >> 1) == (r & 1);
       part[r] = __builtin_fmaf(sum, mine ? __builtin_amdgcn_ldexpf(1.f, -ea[r]) : 0.f, part[r]) * (unit * scale);
@@ -817,7 +807,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   };
 
   // ---- values of step n.  A wavefront has half of the tokens of a block of 128 columns, where there are one or two blocks of every second four.
-  float4v O[NO];                               // column 8 col + (4 quarter +) u of rows 4 kg + e; odd columns in units of 2^-20, even ones of 2^-24
+  float4v O[NO];                               // column 8 col + (4 quarter +) u of rows 4 kg + e (behind the weights' rows those of what their rounding left); odd columns in units of 2^-20, even ones of 2^-24
 #pragma unroll
   for (int u = 0; u < NO; ++u) O[u] = float4v{0, 0, 0, 0};
   int vb0 = wave & (VB - 1), half0 = VB == 2 ? (wave >> 1) & 1 : wave >> 2, quarter = VB == 2 ? wave >> 2 : 0;
@@ -827,13 +817,13 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   auto values = [&](int n) __attribute__((always_inline)) {
     const int vb = vb0;
     if (vb >= CB) return;
-    const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (((n & 1) * VB + vb) * 16 + (NQ == 1 ? 0 : 4 * kg)) * 4);
+    const float4v al = *reinterpret_cast<const float4v*>(lds + ld.alpha + (((n & 1) * VB + vb) * 16 + 4 * (kg & (NQ - 1))) * 4);
     const unsigned char* const at = lds + ld.v + n % VBUFS * ld.v_size + (32 * half0 + 8 * kg) * (v_cols / 2) + vb * 64 + col * 4;
     uint32_t d[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e] = *reinterpret_cast<const uint32_t*>(at + e * (v_cols / 2));
-    const unsigned char* const P = lds + ld.p + (n & 1) * ld.p_size + vb * ld.p_cb + (NQ == 1 || SL == 2 ? col & 7 : col) * kPagedQProbPitch + (32 * half0 + 8 * kg) * 2;
-    const uint4v hi = *reinterpret_cast<const uint4v*>(P), lo = NQ > 1 ? *reinterpret_cast<const uint4v*>(P + kLoRows * kPagedQProbPitch) : hi;
+    const unsigned char* const P = lds + ld.p + (n & 1) * ld.p_size + vb * ld.p_cb + (col & (2 * kLoRows - 1)) * kPagedQProbPitch + (32 * half0 + 8 * kg) * 2;
+    const uint4v p = *reinterpret_cast<const uint4v*>(P);
     if (__any(!(al[0] == 1.f && al[1] == 1.f && al[2] == 1.f && al[3] == 1.f)))
 #pragma unroll
       for (int u = 0; u < NO; ++u) O[u] *= al;
@@ -847,12 +837,8 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
         even[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x & 0x000f000fu) + minus8_even);
         odd[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x & 0x00f000f0u) + minus8_odd);
       }
-      O[2 * j] = mma<F16>(hi, even, O[2 * j]);
-      O[2 * j + 1] = mma<F16>(hi, odd, O[2 * j + 1]);
-      if (NQ > 1) {
-        O[2 * j] = mma<F16>(lo, even, O[2 * j]);
-        O[2 * j + 1] = mma<F16>(lo, odd, O[2 * j + 1]);
-      }
+      O[2 * j] = mma<F16>(p, even, O[2 * j]);
+      O[2 * j + 1] = mma<F16>(p, odd, O[2 * j + 1]);
     }
   };
 
@@ -943,10 +929,10 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
 #pragma unroll
       for (int u = 0; u < NO; ++u) {
         y[u] = O[u][e];
-        if (NQ == 1) y[u] += __shfl_xor(y[u], 16);
+        y[u] += __shfl_xor(y[u], 16 * NQ);
       }
-      const int row = NQ == 1 ? e : 4 * kg + e, h = row / NQ, r = row % NQ;
-      if (h >= nh || h >= HEADS || r >= nr || (NQ == 1 && kg != 0) || (un.n_groups() > 1 && h / per_group != vg)) continue;
+      const int row = 4 * kg + e, h = row / NQ, r = row % NQ;
+      if (h >= nh || h >= HEADS || r >= nr || kg >= NQ || (un.n_groups() > 1 && h / per_group != vg)) continue;
       const float2 f = fin[row * VB + vb];
       const float worth = (tops[row] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(f.y - tops[row])) / kWeightScale;
 #pragma unroll
@@ -961,8 +947,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
 
 namespace {
 template <typename T, int NQ, int VB> PagedQFn pick(const PagedQForm& f) {
-  if constexpr (NQ <= 2)
-    if (f.slices == 2) return pagedq_kernel<T, 8, 2, NQ, 4, VB>;
+  if (f.slices == 2) return pagedq_kernel<T, 8, 2, NQ, 4, VB>;
   if (f.ks == 8) return pagedq_kernel<T, 8, 1, NQ, 2, VB>;
   return f.k_blocks == 2 ? pagedq_kernel<T, 4, 1, NQ, 2, VB> : pagedq_kernel<T, 4, 1, NQ, 1, VB>;
 }

@@ -85,9 +85,8 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
   c->o_stride = sum_rv * m.qpk;
   c->span_steps = pagedq_span_steps(desc->rope_theta);
   c->n_cls = 0;
-  bool sliced = false;
-  for (int j = 0; j < m.n_groups; ++j) sliced = sliced || rk(j) > 256;
-  const int rows = m.qpk <= 2 || sliced ? std::min(m.qpk, 2) : 4;       // (LDS does not hold four rows' parts of two slices)
+  // (four rows at a time do not fit the registers: 4 x 16384 rows of four query rows a head took 178 us against 120 in two passes)
+  const int rows = std::min(m.qpk, 2);
   c->n_row_blocks = ceil_div(m.qpk, rows);
   // Units, as for unquantized latents: whole adjacent groups side by side, or parts of one
   auto side_by_side = [&](int j, int unit_heads) {           // groups from j on
