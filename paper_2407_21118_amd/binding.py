@@ -501,57 +501,62 @@ def _act(desc: LayerDesc):
     return torch.float16 if desc.act_dtype == PALU_F16 else torch.bfloat16
 
 
-def _need_here(*tensors, latents=()) -> None:
-    """Tensors of the current device, whose stream the call goes to; but for `latents`, contiguous ones."""
+def _here(stream):
+    """The current device, and the stream of it that the call goes to; (None, None) without a device."""
     import torch
-    _need_cuda(*tensors)
-    both = [t for t in (*tensors, *latents) if t is not None]
-    if not all(t.is_cuda for t in both):
-        raise ValueError("device tensors required")
+    if not torch.cuda.is_initialized() and not torch.cuda.is_available():
+        return None, None
     here = torch.cuda.current_device()
-    if any(t.device.index != here for t in both):
-        raise ValueError("tensors of the current device required")
+    return here, torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
 
 
-def _need_rows_here(bits, k, v, rows, hk, hv) -> None:
-    """... of the quantized sides, and the row numbers."""
-    _need_here(*[t for side, b in ((k, bits[0]), (v, bits[1])) if b for t in side], rows, latents=[h for h, b in zip((hk, hv), bits) if b])
+def _addresses(here, *tensors, strided=()):
+    """Addresses (None for None) of tensors of the current device; but for `strided`, which come last, contiguous ones."""
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if t.get_device() != here:
+            raise ValueError("tensors of the current device required" if t.is_cuda else "device tensors required")
+        if not t.is_contiguous():
+            raise ValueError("contiguous tensors required")
+        out.append(t.data_ptr())
+    for t in strided:
+        if t is not None and t.get_device() != here:
+            raise ValueError("tensors of the current device required" if t.is_cuda else "device tensors required")
+        out.append(None if t is None else t.data_ptr())
+    return out
 
 
-def _held_rows(desc: LayerDesc, sides, bits):
-    """Rows of the quantized sides [(codes, scale, zero), ..], R channels in `bits` bits each (0: not quantized): all the same number."""
+def _side_rows(codes, scale, zero, R, bits):
+    """Rows of a quantized side of R channels in `bits` bits each."""
     import torch
-    n_rows = None
-    for (codes, scale, zero), R, b in zip(sides, (desc.R_k, desc.R_v), bits):
-        if not b:
-            continue
-        if codes is None or codes.dtype != torch.uint8 or any(t is None or t.dtype != torch.float16 for t in (scale, zero)):
-            raise ValueError("codes need dtype torch.uint8, scales and zero-points torch.float16")
-        widths = (R * b // 8, R // 128, R // 128)
-        if any(t.dim() < 2 or t.shape[-1] != w or t.shape[:-1] != codes.shape[:-1] for t, w in zip((codes, scale, zero), widths)):
-            raise ValueError("codes, scales or zero-points do not fit the layer")
-        rows = codes.numel() // widths[0]
-        if n_rows not in (None, rows):
-            raise ValueError("both caches need the same rows")
-        n_rows = rows
-    return n_rows
+    half = torch.float16
+    if codes is None or scale is None or zero is None or codes.dtype != torch.uint8 or scale.dtype != half or zero.dtype != half:
+        raise ValueError("codes need dtype torch.uint8, scales and zero-points torch.float16")
+    shape, blocks = codes.shape, R // 128
+    if (len(shape) < 2 or shape[-1] * 8 != R * bits or scale.dim() < 2 or zero.dim() < 2 or scale.shape != (*shape[:-1], blocks)
+            or zero.shape != scale.shape):
+        raise ValueError("codes, scales or zero-points do not fit the layer")
+    return codes.numel() // shape[-1]
 
 
-def _bits(desc: LayerDesc):
-    return [{PALU_I4: 4, PALU_I3: 3, PALU_I2: 2}.get(t, 0) for t in (desc.k_latent_dtype, desc.v_latent_dtype)]
+def _same_rows(k_rows, v_rows):
+    if k_rows is not None and v_rows is not None and k_rows != v_rows:
+        raise ValueError("both caches need the same rows")
+    return k_rows if k_rows is not None else v_rows
 
 
-def _latent_rows(desc: LayerDesc, hk, hv, n_tok, bits):
-    """Strides of latent rows hk [n_tok, R_k], hv [n_tok, R_v], whose channels are contiguous."""
-    strides = []
-    for h, R, b in zip((hk, hv), (desc.R_k, desc.R_v), bits):
-        if not b:
-            strides.append(0)
-            continue
-        if h is None or h.dtype != _act(desc) or h.dim() != 2 or tuple(h.shape) != (n_tok, R) or (R > 1 and h.stride(1) != 1):
-            raise ValueError(f"latent rows need dtype {_act(desc)} and shape [{n_tok}, {R}], channels side by side")
-        strides.append(max(int(h.stride(0)), R) if n_tok <= 1 else int(h.stride(0)))
-    return strides
+_BITS = {PALU_I4: 4, PALU_I3: 3, PALU_I2: 2}
+
+
+def _latent_stride(desc: LayerDesc, h, R, n_tok):
+    """Stride of latent rows h [n_tok, R], whose channels are contiguous."""
+    if h is None or h.dtype != _act(desc) or h.shape != (n_tok, R) or (R > 1 and h.stride(1) != 1):
+        raise ValueError(f"latent rows need dtype {_act(desc)} and shape [{n_tok}, {R}], channels side by side")
+    stride = h.stride(0)
+    return max(stride, R) if n_tok <= 1 else stride
 
 
 def _row_numbers(rows, n_tok):
@@ -560,31 +565,35 @@ def _row_numbers(rows, n_tok):
         raise ValueError("row numbers need dtype torch.int32, one per latent row")
 
 
+def _latent_kv(desc: LayerDesc, hk, hv, k, v, numbers, stream):
+    """What the calls between latent rows and quantized ones take: addresses of either side's codes, scales and zero-points, and of the row
+    numbers, rows of the caches, latent rows with their strides, stream."""
+    k_bits, v_bits = _BITS.get(desc.k_latent_dtype, 0), _BITS.get(desc.v_latent_dtype, 0)
+    R_k, R_v = desc.R_k, desc.R_v
+    n_rows = _same_rows(_side_rows(*k, R_k, k_bits) if k_bits else None, _side_rows(*v, R_v, v_bits) if v_bits else None)
+    n_tok = (hk if k_bits or hk is not None else hv).shape[0]
+    k_stride, v_stride = _latent_stride(desc, hk, R_k, n_tok) if k_bits else 0, _latent_stride(desc, hv, R_v, n_tok) if v_bits else 0
+    _row_numbers(numbers, n_tok)
+    here, stream = _here(stream)
+    none = (None, None, None)
+    at = _addresses(here, *(k if k_bits else none), *(v if v_bits else none), numbers,
+                    strided=(hk if k_bits else None, hv if v_bits else None))
+    return at[:6], at[6], n_rows or 0, n_tok, (at[7], k_stride, at[8], v_stride), stream
+
+
 def palu_quant_latent_kv(desc: LayerDesc, hk, hv, k_codes, k_scale, k_zero, v_codes, v_scale, v_zero, dst_row=None, stream=None):
     """Quantizes latent rows hk [n, R_k], hv [n, R_v] into rows dst_row of both caches ([.., R * bits / 8] codes, [.., R / 128] scales and
     zero-points); rows named by no number of the cache are left out."""
-    bits = _bits(desc)
-    n_rows = _held_rows(desc, ((k_codes, k_scale, k_zero), (v_codes, v_scale, v_zero)), bits)
-    n_tok = int((hk if bits[0] or hk is not None else hv).shape[0])
-    strides = _latent_rows(desc, hk, hv, n_tok, bits)
-    _row_numbers(dst_row, n_tok)
-    _need_rows_here(bits, (k_codes, k_scale, k_zero), (v_codes, v_scale, v_zero), dst_row, hk, hv)
-    _check(load_library().palu_quant_latent_kv(desc.ref(), _ptr(hk), strides[0], _ptr(hv), strides[1], n_tok, _ptr(k_codes), _ptr(k_scale),
-                                               _ptr(k_zero), _ptr(v_codes), _ptr(v_scale), _ptr(v_zero), n_rows or 0, _ptr(dst_row),
-                                               _stream(stream)), "palu_quant_latent_kv")
+    held, numbers, n_rows, n_tok, latents, stream = _latent_kv(desc, hk, hv, (k_codes, k_scale, k_zero), (v_codes, v_scale, v_zero), dst_row,
+                                                               stream)
+    _check(load_library().palu_quant_latent_kv(desc.ref(), *latents, n_tok, *held, n_rows, numbers, stream), "palu_quant_latent_kv")
 
 
 def palu_dequant_latent_kv(desc: LayerDesc, k_codes, k_scale, k_zero, v_codes, v_scale, v_zero, src_row, hk, hv, stream=None):
     """Reads rows src_row (None: the first ones) of both caches back into hk [n, R_k], hv [n, R_v]."""
-    bits = _bits(desc)
-    n_rows = _held_rows(desc, ((k_codes, k_scale, k_zero), (v_codes, v_scale, v_zero)), bits)
-    n_tok = int((hk if bits[0] or hk is not None else hv).shape[0])
-    strides = _latent_rows(desc, hk, hv, n_tok, bits)
-    _row_numbers(src_row, n_tok)
-    _need_rows_here(bits, (k_codes, k_scale, k_zero), (v_codes, v_scale, v_zero), src_row, hk, hv)
-    _check(load_library().palu_dequant_latent_kv(desc.ref(), _ptr(k_codes), _ptr(k_scale), _ptr(k_zero), _ptr(v_codes), _ptr(v_scale),
-                                                 _ptr(v_zero), n_rows or 0, _ptr(src_row), n_tok, _ptr(hk), strides[0], _ptr(hv), strides[1],
-                                                 _stream(stream)), "palu_dequant_latent_kv")
+    held, numbers, n_rows, n_tok, latents, stream = _latent_kv(desc, hk, hv, (k_codes, k_scale, k_zero), (v_codes, v_scale, v_zero), src_row,
+                                                               stream)
+    _check(load_library().palu_dequant_latent_kv(desc.ref(), *held, n_rows, numbers, n_tok, *latents, stream), "palu_dequant_latent_kv")
     return hk, hv
 
 
@@ -592,23 +601,23 @@ def palu_encode_kv_w4(desc: LayerDesc, x, Akt, Ak_scale, Ak_zero, Avt, Av_scale,
                       hv_row_stride_elems: int, dst_row=None, stream=None):
     """palu_encode_kv_t from 4-bit weights Akt [R_k, d / 2], Avt [R_v, d / 2] with scales and zero-points [R, d / 128]."""
     import torch
-    d = desc.n_q_heads * desc.d_head
-    n_tok = int(x.shape[0])
-    if x.dim() != 2 or x.shape[1] != d or any(t.dtype != _act(desc) for t in (x, hk, hv)):
-        raise ValueError(f"x, hk and hv need dtype {_act(desc)}, x the shape [tokens, {d}]")
-    for (codes, scale, zero), R in (((Akt, Ak_scale, Ak_zero), desc.R_k), ((Avt, Av_scale, Av_zero), desc.R_v)):
-        if codes.dtype != torch.uint8 or any(t.dtype != torch.float16 for t in (scale, zero)):
+    d, act, half = desc.n_q_heads * desc.d_head, _act(desc), torch.float16
+    if x.dim() != 2 or x.shape[1] != d or x.dtype != act or hk.dtype != act or hv.dtype != act:
+        raise ValueError(f"x, hk and hv need dtype {act}, x the shape [tokens, {d}]")
+    n_tok = x.shape[0]
+    for codes, scale, zero, h, stride, R in ((Akt, Ak_scale, Ak_zero, hk, hk_row_stride_elems, desc.R_k),
+                                             (Avt, Av_scale, Av_zero, hv, hv_row_stride_elems, desc.R_v)):
+        if codes.dtype != torch.uint8 or scale.dtype != half or zero.dtype != half:
             raise ValueError("codes need dtype torch.uint8, scales and zero-points torch.float16")
-        if tuple(codes.shape) != (R, d // 2) or any(tuple(t.shape) != (R, d // 128) for t in (scale, zero)):
+        if codes.shape != (R, d // 2) or scale.shape != (R, d // 128) or zero.shape != scale.shape:
             raise ValueError("weights do not fit the layer")
-    _row_numbers(dst_row, n_tok)
-    for h, stride, R in ((hk, int(hk_row_stride_elems), desc.R_k), (hv, int(hv_row_stride_elems), desc.R_v)):
         if stride < R or (dst_row is None and n_tok and h.numel() < (n_tok - 1) * stride + R):
             raise ValueError("hk or hv does not hold the rows")
-    _need_here(x, Akt, Ak_scale, Ak_zero, Avt, Av_scale, Av_zero, hk, hv, dst_row)
-    _check(load_library().palu_encode_kv_w4(desc.ref(), _ptr(x), n_tok, _ptr(Akt), _ptr(Ak_scale), _ptr(Ak_zero), _ptr(Avt), _ptr(Av_scale),
-                                            _ptr(Av_zero), _ptr(hk), int(hk_row_stride_elems), _ptr(hv), int(hv_row_stride_elems),
-                                            _ptr(dst_row), _stream(stream)), "palu_encode_kv_w4")
+    _row_numbers(dst_row, n_tok)
+    here, stream = _here(stream)
+    x, *weights, hk, hv, dst_row = _addresses(here, x, Akt, Ak_scale, Ak_zero, Avt, Av_scale, Av_zero, hk, hv, dst_row)
+    _check(load_library().palu_encode_kv_w4(desc.ref(), x, n_tok, *weights, hk, int(hk_row_stride_elems), hv, int(hv_row_stride_elems), dst_row,
+                                            stream), "palu_encode_kv_w4")
 
 
 def palu_attn_paged_quant_workspace_bytes(desc: LayerDesc, batch: int, max_len: int, window: int = 0, n_sink: int = 0) -> int:
@@ -629,27 +638,29 @@ def palu_attn_paged_quant(desc: LayerDesc, batch: int, max_len: int, q, q_pos, h
     if workspace is None:
         workspace = torch.empty(palu_attn_paged_quant_workspace_bytes(desc, batch, max_len, window, n_sink), dtype=torch.uint8,
                                 device=q.device)
-    if any(t.dtype != _act(desc) for t in (q, Bk, Bv, out)):
-        raise ValueError(f"q, Bk, Bv and out need dtype {_act(desc)}")
-    if any(t is not None and t.dtype != torch.int32 for t in (q_pos, page_table, seq_lens)):
+    act, i32 = _act(desc), torch.int32
+    if q.dtype != act or Bk.dtype != act or Bv.dtype != act or out.dtype != act:
+        raise ValueError(f"q, Bk, Bv and out need dtype {act}")
+    if page_table.dtype != i32 or (q_pos is not None and q_pos.dtype != i32) or (seq_lens is not None and seq_lens.dtype != i32):
         raise ValueError("q_pos, page_table and seq_lens need dtype torch.int32")
-    if any(b not in (0, 4) for b in _bits(desc)):
+    if _BITS.get(desc.k_latent_dtype, 4) != 4 or _BITS.get(desc.v_latent_dtype, 4) != 4:
         raise PaluError(-2, "palu_attn_paged_quant")
-    _held_rows(desc, ((hk, hk_scale, hk_zero), (hv, hv_scale, hv_zero)), (4, 4))
-    if (hk.dim() != 3 or hv.dim() != 3 or page_table.dim() != 2 or page_table.shape[0] != batch
-            or any(t.numel() != batch * desc.n_q_heads * desc.d_head for t in (q, out))
-            or any(t is not None and t.numel() != batch for t in (q_pos, seq_lens))):
+    _same_rows(_side_rows(hk, hk_scale, hk_zero, desc.R_k, 4), _side_rows(hv, hv_scale, hv_zero, desc.R_v, 4))
+    rows = batch * desc.n_q_heads * desc.d_head
+    if (hk.dim() != 3 or hv.dim() != 3 or page_table.dim() != 2 or page_table.shape[0] != batch or q.numel() != rows or out.numel() != rows
+            or (q_pos is not None and q_pos.numel() != batch) or (seq_lens is not None and seq_lens.numel() != batch)):
         raise ValueError("shapes do not fit the layer and the batch")
-    n_pages, page_rows = int(hk.shape[0]), int(hk.shape[1])
-    if tuple(hv.shape[:2]) != (n_pages, page_rows):
+    n_pages, page_rows = hk.shape[0], hk.shape[1]
+    if hv.shape[0] != n_pages or hv.shape[1] != page_rows:
         raise ValueError("hk and hv need the same pages")
     if (Bk.numel(), Bv.numel()) != desc.b_elems:
         raise ValueError("Bk or Bv does not fit the layer's ranks")
     if rope_table.numel() * rope_table.element_size() < palu_rope_table_bytes(desc.d_head, int(rope_table_len)):
         raise ValueError("rope_table holds fewer than rope_table_len positions")
-    _need_here(q, q_pos, hk, hk_scale, hk_zero, hv, hv_scale, hv_zero, page_table, seq_lens, Bk, Bv, rope_table, out, workspace)
+    here, stream = _here(stream)
+    q, q_pos, *pages, table, seq_lens, Bk, Bv, rope_table, to, space = _addresses(
+        here, q, q_pos, hk, hk_scale, hk_zero, hv, hv_scale, hv_zero, page_table, seq_lens, Bk, Bv, rope_table, out, workspace)
     _check(load_library().palu_attn_paged_quant(
-        desc.ref(), batch, max_len, window, n_sink, _ptr(q), _ptr(q_pos), _ptr(hk), _ptr(hk_scale), _ptr(hk_zero), _ptr(hv), _ptr(hv_scale),
-        _ptr(hv_zero), n_pages, page_rows, _ptr(page_table), int(page_table.shape[1]), _ptr(seq_lens), _ptr(Bk), _ptr(Bv), _ptr(rope_table),
-        int(rope_table_len), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)), "palu_attn_paged_quant")
+        desc.ref(), batch, max_len, window, n_sink, q, q_pos, *pages, n_pages, page_rows, table, page_table.shape[1], seq_lens, Bk, Bv,
+        rope_table, int(rope_table_len), to, space, workspace.numel() * workspace.element_size(), stream), "palu_attn_paged_quant")
     return out
