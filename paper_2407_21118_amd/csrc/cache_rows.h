@@ -23,6 +23,6 @@ struct CacheRowsArgs {
 using CacheRowsFn = void (*)(CacheRowsArgs);
 // wide: latent rows begin on whole 16 bytes
 CacheRowsFn cache_rows_form(int act, bool quantize, bool wide);
-constexpr int kCacheRowsThreads = 256, kCacheRowsItems = 16;   // workgroup; blocks (of 16 threads each) that it takes
+constexpr int kCacheRowsThreads = 256, kCacheRowsItems = kCacheRowsThreads / 8;          // workgroup; blocks (of 8 threads each) that it takes
 
 }  // namespace palu
