@@ -11,7 +11,7 @@ struct EncodeW4Side {
   const uint16_t* zero;
   uint16_t* latent;
   long long stride;          // elements between latent rows
-  int tiles;                 // R / 16
+  int tiles;                 // workgroups side by side: R / 16 / columns
 };
 struct EncodeW4Args {
   EncodeW4Side side[2];
@@ -21,7 +21,10 @@ struct EncodeW4Args {
 };
 using EncodeW4Fn = void (*)(EncodeW4Args);
 constexpr int kW4Threads = 512;
-// tiles: blocks of 16 tokens that a workgroup takes, 1, 2 or 4
-EncodeW4Fn encode_w4_form(int act, int tiles);
+// Blocks of 16 tokens and of 16 columns that a workgroup takes: 1 or 2 by 1, 2 by 4
+struct EncodeW4Form {
+  int tokens, columns;
+};
+EncodeW4Fn encode_w4_form(int act, const EncodeW4Form& f);
 
 }  // namespace palu

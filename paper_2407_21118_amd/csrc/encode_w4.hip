@@ -9,6 +9,7 @@
 // the offset going to the zero-point.  So every product is exact and sums are float32; the only rounding to 16 bits is the result's.
 
 #include "encode_w4.h"
+#include "paged_dev.h"
 
 namespace palu {
 
@@ -30,82 +31,162 @@ template <> struct W4Codes<BF16> {
   }
 };
 
-// Eight codes as eight 16-bit numbers, in the order 0 4 1 5 2 6 3 7
+// Eight codes as eight 16-bit numbers
 template <typename T> __device__ __forceinline__ uint4v spread(uint32_t w, uint32_t offset) {
+  const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
   uint4v r;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) r[u] = ((w >> (4 * u)) & 0x000f000fu) | offset;
+  for (int u = 0; u < 4; ++u) r[u] = __builtin_amdgcn_perm(odd, even, 0x0c040c00u + 0x00010001u * u) | offset;
   return r;
 }
-// eight 16-bit numbers in that order
-__device__ __forceinline__ uint4v reorder(uint4v x) {
-  return uint4v{__builtin_amdgcn_perm(x.z, x.x, 0x05040100u), __builtin_amdgcn_perm(x.z, x.x, 0x07060302u),
-                __builtin_amdgcn_perm(x.w, x.y, 0x05040100u), __builtin_amdgcn_perm(x.w, x.y, 0x07060302u)};
+
+// Number i of lane group g (of four of 16 lanes) goes to number g of lane group i
+__device__ __forceinline__ uint4v transpose(uint4v w) {
+  uint32_t x[4] = {w[0], w[1], w[2], w[3]};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x[i], x[i + 2], false, false);
+    x[i] = r[0];
+    x[i + 2] = r[1];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x[i], x[i + 1], false, false);
+    x[i] = r[0];
+    x[i + 1] = r[1];
+  }
+  return uint4v{x[0], x[1], x[2], x[3]};
 }
 
-template <typename T, int NT>
-__global__ __launch_bounds__(kW4Threads) void encode_w4_kernel(EncodeW4Args a) {
-  constexpr int kWaves = kW4Threads / 64;
-  __shared__ float part[kWaves][NT * 16][17];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
-  const int s = (int)blockIdx.x >= a.side[0].tiles;
+template <typename T, int NT, int NC, int U>
+__global__ __launch_bounds__(kW4Threads, 2) void encode_w4_kernel(EncodeW4Args a) {
+  constexpr int kWaves = kW4Threads / 64, kPitch = 16 * NC + 1;
+  constexpr int kRows = NT * 16 * 256;         // bytes of a group's inputs
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * U * kRows > kWaves * NT * 16 * kPitch * 4 ? kWaves * U * kRows : kWaves * NT * 16 * kPitch * 4];
+  float (*const part)[NT * 16][kPitch] = reinterpret_cast<float (*)[NT * 16][kPitch]>(lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, kg = lane >> 4;
+  const int s = (int)blockIdx.y >= a.side[0].tiles;
   const EncodeW4Side& sd = a.side[s];
-  const int c0 = 16 * (blockIdx.x - (s ? a.side[0].tiles : 0));
-  const int t0 = blockIdx.y * (NT * 16), groups = a.d / 128;
+  const int c0 = 16 * NC * (blockIdx.y - (s ? a.side[0].tiles : 0));
+  const int t0 = blockIdx.x * (NT * 16), groups = a.d / 128;
   const uint32_t offset = W4Codes<T>::kOffset == 0 ? 0u : per_lane_constant(W4Codes<T>::kOffset);
   const uint4v ones = {W4Codes<T>::kOne, W4Codes<T>::kOne, W4Codes<T>::kOne, W4Codes<T>::kOne};
-  const uint8_t* codes = sd.codes + (size_t)(c0 + col) * (a.d / 2) + kg * 16;
-  const uint16_t* scale = sd.scale + (size_t)(c0 + col) * groups;
-  const uint16_t* zero = sd.zero + (size_t)(c0 + col) * groups;
-  const uint16_t* x[NT];
+  const uint8_t* const codes = sd.codes + (size_t)(c0 + col) * (a.d / 2) + kg * 16;
+  const uint16_t* const scale = sd.scale + (size_t)(c0 + (NC == 1 ? col : lane)) * groups;
+  const uint16_t* const zero = sd.zero + (size_t)(c0 + (NC == 1 ? col : lane)) * groups;
+  const bool wide = groups % 4 == 0 && ((reinterpret_cast<uintptr_t>(sd.scale) | reinterpret_cast<uintptr_t>(sd.zero)) & 7) == 0;
+  auto four = [&](const uint16_t* p, int here) __attribute__((always_inline)) {    // the first `here` of four numbers (and others)
+    if (wide) return *reinterpret_cast<const uint2v*>(p);
+    return uint2v{(uint32_t)p[0] | (uint32_t)p[min(1, here - 1)] << 16, (uint32_t)p[min(2, here - 1)] | (uint32_t)p[min(3, here - 1)] << 16};
+  };
+  // Inputs go by LDS, in pieces of 16 bytes: token t's piece p at place p ^ t of its 16.  An instruction takes 256 bytes of each of four tokens.  (Read as
+  // operands, 64 bytes of each of 16 tokens, they lie a power of two apart in few sets of the first cache: 24 tokens took 12 us against TIME.)
+  const uint16_t* x[4 * NT];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) x[n] = a.x + (size_t)min(t0 + 16 * n + col, a.n_tok - 1) * a.d + kg * 32;   // (tokens behind the last: the last again)
-  float4v h[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) h[n] = float4v{0, 0, 0, 0};
-  for (int g = wave; g < groups; g += kWaves) {
-    const uint4v w = *reinterpret_cast<const uint4v*>(codes + g * 64);
-    const float sc = F16::to_float(scale[g]), z = F16::to_float(zero[g]) + W4Codes<T>::kZero;
-    float4v dot[NT], sum[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) dot[n] = sum[n] = float4v{0, 0, 0, 0};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint4v b = spread<T>(w[j], offset);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint4v v = reorder(*reinterpret_cast<const uint4v*>(x[n] + g * 128 + j * 8));
-        dot[n] = W4Codes<T>::mma(v, b, dot[n]);
-        sum[n] = W4Codes<T>::mma(v, ones, sum[n]);
-      }
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) h[n][e] += sc * (dot[n][e] * W4Codes<T>::kUnit - z * sum[n][e]);
+  for (int i = 0; i < 4 * NT; ++i) {
+    const int t = 4 * i + kg;                  // (tokens behind the last: the last again)
+    x[i] = a.x + (size_t)min(t0 + t, a.n_tok - 1) * a.d + ((col ^ t) & 15) * 8;
   }
+  unsigned char* const mine = lds + wave * U * kRows;
+  const uint32_t mine0 = lds_addr(mine);
+  float4v h[NT][NC];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) part[wave][16 * n + 4 * kg + e][col] = h[n][e];
+    for (int c = 0; c < NC; ++c) h[n][c] = float4v{0, 0, 0, 0};
+  // Four groups in turn per wavefront, every workgroup from others on: tokens lie a power of two apart, and all would ask the same channels of L2.
+  const int quads = (groups + 3) / 4;
+  for (int q0 = wave; q0 < quads; q0 += kWaves) {
+    const int q = (q0 + (int)blockIdx.y) % quads, here = min(4, groups - 4 * q);
+    // a lane takes four scales and zero-points of one column of the workgroup, and hands them to those that need them
+    const uint2v mine_s = four(scale + 4 * q, here), mine_z = four(zero + 4 * q, here);
+    uint2v sc[NC], z[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        sc[c][e] = NC == 1 ? mine_s[e] : (uint32_t)__shfl((int)mine_s[e], 16 * c + col);
+        z[c][e] = NC == 1 ? mine_z[e] : (uint32_t)__shfl((int)mine_z[e], 16 * c + col);
+      }
+#pragma unroll
+    for (int i0 = 0; i0 < 4; i0 += U) {
+      uint4v w[U][NC];                         // U groups' loads before anything else
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int g = 4 * q + min(i0 + i, here - 1);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) w[i][c] = *reinterpret_cast<const uint4v*>(codes + (size_t)(16 * c) * (a.d / 2) + g * 64);
+#pragma unroll
+        for (int k = 0; k < 4 * NT; ++k)
+          if (k == 0 || t0 + 4 * k < a.n_tok) load_to_lds(x[k] + g * 128, mine0 + i * kRows + k * 1024);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (i0 + i >= here) break;
+        float4v dot[NT][NC], sum[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          sum[n] = float4v{0, 0, 0, 0};
+#pragma unroll
+          for (int c = 0; c < NC; ++c) dot[n][c] = float4v{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) w[i][c] = transpose(w[i][c]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint4v v[NT];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            v[n] = *reinterpret_cast<const uint4v*>(mine + i * kRows + (16 * n + col) * 256 + (((4 * j + kg) ^ col) & 15) * 16);
+            sum[n] = W4Codes<T>::mma(v[n], ones, sum[n]);
+          }
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const uint4v b = spread<T>(w[i][c][j], offset);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) dot[n][c] = W4Codes<T>::mma(v[n], b, dot[n][c]);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int k = i0 + i;
+          const float s1 = F16::to_float((uint16_t)(sc[c][k >> 1] >> (16 * (k & 1)))), z1 = F16::to_float((uint16_t)(z[c][k >> 1] >> (16 * (k & 1)))) + W4Codes<T>::kZero;
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[n][c][e] += s1 * (dot[n][c][e] * W4Codes<T>::kUnit - z1 * sum[n][e]);
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the inputs have been read)
+    }
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < NT * 16 * 16; i += kW4Threads) {
-    const int t = i >> 4, c = i & 15;
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[wave][16 * n + 4 * kg + e][16 * c + col] = h[n][c][e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < NT * 16 * NC * 16; i += kW4Threads) {
+    const int t = i / (16 * NC), c = i % (16 * NC);
     if (t0 + t >= a.n_tok) continue;
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += part[w][t][c];
+    for (int u = 0; u < kWaves; ++u) sum += part[u][t][c];
     const long long row = a.dst_row ? a.dst_row[t0 + t] : t0 + t;
     if (row >= 0) sd.latent[row * sd.stride + c0 + c] = T::from_float(sum);
   }
 }
 
-template <typename T> EncodeW4Fn pick(int tiles) {
-  return tiles == 1 ? encode_w4_kernel<T, 1> : (tiles == 2 ? encode_w4_kernel<T, 2> : encode_w4_kernel<T, 4>);
+template <typename T> EncodeW4Fn pick(const EncodeW4Form& f) {
+  if (f.columns == 4) return encode_w4_kernel<T, 2, 4, 2>;
+  return f.tokens == 1 ? encode_w4_kernel<T, 1, 1, 4> : encode_w4_kernel<T, 2, 1, 2>;
 }
 
 }  // namespace
 
-EncodeW4Fn encode_w4_form(int act, int tiles) { return act == PALU_F16 ? pick<F16>(tiles) : pick<BF16>(tiles); }
+EncodeW4Fn encode_w4_form(int act, const EncodeW4Form& f) { return act == PALU_F16 ? pick<F16>(f) : pick<BF16>(f); }
 
 }  // namespace palu

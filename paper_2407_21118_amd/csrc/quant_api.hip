@@ -179,18 +179,21 @@ int palu_encode_kv_w4(const palu_layer_desc* desc, const void* x, int32_t n_tok,
   const int Rk = m.k_off[m.n_groups], Rv = m.v_off[m.n_groups];
   if (hk_row_stride_elems < Rk || hv_row_stride_elems < Rv) return PALU_ERR_INVALID_ARG;
   if (n_tok == 0) return PALU_OK;
+  // 64 columns a workgroup where 32 tokens by 64 columns make one for every second compute unit, else 16: W4RULE
+  EncodeW4Form f{n_tok <= 16 ? 1 : 2, 1};
+  const long long blocks = ((long long)n_tok + 16 * f.tokens - 1) / (16 * f.tokens);
+  if (Rk % 64 == 0 && Rv % 64 == 0 && f.tokens == 2 && 2 * blocks * ((Rk + Rv) / 64) >= device_cu_count()) f.columns = 4;
   EncodeW4Args a;
   std::memset(&a, 0, sizeof(a));
-  a.side[0] = EncodeW4Side{Akt, (const uint16_t*)Ak_scale, (const uint16_t*)Ak_zero, (uint16_t*)hk, hk_row_stride_elems, Rk / 16};
-  a.side[1] = EncodeW4Side{Avt, (const uint16_t*)Av_scale, (const uint16_t*)Av_zero, (uint16_t*)hv, hv_row_stride_elems, Rv / 16};
+  a.side[0] = EncodeW4Side{Akt, (const uint16_t*)Ak_scale, (const uint16_t*)Ak_zero, (uint16_t*)hk, hk_row_stride_elems, Rk / (16 * f.columns)};
+  a.side[1] = EncodeW4Side{Avt, (const uint16_t*)Av_scale, (const uint16_t*)Av_zero, (uint16_t*)hv, hv_row_stride_elems, Rv / (16 * f.columns)};
   a.x = static_cast<const uint16_t*>(x);
   a.dst_row = dst_row;
   a.n_tok = n_tok;
   a.d = m.n_heads * PALU_D_HEAD;
-  const int tiles = n_tok <= 16 ? 1 : (n_tok <= 32 ? 2 : 4), blocks = ceil_div(n_tok, 16 * tiles);
-  if (blocks > 65535) return PALU_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(encode_w4_form(desc->act_dtype, tiles), dim3((unsigned)(a.side[0].tiles + a.side[1].tiles), (unsigned)blocks),
-                     dim3(kW4Threads), 0, static_cast<hipStream_t>(stream), a);
+  if (blocks * kW4Threads > 0xffffffffLL) return PALU_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL(encode_w4_form(desc->act_dtype, f), dim3((unsigned)blocks, (unsigned)(a.side[0].tiles + a.side[1].tiles)), dim3(kW4Threads), 0,
+                     static_cast<hipStream_t>(stream), a);
   return launch_ok();
 }
 
