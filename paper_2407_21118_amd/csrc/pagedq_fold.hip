@@ -275,50 +275,101 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     }
   };
 
-  // ---- prologue: rows of the first four steps
-  if (wave < min(4, n_steps)) put_rows(wave, *entry_of(wave));
-  // queries, rotated to their position and scaled, [row][feature]
-  float* const qs = reinterpret_cast<float*>(lds + ld.q) + hw * NQ * kDHead;
-  float q_max[NQ], q_sum[NQ];                  // of the folded pairs
-  {
-    const int pos = max(0, min(a.q_pos ? a.q_pos[seq] : L - 1, a.rope_len - 1));
-    const float c = a.rope[rope_f32_index(pos, lane, 0, kRopeTableStride)], s = a.rope[rope_f32_index(pos, lane, 1, kRopeTableStride)];
+  // ---- prologue: everything that memory has to give is requested first: page-table entries of the first four steps, queries, angles, weights
+  const int first_entry = wave < min(4, n_steps) ? *entry_of(wave) : 0;
+  float* const qs = reinterpret_cast<float*>(lds + ld.q) + hw * NQ * kDHead;         // queries, rotated to their position and scaled, [row][feature]
+  const int q_pos = max(0, min(a.q_pos ? a.q_pos[seq] : L - 1, a.rope_len - 1));
+  const float q_cos = a.rope[rope_f32_index(q_pos, lane, 0, kRopeTableStride)], q_sin = a.rope[rope_f32_index(q_pos, lane, 1, kRopeTableStride)];
+  uint16_t q_raw[NQ][2];
 #pragma unroll
-    for (int r = 0; r < NQ; ++r) {
-      const uint16_t* q = a.q + ((size_t)seq * m.n_heads * m.qpk + (h0 + hh) * m.qpk + row0 + min(r, nr - 1)) * kDHead;
-      const float x0 = T::to_float(q[lane]), x1 = T::to_float(q[lane + kHalf]);
-      const float y0 = (x0 * c - x1 * s) * a.scale, y1 = (x1 * c + x0 * s) * a.scale;
-      qs[r * kDHead + lane] = y0;
-      qs[r * kDHead + kHalf + lane] = y1;
-      const float size = lane >= kPagedQLow ? fabsf(y0) + fabsf(y1) : 0.f;
-      q_max[r] = max_of_wave(size);
-      q_sum[r] = sum_of_wave(size);
-    }
+  for (int r = 0; r < NQ; ++r) {
+    const uint16_t* q = a.q + ((size_t)seq * m.n_heads * m.qpk + (h0 + hh) * m.qpk + row0 + min(r, nr - 1)) * kDHead;
+    q_raw[r][0] = q[lane];
+    q_raw[r][1] = q[lane + kHalf];
   }
-  if (tid < kPagedQSpan) {                     // Lagrange polynomials of the span's Chebyshev nodes (barycentric form), per position
-    const double T2 = 0.5 * kSteps * a.span_steps, x = (tid - (T2 - 0.5)) / T2;
+  // rebuilt pairs: of a token of 16; 16 tokens on, pairs 16 half + 4 kg + p
+  const float turn_cos = a.rope[rope_f32_index(min(tid >> 5, a.rope_len - 1), tid & 31, 0, kRopeTableStride)];
+  const float turn_sin = a.rope[rope_f32_index(min(tid >> 5, a.rope_len - 1), tid & 31, 1, kRopeTableStride)];
+  float tc[4], ts[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int f = 16 * half + 4 * kg + p, at16 = min(16, a.rope_len - 1);
+    tc[p] = a.rope[rope_f32_index(at16, f, 0, kRopeTableStride)];
+    ts[p] = a.rope[rope_f32_index(at16, f, 1, kRopeTableStride)];
+  }
+  // Weights, as operand rows.  W: tile j's row 2 x (+ 1) is feature 16 half + 2 x + j (+ 64), x < 8.  Those to be folded: a channel's features
+  // 32 + 8 kg .. and 96 + 8 kg .., read for every span.  The halves take neighbouring steps of channels in the other order, and fold every second one.
+  auto step_of = [&](int i) __attribute__((always_inline)) { return i ^ half; };
+  const uint32_t b_pitch = width * 2;
+  auto row_of = [&](int i, int x) __attribute__((always_inline)) {         // channel x of the step; steps behind the rank: the last, and zero instead
+    const int ks = SL == 1 ? step_of(i) : min(step_of(i), ks_here - 1);
+    return reinterpret_cast<const unsigned char*>(B) + (uint32_t)(slice * KS * 32 + 32 * ks + x) * b_pitch;
+  };
+  auto keep_of = [&](int i) __attribute__((always_inline)) { return SL == 1 || step_of(i) < ks_here ? 0xffffffffu : 0u; };
+  uint4v W[KS][2];
+  auto fold_weights = [&](int i, uint4v (&f)[2][2]) __attribute__((always_inline)) {
+    const uint32_t at = col * b_pitch + (kPagedQLow + 8 * kg) * 2;
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) f[v][e] = *reinterpret_cast<const uint4v*>(row_of(2 * i, 16 * v) + (at + e * kHalf * 2));
+    if (SL == 2)
+#pragma unroll
+      for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) f[v][e] &= keep_of(2 * i);
+  };
+  {
+    const uint32_t at = 4 * kg * b_pitch + ((col & 1) * kHalf + 16 * half + 2 * (col >> 1)) * 2;
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) W[i][v][u] = *reinterpret_cast<const uint32_t*>(row_of(i, 16 * v + u) + at);     // (two features each; see below)
+  }
+  uint4v F[KS / 2][2][2];
+#pragma unroll
+  for (int i = 0; i < KS / 2; ++i) fold_weights(i, F[i]);
+  __builtin_amdgcn_sched_barrier(0);
+
+  if (wave < min(4, n_steps)) put_rows(wave, first_entry);
+  float q_max[NQ], q_sum[NQ];                  // of the folded pairs
+#pragma unroll
+  for (int r = 0; r < NQ; ++r) {
+    const float x0 = T::to_float(q_raw[r][0]), x1 = T::to_float(q_raw[r][1]);
+    const float y0 = (x0 * q_cos - x1 * q_sin) * a.scale, y1 = (x1 * q_cos + x0 * q_sin) * a.scale;
+    qs[r * kDHead + lane] = y0;
+    qs[r * kDHead + kHalf + lane] = y1;
+    const float size = lane >= kPagedQLow ? fabsf(y0) + fabsf(y1) : 0.f;
+    q_max[r] = max_of_wave(size);
+    q_sum[r] = sum_of_wave(size);
+  }
+  if (tid < kPagedQSpan) {
+    // Lagrange polynomials of the span's Chebyshev nodes, per position, in their barycentric form.  (x is exact and so, but for one rounding, is its
+    // distance to a node; that rounding moves an interpolated angle by 1e-7 of the span.)
+    const float T2 = 0.5f * kSteps * a.span_steps, x = (tid - (T2 - 0.5f)) / T2;
     // cos((2 i + 1) pi / 16) and the barycentric weights (-1)^i sin((2 i + 1) pi / 16)
-    constexpr double kNode[4] = {0.98078528040323044913, 0.83146961230254523708, 0.55557023301960222474, 0.19509032201612826785};
-    double w[8], sum = 0.0;
+    constexpr float kNode[4] = {0.98078528040323044913f, 0.83146961230254523708f, 0.55557023301960222474f, 0.19509032201612826785f};
+    float w[8], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const double node = i < 4 ? kNode[i] : -kNode[7 - i], weight = (i & 1 ? -1.0 : 1.0) * kNode[i < 4 ? 3 - i : i - 4];
+      const float node = i < 4 ? kNode[i] : -kNode[7 - i], weight = (i & 1 ? -1.f : 1.f) * kNode[i < 4 ? 3 - i : i - 4];
       w[i] = weight / (x - node);
       sum += w[i];
     }
     float* const basis = reinterpret_cast<float*>(lds + ld.basis) + tid * 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) basis[i] = (float)(w[i] / sum);
+    for (int i = 0; i < 8; ++i) basis[i] = w[i] / sum;
     const int i = tid >> 5, f = tid & 31;      // a node, a folded pair
-    const float node = (float)(T2 - 0.5) + (float)T2 * (float)(i < 4 ? kNode[i & 3] : -kNode[7 - i & 3]);
+    const float node = (T2 - 0.5f) + T2 * (i < 4 ? kNode[i & 3] : -kNode[7 - i & 3]);
     float* const at = reinterpret_cast<float*>(lds + ld.nodes + i * kPagedQTurnPitch) + f;
     sincosf(a.w_low[f] * node, at + kPagedQLow, at);
   }
   {
-    const int i = tid >> 5, f = tid & 31, pos = min(i, a.rope_len - 1);    // a token of 16, a rebuilt pair
-    float* const at = reinterpret_cast<float*>(lds + ld.turns + i * kPagedQTurnPitch) + f;
-    at[0] = a.rope[rope_f32_index(pos, f, 0, kRopeTableStride)];
-    at[kPagedQLow] = a.rope[rope_f32_index(pos, f, 1, kRopeTableStride)];
+    float* const at = reinterpret_cast<float*>(lds + ld.turns + (tid >> 5) * kPagedQTurnPitch) + (tid & 31);
+    at[0] = turn_cos;
+    at[kPagedQLow] = turn_sin;
   }
   lds_barrier();
   request_keys(0);
@@ -326,26 +377,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   if (wave == 3) request_entry(min(4, n_steps - 1));
   if (wave >= 4 && wave < 7 && span_step(wave - 4) < n_steps) request_anchors(wave - 4);
 
-  // ---- weights, as operand rows.  W: tile j's row 2 x (+ 1) is feature 16 half + 2 x + j (+ 64), x < 8; it stays in the accumulation registers, which
-  // the matrix instructions read as they are.  Those to be folded: a channel's features 32 + 8 kg .. and 96 + 8 kg .., read for every span.  The halves
-  // take neighbouring steps of channels in the other order, and fold every second one.
-  auto step_of = [&](int i) __attribute__((always_inline)) { return i ^ half; };
-  uint4v W[KS][2];
-  const uint16_t* const BF = B + kPagedQLow + 8 * kg;
-  auto fold_weights = [&](int i, uint4v (&f)[2][2]) __attribute__((always_inline)) {
-    const int ks = step_of(2 * i);
-    const uint32_t keep = ks < ks_here ? 0xffffffffu : 0u;   // channels behind the rank: zero
-#pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      const int ch = min(slice * KS * 32 + 32 * ks + 16 * v + col, rk - 1);
-      f[v][0] = *reinterpret_cast<const uint4v*>(BF + (size_t)ch * width);
-      f[v][1] = *reinterpret_cast<const uint4v*>(BF + (size_t)ch * width + kHalf);
-      if (SL == 2)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) f[v][e] &= keep;
-    }
-  };
-  int shift = 0;                               // they are held times 2^shift
+  int shift = 0;                               // weights are held times 2^shift
   float b_max = 0.f;                           // of those to be folded
   auto prepare_weights = [&](uint4v (&f)[2][2]) __attribute__((always_inline)) {
     if (!__is_same(T, F16))
@@ -360,36 +392,22 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     uint32_t top = 0, top_f = 0;               // the largest, without its sign
     auto larger = [](uint32_t t, uint32_t w) __attribute__((always_inline)) { return max(t, max(w & 0x7fffu, (w >> 16) & 0x7fffu)); };
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      const int ks = step_of(i);
-      const uint32_t keep = ks < ks_here ? 0xffffffffu : 0u;
+    for (int i = 0; i < KS; ++i)
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        uint32_t x[2];
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const int ch = min(slice * KS * 32 + 32 * ks + 16 * v + 4 * kg + u, rk - 1);
-          x[v] = *reinterpret_cast<const uint32_t*>(B + (size_t)ch * width + (col & 1) * kHalf + 16 * half + 2 * (col >> 1));
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          W[i][j][u] = keep & __builtin_amdgcn_perm(x[1], x[0], j & 1 ? 0x07060302u : 0x05040100u);
-          if (!__is_same(T, F16)) top = larger(top, W[i][j][u]);
-        }
+        const uint32_t x0 = W[i][0][u] & keep_of(i), x1 = W[i][1][u] & keep_of(i);
+        W[i][0][u] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+        W[i][1][u] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+        if (!__is_same(T, F16)) top = larger(larger(top, x0), x1);
       }
-      if (__is_same(T, F16))
 #pragma unroll
-        for (int j = 0; j < 2; ++j) asm volatile("" : "+v"(W[i][j]));
-      if (i & 1) continue;
-      uint4v f[2][2];
-      fold_weights(i / 2, f);
+    for (int i = 0; i < KS / 2; ++i)
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int v = 0; v < 2; ++v)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) top_f = larger(top_f, f[v][e][u]);
-    }
+          for (int e = 0; e < 2; ++e) top_f = larger(top_f, F[i][v][e][u]);
     b_max = max_of_wave(T::to_float((uint16_t)top_f));
     if (!__is_same(T, F16)) {
       const float all = max_of_wave(T::to_float((uint16_t)max(top, top_f)));
@@ -398,22 +416,16 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
 #pragma unroll
       for (int i = 0; i < KS; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int u = 0; u < 4; ++u) W[i][j][u] = to_f16<T>(W[i][j][u], shift);
-          asm volatile("" : "+v"(W[i][j]));
-        }
     }
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) asm volatile("" : "+v"(W[i][j]));
   }
 
-  // ---- Rebuilt pairs 16 half + 4 kg + p at token col of 16; folded pairs 32 + 8 kg + p at node col % 8 of a span.
-  float tc[4], ts[4];                          // cos and sin of 16 positions
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const int f = 16 * half + 4 * kg + p, at16 = min(16, a.rope_len - 1);
-    tc[p] = a.rope[rope_f32_index(at16, f, 0, kRopeTableStride)];
-    ts[p] = a.rope[rope_f32_index(at16, f, 1, kRopeTableStride)];
-  }
   const float unit = __builtin_amdgcn_ldexpf(1.f, -shift);
   int ea[NQ];
 #pragma unroll
@@ -857,6 +869,17 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(k_off[i]));
   };
   const int n_end = n_steps + (TWO ? 1 : 2);
+  if (AHEAD) {                                 // the first span's
+    nodes_of(0, nodes);
+#pragma unroll
+    for (int i = 0; i < KS / 2; ++i) {
+      uint4v g[NG];
+      prepare_weights(F[i]);
+      fold_one(F[i], nodes, g);
+      H[AHEAD ? i : 0][0] = g[0];
+    }
+    ready = KS / 2;
+  }
   for (int n = 0; n < n_end; ++n) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // what interval n - 1 requested
 #pragma unroll
