@@ -319,15 +319,37 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) f[v][e] &= keep_of(2 * i);
   };
-  {
-    const uint32_t at = 4 * kg * b_pitch + ((col & 1) * kHalf + 16 * half + 2 * (col >> 1)) * 2;
+  // W comes by LDS, half of the steps at a time, where keys and values will be: a step's 32 channels x 16 features twice in 2 KiB, the channels in an
+  // order that spreads a lane group's over the banks.  (Loaded as operands, 4 bytes a lane, the weights took half of a prologue of 49000 cycles.)
+  constexpr int kBatch = KS / 2;
+  static_assert(ld.total - ld.p >= kBatch * 2048 * (kThreads / 64), "LDS");
+  const int w_stage = ld.p + wave * (kBatch * 2048);
+  auto request_weights = [&](int first) __attribute__((always_inline)) {
+    const uint32_t at = (uint32_t)(16 * (lane >> 5) + 4 * ((lane >> 1) & 3) + ((lane >> 3) & 3)) * b_pitch + (16 * half + 8 * (lane & 1)) * 2;
 #pragma unroll
-    for (int i = 0; i < KS; ++i)
+    for (int i = 0; i < kBatch; ++i)
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int e = 0; e < 2; ++e) load_to_lds(row_of(first + i, 0) + (at + e * kHalf * 2), lds0 + w_stage + i * 2048 + e * 1024);
+  };
+  uint32_t top = 0;                            // the largest, without its sign
+  auto larger = [](uint32_t t, uint32_t w) __attribute__((always_inline)) { return max(t, max(w & 0x7fffu, (w >> 16) & 0x7fffu)); };
+  auto take_weights = [&](int first) __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int v = 0; v < 2; ++v) W[i][v][u] = *reinterpret_cast<const uint32_t*>(row_of(i, 16 * v + u) + at);     // (two features each; see below)
-  }
+    for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint32_t x[2];
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+          x[v] = keep_of(first + i) & *reinterpret_cast<const uint32_t*>(lds + w_stage + i * 2048 + (col & 1) * 1024 + ((4 * v + u) * 8 + 2 * kg) * 16 + (col >> 1) * 4);
+        W[first + i][0][u] = __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
+        W[first + i][1][u] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
+        if (!__is_same(T, F16)) top = larger(larger(top, x[0]), x[1]);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  request_weights(0);
   uint4v F[KS / 2][2][2];
 #pragma unroll
   for (int i = 0; i < KS / 2; ++i) fold_weights(i, F[i]);
@@ -389,17 +411,9 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
           for (int e = 0; e < 2; ++e) f[v][e][i] = to_f16<T>(f[v][e][i], shift);
   };
   {
-    uint32_t top = 0, top_f = 0;               // the largest, without its sign
-    auto larger = [](uint32_t t, uint32_t w) __attribute__((always_inline)) { return max(t, max(w & 0x7fffu, (w >> 16) & 0x7fffu)); };
-#pragma unroll
-    for (int i = 0; i < KS; ++i)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t x0 = W[i][0][u] & keep_of(i), x1 = W[i][1][u] & keep_of(i);
-        W[i][0][u] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
-        W[i][1][u] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
-        if (!__is_same(T, F16)) top = larger(larger(top, x0), x1);
-      }
+    uint32_t top_f = 0;
+    take_weights(0);
+    request_weights(kBatch);
 #pragma unroll
     for (int i = 0; i < KS / 2; ++i)
 #pragma unroll
@@ -409,6 +423,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) top_f = larger(top_f, F[i][v][e][u]);
     b_max = max_of_wave(T::to_float((uint16_t)top_f));
+    take_weights(kBatch);
     if (!__is_same(T, F16)) {
       const float all = max_of_wave(T::to_float((uint16_t)max(top, top_f)));
       shift = __builtin_amdgcn_readfirstlane(15 - __builtin_amdgcn_frexp_expf(all));
