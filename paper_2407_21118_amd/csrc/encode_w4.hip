@@ -6,7 +6,7 @@
 // their sums in LDS.  The sums of x come from the matrix instruction, too, with ones for weights, which lays them out like the products.
 // Codes enter as they are: in float16 as the subnormal numbers c * 2^-24 (exact, also on the matrix cores), in bfloat16 as 128 + c,
 // the offset going to the zero-point.  So every product is exact and sums are float32; the only rounding to 16 bits is the result's.
-// Bound by latency: the weights' bytes (8.4 MB of 4096 inputs by 4096 columns) are worth 1.6 us, the launch 2.4, a kernel without its loop 2.4; it takes
+// Bound by latency: the weights' bytes (8.4 MB of 4096 inputs by 4096 columns) are worth 1.6 us, and a kernel without its loop takes 2.4; it takes
 // 5.2 us for a token, 7.0 for 24; 333 tokens by 1024 columns 14 (a workgroup's 32 by 64 results: 12.5).  64 tokens by 64 columns were slower (22 us a
 // round of workgroups).
 

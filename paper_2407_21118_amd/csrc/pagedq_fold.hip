@@ -9,6 +9,17 @@
 //   sum_{f >= 32} = sum_{i < 8} L_i(t)  h_t . g_i,   g_i[r] = sum_f B_k[r, f] a_f(t_i) + B_k[r, f + 64] b_f(t_i),
 // with t_i the Chebyshev nodes of the span and L_i their Lagrange polynomials: 16 rows of weights (g_i as a pair of float16
 // numbers) instead of 64, made anew once per span by a sixteenth of the work that they save.
+//
+// A workgroup takes up to four heads of a group (or of groups side by side; two heads, in halves of their channels, for key ranks above 256) and a run of
+// steps of 64 tokens.  Eight wavefronts, two to a SIMD: a head's rebuilt pairs half each, weights in registers for the whole run.  Codes are staged in LDS
+// as exact float16 integers; a token's scales multiply sums, not codes.  In an interval one of the two wavefronts makes the scores of step n while the
+// other weighs step n - 1, adds up the values of n - 2 and converts the codes of n + 1, and then the other way round: matrix and vector instructions go
+// together without being mixed by hand.  (One wavefront per SIMD with 512 registers, its scores, weights, values and codes dealt out between the matrix
+// instructions: 312 us for 16 x 8192 rows of 32 heads of rank 256 against 282, 177 against 157 for one sequence of 65536, and 193 against 111 for 4 x 16384
+// rows with four query rows a head, two of which are taken at a time here.)
+//
+// Bound by the instructions of two wavefronts a SIMD and their latencies: 8700 cycles an interval, of which the matrix pipe is busy 2800 and the vector
+// unit 5200; the start of a run takes 34000 (weights of 256 KB a workgroup from L2) and its end 4000.
 
 #include "paged_dev.h"
 #include "pagedq.h"

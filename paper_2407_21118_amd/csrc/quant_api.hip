@@ -133,6 +133,7 @@ int plan_pagedq(const palu_layer_desc* desc, int batch, int max_len, int window,
     double best = 1e300;
     for (int n = 1; n <= std::min<long long>(ceil_div(c->max_tiles, 2), most); ++n) {
       const int tiles = ceil_div(ceil_div(c->max_tiles, n), 2) * 2, used = ceil_div(c->max_tiles, tiles);
+      if (best < 1e300 && wgs * used * kPagedQFoldThreads > 0xffffffffLL) break;           // (work items of a launch)
       const double cost = paged_makespan(wgs * used, 8.0 + tiles, 0, 8.0 + tiles, cus) + 0.05 * used;
       if (cost >= best) continue;
       best = cost;

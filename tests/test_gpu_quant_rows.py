@@ -150,6 +150,29 @@ def test_many_rows_and_offsets_beyond_32_bits():
         assert torch.equal(o[pick].cpu(), torch.from_numpy(O.dequant_latent(*held)).half())
 
 
+@pytest.mark.parametrize("bits", [4, 3, 2])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_written_rows_of_every_size_of_number(dtype, bits):
+    """Numbers of all exponents beside one another, blocks whose range is infinite: the oracle's float32 steps, bit for bit."""
+    R, n = 256, 1500
+    rng = np.random.default_rng(bits)
+    raw = torch.from_numpy(rng.integers(0, 2 ** 16, (n, R)).astype(np.uint16).view(np.int16)).view(torch_dtype(dtype))
+    raw = torch.where(torch.isfinite(raw), raw, torch.ones_like(raw))
+    lane = np.arange(R)
+    for i in range(200):                                       # blocks of a few exponents only
+        keep = torch.from_numpy(rng.integers(-12, 13, R).astype(np.float32) * np.float32(2.0) ** rng.integers(-24, 15) * (1 + lane % 7))
+        raw[i] = keep.to(raw.dtype).nan_to_num(0.0, 6e4, -6e4)
+    desc = make_desc(dtype, bits, bits, rk=R, rv=R, groups=1)
+    x = raw.cuda()
+    k, v = caches(n, R, bits), caches(n, R, bits)
+    P.palu_quant_latent_kv(desc, x, x, *k, *v)
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = O.quant_latent(raw.float().numpy(), bits=bits)
+    for a, b, c in zip(k, v, want):
+        a, b = a.cpu().numpy(), b.cpu().numpy()
+        assert np.array_equal(a.view(np.uint8), c.view(np.uint8)) and np.array_equal(a.view(np.uint8), b.view(np.uint8))
+
+
 # ---- the projection
 
 def weights(R, d, seed, shape="normal"):
@@ -217,6 +240,32 @@ def test_projection_of_layers(dtype, heads, q_per_kv, k_off, v_off):
             rest = np.ones(2 * n, bool)
             rest[dst[keep]] = False
             assert (got[torch.from_numpy(rest).cuda()] == 99.0).all() and (got[:, R:] == 99.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,n", [(3, 513), (4, 700), (8, 609), (1, 540)])
+def test_projection_of_many_tokens(dtype, heads, n):
+    """Sixty-four columns a workgroup; scales and zero-points on no more than their own two bytes' alignment, one to eight groups of inputs."""
+    say(f"[project] {dtype} {heads} heads, {n} tokens")
+    desc = P.LayerDesc(heads, 128, [0, heads], [0, 512], [0, 576], P.PALU_F16 if dtype == "f16" else P.PALU_BF16)
+    d = heads * 128
+    x = latents(n, d, dtype, n)
+    Ak, Av = weights(desc.R_k, d, 6, "any"), weights(desc.R_v, d, 7, "any")
+    for odd in (0, 1):
+        dev = []
+        for y in Ak + Av:
+            y = torch.from_numpy(y)
+            if odd and y.dtype == torch.float16:
+                y = torch.cat([y.flatten()[:1], y.flatten()]).cuda()[1:].view(y.shape)
+            dev.append(y.cuda())
+        dst = np.arange(n, dtype=np.int32)
+        dst[::9] = -1
+        out = [torch.full((n, R), 99.0, dtype=x.dtype, device="cuda") for R in (desc.R_k, desc.R_v)]
+        P.palu_encode_kv_w4(desc, x, *dev, out[0], desc.R_k, out[1], desc.R_v, dst_row=torch.from_numpy(dst).cuda())
+        keep = torch.from_numpy(dst >= 0).cuda()
+        for got, w in zip(out, (Ak, Av)):
+            hold_projection(got[keep], x[keep], w, dtype)
+            assert (got[~keep] == 99.0).all()
 
 
 def test_projection_beyond_the_types_middle():
