@@ -313,6 +313,13 @@ def test_same_bits_every_time_and_sequences_apart():
     assert torch.equal(first[0], again[0]) and torch.equal(first[3], again[3]) and not again[1].any()
 
 
+@pytest.mark.parametrize("name", ["4x256", "gqa2", "8x512", "4x128-384", "gqa2-128-512"])
+def test_short_sequences_and_angle_tables_no_longer_than_they(name):
+    for seed, lens in enumerate(([1], [3], [16], [17], [33, 1], [64, 65, 2])):
+        say(f"[paged 4 bits] {name}, {lens} rows")
+        check(Pool(LAYERS[name](), "f16", lens, 16, seed=seed))
+
+
 def test_many_query_rows_over_a_window_with_sinks_far_apart():
     """The jump from the sinks to the window lies inside a workgroup's run of tiles."""
     for name in ("4x256", "gqa4", "gqa20-512", "gqa70"):

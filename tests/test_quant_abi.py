@@ -54,6 +54,13 @@ def test_attention_refuses_layers(kw, status):
     assert attend(None) == -1
 
 
+def test_large_batches_have_a_launch():
+    for heads, max_len in ((8, 1 << 20), (32, 1 << 20), (128, 100)):
+        off = [4 * j for j in range(heads // 4 + 1)]
+        d = P.LayerDesc(heads, 128, off, [64 * x for x in off], [64 * x for x in off], k_latent_dtype=P.PALU_I4, v_latent_dtype=P.PALU_I4)
+        assert P.palu_attn_paged_quant_workspace_bytes(d, 65535, max_len) > 0
+
+
 def test_attention_workspace():
     lib, out = P.load_library(), ctypes.c_size_t(0)
     for act in (P.PALU_F16, P.PALU_BF16):
