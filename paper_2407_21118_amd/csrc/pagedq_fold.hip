@@ -724,7 +724,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     return scores + (((TWO ? 0 : n & 1) * HEADS + hw) * NQ + r) * PARTS * kSteps + lane;
   };
   constexpr bool AHEAD = NQ == 1 && VB == 2 && SL == 1;
-  uint4v H[AHEAD ? KS / 2 : 1][1];
+  uint4v H[AHEAD ? KS / 2 : 1][NG];
   Nodes nodes;
   int ready = 0;                               // steps of channels of the next span that are folded
   // One query row: of the next span's folded weights, one step of channels in every step of a span of four
@@ -740,9 +740,9 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     ++ready;
   };
   auto begin_span = [&](int n) __attribute__((always_inline)) {
-    if (AHEAD && ready == KS / 2) {
+    if (ready == KS / 2) {                     // (or in G already)
 #pragma unroll
-      for (int i = 0; i < KS / 2; ++i) G[i][0] = H[AHEAD ? i : 0][0];
+      for (int i = 0; i < (AHEAD ? KS / 2 : 0); ++i) G[i][0] = H[AHEAD ? i : 0][0];
     } else {
       fold(n);
     }
@@ -895,14 +895,13 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(k_off[i]));
   };
   const int n_end = n_steps + (TWO ? 1 : 2);
-  if (AHEAD) {                                 // the first span's
+  if (NQ == 1) {                               // the first span's.  (With two rows the weights' registers are wanted, and it reads them again.)
     nodes_of(0, nodes);
 #pragma unroll
     for (int i = 0; i < KS / 2; ++i) {
-      uint4v g[NG];
       prepare_weights(F[i]);
-      fold_one(F[i], nodes, g);
-      H[AHEAD ? i : 0][0] = g[0];
+      if (AHEAD) fold_one(F[i], nodes, H[AHEAD ? i : 0]);
+      else fold_one(F[i], nodes, G[i]);
     }
     ready = KS / 2;
   }
@@ -915,7 +914,8 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     if (n + 2 < n_steps) request_keys(n + 2);
     if (n < n_steps) request_values(n);
     request(n);
-    if (n < n_steps && folds(n)) begin_span(n);
+    constexpr bool kAtTop = AHEAD || TWO;      // (else one wavefront of a SIMD folds while the other does the rest)
+    if (kAtTop && n < n_steps && folds(n)) begin_span(n);
     if constexpr (TWO) {
       here();
       if (n < n_steps) all_keys(n);
@@ -929,6 +929,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
       for (int turn = 0; turn < 2; ++turn) {
         here();
         if (turn == half) {
+          if (!kAtTop && n < n_steps && folds(n)) begin_span(n);
           if (n < n_steps) all_keys(n);
         } else {
           const bool more = ahead(n);
