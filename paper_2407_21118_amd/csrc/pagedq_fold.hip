@@ -15,7 +15,7 @@
 // as exact float16 integers; a token's scales multiply sums, not codes.  In an interval one of the two wavefronts makes the scores of step n while the
 // other weighs step n - 1, adds up the values of n - 2 and converts the codes of n + 1, and then the other way round: matrix and vector instructions go
 // together without being mixed by hand.  (One wavefront per SIMD with 512 registers, its scores, weights, values and codes dealt out between the matrix
-// instructions: 312 us for 16 x 8192 rows of 32 heads of rank 256 against 282, 177 against 157 for one sequence of 65536, and 193 against 111 for 4 x 16384
+// instructions: 312 us for 16 x 8192 rows of 32 heads of rank 256 against 282, 177 against 157 for one sequence of 65536, and 193 against 106 for 4 x 16384
 // rows with four query rows a head, two of which are taken at a time here.)
 //
 // Bound by the instructions of two wavefronts a SIMD and their latencies: 8700 cycles an interval, of which the matrix pipe is busy 2800 and the vector
@@ -118,7 +118,8 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   const PagedSpan span = paged_span(L, 0, a.window, a.n_sink);
   const int n_chunks = (span.n_tiles + a.chunk_tiles - 1) / a.chunk_tiles;
   if (chunk >= n_chunks) return;
-  const int i0 = (int)((long long)span.n_tiles * chunk / n_chunks), i1 = (int)((long long)span.n_tiles * (chunk + 1) / n_chunks);
+  const int share = span.n_tiles / n_chunks, longer = span.n_tiles - share * n_chunks;   // the first runs are a tile longer
+  const int i0 = chunk * share + min(chunk, longer), i1 = i0 + share + (chunk < longer ? 1 : 0);
   const int g = un.group(), nh = un.nh(), h0 = un.h0();
   const int rk = m.k_off[g + 1] - m.k_off[g], rv = m.v_off[g + 1] - m.v_off[g], per_group = m.head_off[g + 1] - m.head_off[g];
   int k_cols = un.n_groups() * rk, v_cols = un.n_groups() * rv, CB = v_cols / 128;
