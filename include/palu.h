@@ -556,7 +556,8 @@ int palu_dequant_latent_kv(const palu_layer_desc* desc, const uint8_t* k_codes, 
  *                latent dtypes: the rows of a quantized cache are then written with palu_quant_latent_kv)
  *   dst_row      DEVICE int32 [n_tok], or NULL for row t; tokens with a negative row are not written
  *   n_tok        >= 0
- * Products are exact, sums float32 (of 128 products, then scaled and added up), rounded once to act_dtype.
+ * Products are exact, sums float32 (of 128 products by 16 + code, less 16 + zero times the inputs' sum, then scaled and added up),
+ * rounded once to act_dtype.
  */
 int palu_encode_kv_w4(const palu_layer_desc* desc, const void* x, int32_t n_tok,
                       const uint8_t* Akt, const void* Ak_scale, const void* Ak_zero,

@@ -4,8 +4,9 @@
 //
 // A workgroup takes 16 or 64 columns c (one row of codes each) and 16 or 32 tokens; its eight wavefronts take the groups, four in turn, and add up
 // their sums in LDS.  The sums of x come from the matrix instruction, too, with ones for weights, which lays them out like the products.
-// Codes enter as they are: in float16 as the subnormal numbers c * 2^-24 (exact, also on the matrix cores), in bfloat16 as 128 + c,
-// the offset going to the zero-point.  So every product is exact and sums are float32; the only rounding to 16 bits is the result's.
+// Codes enter as 16 + c, a normal number with the code in its uppermost bits, the offset going to the zero-point.  So every product is exact and sums
+// are float32; the only rounding to 16 bits is the result's.  (The matrix cores keep 24 bits below the largest exponent of an instruction's products and
+// take a subnormal operand's for 2^-14: codes as the float16 numbers c * 2^-24 lost what lies 2^-15 below the largest input.)
 // Bound by latency: the weights' bytes (8.4 MB of 4096 inputs by 4096 columns) are worth 1.6 us, and a kernel without its loop takes 2.4; it takes
 // 5.2 us for a token, 7.0 for 24; 333 tokens by 1024 columns 14 (a workgroup's 32 by 64 results: 12.5).  64 tokens by 64 columns were slower (22 us a
 // round of workgroups).
@@ -19,26 +20,26 @@ namespace {
 
 template <typename T> struct W4Codes;
 template <> struct W4Codes<F16> {
-  static constexpr uint32_t kOne = 0x3c003c00u, kOffset = 0u;
-  static constexpr float kUnit = 16777216.f, kZero = 0.f;    // a code is worth 1 / kUnit; what is added to it
+  static constexpr uint32_t kOne = 0x3c003c00u, kSixteen = 0x4c004c00u;
+  static constexpr int kShift = 6;             // of a code, to add it to 16
   static __device__ __forceinline__ float4v mma(uint4v a, uint4v b, float4v c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
   }
 };
 template <> struct W4Codes<BF16> {
-  static constexpr uint32_t kOne = 0x3f803f80u, kOffset = 0x43004300u;
-  static constexpr float kUnit = 1.f, kZero = 128.f;
+  static constexpr uint32_t kOne = 0x3f803f80u, kSixteen = 0x41804180u;
+  static constexpr int kShift = 3;
   static __device__ __forceinline__ float4v mma(uint4v a, uint4v b, float4v c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
 };
 
-// Eight codes as eight 16-bit numbers
-template <typename T> __device__ __forceinline__ uint4v spread(uint32_t w, uint32_t offset) {
+// Eight codes as eight 16-bit numbers 16 + c
+template <typename T> __device__ __forceinline__ uint4v spread(uint32_t w, uint32_t sixteen) {
   const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
   uint4v r;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) r[u] = __builtin_amdgcn_perm(odd, even, 0x0c040c00u + 0x00010001u * u) | offset;
+  for (int u = 0; u < 4; ++u) r[u] = __builtin_amdgcn_perm(odd, even, 0x0c040c00u + 0x00010001u * u) << W4Codes<T>::kShift | sixteen;
   return r;
 }
 
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(kW4Threads, 2) void encode_w4_kernel(EncodeW4Args a
   const EncodeW4Side& sd = a.side[s];
   const int c0 = 16 * NC * (blockIdx.y - (s ? a.side[0].tiles : 0));
   const int t0 = blockIdx.x * (NT * 16), groups = a.d / 128;
-  const uint32_t offset = W4Codes<T>::kOffset == 0 ? 0u : per_lane_constant(W4Codes<T>::kOffset);
+  const uint32_t sixteen = per_lane_constant(W4Codes<T>::kSixteen);
   const uint4v ones = {W4Codes<T>::kOne, W4Codes<T>::kOne, W4Codes<T>::kOne, W4Codes<T>::kOne};
   const uint8_t* const codes = sd.codes + (size_t)(c0 + col) * (a.d / 2) + kg * 16;
   const uint16_t* const scale = sd.scale + (size_t)(c0 + (NC == 1 ? col : lane)) * groups;
@@ -146,7 +147,7 @@ __global__ __launch_bounds__(kW4Threads, 2) void encode_w4_kernel(EncodeW4Args a
           }
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
-            const uint4v b = spread<T>(w[i][c][j], offset);
+            const uint4v b = spread<T>(w[i][c][j], sixteen);
 #pragma unroll
             for (int n = 0; n < NT; ++n) dot[n][c] = W4Codes<T>::mma(v[n], b, dot[n][c]);
           }
@@ -154,11 +155,11 @@ __global__ __launch_bounds__(kW4Threads, 2) void encode_w4_kernel(EncodeW4Args a
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const int k = i0 + i;
-          const float s1 = F16::to_float((uint16_t)(sc[c][k >> 1] >> (16 * (k & 1)))), z1 = F16::to_float((uint16_t)(z[c][k >> 1] >> (16 * (k & 1)))) + W4Codes<T>::kZero;
+          const float s1 = F16::to_float((uint16_t)(sc[c][k >> 1] >> (16 * (k & 1)))), z1 = F16::to_float((uint16_t)(z[c][k >> 1] >> (16 * (k & 1))));
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[n][c][e] += s1 * (dot[n][c][e] * W4Codes<T>::kUnit - z1 * sum[n][e]);
+            for (int e = 0; e < 4; ++e) h[n][c][e] = __builtin_fmaf(s1, __builtin_fmaf(-z1, sum[n][e], __builtin_fmaf(-16.f, sum[n][e], dot[n][c][e])), h[n][c][e]);
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the inputs have been read)

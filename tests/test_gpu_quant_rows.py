@@ -284,6 +284,34 @@ def test_projection_beyond_the_types_middle():
     assert torch.equal(out[0], out[1])
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 20, 600])
+@pytest.mark.parametrize("large", [0, 1, 15])
+def test_small_products_beside_large_ones_that_cancel(dtype, n, large):
+    """Every token has one large input, its negative and one 2^-14.2 of it, at places that differ from token to token; the weights of the
+    large two are equal.  Sums of three products are two float32 additions, off by 2^-23 of the largest magnitude each where bits are cut
+    off; codes enter as 16 + c, so that magnitude is 31 inputs for the products and 16 for the zero-point's share."""
+    desc = P.LayerDesc(2, 128, [0, 2], [0, 64], [0, 64], P.PALU_F16 if dtype == "f16" else P.PALU_BF16)
+    d, top = 256, 4096.0
+    x, codes = torch.zeros(n, d, dtype=torch.float64), np.full((64, d), large, np.uint8)
+    small = torch.tensor(top * 2.0 ** -14.2).to(torch_dtype(dtype)).double()
+    rng = np.random.default_rng(large)
+    ones = rng.choice(d, 40, replace=False)                    # inputs whose weights are 1
+    codes[:, ones] = 1
+    for t in range(n):
+        a, b = rng.choice([i for i in range(128) if i not in ones], 2, replace=False)
+        x[t, a], x[t, b], x[t, rng.choice(ones)] = top, -top, small
+    w = (codes[:, 0::2] | codes[:, 1::2] << 4, np.ones((64, 2), np.float16), np.zeros((64, 2), np.float16))
+    dev = [torch.from_numpy(np.ascontiguousarray(y)).cuda() for y in w]
+    out = [torch.empty(n, 64, dtype=torch_dtype(dtype), device="cuda") for _ in range(2)]
+    P.palu_encode_kv_w4(desc, x.to(torch_dtype(dtype)).cuda(), *dev, *dev, out[0], 64, out[1], 64)
+    room = 2 * 2.0 ** -23 * (31 + 16) * top + (2.0 ** -11 if dtype == "f16" else 2.0 ** -8) * small
+    for got in out:
+        off = (got.double().cpu() - small).abs().max()
+        say(f"[project] {dtype} {n} tokens, weights {large}: off by {float(off):.4f} of {float(small):.4f}, tolerance {float(room):.4f}")
+        assert off <= room
+
+
 # ---- as they are used together
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
