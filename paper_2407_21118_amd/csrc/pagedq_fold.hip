@@ -846,13 +846,15 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
   };
 
   // ---- values of step n.  A wavefront has half of the tokens of a block of 128 columns, where there are one or two blocks of every second four.
-  float4v O[NO];                               // column 8 col + (4 quarter +) u of rows 4 kg + e (behind the weights' rows those of what their rounding left); odd columns in units of 2^-20, even ones of 2^-24
+  float4v O[NO];                               // column 8 col + (4 quarter +) u of rows 4 kg + e (behind the weights' rows those of what their rounding left); odd columns in units of 1/16
 #pragma unroll
   for (int u = 0; u < NO; ++u) O[u] = float4v{0, 0, 0, 0};
   int vb0 = wave & (VB - 1), half0 = VB == 2 ? (wave >> 1) & 1 : wave >> 2, quarter = VB == 2 ? wave >> 2 : 0;
   // Codes enter as code - 8: most zero-points are near 8, and sums of codes and of zero-points, which all but cancel over many tokens, would leave their
-  // rounding (4e-5 of the largest output at 3000 tokens, against 4e-6).
-  const half2v minus8_even = __builtin_bit_cast(half2v, 0x80088008u), minus8_odd = __builtin_bit_cast(half2v, 0x80808080u);
+  // rounding (4e-5 of the largest output at 3000 tokens, against 4e-6).  As normal numbers, by way of 1024 + code or 1024 + 16 code: the matrix cores keep 24
+  // bits below the largest exponent of an instruction's products and take a subnormal operand's for 2^-14 (codes in units of 2^-24 and 2^-20 added an error of
+  // 5.4e-5 of the output, 2-norm, to 65536 rows).
+  const half2v minus8_even = __builtin_bit_cast(half2v, 0xe408e408u), minus8_odd = __builtin_bit_cast(half2v, 0xe480e480u);   // -1032, -1152
   auto values = [&](int n) __attribute__((always_inline)) {
     const int vb = vb0;
     if (vb >= CB) return;
@@ -873,8 +875,8 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {            // tokens 2 i, 2 i + 1
         const uint32_t x = __builtin_amdgcn_perm(d[2 * i + 1], d[2 * i], pick);
-        even[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x & 0x000f000fu) + minus8_even);
-        odd[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, x & 0x00f000f0u) + minus8_odd);
+        even[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, (x & 0x000f000fu) | k1024) + minus8_even);
+        odd[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, (x & 0x00f000f0u) | k1024) + minus8_odd);
       }
       O[2 * j] = mma<F16>(p, even, O[2 * j]);
       O[2 * j + 1] = mma<F16>(p, odd, O[2 * j + 1]);
@@ -987,7 +989,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
       const float2 f = fin[row * VB + vb];
       const float worth = (tops[row] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(f.y - tops[row])) / kWeightScale;
 #pragma unroll
-      for (int u = 0; u < NO; ++u) y[u] = (y[u] * ((u & 1 ? 1048576.f : 16777216.f)) - f.x) * worth;
+      for (int u = 0; u < NO; ++u) y[u] = (y[u] * (u & 1 ? 0.0625f : 1.f) - f.x) * worth;
       const int ohead = m.o_off[g] + (h0 + h - m.head_off[g]) * rv;
       float* const o = a.o_part + slot * a.o_stride + (size_t)m.qpk * ohead + (size_t)(row0 + r) * rv + 128 * vb - vg * rv + 8 * col + 4 * quarter;
 #pragma unroll

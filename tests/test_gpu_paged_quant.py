@@ -357,3 +357,50 @@ def test_two_calls_at_once_on_two_streams():
                 got.append((alone, pool.call(d)))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in got)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("name", ["4x128", "4x256", "4x128-384", "gqa4", "8x512"])
+def test_small_values_beside_large_ones_that_cancel(name, dtype):
+    """Equal scores; of 40 rows two have values of 15 and -15 times a scale, one has 7 of a scale 2^-17 as large, the others none.  The weights of
+    the large two are equal, so that their rounding cancels; what is left are float32 sums of three products, of at most 8 weights each, and of three
+    zero-points' shares, at most 8 weights each: four additions, off by 2^-23 of 15 weights each where bits are cut off, 2^-17 of a weight.
+    (The output, 1.3e-6, is among the float16 numbers that are 2^-24 apart.)"""
+    layer = LAYERS[name]()
+    for first in ((0, 1, 2), (3, 39, 17), (30, 12, 38)):
+        pool = Pool(layer, dtype, [40], 16, seed=21)
+        pool.q[:] = 0
+        packed, s, z = (x.copy() for x in pool.rows["v"][0])
+        packed[:], s[:], z[:] = 0x88, 1.0, 8.0
+        a, b, c = first
+        packed[a], z[a] = 0xFF, 0.0
+        packed[b], z[b] = 0x00, 15.0
+        packed[c], s[c] = 0xFF, 2.0 ** -17
+        pool.rows["v"][0] = (packed, s, z)
+        for j in range(layer.n_groups):                        # output f is latent channel f of its group's values
+            n, rv = layer.group_size(j), layer.v_rank_off[j + 1] - layer.v_rank_off[j]
+            at = sum(layer.group_size(i) * 128 * (layer.v_rank_off[i + 1] - layer.v_rank_off[i]) for i in range(j))
+            one = np.zeros((rv, n, 128), np.float32)
+            one[np.arange(128), :, np.arange(128)] = 1.0
+            pool.Bv[at:at + one.size] = one.reshape(-1)
+        pool.put()
+        got, want = pool.call(pool.device()).double().cpu().numpy(), 7 * 2.0 ** -17 / 40
+        room = (2.0 ** -17 + TOL[dtype][0] * 7 * 2.0 ** -17) / 40 + (2.0 ** -25 if dtype == "f16" else 0.0)
+        off = np.abs(got - want).max()
+        say(f"[paged 4 bits] {name} {dtype}: off by {off / want:.4f} of it, tolerance {room / want:.4f}")
+        assert off <= room
+
+
+def test_error_of_a_long_sequence_beside_that_of_rounding():
+    """65536 rows.  With E the distance of the output from 64 bits and R that of the rounded 64-bit output, relative 2-norms, E^2 - R^2 is the square of
+    what the arithmetic adds.  Logits: 64 pairs, each right to 2e-6 of |q||k|, 3 on average, with either sign, over sqrt(128): 4.2e-6.
+    Weights and values: pairs of 2^-22, sums of float32: as much again at most.  Together below 2^-17; 2^-16 for an estimate from 2048 outputs."""
+    pool = Pool(synth.uniform_layer(16, 4, 128), "f16", [65536], 64, seed=22)
+    pool.put()
+    ref = pool.reference()
+    got = pool.call(pool.device()).double().cpu().numpy()
+    size = np.linalg.norm(ref)
+    E, R = np.linalg.norm(got - ref) / size, np.linalg.norm(ref.astype(np.float16).astype(np.float64) - ref) / size
+    more = np.sqrt(max(0.0, E ** 2 - R ** 2))
+    say(f"[paged 4 bits] 1 x 65536 rows: {E:.3e} from 64 bits, rounding {R:.3e}, the arithmetic adds {more:.2e}")
+    assert more <= 2.0 ** -16
