@@ -148,6 +148,7 @@ struct PagedMergeArgs {
   int max_len, first, window, n_sink;
   int batch;
   int chunk_tiles, n_slots, n_shared;
+  int scaled;                                  // merged latents may lie anywhere in float32
   long long o_stride, o_shared_stride;
   PagedMeta meta;
 };

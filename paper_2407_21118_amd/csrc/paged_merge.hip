@@ -7,6 +7,8 @@ namespace palu {
 // A workgroup takes R rows (sequence, query head) of one key/value head: weights exp2(max - largest max) of their partial results, the
 // weighted sums of the latents, normalised and split into pairs of 16-bit numbers hi + lo (float16: 2^-21, or 2^-25 absolute below
 // 1/8), times the head's 128 columns of B_v (a wavefront makes 32; its weights are requested first, and arrive meanwhile).
+// Where latents come from codes and scales their values may exceed float16's range, or lie below it: a row is then held times a power of two that
+// puts its largest latent at 2^14 or above, and pairs are right to 2^-21, or 2^-39 of the row's largest.
 // grid (blocks of R rows, key/value heads), 256 threads.
 // Bound by the latency of its few dependent steps where there are few rows, else by reading the partial results: R is as
 // small as it takes for a workgroup or two per compute unit.
@@ -17,6 +19,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
   __shared__ __attribute__((aligned(16))) float Part[256 * 4];
   __shared__ float Weight[R][kBlock];
   __shared__ float Inv[R], Top[R];
+  __shared__ uint32_t Size[R];                 // a row's largest latent, as bits
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, kg = lane >> 4;
   const PagedMeta& m = a.meta;
@@ -72,6 +75,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
     if (tid % kPer == 0) {
       Top[r] = top;
       Inv[r] = sum == 0.f ? 0.f : 1.f / sum;
+      Size[r] = 0;
     }
   }
 
@@ -115,8 +119,16 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
       }
     }
   }
-  auto put = [&](int r, int c, float4v x) {
+  const bool scaled = __is_same(T, F16) && a.scaled;
+  auto shift_of = [&](int r) { return 15 - __builtin_amdgcn_frexp_expf(__builtin_bit_cast(float, Size[r])); };
+  auto finish = [&](int r, float4v& x) {
     x *= Inv[r];
+    if (scaled) atomicMax(&Size[r], __builtin_bit_cast(uint32_t, fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])))));
+  };
+  auto put = [&](int r, int c, float4v x) {
+    if (scaled)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_ldexpf(x[e], shift_of(r));
     uint32_t hi[2], lo[2];
     split2<T>(x[0], x[1], &hi[0], &lo[0]);
     split2<T>(x[2], x[3], &hi[1], &lo[1]);
@@ -124,19 +136,21 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
     *reinterpret_cast<uint2v*>(&Oh[1][r * kPitch + c]) = uint2v{lo[0], lo[1]};
   };
   __syncthreads();
+  int n_mine = kItems;                                       // columns of four that this thread puts
   if (n_parts > 1) {
     if (tid < items * n_parts) *reinterpret_cast<float4v*>(&Part[tid * 4]) = o[0];
     __syncthreads();
-    if (tid < items) {
-      float4v x = o[0];
-      for (int p = 1; p < n_parts; ++p) x += *reinterpret_cast<const float4v*>(&Part[(p * items + tid) * 4]);
-      put(tid / quads, tid % quads * 4, x);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kItems; ++i)
-      if (tid + 256 * i < items) put((tid + 256 * i) / quads, (tid + 256 * i) % quads * 4, o[i]);
+    n_mine = tid < items;
+    if (tid < items)
+      for (int p = 1; p < n_parts; ++p) o[0] += *reinterpret_cast<const float4v*>(&Part[(p * items + tid) * 4]);
   }
+#pragma unroll
+  for (int i = 0; i < kItems; ++i)
+    if (i < n_mine && tid + 256 * i < items) finish((tid + 256 * i) / quads, o[i]);
+  if (scaled) __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kItems; ++i)
+    if (i < n_mine && tid + 256 * i < items) put((tid + 256 * i) / quads, (tid + 256 * i) % quads * 4, o[i]);
   __syncthreads();
 
   float4v acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -169,6 +183,10 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedMergeArgs a) {
     const int r = 4 * kg + e;
     if (r < n) {
       const int row = row0 + r, b = row / m.qpk;
+      if (scaled) {
+        acc[0][e] = __builtin_amdgcn_ldexpf(acc[0][e], -shift_of(r));
+        acc[1][e] = __builtin_amdgcn_ldexpf(acc[1][e], -shift_of(r));
+      }
       uint16_t* out = a.out + ((size_t)b * m.n_heads * m.qpk + h * m.qpk + row - b * m.qpk) * kDHead + 32 * wave + 2 * col;
       *reinterpret_cast<uint32_t*>(out) = pack2<T>(acc[0][e], acc[1][e]);
     }

@@ -290,6 +290,7 @@ int palu_attn_paged_quant(const palu_layer_desc* desc, int32_t batch, int32_t ma
   e.batch = batch;
   e.chunk_tiles = c.chunk_tiles;
   e.n_slots = c.n_slots;
+  e.scaled = 1;
   e.o_stride = c.o_stride;
   e.meta = m;
   return launch_paged_merge(e, desc->act_dtype, s);

@@ -404,3 +404,22 @@ def test_error_of_a_long_sequence_beside_that_of_rounding():
     more = np.sqrt(max(0.0, E ** 2 - R ** 2))
     say(f"[paged 4 bits] 1 x 65536 rows: {E:.3e} from 64 bits, rounding {R:.3e}, the arithmetic adds {more:.2e}")
     assert more <= 2.0 ** -16
+
+
+@pytest.mark.parametrize("name", ["4x128", "gqa4", "8x512"])
+@pytest.mark.parametrize("size,rows", [(2.0 ** -12, 5000), (2.0 ** 14, 700), (6e4, 60)])
+def test_values_of_any_size(name, size, rows):
+    """Latents far from 1 beside weights that make up for it: their mean may lie among the float16 numbers that are 2^-24 apart, a row's values (65520
+    where 65504 was quantised beside zeros) beyond the largest.  The tolerance is the other tests', relative to the outputs."""
+    pool = Pool(LAYERS[name](), "f16", [rows, 7, 33], 16, seed=23)
+    rng = np.random.default_rng(24)
+    for b, n in enumerate(pool.lens):
+        h = np.clip(size * rng.standard_normal((n, pool.layer.R_v)), -65504.0, 65504.0)
+        if size > 5e4:
+            h = np.where(rng.random(h.shape) < 0.5, 65504.0, 0.0)
+        pool.rows["v"][b] = O.quant_latent(h.astype(np.float16))
+    if size < 1:
+        pool.q *= 0.05                                         # means over many rows
+    pool.Bv = synth.round_to(pool.Bv * 2.0 ** -np.round(np.log2(size)), "f16")
+    pool.put()
+    hold(pool.call(pool.device()), pool.reference(), "f16")
