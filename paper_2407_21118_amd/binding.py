@@ -177,6 +177,20 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _empty(shape, dtype, device, stream, kept=False):
+    """Memory for a call on `stream` (None: the current one).  It is that stream's: what the current stream has freed may still be in use there, and
+    what is freed here goes to calls that come behind this one.  kept: the caller's, who may free it while the current stream uses it."""
+    import torch
+    current = None if stream is None else torch.cuda.current_stream(stream.device)
+    if stream == current:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if kept:
+        t.record_stream(current)
+    return t
+
+
 def _check(status: int, where: str) -> None:
     if status != 0:
         raise PaluError(status, where)
@@ -212,7 +226,7 @@ def palu_rope_table_init(rope_theta: float, d_head: int, n_pos: int, table=None,
     """Fills (allocating with torch when `table` is None) and returns the table tensor."""
     import torch
     if table is None:
-        table = torch.empty(palu_rope_table_bytes(d_head, n_pos), dtype=torch.uint8, device="cuda")
+        table = _empty(palu_rope_table_bytes(d_head, n_pos), torch.uint8, "cuda", stream, kept=True)
     _need_cuda(table)
     _check(load_library().palu_rope_table_init(float(rope_theta), d_head, n_pos, _ptr(table), _stream(stream)),
            "palu_rope_table_init")
@@ -231,7 +245,7 @@ def palu_encode(desc: LayerDesc, which: int, x, A, latent, row_stride_elems: int
     import torch
     n_tok = int(x.shape[0])
     if workspace is None:
-        workspace = torch.empty(palu_encode_workspace_bytes(desc, which, n_tok), dtype=torch.uint8, device=x.device)
+        workspace = _empty(palu_encode_workspace_bytes(desc, which, n_tok), torch.uint8, x.device, stream)
     _need_cuda(x, A, latent, dst_row, workspace)
     _check(load_library().palu_encode(desc.ref(), which, _ptr(x), n_tok, _ptr(A), _ptr(latent),
                                       int(row_stride_elems), _ptr(dst_row), _ptr(workspace),
@@ -244,7 +258,7 @@ def palu_encode_kv(desc: LayerDesc, x, Ak, Av, hk, hk_row_stride_elems: int, hv,
     import torch
     n_tok = int(x.shape[0])
     if workspace is None:
-        workspace = torch.empty(palu_encode_workspace_bytes(desc, 2, n_tok), dtype=torch.uint8, device=x.device)
+        workspace = _empty(palu_encode_workspace_bytes(desc, 2, n_tok), torch.uint8, x.device, stream)
     _need_cuda(x, Ak, Av, hk, hv, dst_row, workspace)
     _check(load_library().palu_encode_kv(desc.ref(), _ptr(x), n_tok, _ptr(Ak), _ptr(Av), _ptr(hk),
                                          int(hk_row_stride_elems), _ptr(hv), int(hv_row_stride_elems),
@@ -284,10 +298,9 @@ def palu_attn_decode(desc: LayerDesc, batch: int, seq_len: int, max_seq: int, q,
     already recorded once (so that their HIP handles exist); routes through palu_attn_decode_staged."""
     import torch
     if out is None:
-        out = torch.empty((batch, desc.n_q_heads, desc.d_head), dtype=torch.float32, device=q.device)
+        out = _empty((batch, desc.n_q_heads, desc.d_head), torch.float32, q.device, stream, kept=True)
     if workspace is None:
-        workspace = torch.empty(palu_attn_decode_workspace_bytes(desc, batch, max_seq), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(palu_attn_decode_workspace_bytes(desc, batch, max_seq), torch.uint8, q.device, stream)
     _need_cuda(q, q_pos, hk, hv, Bk, Bv, rope_table, out, workspace, k_pos, seq_lens, hk_scale, hk_zero,
                hv_scale, hv_zero)
     args = (desc.ref(), batch, seq_len, max_seq, _ptr(q), _ptr(q_pos), _ptr(hk), _ptr(hk_scale), _ptr(hk_zero),
@@ -324,10 +337,9 @@ def palu_attn_decode_latent(desc: LayerDesc, batch: int, seq_len: int, max_seq: 
     if out_latent is None:
         width = sum((desc.v_rank_off[j + 1] - desc.v_rank_off[j]) * (desc.group_head_off[j + 1] - desc.group_head_off[j])
                     for j in range(desc.n_groups)) * max(desc.q_per_kv, 1)
-        out_latent = torch.empty((batch, width), dtype=torch.float32, device=q.device)
+        out_latent = _empty((batch, width), torch.float32, q.device, stream, kept=True)
     if workspace is None:
-        workspace = torch.empty(palu_attn_decode_workspace_bytes(desc, batch, max_seq), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(palu_attn_decode_workspace_bytes(desc, batch, max_seq), torch.uint8, q.device, stream)
     _need_cuda(q, q_pos, hk, hv, Bk, rope_table, out_latent, workspace, k_pos, seq_lens, hk_scale, hk_zero,
                hv_scale, hv_zero)
     _check(load_library().palu_attn_decode_latent(
@@ -361,12 +373,12 @@ def palu_attn_decode_multi(desc: LayerDesc, batch: int, n_q: int, seq_len: int, 
     import torch
     lib = load_library()
     if out is None:
-        out = torch.empty((batch, n_q, desc.n_q_heads, desc.d_head), dtype=torch.float32, device=q.device)
+        out = _empty((batch, n_q, desc.n_q_heads, desc.d_head), torch.float32, q.device, stream, kept=True)
     if workspace is None:
         nbytes = ctypes.c_size_t(0)
         _check(lib.palu_attn_decode_multi_workspace_bytes(desc.ref(), batch, n_q, max_seq, ctypes.byref(nbytes)),
                "palu_attn_decode_multi_workspace_bytes")
-        workspace = torch.empty(int(nbytes.value), dtype=torch.uint8, device=q.device)
+        workspace = _empty(int(nbytes.value), torch.uint8, q.device, stream)
     _need_cuda(q, q_pos, q_len, hk, hv, Bk, Bv, rope_table, out, workspace, k_pos, seq_lens, hk_scale, hk_zero,
                hv_scale, hv_zero)
     _check(lib.palu_attn_decode_multi(desc.ref(), batch, n_q, seq_len, max_seq, _ptr(q), _ptr(q_pos), _ptr(q_len),
@@ -395,10 +407,9 @@ def palu_decode_step_t(desc: LayerDesc, batch: int, seq_len: int, max_seq: int, 
     """palu_decode_step from transposed weights (Akt [R_k, d], Avt [R_v, d])."""
     import torch
     if out is None:
-        out = torch.empty((batch, desc.n_q_heads, desc.d_head), dtype=torch.float32, device=q.device)
+        out = _empty((batch, desc.n_q_heads, desc.d_head), torch.float32, q.device, stream, kept=True)
     if workspace is None:
-        workspace = torch.empty(palu_attn_decode_workspace_bytes(desc, batch, max_seq), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(palu_attn_decode_workspace_bytes(desc, batch, max_seq), torch.uint8, q.device, stream)
     _need_cuda(x, Akt, Avt, dst_row, q, q_pos, hk, hv, Bk, Bv, rope_table, out, workspace, k_pos, seq_lens)
     _check(load_library().palu_decode_step_t(
         desc.ref(), batch, seq_len, max_seq, _ptr(x), _ptr(Akt), _ptr(Avt), _ptr(dst_row), _ptr(q), _ptr(q_pos),
@@ -413,12 +424,11 @@ def palu_decode_step(desc: LayerDesc, batch: int, seq_len: int, max_seq: int, x,
     """Append the new tokens (x) to both caches and attend, in one call."""
     import torch
     if out is None:
-        out = torch.empty((batch, desc.n_q_heads, desc.d_head), dtype=torch.float32, device=q.device)
+        out = _empty((batch, desc.n_q_heads, desc.d_head), torch.float32, q.device, stream, kept=True)
     if workspace is None:
-        workspace = torch.empty(palu_attn_decode_workspace_bytes(desc, batch, max_seq), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(palu_attn_decode_workspace_bytes(desc, batch, max_seq), torch.uint8, q.device, stream)
     if encode_workspace is None:
-        encode_workspace = torch.empty(palu_encode_workspace_bytes(desc, 2, batch), dtype=torch.uint8, device=q.device)
+        encode_workspace = _empty(palu_encode_workspace_bytes(desc, 2, batch), torch.uint8, q.device, stream)
     _need_cuda(x, Ak, Av, dst_row, q, q_pos, hk, hv, Bk, Bv, rope_table, out, workspace, encode_workspace, k_pos, seq_lens)
     _check(load_library().palu_decode_step(
         desc.ref(), batch, seq_len, max_seq, _ptr(x), _ptr(Ak), _ptr(Av), _ptr(dst_row), _ptr(encode_workspace),
@@ -475,10 +485,9 @@ def palu_attn_paged(desc: LayerDesc, batch: int, max_len: int, q, q_pos, hk, hv,
     `n_sink` rows (window 0: all rows)."""
     import torch
     if out is None:
-        out = torch.empty((batch, desc.n_q_heads, desc.d_head), dtype=q.dtype, device=q.device)
+        out = _empty((batch, desc.n_q_heads, desc.d_head), q.dtype, q.device, stream, kept=True)
     if workspace is None:
-        workspace = torch.empty(palu_attn_paged_workspace_bytes(desc, batch, max_len, window, n_sink), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(palu_attn_paged_workspace_bytes(desc, batch, max_len, window, n_sink), torch.uint8, q.device, stream)
     return _paged_call(load_library().palu_attn_paged, "palu_attn_paged", desc, (batch, max_len, window, n_sink), q, q_pos, hk, hv,
                        page_table, seq_lens, Bk, Bv, rope_table, rope_table_len, out, workspace, stream)
 
@@ -488,10 +497,9 @@ def palu_attn_prefix(desc: LayerDesc, batch: int, prefix_len: int, max_len: int,
     """Decode attention of a batch whose first `prefix_len` rows are those of sequence 0, read and rebuilt once for all."""
     import torch
     if out is None:
-        out = torch.empty((batch, desc.n_q_heads, desc.d_head), dtype=q.dtype, device=q.device)
+        out = _empty((batch, desc.n_q_heads, desc.d_head), q.dtype, q.device, stream, kept=True)
     if workspace is None:
-        workspace = torch.empty(palu_attn_prefix_workspace_bytes(desc, batch, prefix_len, max_len), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(palu_attn_prefix_workspace_bytes(desc, batch, prefix_len, max_len), torch.uint8, q.device, stream)
     return _paged_call(load_library().palu_attn_prefix, "palu_attn_prefix", desc, (batch, prefix_len, max_len), q, q_pos, hk, hv,
                        page_table, seq_lens, Bk, Bv, rope_table, rope_table_len, out, workspace, stream)
 
@@ -634,10 +642,9 @@ def palu_attn_paged_quant(desc: LayerDesc, batch: int, max_len: int, q, q_pos, h
     [n_pages, page_rows, R / 128]."""
     import torch
     if out is None:
-        out = torch.empty((batch, desc.n_q_heads, desc.d_head), dtype=q.dtype, device=q.device)
+        out = _empty((batch, desc.n_q_heads, desc.d_head), q.dtype, q.device, stream, kept=True)
     if workspace is None:
-        workspace = torch.empty(palu_attn_paged_quant_workspace_bytes(desc, batch, max_len, window, n_sink), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(palu_attn_paged_quant_workspace_bytes(desc, batch, max_len, window, n_sink), torch.uint8, q.device, stream)
     act, i32 = _act(desc), torch.int32
     if q.dtype != act or Bk.dtype != act or Bv.dtype != act or out.dtype != act:
         raise ValueError(f"q, Bk, Bv and out need dtype {act}")
