@@ -3,8 +3,9 @@
 // 8 lanes take a block of 128 channels, 8 of either half each: twice 16 bytes of the latents, and 4, 3 or 2 bytes of codes.
 //   write  s = f16((max - min) / (2^B - 1)), 0 -> 1;  z = f16(clamp(rint(-min / s)));  c = clamp(rint(x / s) + z, 0, 2^B - 1), every step one
 //          float32 operation (ties to even): the numbers that quant_kernel writes
-//   read   (c - z) * s: the difference and the product are exact in float32 for zero-points up to 2^12 (else each is rounded to 2^-24),
-//          then one rounding to the layer's type
+//   read   (c - z) * s, rounded once to the layer's type: exact in float32 for whole zero-points up to 2^12 (13 bits by 11), else a float32
+//          number with its last bit set where it is inexact, which the second rounding cannot take for a tie (16384 bfloat16 rows of 4096 channels a
+//          side whose zero-points have fractions: 85 us against 57)
 // Bound by the memory, and writing by the vector unit beside it: a value is 2 bytes on one side and 1/2 + 1/32 on the other.  16384 rows of 4096 channels
 // are read in 42 us, 16000 written in 39, 4.1 and 4.2 TB/s of the 5.1 of a copy.  (16 lanes a block, with the side's numbers indexed by lane: 70; chosen
 // from registers: 54, bound by the address units, of which 8 lanes a block take half as many row numbers, scales and zero-points.  Two or four blocks per
@@ -49,6 +50,14 @@ template <bool WIDE> __device__ __forceinline__ void store8(uint16_t* p, uint4v 
       p[2 * i + 1] = (uint16_t)(v[i] >> 16);
     }
   }
+}
+
+// x + y in float32, with the last bit set where that is inexact: of the two neighbours the odd one.  (What the rounding leaves is a float32 number.)
+__device__ __forceinline__ float sum_to_odd(float x, float y) {
+  const float sum = x + y, back = sum - x, left = (x - (sum - back)) + (y - back);
+  int u = __builtin_bit_cast(int, sum);
+  if (fabsf(left) > 0.f && (u & 1) == 0) u += (u ^ __builtin_bit_cast(int, left)) >> 31 | 1;       // (towards what is left; not for what is not a number)
+  return __builtin_bit_cast(float, u);
 }
 
 // Its side, chosen from registers (an index into the arguments, which differs by lane, would load them by lane)
@@ -168,22 +177,28 @@ __global__ __launch_bounds__(kCacheRowsThreads) void dequant_rows_kernel(CacheRo
     if (sd.bits == 3) third[p] = codes[R / 4 + at];
   }
   const uint16_t s16 = sd.scale[it.row * sd.n_blocks + it.block];
-  // (c - z) s = c s - z s: z s is exact (22 bits), so that one fma rounds what the difference and the product would
+  // (c - z) s = c s - z s: both products are exact (15 and 22 bits), so one fma rounds the difference once, if at all
   const float s = F16::to_float(s16), z = F16::to_float(sd.zero[it.row * sd.n_blocks + it.block]), off = -(z * s);
-  const bool infinite = (s16 & 0x7fffu) == 0x7c00u;          // (there it would not)
+  const bool infinite = (s16 & 0x7fffu) == 0x7c00u;          // (there the products' difference is not a number)
+  const bool seldom = __any(infinite || !(fabsf(z) <= 4096.f && z == rintf(z)));
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     const uint32_t c = sd.bits == 4 ? w[p] : expand_low_bits(w[p], third[p], sd.bits == 3);
     const uint32_t even = c & 0x0f0f0f0fu, odd = (c >> 4) & 0x0f0f0f0fu;
     uint4v out;
+    if (!seldom) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float c0 = (float)((even >> (8 * e)) & 255u), c1 = (float)((odd >> (8 * e)) & 255u);
-      out[e] = pack2<T>(__builtin_fmaf(c0, s, off), __builtin_fmaf(c1, s, off));
+      for (int e = 0; e < 4; ++e) {
+        const float c0 = (float)((even >> (8 * e)) & 255u), c1 = (float)((odd >> (8 * e)) & 255u);
+        out[e] = pack2<T>(__builtin_fmaf(c0, s, off), __builtin_fmaf(c1, s, off));
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float c0 = (float)((even >> (8 * e)) & 255u), c1 = (float)((odd >> (8 * e)) & 255u);
+        out[e] = pack2<T>(infinite ? (c0 - z) * s : sum_to_odd(c0 * s, off), infinite ? (c1 - z) * s : sum_to_odd(c1 * s, off));
+      }
     }
-    if (__any(infinite))                       // (seldom; the difference and the product are right for all)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) out[e] = pack2<T>(((float)((even >> (8 * e)) & 255u) - z) * s, ((float)((odd >> (8 * e)) & 255u) - z) * s);
     store8<WIDE>(sd.latent + it.i * sd.stride + it.block * 128 + 64 * p + l * 8, out);
   }
 }

@@ -123,6 +123,43 @@ def test_read_back_any_scale_and_zero_point(dtype, bits):
         assert torch.equal(torch.nan_to_num(got.cpu(), nan=1234.0), torch.nan_to_num(want, nan=1234.0))
 
 
+def rounded_once(x, dtype):
+    """64-bit numbers in the type: by way of float32 numbers whose last bit is set wherever they are inexact, which no second rounding can take
+    for a tie."""
+    with np.errstate(over="ignore", invalid="ignore"):
+        f = x.astype(np.float32)
+        u, to = f.view(np.uint32).copy(), np.abs(x) > np.abs(f.astype(np.float64))
+        even = (f.astype(np.float64) != x) & np.isfinite(x) & (u & 1 == 0)
+    u = np.where(even, np.where(to, u + 1, u - 1), u).astype(np.uint32)
+    return torch.from_numpy(u.view(np.float32)).to(torch_dtype(dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("bits", [4, 3, 2])
+def test_read_back_is_rounded_once(dtype, bits):
+    """Zero-points with fractions of any size, and large ones: the product takes up to 39 bits, and float32 numbers that were rounded to ties of the
+    layer's type would be rounded twice."""
+    desc = make_desc(dtype, bits, bits, rk=1024, rv=1024, groups=4)
+    rng = np.random.default_rng(bits)
+    n, R = 1500, desc.R_k
+    codes = rng.integers(0, 256, (n, R * bits // 8)).astype(np.uint8)
+    s = (10.0 ** rng.uniform(-3, 1, (n, R // 128)) * rng.choice([1, -1], (n, R // 128))).astype(np.float16)
+    z = np.concatenate([rng.uniform(0.001, 0.2, (n // 2, R // 128)), 10.0 ** rng.uniform(-7, 4.8, (n - n // 2, R // 128)) *
+                        rng.choice([1, -1], (n - n // 2, R // 128))]).astype(np.float16)
+    codes[0, :64] = 0xBB                                       # 11 - 0.14978 times 0.88672: 9.6171875 in float16, 9.625 by way of float32
+    s[0, 0], z[0, 0] = 0.88671875, 0.1497802734375
+    s[1], z[2], s[3, :8], s[4, 3] = np.inf, np.nan, -np.inf, np.nan
+    dev = [torch.from_numpy(x).cuda() for x in (codes, s, z)]
+    out = [torch.empty(n, R, dtype=torch_dtype(dtype), device="cuda") for _ in range(2)]
+    P.palu_dequant_latent_kv(desc, *dev, *dev, None, *out)
+    with np.errstate(invalid="ignore"):
+        want = torch.nan_to_num(rounded_once(O.dequant_latent(codes, s, z, bits=bits), dtype), nan=1234.0)
+    for got in out:
+        got = torch.nan_to_num(got.cpu(), nan=1234.0)
+        say(f"[read] {dtype} {bits} bits: {int((got != want).sum())} of {want.numel()} differ")
+        assert torch.equal(got, want)
+
+
 def test_no_rows_at_all():
     desc = make_desc()
     k, v = caches(4, desc.R_k, 4), caches(4, desc.R_v, 4)
