@@ -579,7 +579,8 @@ def _latent_kv(desc: LayerDesc, hk, hv, k, v, numbers, stream):
     k_bits, v_bits = _BITS.get(desc.k_latent_dtype, 0), _BITS.get(desc.v_latent_dtype, 0)
     R_k, R_v = desc.R_k, desc.R_v
     n_rows = _same_rows(_side_rows(*k, R_k, k_bits) if k_bits else None, _side_rows(*v, R_v, v_bits) if v_bits else None)
-    n_tok = (hk if k_bits or hk is not None else hv).shape[0]
+    h = hk if k_bits else hv if v_bits else None               # (a side that is not quantised is not looked at)
+    n_tok = 0 if h is None else h.shape[0]
     k_stride, v_stride = _latent_stride(desc, hk, R_k, n_tok) if k_bits else 0, _latent_stride(desc, hv, R_v, n_tok) if v_bits else 0
     _row_numbers(numbers, n_tok)
     here, stream = _here(stream)

@@ -88,3 +88,24 @@ def test_rows_whose_channels_are_apart():
         call, good = CALLS[name]
         with pytest.raises(ValueError, match="side by side"):
             call(**{**good(), "hk": zeros(384, 4).t()})
+
+
+@pytest.mark.parametrize("name", ["write", "read"])
+@pytest.mark.parametrize("side", ["k", "v"])
+def test_nothing_of_a_side_that_is_not_quantised_is_looked_at(name, side):
+    call, good = CALLS[name]
+    d = desc(**{side + "_latent_dtype": P.PALU_F16})
+    for other in (zeros(7, 5), zeros(384, 4).t(), zeros(3, dtype=torch.float64), None):
+        codes = None if other is None else zeros(1)
+        with pytest.raises(ValueError, match="device"):
+            call(d, **{**good(), "h" + side: other, **{side + x: codes for x in ("_codes", "_scale", "_zero")}})
+
+
+@pytest.mark.parametrize("name", ["write", "read"])
+def test_latents_that_are_missing(name):
+    call, good = CALLS[name]
+    for h in ("hk", "hv"):
+        with pytest.raises(ValueError, match="latent rows"):
+            call(**{**good(), h: None})
+    with pytest.raises(P.PaluError):                           # no side to move
+        call(desc(k_latent_dtype=P.PALU_F16, v_latent_dtype=P.PALU_F16), **{k: None for k in good()})
