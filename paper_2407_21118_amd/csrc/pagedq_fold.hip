@@ -659,12 +659,14 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
     }
 #pragma unroll
     for (int p = 0; p < 4; ++p) pair(z, p, qa, qb, part);
+    // (lanes of the folded pairs' rows 0 and 1: what is not a number stays in its row)
+    const float sum = __builtin_fmaf(z.low[0], basis[0], __builtin_fmaf(z.low[1], basis[1], __builtin_fmaf(z.low[2], basis[2], z.low[3] * basis[3])));
+    if (NQ == 1) {
+      part[0] = __builtin_fmaf(sum, __builtin_amdgcn_ldexpf(1.f, -ea[0]), part[0]) * (unit * scale);
+    } else {
+      const float low = __builtin_amdgcn_ldexpf(sum, -(kg < 2 ? ea[0] : ea[NQ - 1]));
 #pragma unroll
-    for (int r = 0; r < NQ; ++r) {
-      const float4v x = z.low;
-      const float sum = __builtin_fmaf(x[0], basis[0], __builtin_fmaf(x[1], basis[1], __builtin_fmaf(x[2], basis[2], x[3] * basis[3])));
-      const bool mine = NQ == 1 || (kg >> 1) == (r & 1);
-      part[r] = __builtin_fmaf(sum, mine ? __builtin_amdgcn_ldexpf(1.f, -ea[r]) : 0.f, part[r]) * (unit * scale);
+      for (int r = 0; r < NQ; ++r) part[r] = (part[r] + (kg >> 1 == r ? low : 0.f)) * (unit * scale);
     }
   };
   auto keys = [&](int n, int sub, float (&part)[NQ]) __attribute__((always_inline)) {

@@ -423,3 +423,36 @@ def test_values_of_any_size(name, size, rows):
     pool.Bv = synth.round_to(pool.Bv * 2.0 ** -np.round(np.log2(size)), "f16")
     pool.put()
     hold(pool.call(pool.device()), pool.reference(), "f16")
+
+
+@pytest.mark.parametrize("name,dtype", [("gqa2", "f16"), ("gqa4", "bf16"), ("gqa20-512", "f16"), ("uneven-gqa3", "bf16"), ("theta30", "f16"), ("gqa70", "f16"),
+                                        ("1x128", "f16"), ("2x128-256", "bf16"), ("8x512", "f16")])
+def test_numbers_that_are_not_finite_stay_in_their_heads(name, dtype):
+    """A query's NaN or infinity makes its own head's outputs NaN; a NaN in an attended row's scale or zero-point those of all heads of its group.
+    All others are as without it."""
+    layer = LAYERS[name]()
+    pool = Pool(layer, dtype, [70, 1, 90], 16, seed=25)
+    pool.put()
+    ref, qk = pool.reference(), layer.q_per_kv
+
+    def one(d, b, heads, what):
+        got = pool.call(d).cpu()
+        assert got[b, heads].isnan().all(), what
+        got[b, heads] = torch.from_numpy(ref[b, heads]).to(got.dtype)
+        hold(got, ref, dtype)
+
+    for b, head, feature, value in ((0, 0, 3, "nan"), (1, 1, 40, "nan"), (2, layer.n_q_heads - 1, 100, "inf"), (1, 0, 5, "inf"), (1, 0, 5, "-inf"),
+                                    (1, layer.n_q_heads // 2, 70, "inf"), (1, layer.n_q_heads // 2, 70, "-inf")):
+        say(f"[paged 4 bits] {name} {dtype}: {value} in feature {feature} of query {head} of sequence {b}")
+        d = pool.device()
+        d["q"][b, head, feature] = float(value)
+        one(d, b, [head], "query")
+    for side, off in (("k", layer.k_rank_off), ("v", layer.v_rank_off)):
+        for j in sorted({0, layer.n_groups - 1}):
+            heads = list(range(layer.group_head_off[j] * qk, layer.group_head_off[j + 1] * qk))
+            for b, t, value in ((2, 17, "nan"), (1, 0, "nan")):
+                for what in ("scale", "zero"):
+                    for block in sorted({off[j] // 128, off[j + 1] // 128 - 1}):
+                        d = pool.device()
+                        d[f"h{side}_{what}"][int(pool.table[b, t // 16]), t % 16, block] = float(value)
+                        one(d, b, heads, f"{side} {what} {value}, group {j}, block {block}")
