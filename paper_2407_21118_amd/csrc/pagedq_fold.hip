@@ -800,7 +800,7 @@ __global__ __launch_bounds__(kThreads, 2) void pagedq_kernel(PagedQArgs a) {
       float sum = at[0];
 #pragma unroll
       for (int i = 1; i < PARTS; ++i) sum += at[i * kSteps];
-      x[r] = seen ? sum : -INFINITY;
+      x[r] = seen ? sum + (sum - sum) : -INFINITY;             // (of an infinite score nothing is known: not a number)
       rises = rises || x[r] > run_max[r] + kSlack;
 #pragma unroll
       for (int i = 0; i < MB; ++i) {

@@ -428,8 +428,8 @@ def test_values_of_any_size(name, size, rows):
 @pytest.mark.parametrize("name,dtype", [("gqa2", "f16"), ("gqa4", "bf16"), ("gqa20-512", "f16"), ("uneven-gqa3", "bf16"), ("theta30", "f16"), ("gqa70", "f16"),
                                         ("1x128", "f16"), ("2x128-256", "bf16"), ("8x512", "f16")])
 def test_numbers_that_are_not_finite_stay_in_their_heads(name, dtype):
-    """A query's NaN or infinity makes its own head's outputs NaN; a NaN in an attended row's scale or zero-point those of all heads of its group.
-    All others are as without it."""
+    """A query's NaN or infinity makes its own head's outputs NaN, also where every score is -infinity; one in an attended row's scale or zero-point
+    those of all heads of its group.  All others are as without it."""
     layer = LAYERS[name]()
     pool = Pool(layer, dtype, [70, 1, 90], 16, seed=25)
     pool.put()
@@ -450,7 +450,7 @@ def test_numbers_that_are_not_finite_stay_in_their_heads(name, dtype):
     for side, off in (("k", layer.k_rank_off), ("v", layer.v_rank_off)):
         for j in sorted({0, layer.n_groups - 1}):
             heads = list(range(layer.group_head_off[j] * qk, layer.group_head_off[j + 1] * qk))
-            for b, t, value in ((2, 17, "nan"), (1, 0, "nan")):
+            for b, t, value in ((2, 17, "nan"), (2, 17, "inf"), (1, 0, "inf"), (1, 0, "-inf")):
                 for what in ("scale", "zero"):
                     for block in sorted({off[j] // 128, off[j + 1] // 128 - 1}):
                         d = pool.device()
