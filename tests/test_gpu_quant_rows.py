@@ -210,6 +210,24 @@ def test_written_rows_of_every_size_of_number(dtype, bits):
         assert np.array_equal(a.view(np.uint8), c.view(np.uint8)) and np.array_equal(a.view(np.uint8), b.view(np.uint8))
 
 
+@pytest.mark.parametrize("bits", [4, 3, 2])
+def test_written_rows_that_are_not_finite(bits):
+    """NaN and infinities among the latents: the bytes of palu_quant_latent."""
+    R, n = 256, 300
+    rng = np.random.default_rng(bits)
+    x = rng.standard_normal((n, R)).astype(np.float16)
+    for value in (np.nan, np.inf, -np.inf):
+        x[rng.random((n, R)) < 0.01] = value
+    x[0], x[1, :128], x[2, :128], x[3] = np.nan, np.inf, -np.inf, rng.choice([np.nan, np.inf], R)
+    desc = make_desc("f16", bits, bits, rk=R, rv=R, groups=1)
+    h = torch.from_numpy(x).cuda()
+    k, v, want = caches(n, R, bits), caches(n, R, bits), caches(n, R, bits)
+    P.palu_quant_latent_kv(desc, h, h, *k, *v)
+    P.palu_quant_latent(desc, 0, h, R, n, *want)
+    for a, b, c in zip(k, v, want):
+        assert torch.equal(a.view(torch.uint8), c.view(torch.uint8)) and torch.equal(b.view(torch.uint8), c.view(torch.uint8))
+
+
 # ---- the projection
 
 def weights(R, d, seed, shape="normal"):
@@ -347,6 +365,35 @@ def test_small_products_beside_large_ones_that_cancel(dtype, n, large):
         off = (got.double().cpu() - small).abs().max()
         say(f"[project] {dtype} {n} tokens, weights {large}: off by {float(off):.4f} of {float(small):.4f}, tolerance {float(room):.4f}")
         assert off <= room
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [3, 40, 600])
+def test_projection_of_numbers_that_are_not_finite(dtype, n):
+    """A token's NaN or infinity stays in its row, a scale's or zero-point's in its channel."""
+    desc = make_desc(dtype, rk=128, rv=128, groups=1, group=4)
+    d = desc.n_q_heads * 128
+    x = latents(n, d, dtype, 5)
+    w = weights(128, d, 8)
+    dev = [torch.from_numpy(y).cuda() for y in w]
+
+    def run(x, w):
+        out = [torch.empty(n, 128, dtype=x.dtype, device="cuda") for _ in "kv"]
+        P.palu_encode_kv_w4(desc, x, *w, *dev, out[0], 128, out[1], 128)
+        return out
+
+    plain = run(x, dev)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        y = x.clone()
+        y[2, 77] = value
+        for got, want in zip(run(y, dev), plain):
+            assert not got[2].isfinite().any() and torch.equal(got[:2], want[:2]) and torch.equal(got[3:], want[3:])
+        for which in (1, 2):
+            other = [z.clone() for z in dev]
+            other[which][17, 1] = value
+            (got, same), (want, _) = run(x, other), plain
+            assert not got[:, 17][x[:, 128:256].any(1)].isfinite().any() and torch.equal(same, plain[1])
+            assert torch.equal(got[:, :17], want[:, :17]) and torch.equal(got[:, 18:], want[:, 18:])
 
 
 # ---- as they are used together
