@@ -576,10 +576,11 @@ int palu_encode_kv_w4(const palu_layer_desc* desc, const void* x, int32_t n_tok,
  * positions of every 256, 128 or 64 (the fewer, the smaller rope_theta), between which its angles are polynomials right to
  * 2e-6; sums are float32, folded weights, probabilities and B_v's operands pairs of 16-bit numbers, bfloat16 weights float16
  * ones times a power of two (right to 2^-31 of a head's largest).  So a logit is right to 2e-6 of sum |q k| / sqrt(128), and a
- * probability to as much, relative: the larger the logits, the more.  Weighted sums are right to 2^-21 of sum p |value|, whatever
- * the values' size, in a bfloat16 layer each merged latent then to 2^-16 of itself.  With logits of a few units that is 1e-6 of a float16 layer's outputs
- * and 3e-6 of a bfloat16 layer's (2-norm, up to 65536 rows), before they are rounded to act_dtype.  Layers with 0 < rope_theta <
- * 606, whose slow pairs turn too fast for that, take float32 sums over every channel instead, many times slower.
+ * probability to as much, relative: the larger the logits, the more.  Weighted sums are right to 2^-21 of sum p |value|,
+ * whatever the values' size, in a bfloat16 layer each merged latent then to 2^-16 of itself.  With logits of a few units that is
+ * 1e-6 of a float16 layer's outputs and 3e-6 of a bfloat16 layer's (2-norm, up to 65536 rows), before they are rounded to
+ * act_dtype.  Layers with 0 < rope_theta < 606, whose slow pairs turn too fast for that, take float32 sums over every channel
+ * instead, many times slower.
  */
 int palu_attn_paged_quant_workspace_bytes(const palu_layer_desc* desc, int32_t batch, int32_t max_len, int32_t window,
                                           int32_t n_sink, size_t* out_bytes);

@@ -8,8 +8,9 @@
 // are float32; the only rounding to 16 bits is the result's.  (The matrix cores keep 24 bits below the largest exponent of an instruction's products and
 // take a subnormal operand's for 2^-14: codes as the float16 numbers c * 2^-24 lost what lies 2^-15 below the largest input.)
 // Bound by latency: the weights' bytes (8.4 MB of 4096 inputs by 4096 columns) are worth 1.6 us, and a kernel without its loop takes 2.4; it takes
-// 5.2 us for a token, 7.0 for 24; 333 tokens by 1024 columns 14 (a workgroup's 32 by 64 results: 12.5).  64 tokens by 64 columns were slower (22 us a
-// round of workgroups).
+// 4.8 us for a token, 6.1 for 24; 333 tokens by 1024 columns 13.6 (a workgroup's 32 by 64 results: 12.5).  64 tokens by 64 columns were slower (22 us a
+// round of workgroups).  4096 tokens by 4096 columns take 354 us, 390 TFLOP/s: codes are spread for the matrix instructions anew for every 32 tokens, which keeps
+// the matrix pipe at 20 %.
 
 #include "encode_w4.h"
 #include "paged_dev.h"

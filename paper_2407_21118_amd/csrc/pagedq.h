@@ -1,4 +1,4 @@
-// What the host side and the kernels of attention over a paged 4-bit latent cache share (pagedq.hip).
+// What the host side and the kernels of attention over a paged 4-bit latent cache share (pagedq_fold.hip and, for angles that turn too fast, pagedq.hip).
 #pragma once
 
 #include "paged.h"
@@ -12,7 +12,7 @@ struct PagedQSide {
   int row_bytes, n_blocks;   // R / 2, R / 128
 };
 constexpr int kPagedQStep = 64;                // tokens per step: two tiles
-constexpr int kPagedQLow = 32;                 // rotation pairs from this one on are folded with the query (pagedq.hip)
+constexpr int kPagedQLow = 32;                 // rotation pairs from this one on are folded with the query (pagedq_fold.hip)
 constexpr int kPagedQNodes = 8;                // positions at which they are
 constexpr int kPagedQSpan = 256;               // positions between two foldings, at most
 

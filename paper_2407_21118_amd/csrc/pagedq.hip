@@ -2,7 +2,8 @@
 //
 //   out = softmax_t( RoPE(q, p) . RoPE(H_k[t] B_k, t) / sqrt(d_h) ) H_v[t] B_v,   H[t, r] = (code - zero) * scale
 //
-// Partial results (unnormalised sums, maxima, row sums) are merged, normalised and multiplied by B_v in paged_merge_kernel.
+// Partial results (unnormalised sums, maxima, row sums) are merged, normalised and multiplied by B_v in paged_merge_kernel.  This kernel is for rotations whose
+// slow half turns too fast to be folded with the query (pagedq_fold.hip).
 
 #include "pagedq.h"
 

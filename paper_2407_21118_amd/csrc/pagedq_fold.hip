@@ -15,11 +15,14 @@
 // as exact float16 integers; a token's scales multiply sums, not codes.  In an interval one of the two wavefronts makes the scores of step n while the
 // other weighs step n - 1, adds up the values of n - 2 and converts the codes of n + 1, and then the other way round: matrix and vector instructions go
 // together without being mixed by hand.  (One wavefront per SIMD with 512 registers, its scores, weights, values and codes dealt out between the matrix
-// instructions: 312 us for 16 x 8192 rows of 32 heads of rank 256 against 282, 177 against 157 for one sequence of 65536, and 193 against 106 for 4 x 16384
-// rows with four query rows a head, two of which are taken at a time here.)
+// instructions, as graph replays: 312 us for 16 x 8192 rows of 32 heads of rank 256 against 282, 177 against 157 for one sequence of 65536, and 193 against
+// 106 for 4 x 16384 rows with four query rows a head, two of which are taken at a time here.  Calls among others take 278, 154 and 100.)
 //
 // Bound by the instructions of two wavefronts a SIMD and their latencies: 8700 cycles an interval, of which the matrix pipe is busy 2800 and the vector
-// unit 5200; the start of a run takes 34000 (weights of 256 KB a workgroup from L2) and its end 4000.
+// unit 5200; the start of a run takes 34000 (weights of 256 KB a workgroup from L2) and its end 4000.  One query row takes 64 + 16 operand rows a head
+// where rebuilding takes 128; two rows 64 + 32, for which four rows rebuild every key twice: 4 x 16384 rows from 16-bit pages, rebuilt once for all, take
+// 61 us.  Seven of the 32 forms spill 4 to 36 registers (20 to 92 bytes a lane), all with eight steps of channels: bfloat16 ones, and two rows with four
+// value blocks.
 
 #include "paged_dev.h"
 #include "pagedq.h"
